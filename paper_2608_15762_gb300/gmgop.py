@@ -1,0 +1,420 @@
+"""Thin Python binding of the decoder-layer operators in ``include/gmgop.h``.
+
+The operators are what an executor runs of a placed graph: products with their
+epilogue (``linear``), rotary positions (``rope``, ``rope_append``), a paged cache
+(``PageCache``) and attention over shared prefixes (``AttendPlan``, ``attend``).
+Argument marshalling only; PyTorch provides device memory and streams.  Calls
+are asynchronous on the current stream, or on ``stream``, where their results'
+memory then belongs.  What the C ABI refuses raises ``GmgError``; tensors of the
+wrong shape, type or device raise ``ValueError``.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+import math
+from typing import Optional, Sequence
+
+import numpy as np
+
+from . import gmgsim as G
+from .gmgsim import GmgError, _aligned_empty, _check, _stream_handle, _traced
+
+EXPORTED = ("op_page_scratch_bytes", "op_free", "op_fork", "op_grow", "op_compact", "op_rope", "op_rope_append",
+            "op_attend_plan", "op_attend", "op_linear_work_bytes", "op_linear")
+
+F32, BF16, F16 = 0, 1, 2
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+PAGE_OK, PAGE_FULL, PAGE_SEQ, PAGE_TWICE, PAGE_LONG, PAGE_USED = range(6)
+
+
+class _Cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pool", "table", "lens", "refs", "status")] + [
+        (n, C.c_int32) for n in ("dtype", "n_pages", "n_layers", "n_kv_heads", "page_tokens", "head_dim", "n_seq",
+                                 "max_pages")]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rotary", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float)]
+
+
+class _AttendDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_batch", "n_heads", "n_kv_heads", "head_dim", "page_tokens",
+                                         "n_groups")] + [
+        (n, C.c_void_p) for n in ("q_len", "kv_len", "seq", "group_off", "prefix")]
+
+
+class _AttendPlan(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_batch", "n_heads", "n_kv_heads", "head_dim", "page_tokens", "n_items",
+                                         "n_joins", "max_seq", "max_kv", "reserved")] + [
+        ("n_tokens", C.c_int64), ("part_rows", C.c_int64), ("plan_bytes", C.c_size_t), ("work_bytes", C.c_size_t)]
+
+
+class _Linear(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "act", "gated", "reserved")] + [
+        (n, C.c_int64) for n in ("m", "n", "k")] + [
+        (n, C.c_void_p) for n in ("x", "w", "gate", "bias", "gate_bias", "residual", "y")] + [
+        (n, C.c_int64) for n in ("x_row", "w_row", "gate_row", "residual_row", "y_row")]
+
+
+_LIB = None
+
+
+def lib():
+    global _LIB
+    if _LIB is None:
+        L = G.lib()
+        vp, i32, i64, sz, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
+        sig = {
+            "op_page_scratch_bytes": ([vp], sz),
+            "op_free": ([vp, vp, i32, vp, sz, vp], C.c_int),
+            "op_fork": ([vp, vp, vp, vp, i32, vp, sz, vp], C.c_int),
+            "op_grow": ([vp, vp, vp, i32, vp, sz, vp], C.c_int),
+            "op_compact": ([vp, vp, sz, vp], C.c_int),
+            "op_rope": ([vp, i32, i64, i32, i32, vp, i64, i64, vp, i32, vp, i64, i64, vp], C.c_int),
+            "op_rope_append": ([vp, vp, i32, i64, i32] + [vp, i64, i64] * 3 + [vp, vp, vp, i64, i64, vp], C.c_int),
+            "op_attend_plan": ([vp, i32, vp, vp, sz], C.c_int),
+            "op_attend": ([vp, vp, vp, i32, vp, i64, i64, f32, vp, i64, i64, vp, vp, sz, vp], C.c_int),
+            "op_linear_work_bytes": ([vp], sz),
+            "op_linear": ([vp, vp, sz, vp], C.c_int),
+        }
+        for name, (args, res) in sig.items():
+            f = getattr(L, name)
+            f.argtypes = args
+            f.restype = res
+        _LIB = L
+    return _LIB
+
+
+def _dtype(t) -> int:
+    import torch
+    d = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    if d is None:
+        raise ValueError("element type %s: fp32, bf16 or fp16" % t.dtype)
+    return d
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(stream):
+    """Memory allocated inside belongs to `stream`."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _list(t, device, what: str) -> None:
+    import torch
+    _need(t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.device == device,
+          "%s: a contiguous int32 list on the operands' GPU" % what)
+
+
+# ---------------------------------------------------------------------------
+# Pages of a cache
+# ---------------------------------------------------------------------------
+
+class PageCache:
+    """A paged cache of keys and values: pool [n_pages, n_layers, 2, n_kv_heads,
+    page_tokens, head_dim] and, int32, table [n_seq, max_pages] (-1: no page), lens
+    [n_seq] and refs [n_pages].  What is not given starts empty.  The page calls take
+    int32 lists on the GPU and do not synchronise; ``code()`` does, and says how the
+    last one went."""
+
+    def __init__(self, pool, n_seq: int = 0, max_pages: int = 0, table=None, lens=None, refs=None):
+        import torch
+        _need(pool.is_cuda and pool.dim() == 6 and pool.shape[2] == 2 and pool.is_contiguous(),
+              "pool: contiguous, [n_pages, n_layers, 2, n_kv_heads, page_tokens, head_dim], on a GPU")
+        dev, i32 = pool.device, torch.int32
+        if table is None:
+            table = torch.full((n_seq, max_pages), -1, dtype=i32, device=dev)
+        n_seq, max_pages = table.shape
+        lens = torch.zeros(n_seq, dtype=i32, device=dev) if lens is None else lens
+        refs = torch.zeros(pool.shape[0], dtype=i32, device=dev) if refs is None else refs
+        _need(table.dtype == i32 and table.is_contiguous() and table.device == dev, "table: contiguous int32")
+        _list(lens, dev, "lens")
+        _list(refs, dev, "refs")
+        _need(lens.numel() == n_seq and refs.numel() == pool.shape[0], "lens, refs: one entry a row, one a page")
+        self.pool, self.table, self.lens, self.refs = pool, table, lens, refs
+        self.status = torch.zeros(8, dtype=i32, device=dev)
+        p = pool.shape
+        self.n_layers, self.n_kv_heads, self.page_tokens, self.head_dim = p[1], p[3], p[4], p[5]
+        self.c = _Cache(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(), self.status.data_ptr(),
+                        _dtype(pool), p[0], p[1], p[3], p[4], p[5], n_seq, max_pages)
+        self.ref = C.addressof(self.c)
+        nbytes = lib().op_page_scratch_bytes(self.ref)
+        if nbytes == 0:
+            raise GmgError(G.GMG_EINVAL, "op_page_scratch_bytes")
+        self.scratch = _aligned_empty(nbytes, dev)
+        self.scratch.zero_()
+
+    def code(self):
+        """(PAGE_* code of the last page call, the list entry or the missing pages)."""
+        return tuple(self.status[:2].tolist())
+
+    def _tail(self, stream):
+        return self.scratch.data_ptr(), self.scratch.numel(), _stream_handle(stream)
+
+    @_traced("op_free")
+    def free(self, seq, stream=None):
+        """Empty the listed rows and drop their references."""
+        _list(seq, self.pool.device, "seq")
+        _check(lib().op_free(self.ref, seq.data_ptr(), seq.numel(), *self._tail(stream)), "op_free")
+
+    @_traced("op_fork")
+    def fork(self, src, dst, keep=None, stream=None):
+        """The empty rows dst get the first ``keep`` tokens (all) of rows src by reference."""
+        for t, name in ((src, "src"), (dst, "dst")) + (((keep, "keep"),) if keep is not None else ()):
+            _list(t, self.pool.device, name)
+            _need(t.numel() == src.numel(), "src, dst, keep: one length")
+        _check(lib().op_fork(self.ref, src.data_ptr(), dst.data_ptr(), None if keep is None else keep.data_ptr(),
+                             src.numel(), *self._tail(stream)), "op_fork")
+
+    @_traced("op_grow")
+    def grow(self, seq, add, stream=None):
+        """Room for ``add`` more tokens in the listed rows, whose lengths grow by them; a
+        partly filled last page that others hold too is copied first."""
+        _list(seq, self.pool.device, "seq")
+        _list(add, self.pool.device, "add")
+        _need(seq.numel() == add.numel(), "seq, add: one length")
+        _check(lib().op_grow(self.ref, seq.data_ptr(), add.data_ptr(), seq.numel(), *self._tail(stream)), "op_grow")
+
+    @_traced("op_compact")
+    def compact(self, stream=None):
+        """Move the pages in use to the lowest page numbers."""
+        _check(lib().op_compact(self.ref, *self._tail(stream)), "op_compact")
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+
+def rope_freqs(rotary: int, base: float = 10000.0, scaling: str = "none", scale: float = 1.0, length: int = 0,
+               low: float = 1.0, high: float = 32.0):
+    """(angle per position of each pair in 64 bits, factor of the magnitude).
+
+    none: f_i = base^(-2i / rotary).  linear: f_i / scale.  base: the base grown to
+    base * scale^(rotary / (rotary - 2)), which divides the lowest frequency by scale.
+    parts: pairs that turn ``high`` times or more over ``length`` positions keep their
+    frequency, those that turn ``low`` times or less have it divided by scale, a
+    linear mix between; the factor is 0.1 ln(scale) + 1."""
+    _need(rotary % 2 == 0 and rotary > 0 and base > 1.0 and scale >= 1.0, "rotary even, base > 1, scale >= 1")
+    i = np.arange(rotary // 2, dtype=np.float64)
+    if scaling == "base":
+        _need(rotary > 2, "scaling the base takes more than one pair")
+        base = base * scale ** (rotary / (rotary - 2))
+    f = base ** (-2.0 * i / rotary)
+    if scaling in ("none", "base"):
+        return f, 1.0
+    if scaling == "linear":
+        return f / scale, 1.0
+    _need(scaling == "parts", "scaling: none, linear, base or parts")
+    _need(length > 0 and high > low, "parts: length > 0, high > low")
+    keep = np.clip((length * f / (2 * math.pi) - low) / (high - low), 0.0, 1.0)
+    return f * (keep + (1.0 - keep) / scale), 0.1 * math.log(scale) + 1.0
+
+
+class Rope:
+    """The frequencies of rotary positions, on the GPU: fractions of a turn per
+    position in 64 bits.  freqs (64-bit, 0 <= f < 2 pi) and factor as from
+    ``rope_freqs``, or its arguments."""
+
+    def __init__(self, rotary: int, freqs=None, factor: float = 1.0, interleaved: bool = False, device="cuda", **kw):
+        import torch
+        if freqs is None:
+            freqs, factor = rope_freqs(rotary, **kw)
+        freqs = np.asarray(freqs, np.float64)
+        _need(freqs.shape == (rotary // 2,) and rotary % 2 == 0, "freqs: one per pair")
+        _need(bool(np.all((freqs >= 0) & (freqs < 2 * math.pi))), "freqs: 0 <= f < 2 pi")
+        # the top 53 bits in floating point, so that the fraction is f's rounding of 2^64 f / (2 pi)
+        turns = np.array([min(int(round(float(f) / (2 * math.pi) * 2.0 ** 64)), 2 ** 64 - 1) for f in freqs], np.uint64)
+        self.rotary, self.factor, self.interleaved = int(rotary), float(factor), bool(interleaved)
+        self.freq = torch.from_numpy(turns.view(np.int64).copy()).to(device)
+        self.c = _Rope(self.freq.data_ptr(), self.rotary, int(self.interleaved), self.factor)
+        self.ref = C.addressof(self.c)
+
+
+def _heads(t, what: str, n_tokens=None):
+    _need(t.dim() == 3 and (t.shape[2] <= 1 or t.stride(2) == 1) and t.is_cuda,
+          "%s: [tokens, heads, head_dim] on a GPU, contiguous in head_dim" % what)
+    _need(n_tokens is None or t.shape[0] == n_tokens, "%s: one row a token" % what)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+@_traced("op_rope")
+def rope(plan: Rope, x, pos, backward: bool = False, out=None, stream=None):
+    """x [tokens, heads, head_dim] rotated by pos (int32, one a token); ``backward``: by
+    minus the angle, which takes the gradient of the result to that of x.  out may be x."""
+    import torch
+    _list(pos, x.device, "pos")
+    _need(pos.numel() == x.shape[0], "pos: one entry a token")
+    if out is None:
+        with _on(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device, "out: as x")
+    _check(lib().op_rope(plan.ref, _dtype(x), x.shape[0], x.shape[1], x.shape[2], *_heads(x, "x"), pos.data_ptr(),
+                         int(backward), *_heads(out, "out"), _stream_handle(stream)), "op_rope")
+    return out
+
+
+@_traced("op_rope_append")
+def rope_append(plan: Rope, q, k, v, pos, seq, cache: PageCache, layer: int, out=None, stream=None):
+    """q rotated by pos (returned); k rotated and v written to ``layer`` of the cache as
+    token pos[t] of row seq[t] (a negative seq: not written)."""
+    import torch
+    T = q.shape[0]
+    _list(pos, q.device, "pos")
+    _list(seq, q.device, "seq")
+    _need(pos.numel() == T and seq.numel() == T, "pos, seq: one entry a token")
+    D, Hk = cache.head_dim, cache.n_kv_heads
+    _need(q.dtype == k.dtype == v.dtype == cache.pool.dtype and q.device == cache.pool.device,
+          "q, k, v: the cache's type, on its GPU")
+    _need(q.shape[2] == D and tuple(k.shape) == (T, Hk, D) and tuple(v.shape) == (T, Hk, D),
+          "q [tokens, heads, head_dim], k and v [tokens, n_kv_heads, head_dim]")
+    if out is None:
+        with _on(stream):
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype and out.device == q.device, "out: as q")
+    _check(lib().op_rope_append(plan.ref, cache.ref, int(layer), T, q.shape[1], *_heads(q, "q"), *_heads(k, "k"),
+                                *_heads(v, "v"), pos.data_ptr(), seq.data_ptr(), *_heads(out, "out"),
+                                _stream_handle(stream)), "op_rope_append")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Attention
+# ---------------------------------------------------------------------------
+
+_SMS = {}
+
+
+def _n_sm(device) -> int:
+    import torch
+    if device not in _SMS:
+        _SMS[device] = torch.cuda.get_device_properties(device).multi_processor_count
+    return _SMS[device]
+
+
+def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=None, group_off=None, prefix=None,
+                 n_sm: int = 152):
+    """(plan, its int32 array on the host): the work of ``attend`` for these lengths."""
+    arr = [None if a is None else np.ascontiguousarray(a, np.int32) for a in (q_len, kv_len, seq, group_off, prefix)]
+    q, kv, sq, off, pre = arr
+    _need(q.ndim == 1 and kv.shape == q.shape and (sq is None or sq.shape == q.shape),
+          "q_len, kv_len, seq: one entry a request")
+    _need((off is None) == (pre is None) and (off is None or off.shape == (pre.size + 1,)),
+          "group_off: one entry more than prefix")
+    ptr = [None if a is None else a.ctypes.data for a in arr]
+    d = _AttendDesc(q.size, n_heads, n_kv_heads, head_dim, page_tokens, 0 if pre is None else pre.size, *ptr)
+    plan = _AttendPlan()
+    _check(lib().op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), None, 0), "op_attend_plan")
+    items = np.zeros(plan.plan_bytes // 4, np.int32)
+    _check(lib().op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes),
+           "op_attend_plan")
+    return plan, items
+
+
+class AttendPlan:
+    """The work of ``attend`` for requests of q_len new and kv_len cached tokens (the
+    new ones among them), for every layer of a step.  seq: their table rows (0, 1,
+    ...).  group_off, prefix: requests group_off[g] .. group_off[g + 1] share their
+    first prefix[g] tokens."""
+
+    def __init__(self, q_len: Sequence[int], kv_len: Sequence[int], n_heads: int, n_kv_heads: int, head_dim: int,
+                 page_tokens: int, seq: Optional[Sequence[int]] = None, group_off: Optional[Sequence[int]] = None,
+                 prefix: Optional[Sequence[int]] = None, device="cuda", stream=None):
+        import torch
+        dev = torch.device(device)
+        self.c, items = attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq, group_off, prefix,
+                                     _n_sm(dev))
+        self.ref = C.addressof(self.c)
+        self.n_tokens, self.n_heads, self.head_dim = self.c.n_tokens, n_heads, head_dim
+        with _on(stream):
+            self.items = torch.from_numpy(items).to(dev)
+
+
+@_traced("op_attend")
+def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[float] = None, out=None, lse=False,
+           stream=None):
+    """Attention of q [tokens, heads, head_dim] (the requests' new tokens, one request
+    after another) over the cache; with ``lse`` also log sum exp [tokens, heads], fp32."""
+    import torch
+    _need(tuple(q.shape) == (plan.n_tokens, plan.n_heads, plan.head_dim) and q.dtype == cache.pool.dtype
+          and q.device == cache.pool.device, "q: [tokens, heads, head_dim] of the plan, the cache's type")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        z = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse else None
+        work = torch.empty(plan.c.work_bytes, dtype=torch.uint8, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype and out.device == q.device, "out: as q")
+    _check(lib().op_attend(plan.ref, plan.items.data_ptr() if plan.items.numel() else None, cache.ref, int(layer),
+                           *_heads(q, "q"), plan.head_dim ** -0.5 if scale is None else float(scale),
+                           *_heads(out, "out"), None if z is None else z.data_ptr(), work.data_ptr(), work.numel(),
+                           _stream_handle(stream)), "op_attend")
+    return (out, z) if lse else out
+
+
+# ---------------------------------------------------------------------------
+# Products
+# ---------------------------------------------------------------------------
+
+class Workspace:
+    """A workspace of ``linear``: grown on demand, its head zeroed when it is made.
+    Calls that share one must be ordered (one stream)."""
+
+    def __init__(self, device="cuda"):
+        self.device, self.buf = device, None
+
+    def get(self, nbytes: int, stream=None):
+        if self.buf is None or self.buf.numel() < nbytes:
+            with _on(stream):
+                self.buf = _aligned_empty(nbytes, self.device)
+                self.buf[:4096].zero_()
+        return self.buf
+
+
+_WORK = {}
+
+
+def _matrix(t, shape, like, what: str):
+    _need(tuple(t.shape) == shape and t.dtype == like.dtype and t.device == like.device
+          and (shape[-1] <= 1 or t.stride(-1) == 1), "%s: %s, rows contiguous, of x's type and GPU" % (what, list(shape)))
+    return t.data_ptr()
+
+
+@_traced("op_linear")
+def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residual=None, out=None,
+           ws: Optional[Workspace] = None, stream=None):
+    """act(x w^T + bias) + residual or, with a gate, act(x gate^T + gate_bias) * (x w^T +
+    bias) + residual, for x [m, k], w and gate [n, k], biases [n], residual [m, n].
+    act: none, relu, silu, gelu.  out may be residual.  ws: kept per stream by default."""
+    import torch
+    _need(x.dim() == 2 and w.dim() == 2 and x.is_cuda, "x [m, k], w [n, k] on a GPU")
+    m, k = x.shape
+    n = w.shape[0]
+    _need(act in ACTS, "act: one of %s" % ", ".join(ACTS))
+    _need(gate_bias is None or gate is not None, "gate_bias without a gate")
+    if out is None:
+        with _on(stream):
+            out = torch.empty((m, n), dtype=x.dtype, device=x.device)
+
+    def row(t, width):
+        return max(t.stride(0), width) if t is not None and t.shape[0] <= 1 else 0 if t is None else t.stride(0)
+
+    a = _Linear(_dtype(x), ACTS[act], int(gate is not None), 0, m, n, k, _matrix(x, (m, k), x, "x"),
+                _matrix(w, (n, k), x, "w"), None if gate is None else _matrix(gate, (n, k), x, "gate"),
+                None if bias is None else _matrix(bias, (n,), x, "bias"),
+                None if gate_bias is None else _matrix(gate_bias, (n,), x, "gate_bias"),
+                None if residual is None else _matrix(residual, (m, n), x, "residual"), _matrix(out, (m, n), x, "out"),
+                row(x, k), row(w, k), row(gate, k), row(residual, n), row(out, n))
+    ref = C.addressof(a)
+    h = _stream_handle(stream)
+    if ws is None:
+        ws = _WORK.get((x.device, h))
+        if ws is None:
+            ws = _WORK[(x.device, h)] = Workspace(x.device)
+    need = lib().op_linear_work_bytes(ref)
+    buf = ws.get(max(need, 4096), stream)
+    _check(lib().op_linear(ref, buf.data_ptr(), buf.numel(), h), "op_linear")
+    return out

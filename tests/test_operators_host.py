@@ -1,0 +1,167 @@
+"""The decoder-layer operators' C ABI: exported symbols and the refusals that need no GPU
+(arguments are checked before any launch)."""
+import ctypes as C
+import os
+import re
+
+import numpy as np
+import pytest
+
+from paper_2608_15762_gb300 import build, gmgop as P, gmgsim as G
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build.build()
+
+
+def test_exports_every_declared_symbol():
+    hdr = open(os.path.join(ROOT, "include", "gmgop.h")).read()
+    hdr = re.sub(r"/\*.*?\*/", "", hdr, flags=re.S)
+    assert set(re.findall(r"\b(op_\w+)\s*\(", hdr)) == set(P.EXPORTED)
+    for n in P.EXPORTED:
+        assert hasattr(P.lib(), n), n
+
+
+def _linear(**kw):
+    a = dict(dtype=P.BF16, act=0, gated=0, m=4, n=8, k=16, x=256, w=512, y=1024, x_row=16, w_row=16, gate_row=16,
+             residual_row=8, y_row=8)
+    a.update(kw)
+    s = P._Linear()
+    for k, v in a.items():
+        setattr(s, k, v)
+    return s
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=P.F32), dict(dtype=7), dict(act=9), dict(act=-1), dict(m=-1), dict(k=-3),
+                                dict(x=0), dict(w=0), dict(y=0), dict(x_row=15), dict(w_row=8), dict(y_row=7),
+                                dict(residual=256, residual_row=4), dict(gated=1, gate=0), dict(gate_bias=256),
+                                dict(m=2 ** 31)])
+def test_linear_refuses(kw):
+    a = _linear(**kw)
+    assert P.lib().op_linear_work_bytes(C.addressof(a)) == 0
+    assert P.lib().op_linear(C.addressof(a), 256, 1 << 30, None) == G.GMG_EINVAL
+
+
+def test_linear_refuses_a_short_workspace():
+    a = _linear()
+    assert P.lib().op_linear_work_bytes(C.addressof(a)) >= 4096
+    for work, size in ((0, 1 << 30), (128, 1 << 30), (256, 64)):
+        assert P.lib().op_linear(C.addressof(a), work, size, None) == G.GMG_EWS
+
+
+def _cache(**kw):
+    a = dict(pool=256, table=256, lens=256, refs=256, status=256, dtype=P.BF16, n_pages=10, n_layers=2, n_kv_heads=2,
+             page_tokens=16, head_dim=64, n_seq=4, max_pages=6)
+    a.update(kw)
+    s = P._Cache()
+    for k, v in a.items():
+        setattr(s, k, v)
+    return s
+
+
+BAD_CACHES = [dict(pool=0), dict(pool=8), dict(table=0), dict(dtype=P.F32), dict(n_pages=0), dict(page_tokens=12),
+              dict(page_tokens=4), dict(page_tokens=512), dict(head_dim=129), dict(head_dim=12), dict(head_dim=136),
+              dict(n_seq=0), dict(max_pages=0), dict(n_layers=0), dict(n_kv_heads=0)]
+
+
+@pytest.mark.parametrize("kw", BAD_CACHES)
+def test_page_calls_refuse_a_bad_cache(kw):
+    L, r = P.lib(), C.addressof(_cache(**kw))
+    assert L.op_page_scratch_bytes(r) == 0
+    assert L.op_free(r, 256, 1, 256, 1 << 30, None) == G.GMG_EINVAL
+    assert L.op_fork(r, 256, 256, None, 1, 256, 1 << 30, None) == G.GMG_EINVAL
+    assert L.op_grow(r, 256, 256, 1, 256, 1 << 30, None) == G.GMG_EINVAL
+    assert L.op_compact(r, 256, 1 << 30, None) == G.GMG_EINVAL
+
+
+def test_page_calls_refuse_bad_lists_and_scratch():
+    c = _cache()
+    L, r = P.lib(), C.addressof(c)
+    need = L.op_page_scratch_bytes(r)
+    assert need > 0
+    assert L.op_free(r, 256, -1, 256, need, None) == G.GMG_EINVAL
+    assert L.op_free(r, 256, 5, 256, need, None) == G.GMG_EINVAL
+    assert L.op_free(r, None, 2, 256, need, None) == G.GMG_EINVAL
+    assert L.op_fork(r, 256, None, None, 2, 256, need, None) == G.GMG_EINVAL
+    assert L.op_grow(r, 256, None, 2, 256, need, None) == G.GMG_EINVAL
+    for work, size in ((0, need), (64, need), (256, need - 1)):
+        assert L.op_grow(r, 256, 256, 1, work, size, None) == G.GMG_EWS
+        assert L.op_compact(r, work, size, None) == G.GMG_EWS
+
+
+def test_rope_refuses():
+    L = P.lib()
+
+    def rope(rotary=64, freq=256, dtype=P.BF16, tokens=3, heads=2, dim=64, x=256, pos=256, out=256):
+        p = P._Rope(freq, rotary, 0, 1.0)
+        return L.op_rope(C.addressof(p), dtype, tokens, heads, dim, x, 128, 64, pos, 0, out, 128, 64, None)
+
+    for kw in (dict(rotary=63), dict(rotary=66), dict(rotary=-2), dict(freq=None), dict(dtype=5), dict(tokens=-1),
+               dict(heads=-1), dict(dim=0), dict(x=None), dict(pos=None), dict(out=None), dict(rotary=258, dim=300)):
+        assert rope(**kw) == G.GMG_EINVAL, kw
+    assert rope(tokens=0) == G.GMG_OK
+    p = P._Rope(256, 64, 0, 1.0)
+
+    def append(cache, layer=0, k=256, seq=256):
+        return L.op_rope_append(C.addressof(p), C.addressof(cache), layer, 3, 2, 256, 128, 64, k, 128, 64, 256, 128, 64,
+                                256, seq, 256, 128, 64, None)
+
+    assert append(_cache(), layer=2) == append(_cache(), layer=-1) == append(_cache(), k=None) == G.GMG_EINVAL
+    assert append(_cache(), seq=None) == append(_cache(head_dim=32)) == G.GMG_EINVAL
+    for kw in BAD_CACHES:
+        assert append(_cache(**kw)) == G.GMG_EINVAL
+
+
+def _refuses(*a, **kw):
+    with pytest.raises(G.GmgError) as e:
+        P.attend_items(*a, **kw)
+    assert e.value.code == G.GMG_EINVAL
+
+
+def test_attend_plan_refuses():
+    ok = dict(q_len=[1, 2], kv_len=[5, 9], n_heads=8, n_kv_heads=2, head_dim=64, page_tokens=16)
+    P.attend_items(**ok)
+    for kw in (dict(q_len=[1, -1]), dict(kv_len=[-5, 9]), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0),
+               dict(n_heads=258, n_kv_heads=2), dict(head_dim=136), dict(head_dim=60), dict(page_tokens=24),
+               dict(seq=[0, -1]), dict(q_len=[2 ** 30, 1]), dict(n_sm=0),
+               dict(group_off=[0, 1], prefix=[3]), dict(group_off=[1, 2], prefix=[3]),
+               dict(group_off=[0, 2], prefix=[5]), dict(group_off=[0, 2], prefix=[-1]),
+               dict(group_off=[0, 2, 1, 2], prefix=[0, 0, 0])):
+        _refuses(**dict(ok, **kw))
+    for kw in (dict(kv_len=[5]), dict(seq=[1]), dict(group_off=[0, 2]), dict(group_off=[0, 2], prefix=[1, 1])):
+        with pytest.raises(ValueError):
+            P.attend_items(**dict(ok, **kw))
+
+
+def test_attend_refuses():
+    L = P.lib()
+    plan, items = P.attend_items([1, 2], [5, 90], 8, 2, 64, 16)
+
+    def call(cache, layer=0, q=256, out=256, work=256, size=1 << 40, strides=(512, 64, 512, 64), items=256):
+        return L.op_attend(C.addressof(plan), items, C.addressof(cache), layer, q, strides[0], strides[1], 1.0, out,
+                           strides[2], strides[3], None, work, size, None)
+
+    for kw in (dict(layer=2), dict(layer=-1), dict(q=None), dict(q=264), dict(out=None), dict(out=8), dict(items=None),
+               dict(strides=(513, 64, 512, 64)), dict(strides=(512, 60, 512, 64)), dict(strides=(512, 64, 500, 64))):
+        assert call(_cache(), **kw) == G.GMG_EINVAL, kw
+    assert call(_cache(), work=0) == call(_cache(), work=128) == call(_cache(), size=0) == G.GMG_EWS
+    for kw in BAD_CACHES + [dict(head_dim=72), dict(n_kv_heads=4), dict(page_tokens=32), dict(n_seq=1), dict(max_pages=5)]:
+        assert call(_cache(**kw)) == G.GMG_EINVAL, kw
+
+
+def test_rope_freqs_refuses():
+    for a, kw in (((63,), {}), ((0,), {}), ((64,), dict(base=1.0)), ((64,), dict(scaling="none", scale=0.5)),
+                  ((64,), dict(scaling="other")), ((64,), dict(scaling="parts", scale=2.0)), ((2,), dict(scaling="base"))):
+        with pytest.raises(ValueError):
+            P.rope_freqs(*a, **kw)
+
+
+def test_rope_fractions_are_the_rounded_frequencies():
+    f = P.rope_freqs(128)[0]
+    p = P.Rope(128, freqs=f, device="cpu")
+    got = p.freq.numpy().view(np.uint64).astype(object)
+    for a, b in zip(got, f):
+        assert abs(int(a) - b / (2 * np.pi) * 2.0 ** 64) <= 2.0 ** 64 * b / (2 * np.pi) * 2.0 ** -51 + 1
