@@ -189,7 +189,8 @@ typedef struct {
 } op_linear_t;
 
 /* Bytes of the workspace (256-byte aligned; its first 4 KB zeroed once; calls that
- * share it must be ordered).  0 on bad arguments. */
+ * share it must be ordered).  Its first int32 counts waits of op_linear that gave up
+ * (0 unless the GPU is at fault).  0 on bad arguments. */
 size_t op_linear_work_bytes(const op_linear_t* args);
 int op_linear(const op_linear_t* args, void* work, size_t work_bytes, gmg_stream_t stream);
 

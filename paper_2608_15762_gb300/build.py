@@ -23,7 +23,7 @@ SOURCES = ["gmgsim_host.cu", "gmgsim_kernels.cu", "gmgsim_full.cu", "gmgsim_inc.
            "gmgop_linear.cu"]
 HEADERS = ["gmg_layout.h", "gmg_access.h", "gmg_arb.h", "gmg_arbw.h", "gmg_arb_events.h", "gmg_once.h", "gmgsim_sim.cuh", os.path.join("..", "..", "include", "gmgsim.h"),
            os.path.join("..", "..", "include", "gmgest.h"), os.path.join("..", "..", "include", "gmground.h"),
-           os.path.join("..", "..", "include", "gmgop.h"), "gmgop_host.h"]
+           os.path.join("..", "..", "include", "gmgop.h"), "gmgop_host.h", "gmgop_ptx.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 
