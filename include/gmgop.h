@@ -158,14 +158,15 @@ typedef struct {
 } op_attend_plan_t;
 
 /* Fills *plan and, if items is not NULL, items[plan->plan_bytes / 4] (host
- * int32; item_bytes is what it holds).  n_sm: SMs to spread the work over. */
+ * int32, on the device 16-byte aligned; item_bytes is what it holds).  n_sm: SMs to spread the work over. */
 int op_attend_plan(const op_attend_desc_t* desc, int32_t n_sm, op_attend_plan_t* plan, int32_t* items,
                    size_t item_bytes);
 
 /* q, out [n_tokens][n_heads][head_dim] (requests one after another; strides
  * multiples of 8 elements, 16-byte aligned; out contiguous heads), lse
  * [n_tokens][n_heads] fp32 or NULL.  d_items: the plan's array on the device;
- * work: 256-byte aligned.  Types are the cache's. */
+ * work: 256-byte aligned.  Types are the cache's.  A table entry that is no page of
+ * the pool reads as zeros. */
 int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cache_t* cache, int32_t layer,
               const void* q, int64_t q_tok, int64_t q_head, float scale, void* out, int64_t out_tok, int64_t out_head,
               float* lse, void* work, size_t work_bytes, gmg_stream_t stream);

@@ -1,4 +1,21 @@
-// Attention over a paged cache.  The C ABI is declared in include/gmgop.h.
+// Attention over a paged cache, with shared prefixes read once.  The C ABI is declared in
+// include/gmgop.h.
+//
+// A work item is up to 128 rows (queries of consecutive tokens, all query heads of one
+// key/value head: row = token * heads + head) against a run of keys, 64 a step.  One block
+// takes one item:
+//   warp 4   copies: page by page into a ring of 64-key slots, K_0 K_1 V_0 K_2 V_1 ...
+//   warp 5   products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
+//   warps 0 to 3   softmax: a thread holds one row.  It reads S_j, takes p = exp2(s c - m),
+//            adds the sum, and puts P_j, rounded to the values' type, in S_j's place.
+// S_{j+1} is computed while the softmax works on S_j.  The reference m need not be the exact
+// running maximum, as it cancels: O is rescaled only where a score exceeds m by more than
+// 2^8, so p stays below 2^8 (times 2^7 for fp16, whose small p would lose bits below 2^-14).
+//
+// Queries that share a prefix lie next to each other, so a tile of rows reaches over their
+// requests and every page of the prefix is read once a tile.  Long runs of keys are cut into
+// several items; partial results (rows in fp32 with their log-sum-exp) are joined by a second
+// kernel, in a fixed order.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -6,79 +23,496 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <new>
+#include <type_traits>
+#include <vector>
+
 #include "../../include/gmgop.h"
+#include "gmg_once.h"
 #include "gmgop_host.h"
+#include "gmgop_ptx.cuh"
 
 namespace gop {
 namespace {
 
-// A request of the plan.
+constexpr int kKeys = 64;              // a step
+constexpr int kRows = 128;             // of a tile
+constexpr int kThreads = 192;
+constexpr int32_t kSeesAll = 0x7f000000;
+
 struct Item {
-  int32_t tok0, n_q, row, kv;
+  int32_t tok0, n_tok;                 // queries
+  int32_t row;                         // of the table
+  int32_t lo, hi;                      // keys
+  int32_t pos0;                        // position of the first query; kSeesAll: no query is before a key
+  int32_t part;                        // first row of its partial results, or -1: the result itself
+  int32_t reserved;
+};
+
+// Queries whose results are joined from n[i] parts of step[i] rows each, from row base[i] on:
+// those of the prefix (0) and of what follows it (1).
+struct Join {
+  int32_t tok0, n_tok;
+  int32_t base[2], step[2], n[2];
+};
+
+struct AttendArgs {
+  const Item* items;
+  const Join* joins;
+  const int32_t* table;
+  int32_t* status;
+  int32_t max_pages, page_tokens, n_pages, planes, plane;   // planes of the pool: a page's layers and K, V
+  int32_t n_heads, n_kv, group, dim;
+  float scale2;                        // |scale| log2 e
+  int32_t negative;
+  void* out;
+  int64_t o_tok, o_head;
+  float* lse;
+  float *part_o, *part_lse;            // [n_kv][part_rows][dim], [n_kv][part_rows], log2
+  int64_t part_rows;
 };
 
 __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float up(__half v) { return __half2float(v); }
-__device__ __forceinline__ void down(float v, __nv_bfloat16* o) { *o = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void down(float v, __half* o) { *o = __float2half_rn(v); }
+__device__ __forceinline__ uint32_t pack(__nv_bfloat16, float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack(__half, float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float unpack(__nv_bfloat16, uint32_t v, int i) { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
+__device__ __forceinline__ float unpack(__half, uint32_t v, int i) {
+  return __half2float(__ushort_as_half((unsigned short)(i ? v >> 16 : v & 0xffff)));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
-struct AttendArgs {
-  op_cache_t cache;
-  const Item* items;
-  int32_t n_items, n_heads;
-  int64_t n_tokens;
-  const void* q;
-  void* out;
-  float* lse;
-  int64_t q_tok, q_head, o_tok, o_head, page_stride, layer_at;
-  float scale;
+template <int DP>
+struct Shape {
+  static constexpr int kHalves = DP / 64;
+  static constexpr int kQ = kRows * DP * 2;
+  static constexpr int kSlot = kKeys * DP * 2;
+  static constexpr int kSlots = 65536 / kSlot;
+  static constexpr int kSmem = kQ + kSlots * kSlot + 1024;
+  static constexpr int kColumns = 256;                    // of TMEM: O, then two buffers of S
 };
 
-// A warp takes one query head: its lanes hold four elements each and go through the
-// keys one by one, with the running maximum and sum.
-template <class T>
-__global__ void __launch_bounds__(128) attend_kernel(AttendArgs a) {
-  const int64_t w = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
-  const int lane = threadIdx.x & 31;
-  if (w >= a.n_tokens * a.n_heads) return;
-  const int64_t t = w / a.n_heads;
-  const int32_t h = int32_t(w % a.n_heads), hk = h / (a.n_heads / a.cache.n_kv_heads), D = a.cache.head_dim;
-  int32_t lo = 0, hi = a.n_items - 1;   // the last item that starts at or before t (those without queries share a start)
-  while (lo < hi) {
-    const int32_t mid = (lo + hi + 1) / 2;
-    if (a.items[mid].tok0 <= t) lo = mid;
-    else hi = mid - 1;
-  }
-  const Item it = a.items[lo];
-  const int64_t see = (int64_t)it.kv - it.n_q + (t - it.tok0) + 1;
-  float q[4], o[4] = {}, m = -INFINITY, l = 0.f;
-  for (int j = 0; j < 4; ++j) {
-    const int d = lane * 4 + j;
-    q[j] = d < D ? up(static_cast<const T*>(a.q)[t * a.q_tok + h * a.q_head + d]) * a.scale : 0.f;
-  }
-  for (int64_t k = 0; k < see; ++k) {
-    const int32_t page = a.cache.table[int64_t(it.row) * a.cache.max_pages + k / a.cache.page_tokens];
-    if (page < 0 || page >= a.cache.n_pages) continue;
-    const T* key = static_cast<const T*>(a.cache.pool) + page * a.page_stride + a.layer_at +
-                   (int64_t(hk) * a.cache.page_tokens + k % a.cache.page_tokens) * D;
-    const T* val = key + int64_t(a.cache.n_kv_heads) * a.cache.page_tokens * D;
-    float s = 0.f, v[4];
-    for (int j = 0; j < 4; ++j) {
-      const int d = lane * 4 + j;
-      s += d < D ? q[j] * up(key[d]) : 0.f;
-      v[j] = d < D ? up(val[d]) : 0.f;
+// Place of V_j (and of K_j) in the order of copies, of n steps.
+__device__ __forceinline__ int order_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int order_v(int j, int n) { return j == n - 1 ? 2 * n - 1 : 2 * j + 2; }
+
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_constant__ CUtensorMap map_q,
+                                                             const __grid_constant__ CUtensorMap map_kv,
+                                                             const __grid_constant__ AttendArgs a) {
+  using S = Shape<DP>;
+  extern __shared__ unsigned char raw[];
+  __shared__ uint64_t bars[2 * S::kSlots + 6];
+  __shared__ uint32_t tmem_at, failed_word, keep_o, bad[2];
+  volatile uint32_t* failed = &failed_word;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const Item it = a.items[blockIdx.x];
+  const int32_t hk = blockIdx.y;
+  const int32_t rows = it.n_tok * a.group;
+  const int32_t first = it.lo / kKeys, n = it.hi > it.lo ? (it.hi + kKeys - 1) / kKeys - first : 0;
+
+  if (n == 0) {   // queries that see nothing
+    for (int r = threadIdx.x; r < rows; r += kThreads) {
+      const int64_t t = it.tok0 + r / a.group;
+      const int32_t h = hk * a.group + r % a.group;
+      T* o = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+      for (int d = 0; d < a.dim; d += 8) *reinterpret_cast<uint4*>(o + d) = uint4{};
+      if (a.lse) a.lse[t * a.n_heads + h] = -INFINITY;
     }
-    for (int x = 16; x; x /= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
-    const float n = fmaxf(m, s), f = m == n ? 1.f : expf(m - n), p = expf(s - n);
-    l = l * f + p;
-    for (int j = 0; j < 4; ++j) o[j] = o[j] * f + p * v[j];
-    m = n;
+    return;
   }
-  for (int j = 0; j < 4; ++j) {
-    const int d = lane * 4 + j;
-    if (d < D) down(l == 0.f ? 0.f : o[j] / l, static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head + d);
+
+  const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
+  unsigned char* base = raw + (smem - smem_addr(raw));
+  const uint32_t slots = smem + S::kQ;
+  const uint32_t full = smem_addr(bars), empty = full + 8 * S::kSlots, q_full = empty + 8 * S::kSlots,
+                 s_full = q_full + 8, p_ready = s_full + 16, o_done = p_ready + 16;
+  if (warp == 4 && lane == 0) {
+    prefetch_map(&map_q);
+    prefetch_map(&map_kv);
+    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+    bar_init(q_full, 1);
+    bar_init(s_full, 1), bar_init(s_full + 8, 1);
+    bar_init(p_ready, 4), bar_init(p_ready + 8, 4);
+    bar_init(o_done, 1);
+    failed_word = keep_o = bad[0] = bad[1] = 0;
+    fence_bar_init();
   }
-  if (a.lse && lane == 0) a.lse[t * a.n_heads + h] = l == 0.f ? -INFINITY : m + logf(l);
+  if (warp == 5) tmem_alloc<1>(smem_addr(&tmem_at), S::kColumns);
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = tmem_at, tmem_s = tmem + 128;
+
+  if (warp == 4) {
+    const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
+    if (lane == 0) {
+      const int32_t tile_rows = kRows / a.group * a.group;
+      bar_expect(q_full, tile_rows * 128 * S::kHalves);
+      for (int h = 0; h < S::kHalves; ++h) load_3d(smem + h * (kRows * 128), &map_q, h * 64, hk * a.group, it.tok0, q_full);
+    }
+    // a lane brings one box of a slot: its keys, and 64 columns
+    const int boxes = kKeys / box, mine = lane / S::kHalves, half = lane % S::kHalves;
+    int issued = 0;
+    bool go = true;
+    for (int e = 0; e < 2 * n && go; ++e) {
+      // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
+      const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
+      const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
+      const int slot = e % S::kSlots;
+      const int32_t k0 = (first + j) * kKeys;
+      const int from = it.lo > k0 ? (it.lo - k0) / box : 0;
+      const int to = it.hi - k0 < kKeys ? (it.hi - k0 + box - 1) / box : boxes;
+      const int32_t key = k0 + mine * box;
+      const bool here = mine >= from && mine < to;
+      int32_t page = here ? a.table[int64_t(it.row) * a.max_pages + key / a.page_tokens] : -1;
+      if (page < 0 || page >= a.n_pages) page = a.n_pages;   // no such page: read as zeros
+      if (lane == 0) {
+        go = bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed);
+        if (go) bar_expect(full + 8 * slot, (to - from) * box * 128 * S::kHalves);
+      }
+      go = __shfl_sync(0xffffffffu, go, 0);
+      if (!go) break;
+      if (here)
+        load_3d(slots + slot * S::kSlot + half * (kKeys * 128) + mine * box * 128, &map_kv, half * 64,
+                hk * a.page_tokens + (key & (a.page_tokens - 1)), page * a.planes + a.plane + is_v, full + 8 * slot);
+      ++issued;
+    }
+    if (*failed && lane == 0) {   // the copies in flight still have to land: a bounded wait for each
+      uint32_t quiet = 0;
+      for (int e = issued < S::kSlots ? 0 : issued - S::kSlots; e < issued; ++e)
+        bar_wait(full + 8 * (e % S::kSlots), (e / S::kSlots) & 1, &quiet);
+      bar_wait(q_full, 0, &quiet);
+    }
+    __syncwarp();
+  } else if (warp == 5) {
+    if (lane == 0) {
+      constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+      constexpr uint32_t desc_s = mma_desc(kBf16, kRows, kKeys, false), desc_o = mma_desc(kBf16, kRows, DP, true);
+      auto scores = [&](int j) {
+        const int e = order_k(j), slot = e % S::kSlots;
+        if (!bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
+        tc_after_sync();
+        const uint32_t k = slots + slot * S::kSlot;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+          mma_ss<1>(tmem_s + (j & 1) * kKeys, tile_k(smem + (i / 4) * (kRows * 128)) + 2 * (i % 4),
+                    tile_k(k + (i / 4) * (kKeys * 128)) + 2 * (i % 4), desc_s, i > 0);
+        mma_commit(empty + 8 * slot);
+        mma_commit(s_full + 8 * (j & 1));
+        return true;
+      };
+      bool go = bar_wait(q_full, 0, failed) && scores(0) && (n < 2 || scores(1));
+      for (int j = 0; go && j < n; ++j) {
+        const int e = order_v(j, n), slot = e % S::kSlots;
+        if (!bar_wait(p_ready + 8 * (j & 1), (j >> 1) & 1, failed) ||
+            !bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed))
+          break;
+        tc_after_sync();
+        const uint64_t v = tile_n(slots + slot * S::kSlot, kKeys * 128);
+        const bool add = j > 0 || *reinterpret_cast<volatile uint32_t*>(&keep_o);
+#pragma unroll
+        for (int i = 0; i < kKeys / 16; ++i)
+          mma_ts(tmem, tmem_s + (j & 1) * kKeys + i * 8, v + i * (16 * 128 / 16), desc_o, add || i > 0);
+        mma_commit(empty + 8 * slot);
+        mma_commit(o_done);
+        // S_{j+2} takes the place of P_j: once its product is done
+        if (j + 2 < n) go = bar_wait(o_done, j & 1, failed) && scores(j + 2);
+      }
+      // the last arrival that nothing else waits for
+      bar_wait(empty + 8 * ((2 * n - 1) % S::kSlots), ((2 * n - 1) / S::kSlots) & 1, failed);
+    }
+    __syncwarp();
+  } else {
+    const int r = threadIdx.x;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const int32_t tok = r / a.group;
+    const float c = a.scale2;
+    constexpr float kBias = std::is_same<T, __half>::value ? 7.f : 0.f;   // p is at most 2^(8 + kBias)
+    // the keys that this row sees end here; rows beyond the tile's see what the last one does
+    const int32_t own = tok < it.n_tok ? tok : it.n_tok - 1;
+    const int32_t end = it.pos0 + own + 1 < it.hi ? it.pos0 + own + 1 : it.hi;
+    const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
+    float m = -INFINITY, l = 0.f;
+    for (int j = 0; j < n; ++j) {
+      const int32_t k0 = (first + j) * kKeys;
+      bar_wait(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
+      __syncwarp();
+      tc_after_sync();
+      const uint32_t s_at = tmem_s + lanes + (j & 1) * kKeys;
+      uint32_t lo[32], hi[32];
+      tmem_load32(s_at, lo);
+      tmem_load32(s_at + 32, hi);
+      tmem_wait_load();
+      tmem_loaded(lo);
+      tmem_loaded(hi);
+      if (a.negative) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) lo[i] ^= 0x80000000u, hi[i] ^= 0x80000000u;
+      }
+      const bool masked = k0 < it.lo || k0 + kKeys > all_see;
+      // scores that this row does not see become -inf, and their p is set to 0 below
+      uint64_t sees = ~0ull;
+      if (masked) {
+        const int below = it.lo > k0 ? it.lo - k0 : 0, upto = end - k0 < 0 ? 0 : end - k0 < kKeys ? end - k0 : kKeys;
+        sees = upto <= below ? 0 : (upto == 64 ? ~0ull : (1ull << upto) - 1) & ~((1ull << below) - 1);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          if (!(sees >> i & 1)) lo[i] = 0xff800000u;
+          if (!(sees >> (i + 32) & 1)) hi[i] = 0xff800000u;
+        }
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        mx[0] = fmaxf(mx[0], __uint_as_float(lo[i]));
+        mx[1] = fmaxf(mx[1], __uint_as_float(lo[i + 1]));
+        mx[2] = fmaxf(mx[2], __uint_as_float(hi[i]));
+        mx[3] = fmaxf(mx[3], __uint_as_float(hi[i + 1]));
+      }
+      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+      const float here = top == -INFINITY ? -INFINITY : top * c;   // c may be 0
+      const bool raise = here > m + 8.f || (m == -INFINITY && here > -INFINITY);
+      if (__any_sync(0xffffffffu, raise)) {
+        const float f = raise ? (m == -INFINITY ? 0.f : exp2_fast(m - here)) : 1.f;
+        if (raise) m = here;
+        l *= f;
+        if (j > 0) {
+          // (S_j was computed after the product of step j - 2 was done)
+          bar_wait(o_done, (j - 1) & 1, failed);
+          __syncwarp();
+          tc_after_sync();
+#pragma unroll 1
+          for (int d = 0; d < DP; d += 32) {
+            uint32_t o[32];
+            tmem_load32(tmem + lanes + d, o);
+            tmem_wait_load();
+            tmem_loaded(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_store32(tmem + lanes + d, o);
+          }
+          tmem_wait_store();
+        }
+      }
+      // p, packed over the first half of the scores' registers
+      const float shift = m == -INFINITY ? 0.f : kBias - m;
+      float sum[4] = {};
+      uint32_t p[32];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float x = exp2_fast(fmaf(__uint_as_float(lo[2 * i]), c, shift));
+        float y = exp2_fast(fmaf(__uint_as_float(lo[2 * i + 1]), c, shift));
+        float z = exp2_fast(fmaf(__uint_as_float(hi[2 * i]), c, shift));
+        float w = exp2_fast(fmaf(__uint_as_float(hi[2 * i + 1]), c, shift));
+        if (masked) {
+          if (!(sees >> (2 * i) & 1)) x = 0.f;
+          if (!(sees >> (2 * i + 1) & 1)) y = 0.f;
+          if (!(sees >> (2 * i + 32) & 1)) z = 0.f;
+          if (!(sees >> (2 * i + 33) & 1)) w = 0.f;
+        }
+        sum[0] += x, sum[1] += y, sum[2] += z, sum[3] += w;
+        p[i] = pack(T(), x, y);
+        p[16 + i] = pack(T(), z, w);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tmem_store32(s_at, p);
+      tmem_wait_store();
+      if (masked) {
+        // Keys outside the item: whatever lies there must not meet the zeros of P.  So must
+        // no value that is not finite and that some row does not see.
+        const int e = order_v(j, n), slot = e % S::kSlots;
+        bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed);
+        unsigned char* v = base + S::kQ + slot * S::kSlot;
+        const int below = it.lo > k0 ? it.lo - k0 : 0, upto = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
+        for (int i = r; i < kKeys * S::kHalves; i += 128) {
+          const int key = i % kKeys;
+          if (key >= below && key < upto) continue;
+          uint4* at = reinterpret_cast<uint4*>(v + (i / kKeys) * (kKeys * 128) + key * 128);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) at[q] = uint4{};
+        }
+        if (k0 + kKeys > all_see && all_see < it.hi) {
+          constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
+          for (int i = r; i < kKeys * S::kHalves; i += 128) {
+            const int key = i % kKeys;
+            if (key < below || key >= upto) continue;
+            const uint4* at = reinterpret_cast<const uint4*>(v + (i / kKeys) * (kKeys * 128) + key * 128);
+            bool odd = false;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const uint4 x = at[q];
+              const uint32_t w[4] = {x.x & kExp, x.y & kExp, x.z & kExp, x.w & kExp};
+#pragma unroll
+              for (int b = 0; b < 4; ++b) odd |= (w[b] & 0xffff) == (kExp & 0xffff) || w[b] >> 16 == kExp >> 16;
+            }
+            if (odd) atomicOr(&bad[key >> 5], 1u << (key & 31));
+          }
+          part_sync(1, 128);
+          uint64_t found = (uint64_t)*reinterpret_cast<volatile uint32_t*>(&bad[1]) << 32 |
+                           *reinterpret_cast<volatile uint32_t*>(&bad[0]);
+          if (found) {
+            // Their share of O is added here, to the rows that see them; the products get zeros.
+            if (j > 0) {
+              bar_wait(o_done, (j - 1) & 1, failed);
+              __syncwarp();
+              tc_after_sync();
+            }
+#pragma unroll 1
+            for (int d = 0; d < DP; d += 32) {
+              uint32_t o[32];
+              tmem_load32(tmem + lanes + d, o);
+              tmem_wait_load();
+              tmem_loaded(o);
+              if (j == 0) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0;
+              }
+#pragma unroll 1
+              for (uint64_t rest = found; rest; rest &= rest - 1) {
+                const int key = __ffsll((long long)rest) - 1;
+                uint32_t pair;
+                tmem_load1(s_at + key / 2, &pair);
+                tmem_wait_load();
+                asm volatile("" : "+r"(pair));
+                if (sees >> key & 1) {
+                  const float weight = unpack(T(), pair, key & 1);
+                  const T* row = reinterpret_cast<const T*>(v + (d / 64) * (kKeys * 128) + key * 128);
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) {
+                    const int x = (d & 32) + i;
+                    o[i] = __float_as_uint(fmaf(weight, up(row[(((x / 8) ^ (key & 7)) * 8) + x % 8]), __uint_as_float(o[i])));
+                  }
+                }
+                __syncwarp();
+              }
+              tmem_store32(tmem + lanes + d, o);
+            }
+            tmem_wait_store();
+            part_sync(1, 128);
+            for (int i = r; i < kKeys * S::kHalves; i += 128)
+              if (found >> (i % kKeys) & 1) {
+                uint4* at = reinterpret_cast<uint4*>(v + (i / kKeys) * (kKeys * 128) + (i % kKeys) * 128);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) at[q] = uint4{};
+              }
+            if (r == 0) {
+              bad[0] = bad[1] = 0;
+              if (j == 0) keep_o = 1;
+            }
+            part_sync(1, 128);
+          }
+        }
+        fence_async();
+      }
+      tc_before_sync();
+      __syncwarp();
+      if (lane == 0) bar_arrive(p_ready + 8 * (j & 1));
+    }
+    // one phase after the other: a barrier tells a phase from the one before it only
+    if (n > 1) bar_wait(o_done, (n - 2) & 1, failed);
+    bar_wait(o_done, (n - 1) & 1, failed);
+    __syncwarp();
+    tc_after_sync();
+    const bool in = tok < it.n_tok;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float lse2 = l == 0.f ? -INFINITY : m - kBias + log2f(l);
+    const int32_t h = hk * a.group + r - tok * a.group;
+    const int64_t t = it.tok0 + tok;
+    const int64_t part = hk * a.part_rows + it.part + r;
+    T* out = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+    float* part_o = a.part_o + part * a.dim;
+    if (in) {
+      if (it.part >= 0) a.part_lse[part] = lse2;
+      else if (a.lse) a.lse[t * a.n_heads + h] = lse2 * 0.69314718055994531f;
+    }
+#pragma unroll 1
+    for (int d = 0; d < a.dim; d += 32) {
+      uint32_t o[32];
+      tmem_load32(tmem + lanes + d, o);
+      tmem_wait_load();
+      tmem_loaded(o);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(l == 0.f ? 0.f : __uint_as_float(o[i]) * inv);
+      if (in && it.part >= 0) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          if (d + i < a.dim) __stcg(reinterpret_cast<uint4*>(part_o + d + i), uint4{o[i], o[i + 1], o[i + 2], o[i + 3]});
+      } else if (in) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+          if (d + i < a.dim) {
+            uint4 v;
+            v.x = pack(T(), __uint_as_float(o[i]), __uint_as_float(o[i + 1]));
+            v.y = pack(T(), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+            v.z = pack(T(), __uint_as_float(o[i + 4]), __uint_as_float(o[i + 5]));
+            v.w = pack(T(), __uint_as_float(o[i + 6]), __uint_as_float(o[i + 7]));
+            *reinterpret_cast<uint4*>(out + d + i) = v;
+          }
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  if (warp == 5) tmem_free<1>(tmem, S::kColumns);
+  if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
+}
+
+// Joins the parts of a query head: o = sum_i 2^(lse_i - L) o_i with L = log2 sum_i 2^lse_i.  A
+// warp takes one, four elements a lane.
+template <class T>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a) {
+  const int lane = threadIdx.x & 31;
+  const Join j = a.joins[blockIdx.x];
+  const int32_t all = j.n_tok * a.n_heads;
+  for (int32_t w = blockIdx.y * 4 + threadIdx.x / 32; w < all; w += gridDim.y * 4) {
+    const int32_t tok = w / a.n_heads, h = w - tok * a.n_heads, hk = h / a.group;
+    const int32_t r = tok * a.group + h - hk * a.group;
+    const int32_t n = j.n[0] + j.n[1];
+    auto row_of = [&](int32_t i) {
+      return hk * a.part_rows + r +
+             (i < j.n[0] ? j.base[0] + (int64_t)i * j.step[0] : j.base[1] + (int64_t)(i - j.n[0]) * j.step[1]);
+    };
+    float top = -INFINITY;
+    for (int32_t i = lane; i < n; i += 32) top = fmaxf(top, __ldcg(a.part_lse + row_of(i)));
+#pragma unroll
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float4 o = {};
+    float sum = 0.f;
+#pragma unroll 4
+    for (int32_t i = 0; i < n; ++i) {
+      const int64_t row = row_of(i);
+      const float f = exp2f(__ldcg(a.part_lse + row) - ref);
+      sum += f;
+      if (lane * 4 < a.dim) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + row * a.dim + lane * 4));
+        o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
+      }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t t = j.tok0 + tok;
+    if (lane * 4 < a.dim) {
+      uint2 v;
+      v.x = pack(T(), o.x * inv, o.y * inv);
+      v.y = pack(T(), o.z * inv, o.w * inv);
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head + lane * 4) = v;
+    }
+    if (a.lse && lane == 0) a.lse[t * a.n_heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+  }
 }
 
 bool desc_ok(const op_attend_desc_t* d) {
@@ -105,6 +539,139 @@ bool desc_ok(const op_attend_desc_t* d) {
   return true;
 }
 
+// The work items of a batch, cut so that they fill the SMs (two blocks each).
+struct Work {
+  std::vector<Item> items;
+  std::vector<Join> joins;
+  int64_t part_rows = 0;
+};
+
+// A run of queries against a run of keys, before it is cut along the keys.
+struct Run {
+  int32_t tok0, n_tok, row, lo, hi, pos0;
+  bool pooled;        // over the requests of a group
+  int32_t steps() const { return hi > lo ? (hi + kKeys - 1) / kKeys - lo / kKeys : 0; }
+};
+
+constexpr int64_t kMinSteps = 4;   // of an item that is cut
+
+void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
+  const int32_t group = d.n_heads / d.n_kv_heads, tile = kRows / group;
+  std::vector<Run> runs;
+  const int32_t ng = d.n_groups > 0 ? d.n_groups : 1;
+  int32_t tok = 0;
+  for (int32_t g = 0; g < ng; ++g) {
+    const int32_t b0 = d.n_groups > 0 ? d.group_off[g] : 0, b1 = d.n_groups > 0 ? d.group_off[g + 1] : d.n_batch;
+    const int32_t prefix = d.n_groups > 0 ? d.prefix[g] : 0;
+    int64_t tokens = 0, apart = 0;
+    int32_t lead = -1;
+    for (int32_t b = b0; b < b1; ++b) {
+      tokens += d.q_len[b];
+      apart += (d.q_len[b] + tile - 1) / tile;
+      if (lead < 0 && d.q_len[b] > 0) lead = b;
+    }
+    // together, the prefix is read once a tile of all queries; apart, once a tile of each request's
+    const bool pool = prefix >= kKeys && (tokens + tile - 1) / tile < apart;
+    if (pool)
+      for (int64_t t = 0; t < tokens; t += tile)
+        runs.push_back(Run{int32_t(tok + t), int32_t(std::min<int64_t>(tile, tokens - t)), d.seq ? d.seq[lead] : lead, 0,
+                           prefix, kSeesAll, true});
+    for (int32_t b = b0; b < b1; ++b) {
+      const int32_t q = d.q_len[b], before = d.kv_len[b] - q;
+      for (int32_t t = 0; t < q; t += tile) {
+        const int32_t n = std::min(tile, q - t), lo = pool ? prefix : 0;
+        runs.push_back(Run{tok + t, n, d.seq ? d.seq[b] : b, lo, std::max(before + t + n, lo), before + t, false});
+      }
+      tok += q;
+    }
+  }
+  int64_t steps = 0;
+  for (const Run& r : runs) steps += r.steps();
+  const int64_t most = std::max(kMinSteps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
+  // cut; then longest first, so that short items fill the end (equal ones keep their order:
+  // tiles that read the same keys stay together)
+  struct Cut {
+    int32_t run, part, parts;
+  };
+  std::vector<int32_t> parts(runs.size()), base(runs.size(), -1), joined(runs.size(), 0);
+  for (size_t i = 0; i < runs.size(); ++i) parts[i] = int32_t(std::max<int64_t>(1, (runs[i].steps() + most - 1) / most));
+  // a request's queries are joined where a pooled run covers them too, or where they are cut
+  size_t pooled = 0, pooled_end = 0;   // runs of the current group's pool
+  for (size_t i = 0; i < runs.size(); ++i) {
+    if (runs[i].pooled) {
+      if (i == 0 || !runs[i - 1].pooled) pooled = i;
+      pooled_end = i + 1;
+      base[i] = int32_t(w->part_rows);
+      w->part_rows += (int64_t)parts[i] * runs[i].n_tok * group;
+      continue;
+    }
+    const Run& r = runs[i];
+    const bool covered = pooled_end > pooled && r.lo > 0 && r.tok0 >= runs[pooled].tok0 &&
+                         r.tok0 < runs[pooled_end - 1].tok0 + runs[pooled_end - 1].n_tok;
+    if (!covered && parts[i] == 1) continue;
+    base[i] = int32_t(w->part_rows);
+    w->part_rows += (int64_t)parts[i] * r.n_tok * group;
+    for (int32_t t = r.tok0; t < r.tok0 + r.n_tok;) {
+      Join jn{};
+      jn.tok0 = t;
+      jn.n_tok = r.tok0 + r.n_tok - t;
+      if (covered) {
+        const size_t q = pooled + (t - runs[pooled].tok0) / tile;
+        jn.n_tok = std::min(jn.n_tok, runs[q].tok0 + runs[q].n_tok - t);
+        jn.base[0] = base[q] + (t - runs[q].tok0) * group;
+        jn.step[0] = runs[q].n_tok * group;
+        jn.n[0] = parts[q];
+      }
+      jn.base[1] = base[i] + (t - r.tok0) * group;
+      jn.step[1] = r.n_tok * group;
+      jn.n[1] = parts[i];
+      w->joins.push_back(jn);
+      t += jn.n_tok;
+    }
+  }
+  std::vector<Cut> cuts;
+  for (size_t i = 0; i < runs.size(); ++i) {
+    if (runs[i].pooled && i > 0 && runs[i - 1].pooled && runs[i - 1].row == runs[i].row && parts[i - 1] == parts[i]) continue;
+    size_t last = i + 1;    // tiles of one pool: part by part, so that those of one part meet in the L2 cache
+    while (runs[i].pooled && last < runs.size() && runs[last].pooled && runs[last].row == runs[i].row && parts[last] == parts[i]) ++last;
+    for (int32_t p = 0; p < parts[i]; ++p)
+      for (size_t k = i; k < last; ++k) cuts.push_back(Cut{int32_t(k), p, parts[k]});
+  }
+  std::stable_sort(cuts.begin(), cuts.end(), [&](const Cut& x, const Cut& y) {
+    return runs[x.run].steps() / x.parts > runs[y.run].steps() / y.parts;
+  });
+  for (const Cut& cut : cuts) {
+    const Run& r = runs[cut.run];
+    const int64_t s0 = r.lo / kKeys, n = r.steps();
+    const int64_t a = s0 + n * cut.part / cut.parts, b = s0 + n * (cut.part + 1) / cut.parts;
+    Item it{};
+    it.tok0 = r.tok0, it.n_tok = r.n_tok, it.row = r.row, it.pos0 = r.pos0;
+    it.lo = std::max(r.lo, int32_t(a * kKeys));
+    it.hi = int32_t(std::min<int64_t>(r.hi, b * kKeys));
+    if (n == 0) it.lo = it.hi = 0;
+    it.part = base[cut.run] < 0 ? -1 : base[cut.run] + cut.part * r.n_tok * group;
+    w->items.push_back(it);
+  }
+}
+
+template <class T, int DP>
+cudaError_t launch(const op_attend_plan_t& p, const CUtensorMap& q, const CUtensorMap& kv, const AttendArgs& a, cudaStream_t st) {
+  static gsim::OncePerDevice once;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
+  auto kernel = attend_kernel<T, DP>;
+  if (!once.done(dev, [&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kSmem) == cudaSuccess;
+      }))
+    return cudaErrorInvalidValue;
+  kernel<<<dim3((unsigned)p.n_items, (unsigned)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(q, kv, a);
+  if (p.n_joins > 0) {
+    const int64_t warps = (int64_t)std::min<int64_t>(p.n_tokens, kRows) * p.n_heads;
+    attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>((warps + 3) / 4, 64)), 128, 0, st>>>(a);
+  }
+  return cudaGetLastError();
+}
+
 }  // namespace
 }  // namespace gop
 
@@ -113,28 +680,37 @@ using namespace gop;
 extern "C" {
 
 int op_attend_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend_plan_t* plan, int32_t* items,
-                   size_t item_bytes) {
+                   size_t item_bytes) try {
   if (!desc_ok(d) || !plan || n_sm < 1) return GMG_EINVAL;
+  Work w;
+  plan_items(*d, n_sm, &w);
+  if (w.part_rows > 0x7fffffff || w.items.size() > 0x7fffffff) return GMG_ERANGE;
   op_attend_plan_t p{};
   p.n_batch = d->n_batch;
   p.n_heads = d->n_heads;
   p.n_kv_heads = d->n_kv_heads;
   p.head_dim = d->head_dim;
   p.page_tokens = d->page_tokens;
-  p.n_items = d->n_batch;
-  p.plan_bytes = sizeof(Item) * size_t(d->n_batch);
+  p.n_items = int32_t(w.items.size());
+  p.n_joins = int32_t(w.joins.size());
   for (int32_t b = 0; b < d->n_batch; ++b) {
-    const int32_t row = d->seq ? d->seq[b] : b;
-    if (items && item_bytes >= p.plan_bytes)
-      reinterpret_cast<Item*>(items)[b] = Item{int32_t(p.n_tokens), d->q_len[b], row, d->kv_len[b]};
     p.n_tokens += d->q_len[b];
-    if (row > p.max_seq) p.max_seq = row;
-    if (d->kv_len[b] > p.max_kv) p.max_kv = d->kv_len[b];
+    p.max_seq = std::max(p.max_seq, d->seq ? d->seq[b] : b);
+    p.max_kv = std::max(p.max_kv, d->kv_len[b]);
   }
-  p.work_bytes = 256;
-  if (items && item_bytes < p.plan_bytes) return GMG_EWS;
+  p.part_rows = w.part_rows;
+  p.plan_bytes = sizeof(Item) * w.items.size() + sizeof(Join) * w.joins.size();
+  p.work_bytes = 256 + size_t(w.part_rows) * d->n_kv_heads * (d->head_dim + 1) * 4;
+  if (items) {
+    if (item_bytes < p.plan_bytes) return GMG_EWS;
+    Item* to = reinterpret_cast<Item*>(items);
+    std::copy(w.items.begin(), w.items.end(), to);
+    std::copy(w.joins.begin(), w.joins.end(), reinterpret_cast<Join*>(to + w.items.size()));
+  }
   *plan = p;
   return GMG_OK;
+} catch (const std::bad_alloc&) {
+  return GMG_ENOMEM;
 }
 
 int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cache_t* cache, int32_t layer,
@@ -143,29 +719,57 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
   if (!plan || !cache_ok(cache) || layer < 0 || layer >= cache->n_layers) return GMG_EINVAL;
   if (plan->head_dim != cache->head_dim || plan->n_kv_heads != cache->n_kv_heads ||
       plan->page_tokens != cache->page_tokens || plan->max_seq >= cache->n_seq ||
-      plan->max_kv > int64_t(cache->max_pages) * cache->page_tokens)
+      plan->max_kv > int64_t(cache->max_pages) * cache->page_tokens || plan->n_kv_heads > 65535)
     return GMG_EINVAL;
   if (plan->n_tokens == 0) return GMG_OK;
-  if (!d_items || !q || !out || !aligned(q, q_tok, q_head, 2) || !aligned(out, out_tok, out_head, 2)) return GMG_EINVAL;
+  if (!d_items || (reinterpret_cast<uintptr_t>(d_items) & 15) || !q || !out || !aligned(q, q_tok, q_head, 2) ||
+      !aligned(out, out_tok, out_head, 2) || !(scale == scale))
+    return GMG_EINVAL;
   if (!work || (reinterpret_cast<uintptr_t>(work) & 255) || work_bytes < plan->work_bytes) return GMG_EWS;
+  const int64_t plane = int64_t(cache->n_kv_heads) * cache->page_tokens;   // rows of a page's K or V
+  const int64_t planes = int64_t(cache->n_pages) * cache->n_layers * 2;
+  if (planes + 2 * cache->n_layers > 0x7fffffff || plane > 0x7fffffff) return GMG_ERANGE;
   AttendArgs a{};
-  a.cache = *cache;
   a.items = reinterpret_cast<const Item*>(d_items);
-  a.n_items = plan->n_items;
+  a.joins = reinterpret_cast<const Join*>(a.items + plan->n_items);
+  a.table = cache->table;
+  a.status = cache->status;
+  a.max_pages = cache->max_pages;
+  a.page_tokens = cache->page_tokens;
+  a.n_pages = cache->n_pages;
+  a.planes = cache->n_layers * 2;
+  a.plane = layer * 2;
   a.n_heads = plan->n_heads;
-  a.n_tokens = plan->n_tokens;
-  a.q = q, a.q_tok = q_tok, a.q_head = q_head;
+  a.n_kv = plan->n_kv_heads;
+  a.group = plan->n_heads / plan->n_kv_heads;
+  a.dim = plan->head_dim;
+  a.scale2 = fabsf(scale) * 1.4426950408889634f;
+  a.negative = scale < 0.f;
   a.out = out, a.o_tok = out_tok, a.o_head = out_head;
   a.lse = lse;
-  a.scale = scale;
-  const int64_t plane = int64_t(cache->n_kv_heads) * cache->page_tokens * cache->head_dim;
-  a.page_stride = 2 * cache->n_layers * plane;
-  a.layer_at = 2 * layer * plane;
+  a.part_rows = plan->part_rows;
+  a.part_o = reinterpret_cast<float*>(work);
+  a.part_lse = a.part_o + plan->part_rows * plan->n_kv_heads * plan->head_dim;
+  CUtensorMap map_q, map_kv;
+  const int32_t box = cache->page_tokens < kKeys ? cache->page_tokens : kKeys;
+  const int64_t size_q[3] = {plan->head_dim, plan->n_heads, plan->n_tokens};
+  // strides of a single head or token are not used, but have to be legal ones
+  const int64_t stride_q[2] = {plan->n_heads > 1 ? q_head : plan->head_dim, plan->n_tokens > 1 ? q_tok : plan->head_dim};
+  const int32_t box_q[3] = {64, a.group, kRows / a.group};
+  const int64_t size_kv[3] = {plan->head_dim, plane, planes}, stride_kv[2] = {plan->head_dim, plane * plan->head_dim};
+  const int32_t box_kv[3] = {64, box, 1};
+  if (!make_map(&map_q, cache->dtype, 3, q, size_q, stride_q, box_q) ||
+      !make_map(&map_kv, cache->dtype, 3, cache->pool, size_kv, stride_kv, box_kv))
+    return GMG_ECUDA;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const int64_t blocks = (plan->n_tokens * plan->n_heads + 3) / 4;
-  if (cache->dtype == GMG_OP_BF16) attend_kernel<__nv_bfloat16><<<(unsigned)blocks, 128, 0, st>>>(a);
-  else attend_kernel<__half><<<(unsigned)blocks, 128, 0, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? GMG_OK : GMG_ECUDA;
+  cudaError_t e;
+  if (cache->dtype == GMG_OP_BF16)
+    e = plan->head_dim <= 64 ? launch<__nv_bfloat16, 64>(*plan, map_q, map_kv, a, st)
+                             : launch<__nv_bfloat16, 128>(*plan, map_q, map_kv, a, st);
+  else
+    e = plan->head_dim <= 64 ? launch<__half, 64>(*plan, map_q, map_kv, a, st)
+                             : launch<__half, 128>(*plan, map_q, map_kv, a, st);
+  return e == cudaSuccess ? GMG_OK : GMG_ECUDA;
 }
 
 }  // extern "C"

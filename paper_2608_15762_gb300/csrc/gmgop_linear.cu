@@ -52,6 +52,44 @@ __device__ __forceinline__ void finish(const op_linear_t& a, int64_t row, int64_
   down(v, static_cast<T*>(a.y) + row * a.y_row + col);
 }
 
+// Four neighbouring columns of a row; one 8-byte store where the row allows it.
+template <class T, bool kGate>
+__device__ __forceinline__ void finish4(const op_linear_t& a, int64_t row, int64_t col, const float* v, const float* g) {
+  const T* bias = static_cast<const T*>(a.bias) + col;
+  const T* gate_bias = static_cast<const T*>(a.gate_bias) + col;
+  const T* res = static_cast<const T*>(a.residual) + row * a.residual_row + col;
+  T* y = static_cast<T*>(a.y) + row * a.y_row + col;
+  struct alignas(8) Four {
+    T v[4];
+  } old, b, gb, out;
+  const int n = a.n - col < 4 ? int(a.n - col) : 4;
+  if (n <= 0) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i >= n) break;
+    if (a.residual) old.v[i] = res[i];
+    if (a.bias) b.v[i] = bias[i];
+    if (kGate && a.gate_bias) gb.v[i] = gate_bias[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i >= n) break;
+    float r = v[i];
+    if (a.bias) r += up(b.v[i]);
+    if (kGate) r *= act(a.gate_bias ? g[i] + up(gb.v[i]) : g[i], a.act);
+    else r = act(r, a.act);
+    if (a.residual) r += up(old.v[i]);
+    down(r, &out.v[i]);
+  }
+  if (n == 4 && (reinterpret_cast<uintptr_t>(y) & 7) == 0) {
+    *reinterpret_cast<Four*>(y) = out;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) y[i] = out.v[i];
+  }
+}
+
 // ---- operands that start or continue off 16 bytes -------------------------
 
 // A block of 256 threads takes 64 x 64 outputs, a thread 4 x 4, from tiles of 16
@@ -137,6 +175,13 @@ __global__ void __launch_bounds__(128) linear_few_kernel(op_linear_t a) {
   const T* x = static_cast<const T*>(a.x);
   const T* w = static_cast<const T*>(a.w) + col * a.w_row;
   const T* g = kGate ? static_cast<const T*>(a.gate) + col * a.gate_row : nullptr;
+  // what the end needs is on its way while the weight is read
+  T old = T(), b0 = T(), b1 = T();
+  if (lane < M && warp < (kWarps > 1 ? 1 : 4)) {
+    if (a.residual) old = static_cast<const T*>(a.residual)[lane * a.residual_row + col];
+    if (a.bias) b0 = static_cast<const T*>(a.bias)[col];
+    if (kGate && a.gate_bias) b1 = static_cast<const T*>(a.gate_bias)[col];
+  }
   float v[M] = {}, z[M] = {};
   const int64_t whole = a.k & ~int64_t(7), step = 256 * kWarps;
   for (int64_t k0 = (kWarps > 1 ? warp * 256 : 0) + lane * 8; k0 < whole; k0 += step * kAhead) {
@@ -190,7 +235,14 @@ __global__ void __launch_bounds__(128) linear_few_kernel(op_linear_t a) {
   }
 #pragma unroll
   for (int r = 0; r < M; ++r)
-    if (lane == r) finish<T>(a, r, col, v[r], z[r]);
+    if (lane == r) {
+      float y = v[r];
+      if (a.bias) y += up(b0);
+      if (kGate) y *= act(a.gate_bias ? z[r] + up(b1) : z[r], a.act);
+      else y = act(y, a.act);
+      if (a.residual) y += up(old);
+      down(y, static_cast<T*>(a.y) + r * a.y_row + col);
+    }
 }
 
 template <class T, int M, bool kGate>
@@ -229,7 +281,6 @@ template <int NT, bool kGate>
 struct SplitShape {
   static constexpr int kXBytes = NT * kStep * 2;
   static constexpr int kStage = kWeightBytes * (kGate ? 2 : 1) + kXBytes;
-  static constexpr int kPerSm = NT <= 32 ? 2 : 1;
   static constexpr int kStages = (NT <= 32 ? 106 : 212) * 1024 / kStage < 8 ? (NT <= 32 ? 106 : 212) * 1024 / kStage : 8;
   static constexpr int kSmem = kStages * kStage + 1024;
   static constexpr int kColumns = NT * (kGate ? 2 : 1);
@@ -301,8 +352,15 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
         ++issued;
         if (++stage == S::kStages) stage = 0, phase ^= 1;
       }
-      if (*failed) {   // the copies in flight still have to land: a bounded wait for each
-        uint32_t quiet = 0;
+      // every stage comes back before the block ends; after a failure the copies in flight get a
+      // bounded wait each
+      uint32_t quiet = 0;
+      if (!*failed) {
+        for (int i = 0; i < S::kStages; ++i) {
+          if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
+          if (++stage == S::kStages) stage = 0, phase ^= 1;
+        }
+      } else {
         for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
           if (stage == 0) phase ^= 1;
           stage = stage == 0 ? S::kStages - 1 : stage - 1;
@@ -356,24 +414,39 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
   __syncthreads();
   if (warp == 2) tmem_free<1>(tmem, S::kAlloc);
   if (L.split > 1) cluster_sync();
-  for (int r = rank + warp * L.split; r < a.m; r += 8 * L.split) {
-    const uint32_t at = smem + (r * 128 + lane * 4) * 4;
-    float v[4] = {}, g[4] = {};
-#pragma unroll 4
-    for (int32_t w = 0; w < L.split; ++w) {
-      const float4 x = load_peer(at, w);
-      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-      if (kGate) {
-        const float4 y = load_peer(at + NT * 512, w);
-        g[0] += y.x, g[1] += y.y, g[2] += y.z, g[3] += y.w;
+  const int64_t col = (int64_t)tile * 128 + lane * 4;
+  constexpr int R = 4;     // rows at a time, so that their loads overlap
+  for (int r0 = rank + warp * L.split; r0 < a.m; r0 += 8 * R * L.split) {
+    float v[R][4], g[kGate ? R : 1][4];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int r = r0 + 8 * i * L.split;
+      v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0.f;
+      if (kGate) g[kGate ? i : 0][0] = g[kGate ? i : 0][1] = g[kGate ? i : 0][2] = g[kGate ? i : 0][3] = 0.f;
+      if (r >= a.m) continue;
+      const uint32_t at = smem + (r * 128 + lane * 4) * 4;
+#pragma unroll 2
+      for (int32_t w = 0; w < L.split; ++w) {
+        const float4 x = load_peer(at, w);
+        v[i][0] += x.x, v[i][1] += x.y, v[i][2] += x.z, v[i][3] += x.w;
+        if (kGate) {
+          const float4 y = load_peer(at + NT * 512, w);
+          float* z = g[kGate ? i : 0];
+          z[0] += y.x, z[1] += y.y, z[2] += y.z, z[3] += y.w;
+        }
       }
     }
-    const int64_t col = (int64_t)tile * 128 + lane * 4;
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-      if (col + i < a.n) finish<T>(a, r, col + i, v[0], g[0]);
-      v[0] = v[1], v[1] = v[2], v[2] = v[3];
-      g[0] = g[1], g[1] = g[2], g[2] = g[3];
+    for (int i = 0; i < R; ++i) {
+      const int r = r0 + 8 * i * L.split;
+      if (r < a.m) finish4<T, kGate>(a, r, col, v[0], g[0]);
+#pragma unroll
+      for (int j = 0; j + 1 < R; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[j][e] = v[j + 1][e];
+          if (kGate) g[kGate ? j : 0][e] = g[kGate ? j + 1 : 0][e];
+        }
     }
   }
   if (L.split > 1) cluster_sync();   // the others have read this block's sums
@@ -691,10 +764,8 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
       g.x += y.x, g.y += y.y, g.z += y.z, g.w += y.w;
     }
   }
-  finish<T>(a, row, col, v.x, g.x);
-  if (col + 1 < a.n) finish<T>(a, row, col + 1, v.y, g.y);
-  if (col + 2 < a.n) finish<T>(a, row, col + 2, v.z, g.z);
-  if (col + 3 < a.n) finish<T>(a, row, col + 3, v.w, g.w);
+  const float vs[4] = {v.x, v.y, v.z, v.w}, gs[4] = {g.x, g.y, g.z, g.w};
+  finish4<T, kGate>(a, row, col, vs, gs);
 }
 
 int n_sm() {
@@ -801,21 +872,29 @@ cudaError_t launch_split(const op_linear_t& a, int sms, void* work, cudaStream_t
   L.a = a;
   L.steps = int32_t((a.k + kStep - 1) / kStep);
   L.status = static_cast<int32_t*>(work);
-  // as many blocks a tile as fill the SMs once
-  const int64_t tiles = (a.n + 127) / 128, most = (int64_t)sms * S::kPerSm / tiles;
-  L.split = int32_t(most < 1 ? 1 : most > 8 ? 8 : most);
-  if (L.split > L.steps) L.split = L.steps;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(tiles * L.split));
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = S::kSmem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)L.split;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
+  // the widest clusters of which one a tile fits on the GPU at once: a second round costs as
+  // much as the first (6,144 x 1,024, 16 rows, clusters of 6: 12 us, of 3: 7)
+  const int64_t tiles = (a.n + 127) / 128;
+  static int fits[64][9];   // clusters at once, by size; asked once per device
+  for (L.split = L.steps < 8 ? L.steps : 8; L.split > 1; --L.split) {
+    at[0].val.clusterDim.x = (unsigned)L.split;
+    cfg.gridDim = dim3((unsigned)(sms / L.split * L.split));
+    int n = dev < 64 ? fits[dev][L.split] : 0;
+    if (n == 0 && cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) n = 0;
+    if (dev < 64) fits[dev][L.split] = n;
+    if (n >= tiles) break;
+  }
+  at[0].val.clusterDim.x = (unsigned)L.split;
+  cfg.gridDim = dim3((unsigned)(tiles * L.split));
   return cudaLaunchKernelEx(&cfg, kernel, m.w, m.g, m.x, L);
 }
 
