@@ -4,8 +4,9 @@
 // A work item is up to 128 rows (queries of consecutive tokens, all query heads of one
 // key/value head: row = token * heads + head) against a run of keys, 64 a step.  One block
 // takes one item:
-//   warp 4   copies: page by page into a ring of 64-key slots, K_0 K_1 V_0 K_2 V_1 ...
-//   warp 5   products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
+//   warps 4 to 6   copies: page by page into a ring of 64-key slots, K_0 K_1 V_0 K_2 V_1 ...,
+//            a warp every third slot (one warp takes 600 to 1,000 clocks to issue a slot's boxes)
+//   warp 7   products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
 //   warps 0 to 3   softmax: a thread holds one row.  It reads S_j, takes p = exp2(s c - m),
 //            adds the sum, and puts P_j, rounded to the values' type, in S_j's place.
 // S_{j+1} is computed while the softmax works on S_j.  The reference m need not be the exact
@@ -38,7 +39,7 @@ namespace {
 
 constexpr int kKeys = 64;              // a step
 constexpr int kRows = 128;             // of a tile
-constexpr int kThreads = 192;
+constexpr int kThreads = 256, kCopiers = 3;
 constexpr int32_t kSeesAll = 0x7f000000;
 
 struct Item {
@@ -64,8 +65,8 @@ struct AttendArgs {
   int32_t* status;
   int32_t max_pages, page_tokens, n_pages, planes, plane;   // planes of the pool: a page's layers and K, V
   int32_t n_heads, n_kv, group, dim;
-  float scale2;                        // |scale| log2 e
-  int32_t negative;
+  float scale2;                        // |scale| log2 e, > 0
+  int32_t negative;                    // the products take -Q
   void* out;
   int64_t o_tok, o_head;
   float* lse;
@@ -113,12 +114,13 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
                                                              const __grid_constant__ AttendArgs a) {
   using S = Shape<DP>;
   extern __shared__ unsigned char raw[];
-  __shared__ uint64_t bars[2 * S::kSlots + 6];
+  __shared__ uint64_t bars[2 * S::kSlots + 7];
   __shared__ uint32_t tmem_at, failed_word, keep_o, bad[2];
   volatile uint32_t* failed = &failed_word;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const Item it = a.items[blockIdx.x];
-  const int32_t hk = blockIdx.y;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
+  // all heads of an item, then the next item: the long ones start first
+  const int32_t item = blockIdx.x / a.n_kv, hk = blockIdx.x - item * a.n_kv;
+  const Item it = a.items[item];
   const int32_t rows = it.n_tok * a.group;
   const int32_t first = it.lo / kKeys, n = it.hi > it.lo ? (it.hi + kKeys - 1) / kKeys - first : 0;
 
@@ -138,6 +140,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
   const uint32_t slots = smem + S::kQ;
   const uint32_t full = smem_addr(bars), empty = full + 8 * S::kSlots, q_full = empty + 8 * S::kSlots,
                  s_full = q_full + 8, p_ready = s_full + 16, o_done = p_ready + 16;
+  // s_full, p_ready and o_done are two barriers each, for even and odd steps.  A wait tells a phase
+  // from the one before it only, and every wait here has that one behind it: S_j is computed
+  // after the product of step j - 2 is done.
   if (warp == 4 && lane == 0) {
     prefetch_map(&map_q);
     prefetch_map(&map_kv);
@@ -145,94 +150,114 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
     bar_init(q_full, 1);
     bar_init(s_full, 1), bar_init(s_full + 8, 1);
     bar_init(p_ready, 4), bar_init(p_ready + 8, 4);
-    bar_init(o_done, 1);
+    bar_init(o_done, 1), bar_init(o_done + 8, 1);
     failed_word = keep_o = bad[0] = bad[1] = 0;
     fence_bar_init();
   }
-  if (warp == 5) tmem_alloc<1>(smem_addr(&tmem_at), S::kColumns);
+  if (warp == 7) tmem_alloc<1>(smem_addr(&tmem_at), S::kColumns);
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
-  const uint32_t tmem = tmem_at, tmem_s = tmem + 128;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0), tmem_s = tmem + 128;
 
-  if (warp == 4) {
+  if (warp >= 4 && warp < 4 + kCopiers) {
     const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
-    if (lane == 0) {
+    if (warp == 4 && elect_one()) {
       const int32_t tile_rows = kRows / a.group * a.group;
       bar_expect(q_full, tile_rows * 128 * S::kHalves);
       for (int h = 0; h < S::kHalves; ++h) load_3d(smem + h * (kRows * 128), &map_q, h * 64, hk * a.group, it.tok0, q_full);
     }
-    // a lane brings one box of a slot: its keys, and 64 columns
-    const int boxes = kKeys / box, mine = lane / S::kHalves, half = lane % S::kHalves;
-    int issued = 0;
-    bool go = true;
-    for (int e = 0; e < 2 * n && go; ++e) {
+    // the page numbers come 32 at a time, the next 32 on their way: a look-up for each slot took
+    // about 1,000 clocks, twice what its products take
+    const int shift = __ffs(a.page_tokens) - 1;
+    const int32_t last = (it.hi - 1) >> shift;
+    int32_t at0 = first * kKeys >> shift;
+    auto look_up = [&](int32_t i) {
+      const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
+      return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
+    };
+    int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
+    int e = warp - 4;
+    for (; e < 2 * n; e += kCopiers) {
       // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
       const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
       const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
       const int slot = e % S::kSlots;
       const int32_t k0 = (first + j) * kKeys;
-      const int from = it.lo > k0 ? (it.lo - k0) / box : 0;
-      const int to = it.hi - k0 < kKeys ? (it.hi - k0 + box - 1) / box : boxes;
-      const int32_t key = k0 + mine * box;
-      const bool here = mine >= from && mine < to;
-      int32_t page = here ? a.table[int64_t(it.row) * a.max_pages + key / a.page_tokens] : -1;
-      if (page < 0 || page >= a.n_pages) page = a.n_pages;   // no such page: read as zeros
-      if (lane == 0) {
-        go = bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed);
-        if (go) bar_expect(full + 8 * slot, (to - from) * box * 128 * S::kHalves);
+      const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
+      if (is_v && (k0 >> shift) - at0 >= 32) {   // K is at most three steps ahead of V, 24 pages
+        at0 += 32;
+        now = next;
+        next = look_up(at0 + 32 + lane);
       }
-      go = __shfl_sync(0xffffffffu, go, 0);
-      if (!go) break;
-      if (here)
-        load_3d(slots + slot * S::kSlot + half * (kKeys * 128) + mine * box * 128, &map_kv, half * 64,
-                hk * a.page_tokens + (key & (a.page_tokens - 1)), page * a.planes + a.plane + is_v, full + 8 * slot);
-      ++issued;
+      if (!bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed)) break;
+      __syncwarp();
+      const uint32_t bar = full + 8 * slot, dst = slots + slot * S::kSlot;
+      if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * 128 * S::kHalves);
+      for (int32_t k = from; k < to; k += box) {
+        const int32_t rel = ((k0 + k) >> shift) - at0;
+        const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
+        const int32_t y = hk * a.page_tokens + ((k0 + k) & (a.page_tokens - 1)), z = page * a.planes + a.plane + is_v;
+        if (elect_one())
+#pragma unroll
+          for (int h = 0; h < S::kHalves; ++h) load_3d(dst + h * (kKeys * 128) + k * 128, &map_kv, h * 64, y, z, bar);
+      }
     }
     if (*failed && lane == 0) {   // the copies in flight still have to land: a bounded wait for each
       uint32_t quiet = 0;
-      for (int e = issued < S::kSlots ? 0 : issued - S::kSlots; e < issued; ++e)
-        bar_wait(full + 8 * (e % S::kSlots), (e / S::kSlots) & 1, &quiet);
+      for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - S::kSlots; b -= kCopiers)
+        bar_wait(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
       bar_wait(q_full, 0, &quiet);
     }
     __syncwarp();
-  } else if (warp == 5) {
-    if (lane == 0) {
-      constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-      constexpr uint32_t desc_s = mma_desc(kBf16, kRows, kKeys, false), desc_o = mma_desc(kBf16, kRows, DP, true);
-      auto scores = [&](int j) {
-        const int e = order_k(j), slot = e % S::kSlots;
-        if (!bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
-        tc_after_sync();
-        const uint32_t k = slots + slot * S::kSlot;
+  } else if (warp == 7) {
+    // the whole warp goes along, so that what the instructions take is known to be the same in
+    // all lanes; one lane issues
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr uint32_t desc_s = mma_desc(kBf16, kRows, kKeys, false), desc_o = mma_desc(kBf16, kRows, DP, true);
+    const uint32_t with = desc_s | (a.negative ? kMinusA : 0u);
+    const uint64_t q = tile_k(smem), k_ring = tile_k(slots), v_ring = tile_n(slots, kKeys * 128);
+    auto scores = [&](int j) {
+      const int e = order_k(j), slot = e % S::kSlots;
+      if (!bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
+      __syncwarp();
+      tc_after_sync();
+      const uint64_t k = k_ring + slot * (S::kSlot / 16);
+      const uint32_t d = tmem_s + (j & 1) * kKeys;
+      if (elect_one()) {
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i)
-          mma_ss<1>(tmem_s + (j & 1) * kKeys, tile_k(smem + (i / 4) * (kRows * 128)) + 2 * (i % 4),
-                    tile_k(k + (i / 4) * (kKeys * 128)) + 2 * (i % 4), desc_s, i > 0);
+          mma_ss<1>(d, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), k + (i / 4) * (kKeys * 128 / 16) + 2 * (i % 4), with,
+                    i > 0);
         mma_commit(empty + 8 * slot);
         mma_commit(s_full + 8 * (j & 1));
-        return true;
-      };
-      bool go = bar_wait(q_full, 0, failed) && scores(0) && (n < 2 || scores(1));
-      for (int j = 0; go && j < n; ++j) {
-        const int e = order_v(j, n), slot = e % S::kSlots;
-        if (!bar_wait(p_ready + 8 * (j & 1), (j >> 1) & 1, failed) ||
-            !bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed))
-          break;
-        tc_after_sync();
-        const uint64_t v = tile_n(slots + slot * S::kSlot, kKeys * 128);
-        const bool add = j > 0 || *reinterpret_cast<volatile uint32_t*>(&keep_o);
-#pragma unroll
-        for (int i = 0; i < kKeys / 16; ++i)
-          mma_ts(tmem, tmem_s + (j & 1) * kKeys + i * 8, v + i * (16 * 128 / 16), desc_o, add || i > 0);
-        mma_commit(empty + 8 * slot);
-        mma_commit(o_done);
-        // S_{j+2} takes the place of P_j: once its product is done
-        if (j + 2 < n) go = bar_wait(o_done, j & 1, failed) && scores(j + 2);
       }
-      // the last arrival that nothing else waits for
-      bar_wait(empty + 8 * ((2 * n - 1) % S::kSlots), ((2 * n - 1) / S::kSlots) & 1, failed);
+      __syncwarp();
+      return true;
+    };
+    bool go = bar_wait(q_full, 0, failed) && scores(0) && (n < 2 || scores(1));
+    for (int j = 0; go && j < n; ++j) {
+      const int e = order_v(j, n), slot = e % S::kSlots;
+      if (!bar_wait(p_ready + 8 * (j & 1), (j >> 1) & 1, failed) ||
+          !bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed))
+        break;
+      __syncwarp();
+      tc_after_sync();
+      const uint64_t v = v_ring + slot * (S::kSlot / 16);
+      const uint32_t p = tmem_s + (j & 1) * kKeys;
+      const bool add = j > 0 || *reinterpret_cast<volatile uint32_t*>(&keep_o);
+      if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < kKeys / 16; ++i) mma_ts(tmem, p + i * 8, v + i * (16 * 128 / 16), desc_o, add || i > 0);
+        mma_commit(empty + 8 * slot);
+        mma_commit(o_done + 8 * (j & 1));
+      }
+      __syncwarp();
+      // S_{j+2} takes the place of P_j: once its product is done
+      if (j + 2 < n) go = bar_wait(o_done + 8 * (j & 1), (j >> 1) & 1, failed) && scores(j + 2);
     }
+    // the last arrival that nothing else waits for
+    bar_wait(empty + 8 * ((2 * n - 1) % S::kSlots), ((2 * n - 1) / S::kSlots) & 1, failed);
     __syncwarp();
   } else {
     const int r = threadIdx.x;
@@ -257,12 +282,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       tmem_wait_load();
       tmem_loaded(lo);
       tmem_loaded(hi);
-      if (a.negative) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) lo[i] ^= 0x80000000u, hi[i] ^= 0x80000000u;
-      }
       const bool masked = k0 < it.lo || k0 + kKeys > all_see;
-      // scores that this row does not see become -inf, and their p is set to 0 below
+      // scores that this row does not see become -inf, and their p 0 (c > 0)
       uint64_t sees = ~0ull;
       if (masked) {
         const int below = it.lo > k0 ? it.lo - k0 : 0, upto = end - k0 < 0 ? 0 : end - k0 < kKeys ? end - k0 : kKeys;
@@ -282,15 +303,14 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
         mx[3] = fmaxf(mx[3], __uint_as_float(hi[i + 1]));
       }
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      const float here = top == -INFINITY ? -INFINITY : top * c;   // c may be 0
+      const float here = top * c;
       const bool raise = here > m + 8.f || (m == -INFINITY && here > -INFINITY);
       if (__any_sync(0xffffffffu, raise)) {
         const float f = raise ? (m == -INFINITY ? 0.f : exp2_fast(m - here)) : 1.f;
         if (raise) m = here;
         l *= f;
         if (j > 0) {
-          // (S_j was computed after the product of step j - 2 was done)
-          bar_wait(o_done, (j - 1) & 1, failed);
+          bar_wait(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
           __syncwarp();
           tc_after_sync();
 #pragma unroll 1
@@ -312,16 +332,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       uint32_t p[32];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float x = exp2_fast(fmaf(__uint_as_float(lo[2 * i]), c, shift));
-        float y = exp2_fast(fmaf(__uint_as_float(lo[2 * i + 1]), c, shift));
-        float z = exp2_fast(fmaf(__uint_as_float(hi[2 * i]), c, shift));
-        float w = exp2_fast(fmaf(__uint_as_float(hi[2 * i + 1]), c, shift));
-        if (masked) {
-          if (!(sees >> (2 * i) & 1)) x = 0.f;
-          if (!(sees >> (2 * i + 1) & 1)) y = 0.f;
-          if (!(sees >> (2 * i + 32) & 1)) z = 0.f;
-          if (!(sees >> (2 * i + 33) & 1)) w = 0.f;
-        }
+        const float x = exp2_fast(fmaf(__uint_as_float(lo[2 * i]), c, shift));
+        const float y = exp2_fast(fmaf(__uint_as_float(lo[2 * i + 1]), c, shift));
+        const float z = exp2_fast(fmaf(__uint_as_float(hi[2 * i]), c, shift));
+        const float w = exp2_fast(fmaf(__uint_as_float(hi[2 * i + 1]), c, shift));
         sum[0] += x, sum[1] += y, sum[2] += z, sum[3] += w;
         p[i] = pack(T(), x, y);
         p[16 + i] = pack(T(), z, w);
@@ -365,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
           if (found) {
             // Their share of O is added here, to the rows that see them; the products get zeros.
             if (j > 0) {
-              bar_wait(o_done, (j - 1) & 1, failed);
+              bar_wait(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
               __syncwarp();
               tc_after_sync();
             }
@@ -420,9 +434,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       __syncwarp();
       if (lane == 0) bar_arrive(p_ready + 8 * (j & 1));
     }
-    // one phase after the other: a barrier tells a phase from the one before it only
-    if (n > 1) bar_wait(o_done, (n - 2) & 1, failed);
-    bar_wait(o_done, (n - 1) & 1, failed);
+    bar_wait(o_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, failed);
     __syncwarp();
     tc_after_sync();
     const bool in = tok < it.n_tok;
@@ -467,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
   __syncwarp();
   tc_before_sync();
   __syncthreads();
-  if (warp == 5) tmem_free<1>(tmem, S::kColumns);
+  if (warp == 7) tmem_free<1>(tmem, S::kColumns);
   if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
 }
 
@@ -554,6 +566,7 @@ struct Run {
 };
 
 constexpr int64_t kMinSteps = 4;   // of an item that is cut
+constexpr int64_t kJoinSteps = 8;  // what writing and joining a tile's partial results costs, in steps
 
 void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
   const int32_t group = d.n_heads / d.n_kv_heads, tile = kRows / group;
@@ -571,7 +584,9 @@ void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
       if (lead < 0 && d.q_len[b] > 0) lead = b;
     }
     // together, the prefix is read once a tile of all queries; apart, once a tile of each request's
-    const bool pool = prefix >= kKeys && (tokens + tile - 1) / tile < apart;
+    // (at the price of partial results to join: the steps that it saves have to outweigh them)
+    const int64_t together = (tokens + tile - 1) / tile;
+    const bool pool = (apart - together) * (prefix / kKeys) > kJoinSteps * together + apart;
     if (pool)
       for (int64_t t = 0; t < tokens; t += tile)
         runs.push_back(Run{int32_t(tok + t), int32_t(std::min<int64_t>(tile, tokens - t)), d.seq ? d.seq[lead] : lead, 0,
@@ -660,11 +675,9 @@ cudaError_t launch(const op_attend_plan_t& p, const CUtensorMap& q, const CUtens
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
   auto kernel = attend_kernel<T, DP>;
-  if (!once.done(dev, [&] {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::kSmem) == cudaSuccess;
-      }))
+  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP>::kSmem); }))
     return cudaErrorInvalidValue;
-  kernel<<<dim3((unsigned)p.n_items, (unsigned)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(q, kv, a);
+  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(q, kv, a);
   if (p.n_joins > 0) {
     const int64_t warps = (int64_t)std::min<int64_t>(p.n_tokens, kRows) * p.n_heads;
     attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>((warps + 3) / 4, 64)), 128, 0, st>>>(a);
@@ -684,7 +697,7 @@ int op_attend_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend_plan_t* pl
   if (!desc_ok(d) || !plan || n_sm < 1) return GMG_EINVAL;
   Work w;
   plan_items(*d, n_sm, &w);
-  if (w.part_rows > 0x7fffffff || w.items.size() > 0x7fffffff) return GMG_ERANGE;
+  if (w.part_rows > 0x7fffffff || (int64_t)w.items.size() * d->n_kv_heads > 0x7fffffff) return GMG_ERANGE;
   op_attend_plan_t p{};
   p.n_batch = d->n_batch;
   p.n_heads = d->n_heads;
@@ -719,7 +732,7 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
   if (!plan || !cache_ok(cache) || layer < 0 || layer >= cache->n_layers) return GMG_EINVAL;
   if (plan->head_dim != cache->head_dim || plan->n_kv_heads != cache->n_kv_heads ||
       plan->page_tokens != cache->page_tokens || plan->max_seq >= cache->n_seq ||
-      plan->max_kv > int64_t(cache->max_pages) * cache->page_tokens || plan->n_kv_heads > 65535)
+      plan->max_kv > int64_t(cache->max_pages) * cache->page_tokens)
     return GMG_EINVAL;
   if (plan->n_tokens == 0) return GMG_OK;
   if (!d_items || (reinterpret_cast<uintptr_t>(d_items) & 15) || !q || !out || !aligned(q, q_tok, q_head, 2) ||
@@ -743,7 +756,8 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
   a.n_kv = plan->n_kv_heads;
   a.group = plan->n_heads / plan->n_kv_heads;
   a.dim = plan->head_dim;
-  a.scale2 = fabsf(scale) * 1.4426950408889634f;
+  // a scale of 0 gives every key one weight, as a tiny one does, whose product with -inf is -inf
+  a.scale2 = fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-30f);
   a.negative = scale < 0.f;
   a.out = out, a.o_tok = out_tok, a.o_head = out_head;
   a.lse = lse;

@@ -26,6 +26,15 @@ inline bool aligned(const void* p, int64_t s0, int64_t s1, int e) {
   return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(s0 * e) | uintptr_t(s1 * e)) & 15) == 0;
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory, and its SM give all it can to shared
+// memory (left to itself the driver may leave room for one block where two would fit).
+template <class K>
+bool allow_smem(K kernel, int bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess &&
+         cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) ==
+             cudaSuccess;
+}
+
 // The driver's encoder of tensor maps, looked up once; NULL if it has none.
 using MapEncoder = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

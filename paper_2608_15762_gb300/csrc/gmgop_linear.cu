@@ -834,9 +834,7 @@ cudaError_t launch_pairs(const op_linear_t& a, int sms, void* work, cudaStream_t
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
   auto kernel = linear_kernel<T, kGate>;
-  if (!once.done(dev, [&] {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) == cudaSuccess;
-      }))
+  if (!once.done(dev, [&] { return allow_smem(kernel, S::kSmem); }))
     return cudaErrorInvalidValue;
   Maps m;
   if (!make_maps(a, NT / kPair, &m)) return cudaErrorInvalidValue;
@@ -862,9 +860,7 @@ cudaError_t launch_split(const op_linear_t& a, int sms, void* work, cudaStream_t
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
   auto kernel = linear_split_kernel<T, NT_, kGate>;
-  if (!once.done(dev, [&] {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) == cudaSuccess;
-      }))
+  if (!once.done(dev, [&] { return allow_smem(kernel, S::kSmem); }))
     return cudaErrorInvalidValue;
   Maps m;
   if (!make_maps(a, NT_, &m)) return cudaErrorInvalidValue;

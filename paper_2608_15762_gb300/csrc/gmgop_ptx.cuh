@@ -16,6 +16,17 @@ namespace {
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// True in one lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(one));
+  return one != 0;
+}
+
 // ---- mbarriers ------------------------------------------------------------
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
@@ -122,22 +133,22 @@ __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* m, int3
 
 // ---- tensor cores ---------------------------------------------------------
 
+// A block allocates once, and gives up the right to allocate more with it: a second block comes
+// to an SM only then.
 template <int kPair>
 __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns) {
-  if (kPair == 2)
+  if (kPair == 2) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "r"(columns) : "memory");
-  else
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
 }
 template <int kPair>
 __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
-  if (kPair == 2) {
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
-  } else {
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
-  }
+  if (kPair == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
+  else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
 }
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -184,6 +195,8 @@ __host__ __device__ constexpr uint32_t mma_desc(bool bf16, int m, int n, bool b_
   return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_rows ? 1u : 0u) << 16) |
          ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+
+constexpr uint32_t kMinusA = 1u << 13;   // the product takes -A
 
 // A tile in shared memory in the 128-byte swizzle, 1,024-byte aligned.  Columns (K)
 // contiguous: rows of 128 bytes, eight rows after each other; 16 columns on is 32 bytes on.
