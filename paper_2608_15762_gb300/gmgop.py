@@ -16,9 +16,10 @@ import math
 from typing import Optional, Sequence
 
 import numpy as np
+import torch
 
 from . import gmgsim as G
-from .gmgsim import GmgError, _aligned_empty, _check, _stream_handle, _traced
+from .gmgsim import GmgError, _aligned_empty, _check
 
 EXPORTED = ("op_page_scratch_bytes", "op_free", "op_fork", "op_grow", "op_compact", "op_rope", "op_rope_append",
             "op_attend_plan", "op_attend", "op_linear_work_bytes", "op_linear")
@@ -86,29 +87,49 @@ def lib():
     return _LIB
 
 
+# A call of a small operator takes the GPU a few microseconds, so the host's part is kept short:
+# checks are plain comparisons, and a range is pushed only where the environment asks for it.
+_traced = G._traced if G.NVTX else lambda name: lambda fn: fn
+_I32 = torch.int32
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_RAW = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _handle(stream, device_index):
+    """The stream's handle, by default that of the GPU's current stream."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _RAW is not None:
+        return _RAW(device_index)
+    return torch.cuda.current_stream(device_index).cuda_stream
+
+
 def _dtype(t) -> int:
-    import torch
-    d = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    d = _TYPES.get(t.dtype)
     if d is None:
         raise ValueError("element type %s: fp32, bf16 or fp16" % t.dtype)
     return d
 
 
-def _need(ok: bool, what: str) -> None:
+def _need(ok, what: str) -> None:
     if not ok:
         raise ValueError(what)
 
 
+def _fail(rc: int, what: str):
+    raise GmgError(rc, what)
+
+
 def _on(stream):
     """Memory allocated inside belongs to `stream`."""
-    import torch
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def _list(t, device, what: str) -> None:
-    import torch
-    _need(t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.device == device,
-          "%s: a contiguous int32 list on the operands' GPU" % what)
+def _list(t, device, what: str) -> int:
+    """The length of a list on the GPU."""
+    if t.dtype is not _I32 or t.dim() != 1 or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: a contiguous int32 list on the operands' GPU" % what)
+    return t.shape[0]
 
 
 # ---------------------------------------------------------------------------
@@ -123,7 +144,6 @@ class PageCache:
     last one went."""
 
     def __init__(self, pool, n_seq: int = 0, max_pages: int = 0, table=None, lens=None, refs=None):
-        import torch
         _need(pool.is_cuda and pool.dim() == 6 and pool.shape[2] == 2 and pool.is_contiguous(),
               "pool: contiguous, [n_pages, n_layers, 2, n_kv_heads, page_tokens, head_dim], on a GPU")
         dev, i32 = pool.device, torch.int32
@@ -140,50 +160,57 @@ class PageCache:
         self.status = torch.zeros(8, dtype=i32, device=dev)
         p = pool.shape
         self.n_layers, self.n_kv_heads, self.page_tokens, self.head_dim = p[1], p[3], p[4], p[5]
+        self.device, self.dtype, self._index = dev, pool.dtype, pool.get_device()
         self.c = _Cache(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(), self.status.data_ptr(),
                         _dtype(pool), p[0], p[1], p[3], p[4], p[5], n_seq, max_pages)
         self.ref = C.addressof(self.c)
-        nbytes = lib().op_page_scratch_bytes(self.ref)
+        nbytes = (_LIB or lib()).op_page_scratch_bytes(self.ref)
         if nbytes == 0:
             raise GmgError(G.GMG_EINVAL, "op_page_scratch_bytes")
         self.scratch = _aligned_empty(nbytes, dev)
         self.scratch.zero_()
+        self._work = self.scratch.data_ptr(), nbytes
 
     def code(self):
         """(PAGE_* code of the last page call, the list entry or the missing pages)."""
         return tuple(self.status[:2].tolist())
 
-    def _tail(self, stream):
-        return self.scratch.data_ptr(), self.scratch.numel(), _stream_handle(stream)
-
     @_traced("op_free")
     def free(self, seq, stream=None):
         """Empty the listed rows and drop their references."""
-        _list(seq, self.pool.device, "seq")
-        _check(lib().op_free(self.ref, seq.data_ptr(), seq.numel(), *self._tail(stream)), "op_free")
+        n = _list(seq, self.device, "seq")
+        rc = (_LIB or lib()).op_free(self.ref, seq.data_ptr(), n, *self._work, _handle(stream, self._index))
+        if rc:
+            _fail(rc, "op_free")
 
     @_traced("op_fork")
     def fork(self, src, dst, keep=None, stream=None):
         """The empty rows dst get the first ``keep`` tokens (all) of rows src by reference."""
-        for t, name in ((src, "src"), (dst, "dst")) + (((keep, "keep"),) if keep is not None else ()):
-            _list(t, self.pool.device, name)
-            _need(t.numel() == src.numel(), "src, dst, keep: one length")
-        _check(lib().op_fork(self.ref, src.data_ptr(), dst.data_ptr(), None if keep is None else keep.data_ptr(),
-                             src.numel(), *self._tail(stream)), "op_fork")
+        n = _list(src, self.device, "src")
+        if _list(dst, self.device, "dst") != n or (keep is not None and _list(keep, self.device, "keep") != n):
+            raise ValueError("src, dst, keep: one length")
+        rc = (_LIB or lib()).op_fork(self.ref, src.data_ptr(), dst.data_ptr(), None if keep is None else keep.data_ptr(), n,
+                           *self._work, _handle(stream, self._index))
+        if rc:
+            _fail(rc, "op_fork")
 
     @_traced("op_grow")
     def grow(self, seq, add, stream=None):
         """Room for ``add`` more tokens in the listed rows, whose lengths grow by them; a
         partly filled last page that others hold too is copied first."""
-        _list(seq, self.pool.device, "seq")
-        _list(add, self.pool.device, "add")
-        _need(seq.numel() == add.numel(), "seq, add: one length")
-        _check(lib().op_grow(self.ref, seq.data_ptr(), add.data_ptr(), seq.numel(), *self._tail(stream)), "op_grow")
+        n = _list(seq, self.device, "seq")
+        if _list(add, self.device, "add") != n:
+            raise ValueError("seq, add: one length")
+        rc = (_LIB or lib()).op_grow(self.ref, seq.data_ptr(), add.data_ptr(), n, *self._work, _handle(stream, self._index))
+        if rc:
+            _fail(rc, "op_grow")
 
     @_traced("op_compact")
     def compact(self, stream=None):
         """Move the pages in use to the lowest page numbers."""
-        _check(lib().op_compact(self.ref, *self._tail(stream)), "op_compact")
+        rc = (_LIB or lib()).op_compact(self.ref, *self._work, _handle(stream, self._index))
+        if rc:
+            _fail(rc, "op_compact")
 
 
 # ---------------------------------------------------------------------------
@@ -221,7 +248,6 @@ class Rope:
     ``rope_freqs``, or its arguments."""
 
     def __init__(self, rotary: int, freqs=None, factor: float = 1.0, interleaved: bool = False, device="cuda", **kw):
-        import torch
         if freqs is None:
             freqs, factor = rope_freqs(rotary, **kw)
         freqs = np.asarray(freqs, np.float64)
@@ -235,26 +261,41 @@ class Rope:
         self.ref = C.addressof(self.c)
 
 
-def _heads(t, what: str, n_tokens=None):
-    _need(t.dim() == 3 and (t.shape[2] <= 1 or t.stride(2) == 1) and t.is_cuda,
-          "%s: [tokens, heads, head_dim] on a GPU, contiguous in head_dim" % what)
-    _need(n_tokens is None or t.shape[0] == n_tokens, "%s: one row a token" % what)
-    return t.data_ptr(), t.stride(0), t.stride(1)
+def _heads(t, what: str):
+    """(pointer, stride of a token, of a head) of a tensor [tokens, heads, head_dim]."""
+    s = t.stride()
+    if len(s) != 3 or (s[2] != 1 and t.shape[2] > 1):
+        raise ValueError("%s: [tokens, heads, head_dim], contiguous in head_dim" % what)
+    return t.data_ptr(), s[0], s[1]
+
+
+def _like(x, out, stream):
+    """`out`, checked against x, or a new tensor of its shape."""
+    if out is None:
+        if stream is None:
+            return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if out.shape != x.shape or out.dtype is not x.dtype or out.device != x.device:
+        raise ValueError("out: of the input's shape, type and GPU")
+    return out
 
 
 @_traced("op_rope")
 def rope(plan: Rope, x, pos, backward: bool = False, out=None, stream=None):
     """x [tokens, heads, head_dim] rotated by pos (int32, one a token); ``backward``: by
     minus the angle, which takes the gradient of the result to that of x.  out may be x."""
-    import torch
-    _list(pos, x.device, "pos")
-    _need(pos.numel() == x.shape[0], "pos: one entry a token")
-    if out is None:
-        with _on(stream):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device, "out: as x")
-    _check(lib().op_rope(plan.ref, _dtype(x), x.shape[0], x.shape[1], x.shape[2], *_heads(x, "x"), pos.data_ptr(),
-                         int(backward), *_heads(out, "out"), _stream_handle(stream)), "op_rope")
+    kind = _dtype(x)
+    ptr, s0, s1 = _heads(x, "x")
+    T, H, D = x.shape
+    index = x.get_device()
+    if index < 0 or _list(pos, x.device, "pos") != T:
+        raise ValueError("x on a GPU, pos: one entry a token")
+    out = _like(x, out, stream)
+    rc = (_LIB or lib()).op_rope(plan.ref, kind, T, H, D, ptr, s0, s1, pos.data_ptr(), 1 if backward else 0, *_heads(out, "out"),
+                       _handle(stream, index))
+    if rc:
+        _fail(rc, "op_rope")
     return out
 
 
@@ -262,23 +303,19 @@ def rope(plan: Rope, x, pos, backward: bool = False, out=None, stream=None):
 def rope_append(plan: Rope, q, k, v, pos, seq, cache: PageCache, layer: int, out=None, stream=None):
     """q rotated by pos (returned); k rotated and v written to ``layer`` of the cache as
     token pos[t] of row seq[t] (a negative seq: not written)."""
-    import torch
-    T = q.shape[0]
-    _list(pos, q.device, "pos")
-    _list(seq, q.device, "seq")
-    _need(pos.numel() == T and seq.numel() == T, "pos, seq: one entry a token")
-    D, Hk = cache.head_dim, cache.n_kv_heads
-    _need(q.dtype == k.dtype == v.dtype == cache.pool.dtype and q.device == cache.pool.device,
-          "q, k, v: the cache's type, on its GPU")
-    _need(q.shape[2] == D and tuple(k.shape) == (T, Hk, D) and tuple(v.shape) == (T, Hk, D),
-          "q [tokens, heads, head_dim], k and v [tokens, n_kv_heads, head_dim]")
-    if out is None:
-        with _on(stream):
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape and out.dtype == q.dtype and out.device == q.device, "out: as q")
-    _check(lib().op_rope_append(plan.ref, cache.ref, int(layer), T, q.shape[1], *_heads(q, "q"), *_heads(k, "k"),
-                                *_heads(v, "v"), pos.data_ptr(), seq.data_ptr(), *_heads(out, "out"),
-                                _stream_handle(stream)), "op_rope_append")
+    T, H, D = q.shape
+    kv, dt, dev = (T, cache.n_kv_heads, D), cache.dtype, cache.device
+    if D != cache.head_dim or k.shape != kv or v.shape != kv:
+        raise ValueError("q [tokens, heads, head_dim], k and v [tokens, n_kv_heads, head_dim]")
+    if q.dtype is not dt or k.dtype is not dt or v.dtype is not dt or q.device != dev or k.device != dev or v.device != dev:
+        raise ValueError("q, k, v: the cache's type, on its GPU")
+    if _list(pos, dev, "pos") != T or _list(seq, dev, "seq") != T:
+        raise ValueError("pos, seq: one entry a token")
+    out = _like(q, out, stream)
+    rc = (_LIB or lib()).op_rope_append(plan.ref, cache.ref, layer, T, H, *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"),
+                              pos.data_ptr(), seq.data_ptr(), *_heads(out, "out"), _handle(stream, cache._index))
+    if rc:
+        _fail(rc, "op_rope_append")
     return out
 
 
@@ -290,7 +327,6 @@ _SMS = {}
 
 
 def _n_sm(device) -> int:
-    import torch
     if device not in _SMS:
         _SMS[device] = torch.cuda.get_device_properties(device).multi_processor_count
     return _SMS[device]
@@ -308,9 +344,9 @@ def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=
     ptr = [None if a is None else a.ctypes.data for a in arr]
     d = _AttendDesc(q.size, n_heads, n_kv_heads, head_dim, page_tokens, 0 if pre is None else pre.size, *ptr)
     plan = _AttendPlan()
-    _check(lib().op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), None, 0), "op_attend_plan")
+    _check((_LIB or lib()).op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), None, 0), "op_attend_plan")
     items = np.zeros(plan.plan_bytes // 4, np.int32)
-    _check(lib().op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes),
+    _check((_LIB or lib()).op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes),
            "op_attend_plan")
     return plan, items
 
@@ -324,14 +360,16 @@ class AttendPlan:
     def __init__(self, q_len: Sequence[int], kv_len: Sequence[int], n_heads: int, n_kv_heads: int, head_dim: int,
                  page_tokens: int, seq: Optional[Sequence[int]] = None, group_off: Optional[Sequence[int]] = None,
                  prefix: Optional[Sequence[int]] = None, device="cuda", stream=None):
-        import torch
         dev = torch.device(device)
         self.c, items = attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq, group_off, prefix,
                                      _n_sm(dev))
         self.ref = C.addressof(self.c)
-        self.n_tokens, self.n_heads, self.head_dim = self.c.n_tokens, n_heads, head_dim
+        self.n_tokens, self.n_heads, self.head_dim = int(self.c.n_tokens), n_heads, head_dim
+        self.shape = (self.n_tokens, n_heads, head_dim)
+        self.work_bytes = int(self.c.work_bytes)
         with _on(stream):
             self.items = torch.from_numpy(items).to(dev)
+        self._ptr = self.items.data_ptr() if items.size else None
 
 
 @_traced("op_attend")
@@ -339,20 +377,22 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
            stream=None):
     """Attention of q [tokens, heads, head_dim] (the requests' new tokens, one request
     after another) over the cache; with ``lse`` also log sum exp [tokens, heads], fp32."""
-    import torch
-    _need(tuple(q.shape) == (plan.n_tokens, plan.n_heads, plan.head_dim) and q.dtype == cache.pool.dtype
-          and q.device == cache.pool.device, "q: [tokens, heads, head_dim] of the plan, the cache's type")
-    with _on(stream):
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        z = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse else None
-        work = torch.empty(plan.c.work_bytes, dtype=torch.uint8, device=q.device)
-    _need(out.shape == q.shape and out.dtype == q.dtype and out.device == q.device, "out: as q")
-    _check(lib().op_attend(plan.ref, plan.items.data_ptr() if plan.items.numel() else None, cache.ref, int(layer),
-                           *_heads(q, "q"), plan.head_dim ** -0.5 if scale is None else float(scale),
-                           *_heads(out, "out"), None if z is None else z.data_ptr(), work.data_ptr(), work.numel(),
-                           _stream_handle(stream)), "op_attend")
+    if q.shape != plan.shape or q.dtype is not cache.dtype or q.device != cache.device:
+        raise ValueError("q: [tokens, heads, head_dim] of the plan, the cache's type, on its GPU")
+    with _on(stream) if stream is not None else _HERE:
+        out = _like(q, out, None)
+        z = torch.empty(plan.shape[:2], dtype=torch.float32, device=q.device) if lse else None
+        work = torch.empty(plan.work_bytes, dtype=torch.uint8, device=q.device)
+    rc = (_LIB or lib()).op_attend(plan.ref, plan._ptr, cache.ref, layer, *_heads(q, "q"),
+                         plan.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
+                         None if z is None else z.data_ptr(), work.data_ptr(), plan.work_bytes,
+                         _handle(stream, cache._index))
+    if rc:
+        _fail(rc, "op_attend")
     return (out, z) if lse else out
+
+
+_HERE = contextlib.nullcontext()
 
 
 # ---------------------------------------------------------------------------
@@ -364,22 +404,33 @@ class Workspace:
     Calls that share one must be ordered (one stream)."""
 
     def __init__(self, device="cuda"):
-        self.device, self.buf = device, None
+        self.device, self.buf, self.ptr, self.size = device, None, 0, 0
 
     def get(self, nbytes: int, stream=None):
-        if self.buf is None or self.buf.numel() < nbytes:
+        if self.buf is None or self.size < nbytes:
             with _on(stream):
-                self.buf = _aligned_empty(nbytes, self.device)
+                self.buf = _aligned_empty(max(nbytes, 4096), self.device)
                 self.buf[:4096].zero_()
+            self.ptr, self.size = self.buf.data_ptr(), self.buf.numel()
         return self.buf
 
 
 _WORK = {}
 
 
-def _matrix(t, shape, like, what: str):
-    _need(tuple(t.shape) == shape and t.dtype == like.dtype and t.device == like.device
-          and (shape[-1] <= 1 or t.stride(-1) == 1), "%s: %s, rows contiguous, of x's type and GPU" % (what, list(shape)))
+def _rows(t, n, k, dt, dev, what: str):
+    """(pointer, stride of a row) of a matrix [n, k]."""
+    if t.shape != (n, k) or t.dtype is not dt or t.device != dev:
+        raise ValueError("%s: [%d, %d], of x's type and on its GPU" % (what, n, k))
+    s = t.stride()
+    if s[1] != 1 and k > 1:
+        raise ValueError("%s: rows contiguous" % what)
+    return t.data_ptr(), s[0] if n > 1 or s[0] > k else k
+
+
+def _column(t, n, dt, dev, what: str):
+    if t.shape != (n,) or t.dtype is not dt or t.device != dev or not t.is_contiguous():
+        raise ValueError("%s: [%d], contiguous, of x's type and on its GPU" % (what, n))
     return t.data_ptr()
 
 
@@ -389,32 +440,36 @@ def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residu
     """act(x w^T + bias) + residual or, with a gate, act(x gate^T + gate_bias) * (x w^T +
     bias) + residual, for x [m, k], w and gate [n, k], biases [n], residual [m, n].
     act: none, relu, silu, gelu.  out may be residual.  ws: kept per stream by default."""
-    import torch
-    _need(x.dim() == 2 and w.dim() == 2 and x.is_cuda, "x [m, k], w [n, k] on a GPU")
     m, k = x.shape
-    n = w.shape[0]
-    _need(act in ACTS, "act: one of %s" % ", ".join(ACTS))
-    _need(gate_bias is None or gate is not None, "gate_bias without a gate")
+    n, dt, dev, index = w.shape[0], x.dtype, x.device, x.get_device()
+    kind, how = _TYPES.get(dt), ACTS.get(act)
+    if kind is None or how is None or index < 0:
+        raise ValueError("x: bf16 or fp16, on a GPU; act: one of %s" % ", ".join(ACTS))
+    if gate_bias is not None and gate is None:
+        raise ValueError("gate_bias without a gate")
     if out is None:
-        with _on(stream):
-            out = torch.empty((m, n), dtype=x.dtype, device=x.device)
-
-    def row(t, width):
-        return max(t.stride(0), width) if t is not None and t.shape[0] <= 1 else 0 if t is None else t.stride(0)
-
-    a = _Linear(_dtype(x), ACTS[act], int(gate is not None), 0, m, n, k, _matrix(x, (m, k), x, "x"),
-                _matrix(w, (n, k), x, "w"), None if gate is None else _matrix(gate, (n, k), x, "gate"),
-                None if bias is None else _matrix(bias, (n,), x, "bias"),
-                None if gate_bias is None else _matrix(gate_bias, (n,), x, "gate_bias"),
-                None if residual is None else _matrix(residual, (m, n), x, "residual"), _matrix(out, (m, n), x, "out"),
-                row(x, k), row(w, k), row(gate, k), row(residual, n), row(out, n))
-    ref = C.addressof(a)
-    h = _stream_handle(stream)
+        if stream is None:
+            out = torch.empty((m, n), dtype=dt, device=dev)
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty((m, n), dtype=dt, device=dev)
+    xp, xs = _rows(x, m, k, dt, dev, "x")
+    wp, wrow = _rows(w, n, k, dt, dev, "w")
+    yp, ys = _rows(out, m, n, dt, dev, "out")
+    gp, gs = (None, 0) if gate is None else _rows(gate, n, k, dt, dev, "gate")
+    rp, rs = (None, 0) if residual is None else _rows(residual, m, n, dt, dev, "residual")
+    a = _Linear(kind, how, 0 if gate is None else 1, 0, m, n, k, xp, wp, gp,
+                None if bias is None else _column(bias, n, dt, dev, "bias"),
+                None if gate_bias is None else _column(gate_bias, n, dt, dev, "gate_bias"), rp, yp, xs, wrow, gs, rs, ys)
+    ref = C.byref(a)
+    h = _handle(stream, index)
     if ws is None:
-        ws = _WORK.get((x.device, h))
+        ws = _WORK.get((index, h))
         if ws is None:
-            ws = _WORK[(x.device, h)] = Workspace(x.device)
-    need = lib().op_linear_work_bytes(ref)
-    buf = ws.get(max(need, 4096), stream)
-    _check(lib().op_linear(ref, buf.data_ptr(), buf.numel(), h), "op_linear")
+            ws = _WORK[(index, h)] = Workspace(dev)
+    L = _LIB or lib()
+    ws.get(L.op_linear_work_bytes(ref), stream)
+    rc = L.op_linear(ref, ws.ptr, ws.size, h)
+    if rc:
+        _fail(rc, "op_linear")
     return out
