@@ -94,6 +94,31 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// Two fp32 in one 64-bit register pair: one instruction for both.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ void halves(uint64_t v, float* a, float* b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
+  float v;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+  return v;
+}
+
 template <int DP>
 struct Shape {
   static constexpr int kHalves = DP / 64;
@@ -296,11 +321,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       }
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        mx[0] = fmaxf(mx[0], __uint_as_float(lo[i]));
-        mx[1] = fmaxf(mx[1], __uint_as_float(lo[i + 1]));
-        mx[2] = fmaxf(mx[2], __uint_as_float(hi[i]));
-        mx[3] = fmaxf(mx[3], __uint_as_float(hi[i + 1]));
+      for (int i = 0; i < 32; i += 4) {
+        mx[0] = max3(mx[0], lo[i], lo[i + 1]);
+        mx[1] = max3(mx[1], lo[i + 2], lo[i + 3]);
+        mx[2] = max3(mx[2], hi[i], hi[i + 1]);
+        mx[3] = max3(mx[3], hi[i + 2], hi[i + 3]);
       }
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       const float here = top * c;
@@ -328,19 +353,25 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       }
       // p, packed over the first half of the scores' registers
       const float shift = m == -INFINITY ? 0.f : kBias - m;
-      float sum[4] = {};
+      const uint64_t c2 = two(c, c), shift2 = two(shift, shift);
+      uint64_t sum[4] = {};
       uint32_t p[32];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float x = exp2_fast(fmaf(__uint_as_float(lo[2 * i]), c, shift));
-        const float y = exp2_fast(fmaf(__uint_as_float(lo[2 * i + 1]), c, shift));
-        const float z = exp2_fast(fmaf(__uint_as_float(hi[2 * i]), c, shift));
-        const float w = exp2_fast(fmaf(__uint_as_float(hi[2 * i + 1]), c, shift));
-        sum[0] += x, sum[1] += y, sum[2] += z, sum[3] += w;
+        float x, y, z, w;
+        halves(fma2(two(__uint_as_float(lo[2 * i]), __uint_as_float(lo[2 * i + 1])), c2, shift2), &x, &y);
+        halves(fma2(two(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1])), c2, shift2), &z, &w);
+        x = exp2_fast(x), y = exp2_fast(y), z = exp2_fast(z), w = exp2_fast(w);
+        sum[i & 1] = add2(sum[i & 1], two(x, y));
+        sum[2 + (i & 1)] = add2(sum[2 + (i & 1)], two(z, w));
         p[i] = pack(T(), x, y);
         p[16 + i] = pack(T(), z, w);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      {
+        float x, y;
+        halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), &x, &y);
+        l += x + y;
+      }
       tmem_store32(s_at, p);
       tmem_wait_store();
       if (masked) {

@@ -5,9 +5,12 @@
 // handed out in increasing order, so the result of a call does not depend on how
 // its threads run: the r-th page that a call needs is the free page of rank r,
 // found by counting free pages per block of kBlockPages pages, a prefix over the
-// blocks, and a prefix within each block.  Three launches for grow and compact
-// (count and plan / rank / apply and copy), two for free and fork (check / apply).
-// The plan is made by the block that counts last, which alone sees all counts.
+// blocks, and a prefix within each block.  The plan is made by the block that counts
+// last, which alone sees all counts.  Launches: count and plan / rank / apply and copy
+// for grow and compact, check / apply for free and fork; the first two are one where
+// one block holds all pages, and free and fork are one launch of one block while it has
+// at most kFewCells table entries to go through (a step of 84 requests, 4,096 pages: 10
+// launches and copies instead of 13).
 
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -18,9 +21,11 @@
 namespace gop {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;         // of the blocks that apply and copy
+constexpr int kPlanThreads = 1024;    // of those that check, count and plan
 constexpr int kPerThread = 16;
-constexpr int kBlockPages = kThreads * kPerThread;
+constexpr int kBlockPages = kPlanThreads * kPerThread;
+constexpr int64_t kFewCells = 16384;
 constexpr int kCopyBytes = 32768;   // bytes of a page that one block copies at a time
 
 struct Entry {      // what grow needs of a list entry after its plan
@@ -84,9 +89,9 @@ struct Faults {
 };
 constexpr unsigned long long kNoFault = ~0ull;
 
-// Exclusive prefix over the block's threads, and the total.
+// Exclusive prefix over the kPlanThreads threads of the block, and the total.
 __device__ int32_t block_prefix(int32_t v, int32_t* total) {
-  __shared__ int32_t warp_sum[kThreads / 32];
+  __shared__ int32_t warp_sum[32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   int32_t s = v;
 #pragma unroll
@@ -97,14 +102,15 @@ __device__ int32_t block_prefix(int32_t v, int32_t* total) {
   __syncthreads();
   if (lane == 31) warp_sum[w] = s;
   __syncthreads();
-  int32_t before = 0, all = 0;
+  int32_t sums = warp_sum[lane];
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) {
-    if (i < w) before += warp_sum[i];
-    all += warp_sum[i];
+  for (int d = 1; d < 32; d *= 2) {
+    const int32_t t = __shfl_up_sync(0xffffffffu, sums, d);
+    if (lane >= d) sums += t;
   }
-  *total = all;
-  return before + s - v;
+  *total = __shfl_sync(0xffffffffu, sums, 31);
+  const int32_t before = __shfl_sync(0xffffffffu, sums, w > 0 ? w - 1 : 0);
+  return (w > 0 ? before : 0) + s - v;
 }
 
 // Free pages among this thread's kPerThread, as bits; pages beyond the end count as used.
@@ -119,13 +125,13 @@ __device__ uint32_t free_bits(const op_cache_t& c, int64_t first) {
 // Marks every listed row with its entry and reports rows that are out of range or
 // listed twice (the later entries find another's mark).  All threads of one block.
 __device__ void check_rows(const op_cache_t& c, const int32_t* rows, int32_t n, int32_t* mark, Faults f) {
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+  for (int32_t i = threadIdx.x; i < n; i += kPlanThreads) {
     const int32_t r = rows[i];
     if (r < 0 || r >= c.n_seq) f.add(i, GMG_PAGE_SEQ);
     else mark[r] = i;
   }
   __syncthreads();
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+  for (int32_t i = threadIdx.x; i < n; i += kPlanThreads) {
     const int32_t r = rows[i];
     if (r >= 0 && r < c.n_seq && mark[r] != i) f.add(i, GMG_PAGE_TWICE);
   }
@@ -138,37 +144,57 @@ __device__ void write_status(const op_cache_t& c, unsigned long long worst) {
 
 // ---- free and fork -------------------------------------------------------
 
-__global__ void __launch_bounds__(kThreads) free_check_kernel(op_cache_t c, const int32_t* seq, int32_t n, Scratch s) {
+// Entries [i0, i1) of the list, all threads of the block over their table cells.
+__device__ void free_rows(const op_cache_t& c, const int32_t* seq, int32_t i0, int32_t i1) {
+  for (int64_t e = threadIdx.x; e < (int64_t)(i1 - i0) * c.max_pages; e += blockDim.x) {
+    const int32_t i = int32_t(e / c.max_pages);
+    int32_t* cell = c.table + int64_t(seq[i0 + i]) * c.max_pages + (e - (int64_t)i * c.max_pages);
+    const int32_t p = *cell;
+    if (p < 0) continue;
+    if (p < c.n_pages) atomicSub(&c.refs[p], 1);
+    *cell = -1;
+  }
+  for (int32_t i = i0 + threadIdx.x; i < i1; i += blockDim.x) c.lens[seq[i]] = 0;
+}
+
+template <bool kApply>
+__global__ void __launch_bounds__(kPlanThreads) free_check_kernel(op_cache_t c, const int32_t* seq, int32_t n, Scratch s) {
   __shared__ unsigned long long worst;
   if (threadIdx.x == 0) worst = kNoFault;
   __syncthreads();
   check_rows(c, seq, n, s.mark, Faults{&worst});
   __syncthreads();
   if (threadIdx.x == 0) write_status(c, worst);
+  if (kApply && worst == kNoFault) free_rows(c, seq, 0, n);
 }
 
 __global__ void __launch_bounds__(kThreads) free_apply_kernel(op_cache_t c, const int32_t* seq) {
-  if (c.status[0] != GMG_PAGE_OK) return;
-  const int32_t r = seq[blockIdx.x];
-  int32_t* row = c.table + int64_t(r) * c.max_pages;
-  for (int32_t j = threadIdx.x; j < c.max_pages; j += kThreads) {
-    const int32_t p = row[j];
-    if (p < 0) continue;
-    if (p < c.n_pages) atomicSub(&c.refs[p], 1);
-    row[j] = -1;
-  }
-  if (threadIdx.x == 0) c.lens[r] = 0;
+  if (c.status[0] == GMG_PAGE_OK) free_rows(c, seq, blockIdx.x, blockIdx.x + 1);
 }
 
-__global__ void __launch_bounds__(kThreads) fork_check_kernel(op_cache_t c, const int32_t* src, const int32_t* dst,
-                                                              const int32_t* keep, int32_t n, Scratch s) {
+// (A new row is never a source, so the lengths read are those of before the call.)
+__device__ void fork_rows(const op_cache_t& c, const int32_t* src, const int32_t* dst, const int32_t* keep, int32_t i0,
+                          int32_t i1) {
+  for (int64_t e = threadIdx.x; e < (int64_t)(i1 - i0) * c.max_pages; e += blockDim.x) {
+    const int32_t i = i0 + int32_t(e / c.max_pages), j = int32_t(e - (int64_t)(i - i0) * c.max_pages), a = src[i];
+    if (j >= pages_for(keep ? keep[i] : c.lens[a], c.page_tokens)) continue;
+    const int32_t p = c.table[int64_t(a) * c.max_pages + j];
+    c.table[int64_t(dst[i]) * c.max_pages + j] = p;
+    if (p >= 0 && p < c.n_pages) atomicAdd(&c.refs[p], 1);
+  }
+  for (int32_t i = i0 + threadIdx.x; i < i1; i += blockDim.x) c.lens[dst[i]] = keep ? keep[i] : c.lens[src[i]];
+}
+
+template <bool kApply>
+__global__ void __launch_bounds__(kPlanThreads) fork_check_kernel(op_cache_t c, const int32_t* src, const int32_t* dst,
+                                                                  const int32_t* keep, int32_t n, Scratch s) {
   __shared__ unsigned long long worst;
   if (threadIdx.x == 0) worst = kNoFault;
   __syncthreads();
   const Faults f{&worst};
   check_rows(c, dst, n, s.mark, f);
   __syncthreads();
-  for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+  for (int32_t i = threadIdx.x; i < n; i += kPlanThreads) {
     const int32_t a = src[i], b = dst[i];
     if (a < 0 || a >= c.n_seq) {
       f.add(i, GMG_PAGE_SEQ);
@@ -183,22 +209,12 @@ __global__ void __launch_bounds__(kThreads) fork_check_kernel(op_cache_t c, cons
   }
   __syncthreads();
   if (threadIdx.x == 0) write_status(c, worst);
+  if (kApply && worst == kNoFault) fork_rows(c, src, dst, keep, 0, n);
 }
 
 __global__ void __launch_bounds__(kThreads) fork_apply_kernel(op_cache_t c, const int32_t* src, const int32_t* dst,
                                                               const int32_t* keep) {
-  if (c.status[0] != GMG_PAGE_OK) return;
-  const int32_t i = blockIdx.x, a = src[i], b = dst[i];
-  const int32_t len = keep ? keep[i] : c.lens[a];
-  const int32_t np = int32_t(pages_for(len, c.page_tokens));
-  const int32_t* from = c.table + int64_t(a) * c.max_pages;
-  int32_t* to = c.table + int64_t(b) * c.max_pages;
-  for (int32_t j = threadIdx.x; j < np; j += kThreads) {
-    const int32_t p = from[j];
-    to[j] = p;
-    if (p >= 0 && p < c.n_pages) atomicAdd(&c.refs[p], 1);
-  }
-  if (threadIdx.x == 0) c.lens[b] = len;
+  if (c.status[0] == GMG_PAGE_OK) fork_rows(c, src, dst, keep, blockIdx.x, blockIdx.x + 1);
 }
 
 // ---- grow and compact: count, rank, apply --------------------------------
@@ -221,7 +237,7 @@ __device__ bool count_free(const op_cache_t& c, const Scratch& s) {
 // The counts become the free pages before each block; returns their sum.
 __device__ int32_t prefix_blocks(const Scratch& s, int32_t blocks) {
   int32_t before = 0;
-  for (int32_t b0 = 0; b0 < blocks; b0 += kThreads) {
+  for (int32_t b0 = 0; b0 < blocks; b0 += kPlanThreads) {
     const int32_t b = b0 + threadIdx.x;
     int32_t total;
     const int32_t v = b < blocks ? __ldcg(&s.block[b]) : 0;
@@ -237,7 +253,26 @@ __device__ int32_t prefix_blocks(const Scratch& s, int32_t blocks) {
   return before;
 }
 
-__global__ void __launch_bounds__(kThreads) grow_count_kernel(op_cache_t c, const int32_t* seq, const int32_t* add,
+// The free pages of the first ranks go to the list and get their reference.
+__device__ void grow_take(const op_cache_t& c, const Scratch& s, int32_t want) {
+  const int32_t before = s.block[blockIdx.x];
+  if (before >= want) return;
+  const int64_t first = (int64_t)blockIdx.x * kBlockPages + threadIdx.x * kPerThread;
+  const uint32_t bits = free_bits(c, first);
+  int32_t total;
+  int32_t r = before + block_prefix(__popc(bits), &total);
+#pragma unroll
+  for (int j = 0; j < kPerThread; ++j)
+    if (bits >> j & 1) {
+      if (r < want) {
+        s.list[r] = int32_t(first + j);
+        c.refs[first + j] = 1;
+      }
+      ++r;
+    }
+}
+
+__global__ void __launch_bounds__(kPlanThreads) grow_count_kernel(op_cache_t c, const int32_t* seq, const int32_t* add,
                                                               int32_t n, Scratch s) {
   if (!count_free(c, s)) return;
   const int32_t n_free = prefix_blocks(s, gridDim.x);
@@ -247,8 +282,8 @@ __global__ void __launch_bounds__(kThreads) grow_count_kernel(op_cache_t c, cons
   const Faults f{&worst};
   check_rows(c, seq, n, s.mark, f);
   int64_t need = 0;   // of the entries before, the same in all threads
-  for (int32_t i0 = 0; i0 < n; i0 += kThreads) {
-    const int32_t i = i0 + threadIdx.x;
+  for (int32_t i0 = 0; i0 < n; i0 += 256) {
+    const int32_t i = threadIdx.x < 256 ? i0 + threadIdx.x : n;
     int32_t mine = 0;
     Entry e{0, 0, 0, -1};
     if (i < n && seq[i] >= 0 && seq[i] < c.n_seq) {
@@ -275,7 +310,7 @@ __global__ void __launch_bounds__(kThreads) grow_count_kernel(op_cache_t c, cons
       e.off = int32_t(need + p < c.n_pages ? need + p : c.n_pages);
       s.entry[i] = e;
     }
-    need += total;   // a block's needs are below 2^31: 256 rows of at most max_pages <= 2^22
+    need += total;   // a round's needs are below 2^31: 256 rows of at most max_pages <= 2^22
   }
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -287,26 +322,13 @@ __global__ void __launch_bounds__(kThreads) grow_count_kernel(op_cache_t c, cons
     }
     s.plan[0] = c.status[0] == GMG_PAGE_OK ? int32_t(need) : 0;
   }
+  if (gridDim.x == 1) {
+    __syncthreads();
+    grow_take(c, s, s.plan[0]);
+  }
 }
 
-// The free pages of the first ranks go to the list and get their reference.
-__global__ void __launch_bounds__(kThreads) grow_take_kernel(op_cache_t c, Scratch s) {
-  const int32_t want = s.plan[0], before = s.block[blockIdx.x];
-  if (before >= want) return;
-  const int64_t first = (int64_t)blockIdx.x * kBlockPages + threadIdx.x * kPerThread;
-  const uint32_t bits = free_bits(c, first);
-  int32_t total;
-  int32_t r = before + block_prefix(__popc(bits), &total);
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j)
-    if (bits >> j & 1) {
-      if (r < want) {
-        s.list[r] = int32_t(first + j);
-        c.refs[first + j] = 1;
-      }
-      ++r;
-    }
-}
+__global__ void __launch_bounds__(kPlanThreads) grow_take_kernel(op_cache_t c, Scratch s) { grow_take(c, s, s.plan[0]); }
 
 // Bytes [at, at + kCopyBytes) of a page, all threads, eight 16-byte loads in flight each.
 __device__ void copy_part(const op_cache_t& c, size_t bytes, int32_t from, int32_t to, size_t at) {
@@ -351,29 +373,7 @@ __global__ void __launch_bounds__(kThreads) grow_apply_kernel(op_cache_t c, cons
   }
 }
 
-__global__ void __launch_bounds__(kThreads) compact_count_kernel(op_cache_t c, Scratch s) {
-  if (!count_free(c, s)) return;
-  const int32_t n_free = prefix_blocks(s, gridDim.x);
-  const int32_t used = c.n_pages - n_free;
-  // free pages below `used`: whole blocks, then the part of the block that it lies in
-  const int32_t b = used / kBlockPages;
-  int32_t total;
-  const int64_t first = (int64_t)b * kBlockPages + threadIdx.x * kPerThread;
-  uint32_t bits = free_bits(c, first);
-  if (first + kPerThread > used) bits &= first >= used ? 0u : (1u << (used - first)) - 1;
-  block_prefix(__popc(bits), &total);
-  if (threadIdx.x == 0) {
-    const int32_t moves = s.block[b] + total;
-    s.plan[0] = moves;
-    s.plan[1] = used;
-    c.status[0] = GMG_PAGE_OK;
-    c.status[1] = 0;
-    c.status[2] = moves;
-    c.status[3] = used;
-  }
-}
-
-__global__ void __launch_bounds__(kThreads) compact_rank_kernel(op_cache_t c, Scratch s) {
+__device__ void compact_rank(const op_cache_t& c, const Scratch& s) {
   const int32_t moves = s.plan[0], used = s.plan[1];
   const int64_t first = (int64_t)blockIdx.x * kBlockPages + threadIdx.x * kPerThread;
   const uint32_t bits = free_bits(c, first);
@@ -393,6 +393,34 @@ __global__ void __launch_bounds__(kThreads) compact_rank_kernel(op_cache_t c, Sc
     before += is_free;
   }
 }
+
+__global__ void __launch_bounds__(kPlanThreads) compact_count_kernel(op_cache_t c, Scratch s) {
+  if (!count_free(c, s)) return;
+  const int32_t n_free = prefix_blocks(s, gridDim.x);
+  const int32_t used = c.n_pages - n_free;
+  // free pages below `used`: whole blocks, then the part of the block that it lies in
+  const int32_t b = used / kBlockPages;
+  int32_t total;
+  const int64_t first = (int64_t)b * kBlockPages + threadIdx.x * kPerThread;
+  uint32_t bits = free_bits(c, first);
+  if (first + kPerThread > used) bits &= first >= used ? 0u : (1u << (used - first)) - 1;
+  block_prefix(__popc(bits), &total);
+  if (threadIdx.x == 0) {
+    const int32_t moves = s.block[b] + total;
+    s.plan[0] = moves;
+    s.plan[1] = used;
+    c.status[0] = GMG_PAGE_OK;
+    c.status[1] = 0;
+    c.status[2] = moves;
+    c.status[3] = used;
+  }
+  if (gridDim.x == 1) {
+    __syncthreads();
+    compact_rank(c, s);
+  }
+}
+
+__global__ void __launch_bounds__(kPlanThreads) compact_rank_kernel(op_cache_t c, Scratch s) { compact_rank(c, s); }
 
 __global__ void __launch_bounds__(kThreads) compact_apply_kernel(op_cache_t c, size_t bytes, Scratch s) {
   const int32_t moves = s.plan[0], used = s.plan[1];
@@ -447,8 +475,12 @@ int op_free(const op_cache_t* cache, const int32_t* seq, int32_t n, void* scratc
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (n == 0) return empty_list(cache, st);
   if (!seq) return GMG_EINVAL;
-  free_check_kernel<<<1, kThreads, 0, st>>>(*cache, seq, n, s);
-  free_apply_kernel<<<n, kThreads, 0, st>>>(*cache, seq);
+  if ((int64_t)n * cache->max_pages <= kFewCells) {
+    free_check_kernel<true><<<1, kPlanThreads, 0, st>>>(*cache, seq, n, s);
+  } else {
+    free_check_kernel<false><<<1, kPlanThreads, 0, st>>>(*cache, seq, n, s);
+    free_apply_kernel<<<n, kThreads, 0, st>>>(*cache, seq);
+  }
   return done();
 }
 
@@ -460,8 +492,12 @@ int op_fork(const op_cache_t* cache, const int32_t* src, const int32_t* dst, con
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (n == 0) return empty_list(cache, st);
   if (!src || !dst) return GMG_EINVAL;
-  fork_check_kernel<<<1, kThreads, 0, st>>>(*cache, src, dst, keep, n, s);
-  fork_apply_kernel<<<n, kThreads, 0, st>>>(*cache, src, dst, keep);
+  if ((int64_t)n * cache->max_pages <= kFewCells) {
+    fork_check_kernel<true><<<1, kPlanThreads, 0, st>>>(*cache, src, dst, keep, n, s);
+  } else {
+    fork_check_kernel<false><<<1, kPlanThreads, 0, st>>>(*cache, src, dst, keep, n, s);
+    fork_apply_kernel<<<n, kThreads, 0, st>>>(*cache, src, dst, keep);
+  }
   return done();
 }
 
@@ -475,8 +511,8 @@ int op_grow(const op_cache_t* cache, const int32_t* seq, const int32_t* add, int
   if (!seq || !add) return GMG_EINVAL;
   const size_t bytes = page_bytes(*cache);
   const int32_t blocks = blocks_of(*cache);
-  grow_count_kernel<<<blocks, kThreads, 0, st>>>(*cache, seq, add, n, s);
-  grow_take_kernel<<<blocks, kThreads, 0, st>>>(*cache, s);
+  grow_count_kernel<<<blocks, kPlanThreads, 0, st>>>(*cache, seq, add, n, s);
+  if (blocks > 1) grow_take_kernel<<<blocks, kPlanThreads, 0, st>>>(*cache, s);
   const size_t parts = (bytes + kCopyBytes - 1) / kCopyBytes;
   const dim3 grid(unsigned(parts < 64 ? parts : 64), unsigned(n < 65535 ? n : 65535));
   grow_apply_kernel<<<grid, kThreads, 0, st>>>(*cache, add, n, bytes, s);
@@ -489,9 +525,16 @@ int op_compact(const op_cache_t* cache, void* scratch, size_t scratch_bytes, gmg
   if (rc != GMG_OK) return rc;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const int32_t blocks = blocks_of(*cache);
-  compact_count_kernel<<<blocks, kThreads, 0, st>>>(*cache, s);
-  compact_rank_kernel<<<blocks, kThreads, 0, st>>>(*cache, s);
-  compact_apply_kernel<<<152 * 8, kThreads, 0, st>>>(*cache, page_bytes(*cache), s);
+  compact_count_kernel<<<blocks, kPlanThreads, 0, st>>>(*cache, s);
+  if (blocks > 1) compact_rank_kernel<<<blocks, kPlanThreads, 0, st>>>(*cache, s);
+  // as many blocks as there can be parts to copy, up to 64 an SM: a part each keeps more loads
+  // on the way than a few blocks that take them in turn
+  const size_t bytes = page_bytes(*cache);
+  const int64_t parts = (int64_t)((bytes + kCopyBytes - 1) / kCopyBytes) * ((cache->n_pages + 1) / 2);
+  const int64_t cells = ((int64_t)cache->n_seq * cache->max_pages + kThreads - 1) / kThreads;
+  int64_t grid = parts > cells ? parts : cells;
+  if (grid > 152 * 64) grid = 152 * 64;
+  compact_apply_kernel<<<(unsigned)grid, kThreads, 0, st>>>(*cache, bytes, s);
   return done();
 }
 
