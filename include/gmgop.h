@@ -150,7 +150,7 @@ typedef struct {
   int32_t n_batch, n_heads, n_kv_heads, head_dim, page_tokens;
   int32_t n_items, n_joins;   /* work items (per key/value head); joins of partial results */
   int32_t max_seq, max_kv;    /* what table rows and lengths the plan reaches */
-  int32_t reserved;
+  int32_t join_tokens;        /* queries of the largest join */
   int64_t n_tokens;           /* queries in all */
   int64_t part_rows;          /* rows of partial results per key/value head */
   size_t plan_bytes;          /* of the plan's array */

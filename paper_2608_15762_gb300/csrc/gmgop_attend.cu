@@ -515,16 +515,21 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
 }
 
 // Joins the parts of a query head: o = sum_i 2^(lse_i - L) o_i with L = log2 sum_i 2^lse_i.  A
-// warp takes one, four elements a lane.
+// warp takes one head of a token, a lane four elements; with more than 8 parts a block does: its
+// four warps every fourth part, and their sums are then added in order.
 template <class T>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a) {
-  const int lane = threadIdx.x & 31;
+  __shared__ float4 sums[3][32];
+  __shared__ float weights[3];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   const Join j = a.joins[blockIdx.x];
-  const int32_t all = j.n_tok * a.n_heads;
-  for (int32_t w = blockIdx.y * 4 + threadIdx.x / 32; w < all; w += gridDim.y * 4) {
+  const int32_t all = j.n_tok * a.n_heads, n = j.n[0] + j.n[1];
+  const bool wide = n > 8;
+  for (int32_t w0 = blockIdx.y * (wide ? 1 : 4); w0 < all; w0 += gridDim.y * (wide ? 1 : 4)) {
+    const int32_t w = wide ? w0 : w0 + warp;
+    if (w >= all) break;
     const int32_t tok = w / a.n_heads, h = w - tok * a.n_heads, hk = h / a.group;
     const int32_t r = tok * a.group + h - hk * a.group;
-    const int32_t n = j.n[0] + j.n[1];
     auto row_of = [&](int32_t i) {
       return hk * a.part_rows + r +
              (i < j.n[0] ? j.base[0] + (int64_t)i * j.step[0] : j.base[1] + (int64_t)(i - j.n[0]) * j.step[1]);
@@ -537,7 +542,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     float4 o = {};
     float sum = 0.f;
 #pragma unroll 4
-    for (int32_t i = 0; i < n; ++i) {
+    for (int32_t i = wide ? warp : 0; i < n; i += wide ? 4 : 1) {
       const int64_t row = row_of(i);
       const float f = exp2f(__ldcg(a.part_lse + row) - ref);
       sum += f;
@@ -546,15 +551,31 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
         o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
       }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t t = j.tok0 + tok;
-    if (lane * 4 < a.dim) {
-      uint2 v;
-      v.x = pack(T(), o.x * inv, o.y * inv);
-      v.y = pack(T(), o.z * inv, o.w * inv);
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head + lane * 4) = v;
+    if (wide) {
+      if (warp > 0) {
+        sums[warp - 1][lane] = o;
+        if (lane == 0) weights[warp - 1] = sum;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const float4 v = sums[i][lane];
+        o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+        sum += weights[i];
+      }
+      __syncthreads();
     }
-    if (a.lse && lane == 0) a.lse[t * a.n_heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+    if (!wide || warp == 0) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const int64_t t = j.tok0 + tok;
+      if (lane * 4 < a.dim) {
+        uint2 v;
+        v.x = pack(T(), o.x * inv, o.y * inv);
+        v.y = pack(T(), o.z * inv, o.w * inv);
+        *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head + lane * 4) = v;
+      }
+      if (a.lse && lane == 0) a.lse[t * a.n_heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+    }
   }
 }
 
@@ -596,7 +617,7 @@ struct Run {
   int32_t steps() const { return hi > lo ? (hi + kKeys - 1) / kKeys - lo / kKeys : 0; }
 };
 
-constexpr int64_t kMinSteps = 4;   // of an item that is cut
+constexpr int64_t kMinSteps = 6;   // of an item that is cut (16 requests behind 8,000 tokens: 2 25 us, 6 15, 8 15; 8 short ones: 6 11, 8 13)
 constexpr int64_t kJoinSteps = 8;  // what writing and joining a tile's partial results costs, in steps
 
 void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
@@ -710,8 +731,8 @@ cudaError_t launch(const op_attend_plan_t& p, const CUtensorMap& q, const CUtens
     return cudaErrorInvalidValue;
   kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(q, kv, a);
   if (p.n_joins > 0) {
-    const int64_t warps = (int64_t)std::min<int64_t>(p.n_tokens, kRows) * p.n_heads;
-    attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>((warps + 3) / 4, 64)), 128, 0, st>>>(a);
+    const int64_t heads = (int64_t)p.join_tokens * p.n_heads;
+    attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>(heads, 1024)), 128, 0, st>>>(a);
   }
   return cudaGetLastError();
 }
@@ -742,6 +763,7 @@ int op_attend_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend_plan_t* pl
     p.max_seq = std::max(p.max_seq, d->seq ? d->seq[b] : b);
     p.max_kv = std::max(p.max_kv, d->kv_len[b]);
   }
+  for (const Join& j : w.joins) p.join_tokens = std::max(p.join_tokens, j.n_tok);
   p.part_rows = w.part_rows;
   p.plan_bytes = sizeof(Item) * w.items.size() + sizeof(Join) * w.joins.size();
   p.work_bytes = 256 + size_t(w.part_rows) * d->n_kv_heads * (d->head_dim + 1) * 4;

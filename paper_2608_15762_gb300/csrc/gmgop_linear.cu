@@ -155,6 +155,14 @@ cudaError_t launch_any(const op_linear_t& a, cudaStream_t st) {
 
 // ---- few rows of x ---------------------------------------------------------
 
+// A load that stays where it is written.
+template <class T>
+__device__ __forceinline__ T load_now(const T* p) {
+  unsigned short v;
+  asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p) : "memory");
+  return *reinterpret_cast<const T*>(&v);
+}
+
 // A warp (or four, where the weight has few rows) takes one row of the weight against up to
 // two rows of x: 16-byte loads, kAhead of them in flight, x from the L1 cache.  Bound by
 // reading the weight; no piece waits for another.
@@ -175,12 +183,13 @@ __global__ void __launch_bounds__(128) linear_few_kernel(op_linear_t a) {
   const T* x = static_cast<const T*>(a.x);
   const T* w = static_cast<const T*>(a.w) + col * a.w_row;
   const T* g = kGate ? static_cast<const T*>(a.gate) + col * a.gate_row : nullptr;
-  // what the end needs is on its way while the weight is read
+  // what the end needs is on its way while the weight is read (loaded at the end, the residual
+  // took a token's 4,096 x 4,096 product from 9 to 12.5 us)
   T old = T(), b0 = T(), b1 = T();
   if (lane < M && warp < (kWarps > 1 ? 1 : 4)) {
-    if (a.residual) old = static_cast<const T*>(a.residual)[lane * a.residual_row + col];
-    if (a.bias) b0 = static_cast<const T*>(a.bias)[col];
-    if (kGate && a.gate_bias) b1 = static_cast<const T*>(a.gate_bias)[col];
+    if (a.residual) old = load_now(static_cast<const T*>(a.residual) + lane * a.residual_row + col);
+    if (a.bias) b0 = load_now(static_cast<const T*>(a.bias) + col);
+    if (kGate && a.gate_bias) b1 = load_now(static_cast<const T*>(a.gate_bias) + col);
   }
   float v[M] = {}, z[M] = {};
   const int64_t whole = a.k & ~int64_t(7), step = 256 * kWarps;

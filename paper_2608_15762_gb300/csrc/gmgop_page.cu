@@ -116,6 +116,15 @@ __device__ int32_t block_prefix(int32_t v, int32_t* total) {
 // Free pages among this thread's kPerThread, as bits; pages beyond the end count as used.
 __device__ uint32_t free_bits(const op_cache_t& c, int64_t first) {
   uint32_t bits = 0;
+  if (first + kPerThread <= c.n_pages && (reinterpret_cast<uintptr_t>(c.refs) & 15) == 0) {
+    int4 v[kPerThread / 4];
+#pragma unroll
+    for (int j = 0; j < kPerThread / 4; ++j) v[j] = reinterpret_cast<const int4*>(c.refs + first)[j];
+#pragma unroll
+    for (int j = 0; j < kPerThread / 4; ++j)
+      bits |= ((v[j].x == 0) | (v[j].y == 0) << 1 | (v[j].z == 0) << 2 | (v[j].w == 0) << 3) << (4 * j);
+    return bits;
+  }
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j)
     if (first + j < c.n_pages && c.refs[first + j] == 0) bits |= 1u << j;
@@ -224,6 +233,10 @@ __device__ bool count_free(const op_cache_t& c, const Scratch& s) {
   __shared__ bool last;
   int32_t total;
   block_prefix(__popc(free_bits(c, (int64_t)blockIdx.x * kBlockPages + threadIdx.x * kPerThread)), &total);
+  if (gridDim.x == 1) {
+    if (threadIdx.x == 0) s.block[0] = total;
+    return true;
+  }
   if (threadIdx.x == 0) {
     s.block[blockIdx.x] = total;
     __threadfence();

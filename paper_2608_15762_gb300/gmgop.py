@@ -47,7 +47,7 @@ class _AttendDesc(C.Structure):
 
 class _AttendPlan(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_batch", "n_heads", "n_kv_heads", "head_dim", "page_tokens", "n_items",
-                                         "n_joins", "max_seq", "max_kv", "reserved")] + [
+                                         "n_joins", "max_seq", "max_kv", "join_tokens")] + [
         ("n_tokens", C.c_int64), ("part_rows", C.c_int64), ("plan_bytes", C.c_size_t), ("work_bytes", C.c_size_t)]
 
 
