@@ -155,18 +155,13 @@ cudaError_t launch_any(const op_linear_t& a, cudaStream_t st) {
 
 // ---- few rows of x ---------------------------------------------------------
 
-// A load that stays where it is written.
-template <class T>
-__device__ __forceinline__ T load_now(const T* p) {
-  unsigned short v;
-  asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p) : "memory");
-  return *reinterpret_cast<const T*>(&v);
-}
-
 // A warp (or four, where the weight has few rows) takes one row of the weight against up to
 // two rows of x: 16-byte loads, kAhead of them in flight, x from the L1 cache.  Bound by
 // reading the weight; no piece waits for another.
 constexpr int kFewRows = 2;
+// ... and two rows of x only with a weight of few rows (us, here / below: 6,144 x 1,024 7.2 / 8.1,
+// 1,024 x 12,288 10.0 / 12.7, 12,288 x 4,096 29.9 / 24; one row 22.6 there).
+constexpr int64_t kFewTwo = 8192;
 
 template <class T>
 struct alignas(16) Eight {
@@ -183,34 +178,35 @@ __global__ void __launch_bounds__(128) linear_few_kernel(op_linear_t a) {
   const T* x = static_cast<const T*>(a.x);
   const T* w = static_cast<const T*>(a.w) + col * a.w_row;
   const T* g = kGate ? static_cast<const T*>(a.gate) + col * a.gate_row : nullptr;
-  // what the end needs is on its way while the weight is read (loaded at the end, the residual
-  // took a token's 4,096 x 4,096 product from 9 to 12.5 us)
+  // what the end needs is on its way while the weight is read
   T old = T(), b0 = T(), b1 = T();
   if (lane < M && warp < (kWarps > 1 ? 1 : 4)) {
-    if (a.residual) old = load_now(static_cast<const T*>(a.residual) + lane * a.residual_row + col);
-    if (a.bias) b0 = load_now(static_cast<const T*>(a.bias) + col);
-    if (kGate && a.gate_bias) b1 = load_now(static_cast<const T*>(a.gate_bias) + col);
+    if (a.residual) old = static_cast<const T*>(a.residual)[lane * a.residual_row + col];
+    if (a.bias) b0 = static_cast<const T*>(a.bias)[col];
+    if (kGate && a.gate_bias) b1 = static_cast<const T*>(a.gate_bias)[col];
   }
   float v[M] = {}, z[M] = {};
   const int64_t whole = a.k & ~int64_t(7), step = 256 * kWarps;
   for (int64_t k0 = (kWarps > 1 ? warp * 256 : 0) + lane * 8; k0 < whole; k0 += step * kAhead) {
-    Eight<T> b[kAhead], c[kGate ? kAhead : 1];
+    // (x with the weight, not behind it: a cold x took 3.5 us more)
+    Eight<T> b[kAhead], c[kGate ? kAhead : 1], y[M][kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
       if (k0 + j * step < whole) {
         b[j] = *reinterpret_cast<const Eight<T>*>(w + k0 + j * step);
         if (kGate) c[j] = *reinterpret_cast<const Eight<T>*>(g + k0 + j * step);
+#pragma unroll
+        for (int r = 0; r < M; ++r) y[r][j] = *reinterpret_cast<const Eight<T>*>(x + r * a.x_row + k0 + j * step);
       }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
       if (k0 + j * step < whole) {
 #pragma unroll
         for (int r = 0; r < M; ++r) {
-          const Eight<T> y = *reinterpret_cast<const Eight<T>*>(x + r * a.x_row + k0 + j * step);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            v[r] = fmaf(up(y.v[i]), up(b[j].v[i]), v[r]);
-            if (kGate) z[r] = fmaf(up(y.v[i]), up(c[j].v[i]), z[r]);
+            v[r] = fmaf(up(y[r][j].v[i]), up(b[j].v[i]), v[r]);
+            if (kGate) z[r] = fmaf(up(y[r][j].v[i]), up(c[j].v[i]), z[r]);
           }
         }
       }
@@ -924,7 +920,7 @@ bool copyable(const op_linear_t& a) {
 template <class T>
 cudaError_t launch(const op_linear_t& a, int sms, void* work, cudaStream_t st) {
   if (!copyable(a)) return launch_any<T>(a, st);
-  if (a.m <= kFewRows) return a.gated ? launch_few<T, true>(a, sms, st) : launch_few<T, false>(a, sms, st);
+  if (a.m == 1 || (a.m <= kFewRows && a.n <= kFewTwo)) return a.gated ? launch_few<T, true>(a, sms, st) : launch_few<T, false>(a, sms, st);
   return a.gated ? launch_tiles<T, true>(a, sms, work, st) : launch_tiles<T, false>(a, sms, work, st);
 }
 
