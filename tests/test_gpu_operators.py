@@ -597,3 +597,44 @@ def test_a_step_of_requests_end_to_end():
     cache.compact()
     step([2, 3], 1, [0, 2], [45])
     assert cache.code()[0] == 0
+
+
+# ---------------------------------------------------------------------------
+# Together
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("pre", [[200], [321], [1001]])
+@pytest.mark.parametrize("H,Hk,D,page,dtype", [(8, 2, 128, 16, BF), (5, 1, 80, 64, HF), (6, 6, 64, 8, BF)])
+def test_attend_pooled_prefix_of_odd_lengths(pre, H, Hk, D, page, dtype):
+    """Prefixes that end inside a step and a page, read once for all requests (the plan joins)."""
+    n = 40
+    kv = [pre[0] + 1 + (13 * b) % 150 for b in range(n)]
+    _, plan, *_ = _check_attend([1] * n, kv, H, Hk, D, page, dtype, groups=[0, n], prefix=pre)
+    assert plan.c.n_joins >= n
+    q = [1 + b % 3 for b in range(n)]
+    _check_attend(q, [pre[0] + q[b] + (7 * b) % 60 for b in range(n)], H, Hk, D, page, dtype, groups=[0, n], prefix=pre)
+
+
+def test_attend_many_parts():
+    """More than eight parts a head, and few: both ways of joining them."""
+    _check_attend([1], [30011], 2, 1, 128, 16)
+    _check_attend([1, 2], [3000, 900], 2, 1, 64, 32)
+
+
+def test_executor_example():
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(__file__), "..", "examples"))
+    import executor_feedback as E
+    lines = []
+    r = E.main(layers=2, hidden=256, heads=4, kv_heads=2, ffn=320, requests=8, prompt=210, steps=5, n_dev=4, candidates=64,
+               say=lines.append)
+    ex = r["executor"]
+    assert ex.cache.status.tolist()[0] == 0 and ex.cache.status.tolist()[4:6] == [0, 0]
+    assert ex.cache.lens.tolist() == ex.len
+    refs = torch.zeros_like(ex.cache.refs)
+    used = ex.cache.table[ex.cache.table >= 0].long()
+    refs.index_add_(0, used, torch.ones_like(used, dtype=torch.int32))
+    assert torch.equal(refs, ex.cache.refs) and int((refs > 0).sum()) == int((refs[:int((refs > 0).sum())] > 0).sum())
+    assert all(len(s) for s in ex.samples.values()) and any("t = " in s for s in lines)
+    assert r["best"] >= 0 and r["makespan"] > 0 and bool((r["desc"].dur >= 1).all())

@@ -165,3 +165,51 @@ def test_rope_fractions_are_the_rounded_frequencies():
     got = p.freq.numpy().view(np.uint64).astype(object)
     for a, b in zip(got, f):
         assert abs(int(a) - b / (2 * np.pi) * 2.0 ** 64) <= 2.0 ** 64 * b / (2 * np.pi) * 2.0 ** -51 + 1
+
+
+def _covered(q, kv, heads, kv_heads, groups=None, prefix=None):
+    """Every (query, key) of a batch lies in one item, and joins list the parts of exactly those."""
+    plan, items = P.attend_items(q, kv, heads, kv_heads, 64, 16, group_off=groups, prefix=prefix)
+    g, n = heads // kv_heads, plan.n_items
+    cover, joined, used = {t: [] for t in range(sum(q))}, {}, set()
+    for tok0, n_tok, row, lo, hi, pos0, part, _ in items[:8 * n].reshape(n, 8).tolist():
+        assert 0 < n_tok * g <= 128
+        for t in range(tok0, tok0 + n_tok):
+            cover[t].append((lo, hi, row, pos0 + t - tok0, part + (t - tok0) * g if part >= 0 else -1))
+    for tok0, n_tok, b0, b1, s0, s1, n0, n1 in items[8 * n:].reshape(-1, 8).tolist():
+        assert n_tok <= plan.join_tokens
+        for t in range(tok0, tok0 + n_tok):
+            assert t not in joined
+            joined[t] = [b0 + i * s0 + (t - tok0) * g for i in range(n0)] + [b1 + i * s1 + (t - tok0) * g for i in range(n1)]
+    t = 0
+    for b in range(len(q)):
+        for i in range(q[b]):
+            runs, pos, at = sorted(cover[t]), kv[b] - q[b] + i, 0
+            if t in joined:
+                assert sorted(joined[t]) == sorted(r[4] for r in runs)
+                assert all(0 <= x and x + g <= plan.part_rows and x not in used for x in joined[t])
+                used.update(joined[t])
+            else:
+                assert len(runs) == 1 and runs[0][4] == -1
+            for lo, hi, row, p, _ in runs:
+                if hi:
+                    assert lo == at and (p == pos or p >= 0x7f000000)
+                    at = hi
+                    if row != b:
+                        k = [k for k in range(len(prefix)) if groups[k] <= b < groups[k + 1]][0]
+                        assert hi <= prefix[k] and groups[k] <= row < groups[k + 1]
+            assert at >= max(0, pos + 1)
+            t += 1
+
+
+def test_attend_plan_covers_every_key_once():
+    import random
+    r = random.Random(0)
+    for _ in range(150):
+        n, g, hk = r.randint(1, 40), r.choice([1, 2, 3, 4, 8, 40]), r.choice([1, 2, 8])
+        groups = [0] + sorted(r.randint(0, n) for _ in range(r.randint(0, 4))) + [n]
+        prefix = [r.choice([0, 1, 64, 100, 3000]) for _ in groups[1:]]
+        q = [r.choice([0, 1, 1, 1, 2, 9, 200]) for _ in range(n)]
+        kv = [prefix[k] + q[b] + r.choice([0, 0, 5, 70, 5000]) for k in range(len(prefix)) for b in range(groups[k], groups[k + 1])]
+        _covered(q, kv, g * hk, hk, groups, prefix)
+        _covered(q, [max(0, t - r.choice([0, 0, 3, 10 ** 6])) for t in kv], g * hk, hk)
