@@ -276,9 +276,9 @@ constexpr int kWeightBytes = 128 * kStep * 2;
 
 constexpr int kTailMax = 1 << 30;      // steps dealt out, at most
 
-// ---- up to 128 rows of x: a tile's columns split over a cluster
+// ---- few tiles: a tile's columns split over a cluster
 
-// A tile is 128 rows of the weight by all rows of x.  The blocks of a cluster take a share of
+// A tile is 128 rows of the weight by up to 256 rows of x.  The blocks of a cluster take a share of
 // its steps each, leave their sums in shared memory, and then each adds up and finishes a
 // share of the rows, in the order of the blocks.  Bound by reading the weight: two blocks an
 // SM keep 200 KB of it on the way.
@@ -295,7 +295,7 @@ struct SplitShape {
 
 struct SplitArgs {
   op_linear_t a;
-  int32_t split, steps;
+  int32_t split, steps, tiles_n;
   int32_t* status;
 };
 
@@ -308,6 +308,89 @@ __device__ __forceinline__ float4 load_peer(uint32_t addr, uint32_t rank) {
                : "r"(at)
                : "memory");
   return v;
+}
+
+template <class T>
+struct alignas(8) Four {
+  T v[4];
+};
+
+// Adds up and finishes rows first, first + 8 split, ... of the tile: four columns a lane, four rows
+// at a time so that their loads overlap, then one by one.
+template <int kAct, class T, int NT, bool kGate>
+__device__ __forceinline__ void split_rows(const op_linear_t& a, uint32_t smem, int first, int split, int64_t row0, int rows,
+                                           int64_t col) {
+  const int n = a.n - col < 4 ? int(a.n - col) : 4;
+  if (n <= 0) return;
+  float bias[4] = {}, gate_bias[4] = {};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < n) {
+      if (a.bias) bias[e] = up(static_cast<const T*>(a.bias)[col + e]);
+      if (kGate && a.gate_bias) gate_bias[e] = up(static_cast<const T*>(a.gate_bias)[col + e]);
+    }
+  T* y = static_cast<T*>(a.y) + row0 * a.y_row + col;
+  const T* res = a.residual ? static_cast<const T*>(a.residual) + row0 * a.residual_row + col : nullptr;
+  const bool wide_y = n == 4 && ((reinterpret_cast<uintptr_t>(y) | uintptr_t(a.y_row * 2)) & 7) == 0;
+  const bool wide_res = n == 4 && ((reinterpret_cast<uintptr_t>(res) | uintptr_t(a.residual_row * 2)) & 7) == 0;
+  const int step = 8 * split;
+  auto take = [&](int r0, auto count) {
+    constexpr int R = decltype(count)::value;
+    float v[R][4] = {}, g[kGate ? R : 1][4] = {};
+    Four<T> old[R];
+    if (res) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const T* from = res + (r0 + i * step) * a.residual_row;
+        if (wide_res) {
+          old[i] = *reinterpret_cast<const Four<T>*>(from);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < n) old[i].v[e] = from[e];
+        }
+      }
+    }
+#pragma unroll 2
+    for (int32_t w = 0; w < split; ++w) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const uint32_t at = smem + ((r0 + i * step) * 128 + (threadIdx.x & 31) * 4) * 4;
+        const float4 x = load_peer(at, w);
+        v[i][0] += x.x, v[i][1] += x.y, v[i][2] += x.z, v[i][3] += x.w;
+        if (kGate) {
+          const float4 z = load_peer(at + NT * 512, w);
+          float* to = g[kGate ? i : 0];
+          to[0] += z.x, to[1] += z.y, to[2] += z.z, to[3] += z.w;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      T* to = y + (r0 + i * step) * a.y_row;
+      Four<T> out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float f = v[i][e] + bias[e];
+        if (kGate) f *= act_of<kAct>(g[kGate ? i : 0][e] + gate_bias[e]);
+        else f = act_of<kAct>(f);
+        if (res) f += up(old[i].v[e]);
+        down(f, &out.v[e]);
+      }
+      if (wide_y) {
+        *reinterpret_cast<Four<T>*>(to) = out;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < n) to[e] = out.v[e];
+      }
+    }
+  };
+  int r = first;
+#pragma unroll 1
+  for (; r + 3 * step < rows; r += 4 * step) take(r, std::integral_constant<int, 4>{});
+#pragma unroll 1
+  for (; r < rows; r += step) take(r, std::integral_constant<int, 1>{});
 }
 
 template <class T, int NT, bool kGate>
@@ -325,7 +408,10 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
   const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const op_linear_t& a = L.a;
-  const int32_t tile = blockIdx.x / L.split, rank = blockIdx.x - tile * L.split;
+  const int32_t all = blockIdx.x / L.split, rank = blockIdx.x - all * L.split;
+  const int32_t tile_m = all / L.tiles_n, tile = all - tile_m * L.tiles_n;
+  const int64_t row0 = (int64_t)tile_m * NT;
+  const int rows = a.m - row0 < NT ? int(a.m - row0) : NT;
   const int32_t share = L.steps / L.split, more = L.steps - share * L.split;
   const int32_t k0 = rank * share + (rank < more ? rank : more), k1 = k0 + share + (rank < more);
 
@@ -353,7 +439,7 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
         bar_expect(bar, S::kStage);
         load_2d(at, &map_w, k * kStep, tile * 128, bar);
         if (kGate) load_2d(at + kWeightBytes, &map_g, k * kStep, tile * 128, bar);
-        load_2d(at + S::kStage - S::kXBytes, &map_x, k * kStep, 0, bar);
+        load_2d(at + S::kStage - S::kXBytes, &map_x, k * kStep, tile_m * NT, bar);
         ++issued;
         if (++stage == S::kStages) stage = 0, phase ^= 1;
       }
@@ -399,7 +485,6 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
     // the sums, [row of x][row of the weight]; warps of one half of the block take every other 16 rows
     const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     float* to = sums + (warp & 3) * 32 + lane;
-    const int rows = int(a.m);
 #pragma unroll 1
     for (int c0 = (warp >> 2) * 16; c0 < rows; c0 += 32) {
       uint32_t v[16], g[kGate ? 16 : 1];
@@ -420,39 +505,11 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
   if (warp == 2) tmem_free<1>(tmem, S::kAlloc);
   if (L.split > 1) cluster_sync();
   const int64_t col = (int64_t)tile * 128 + lane * 4;
-  constexpr int R = 4;     // rows at a time, so that their loads overlap
-  for (int r0 = rank + warp * L.split; r0 < a.m; r0 += 8 * R * L.split) {
-    float v[R][4], g[kGate ? R : 1][4];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int r = r0 + 8 * i * L.split;
-      v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0.f;
-      if (kGate) g[kGate ? i : 0][0] = g[kGate ? i : 0][1] = g[kGate ? i : 0][2] = g[kGate ? i : 0][3] = 0.f;
-      if (r >= a.m) continue;
-      const uint32_t at = smem + (r * 128 + lane * 4) * 4;
-#pragma unroll 2
-      for (int32_t w = 0; w < L.split; ++w) {
-        const float4 x = load_peer(at, w);
-        v[i][0] += x.x, v[i][1] += x.y, v[i][2] += x.z, v[i][3] += x.w;
-        if (kGate) {
-          const float4 y = load_peer(at + NT * 512, w);
-          float* z = g[kGate ? i : 0];
-          z[0] += y.x, z[1] += y.y, z[2] += y.z, z[3] += y.w;
-        }
-      }
-    }
-#pragma unroll 1
-    for (int i = 0; i < R; ++i) {
-      const int r = r0 + 8 * i * L.split;
-      if (r < a.m) finish4<T, kGate>(a, r, col, v[0], g[0]);
-#pragma unroll
-      for (int j = 0; j + 1 < R; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[j][e] = v[j + 1][e];
-          if (kGate) g[kGate ? j : 0][e] = g[kGate ? j + 1 : 0][e];
-        }
-    }
+  switch (a.act) {
+    case GMG_OP_RELU: split_rows<GMG_OP_RELU, T, NT, kGate>(a, smem, rank + warp * L.split, L.split, row0, rows, col); break;
+    case GMG_OP_SILU: split_rows<GMG_OP_SILU, T, NT, kGate>(a, smem, rank + warp * L.split, L.split, row0, rows, col); break;
+    case GMG_OP_GELU: split_rows<GMG_OP_GELU, T, NT, kGate>(a, smem, rank + warp * L.split, L.split, row0, rows, col); break;
+    default: split_rows<GMG_OP_NONE, T, NT, kGate>(a, smem, rank + warp * L.split, L.split, row0, rows, col);
   }
   if (L.split > 1) cluster_sync();   // the others have read this block's sums
   if (threadIdx.x == 0 && *failed) atomicAdd(L.status, 1);
@@ -884,7 +941,8 @@ cudaError_t launch_split(const op_linear_t& a, int sms, void* work, cudaStream_t
   cfg.numAttrs = 1;
   // the widest clusters of which one a tile fits on the GPU at once: a second round costs as
   // much as the first (6,144 x 1,024, 16 rows, clusters of 6: 12 us, of 3: 7)
-  const int64_t tiles = (a.n + 127) / 128;
+  L.tiles_n = int32_t((a.n + 127) / 128);
+  const int64_t tiles = L.tiles_n * ((a.m + NT_ - 1) / NT_);
   static int fits[64][9];   // clusters at once, by size; asked once per device
   for (L.split = L.steps < 8 ? L.steps : 8; L.split > 1; --L.split) {
     at[0].val.clusterDim.x = (unsigned)L.split;
@@ -899,13 +957,19 @@ cudaError_t launch_split(const op_linear_t& a, int sms, void* work, cudaStream_t
   return cudaLaunchKernelEx(&cfg, kernel, m.w, m.g, m.x, L);
 }
 
+// Whether a call is one of few tiles: those of pairs would leave more than half of the SMs idle.
+bool few_tiles(const op_linear_t& a, int sms) {
+  return a.m <= 128 || 2 * ((a.n + 255) / 256) * ((a.m + 255) / 256) <= sms / kPair;
+}
+
 template <class T, bool kGate>
 cudaError_t launch_tiles(const op_linear_t& a, int sms, void* work, cudaStream_t st) {
+  if (!few_tiles(a, sms)) return launch_pairs<T, kGate>(a, sms, work, st);
   if (a.m <= 16) return launch_split<T, 16, kGate>(a, sms, work, st);
   if (a.m <= 32) return launch_split<T, 32, kGate>(a, sms, work, st);
   if (a.m <= 64) return launch_split<T, 64, kGate>(a, sms, work, st);
-  if (a.m <= 128) return launch_split<T, 128, kGate>(a, sms, work, st);
-  return launch_pairs<T, kGate>(a, sms, work, st);
+  if (a.m <= 128 || kGate) return launch_split<T, 128, kGate>(a, sms, work, st);
+  return launch_split<T, 256, false>(a, sms, work, st);
 }
 
 // Whether bulk copies can read the operands: rows on 16 bytes.
@@ -944,10 +1008,10 @@ extern "C" {
 
 size_t op_linear_work_bytes(const op_linear_t* args) {
   if (!args_ok(args)) return 0;
-  if (args->m <= 128 || args->n == 0 || !copyable(*args)) return kHeadBytes;
-  const int sms = n_sm();
+  const int sms = n_sm() > 1 ? n_sm() : 152;
+  if (few_tiles(*args, sms) || args->n == 0 || !copyable(*args)) return kHeadBytes;
   size_t bytes;
-  sched_for(*args, sms > 1 ? sms : 152, &bytes);
+  sched_for(*args, sms, &bytes);
   return bytes;
 }
 
