@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
   const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
   float* sums = reinterpret_cast<float*>(raw + (smem - smem_addr(raw)));   // [columns][128], after the products
   const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   const op_linear_t& a = L.a;
   const int32_t all = blockIdx.x / L.split, rank = blockIdx.x - all * L.split;
   const int32_t tile_m = all / L.tiles_n, tile = all - tile_m * L.tiles_n;
@@ -428,54 +428,62 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
-  const uint32_t tmem = tmem_at;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
 
+  // a whole warp goes along with one lane that issues, so that what the instructions take is known
+  // to be the same in all lanes
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0, issued = 0;
-      for (int32_t k = k0; k < k1; ++k) {
-        if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
-        const uint32_t at = smem + stage * S::kStage, bar = full + 8 * stage;
+    uint32_t stage = 0, phase = 0, issued = 0;
+    for (int32_t k = k0; k < k1; ++k) {
+      if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
+      __syncwarp();
+      const uint32_t at = smem + stage * S::kStage, bar = full + 8 * stage;
+      if (elect_one()) {
         bar_expect(bar, S::kStage);
         load_2d(at, &map_w, k * kStep, tile * 128, bar);
         if (kGate) load_2d(at + kWeightBytes, &map_g, k * kStep, tile * 128, bar);
         load_2d(at + S::kStage - S::kXBytes, &map_x, k * kStep, tile_m * NT, bar);
-        ++issued;
+      }
+      ++issued;
+      if (++stage == S::kStages) stage = 0, phase ^= 1;
+    }
+    // every stage comes back before the block ends; after a failure the copies in flight get a
+    // bounded wait each
+    uint32_t quiet = 0;
+    if (!*failed) {
+      for (int i = 0; i < S::kStages; ++i) {
+        if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
         if (++stage == S::kStages) stage = 0, phase ^= 1;
       }
-      // every stage comes back before the block ends; after a failure the copies in flight get a
-      // bounded wait each
-      uint32_t quiet = 0;
-      if (!*failed) {
-        for (int i = 0; i < S::kStages; ++i) {
-          if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
-          if (++stage == S::kStages) stage = 0, phase ^= 1;
-        }
-      } else {
-        for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
-          if (stage == 0) phase ^= 1;
-          stage = stage == 0 ? S::kStages - 1 : stage - 1;
-          bar_wait(full + 8 * stage, phase, &quiet);
-        }
+    } else {
+      for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
+        if (stage == 0) phase ^= 1;
+        stage = stage == 0 ? S::kStages - 1 : stage - 1;
+        bar_wait(full + 8 * stage, phase, &quiet);
       }
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
     constexpr uint32_t idesc = mma_desc(std::is_same<T, __nv_bfloat16>::value, 128, NT, false);
+    const uint64_t ring = tile_k(smem);
     uint32_t stage = 0, phase = 0;
     for (int32_t k = k0; k < k1; ++k) {
       if (!bar_wait(full + 8 * stage, phase, failed)) break;
+      __syncwarp();
       tc_after_sync();
-      const uint32_t at = smem + stage * S::kStage;
-      const uint64_t w = tile_k(at), g = tile_k(at + kWeightBytes), x = tile_k(at + S::kStage - S::kXBytes);
+      const uint64_t w = ring + stage * (S::kStage / 16), g = w + kWeightBytes / 16, x = w + (S::kStage - S::kXBytes) / 16;
+      const bool add = k > k0;
+      if (elect_one()) {
 #pragma unroll
-      for (int j = 0; j < kStep / 16; ++j) {
-        mma_ss<1>(tmem, w + 2 * j, x + 2 * j, idesc, k > k0 || j > 0);
-        if (kGate) mma_ss<1>(tmem + NT, g + 2 * j, x + 2 * j, idesc, k > k0 || j > 0);
+        for (int j = 0; j < kStep / 16; ++j) {
+          mma_ss<1>(tmem, w + 2 * j, x + 2 * j, idesc, add || j > 0);
+          if (kGate) mma_ss<1>(tmem + NT, g + 2 * j, x + 2 * j, idesc, add || j > 0);
+        }
+        mma_commit(empty + 8 * stage);
       }
-      mma_commit(empty + 8 * stage);
+      __syncwarp();
       if (++stage == S::kStages) stage = 0, phase ^= 1;
     }
-    mma_commit(done);
+    if (elect_one()) mma_commit(done);
   }
   __syncwarp();
   bar_wait(done, 0, failed);   // every copy has landed and been read
@@ -636,7 +644,7 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
   const uint32_t smem = (smem_addr(raw) + 1023) & ~1023u;
   const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages,
                  drained = done + 8 * S::kBuffers;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int32_t worker = blockIdx.x / kPair;
   const Sched& s = L.s;
@@ -655,51 +663,52 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
   __syncthreads();
   cluster_sync();
   tc_after_sync();
-  const uint32_t tmem = tmem_at;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
 
   if (warp == 0) {
-    if (lane == 0) {
-      // copies: a ring of stages, refilled as the products that read them complete
-      uint32_t stage = 0, phase = 0, issued = 0;
-      bool go = true;
-      Pieces it(s, worker);
-      Piece p;
-      while (go && it.next(&p)) {
-        const int32_t row_w = p.tile_n * (128 * kPair) + rank * 128, row_x = p.tile_m * NT + rank * (NT / kPair);
-        for (int32_t k = p.k0; k < p.k1; ++k) {
-          if (!(go = bar_wait(empty + 8 * stage, phase ^ 1, failed))) break;
-          const uint32_t at = smem + stage * S::kStage;
-          uint32_t bar = full + 8 * stage;
+    // copies: a ring of stages, refilled as the products that read them complete
+    uint32_t stage = 0, phase = 0, issued = 0;
+    bool go = true;
+    Pieces it(s, worker);
+    Piece p;
+    while (go && it.next(&p)) {
+      const int32_t row_w = p.tile_n * (128 * kPair) + rank * 128, row_x = p.tile_m * NT + rank * (NT / kPair);
+      for (int32_t k = p.k0; k < p.k1; ++k) {
+        if (!(go = bar_wait(empty + 8 * stage, phase ^ 1, failed))) break;
+        __syncwarp();
+        const uint32_t at = smem + stage * S::kStage;
+        if (elect_one()) {
           // both blocks' copies count on the first block's barrier
-          if (rank == 0) bar_expect(bar, 2 * S::kStage);
-          bar = bar_of(bar, 0);
+          if (rank == 0) bar_expect(full + 8 * stage, 2 * S::kStage);
+          const uint32_t bar = bar_of(full + 8 * stage, 0);
           load_2d_pair(at, &map_w, k * kStep, row_w, bar);
           if (kGate) load_2d_pair(at + kWeightBytes, &map_g, k * kStep, row_w, bar);
           load_2d_pair(at + S::kStage - S::kXBytes, &map_x, k * kStep, row_x, bar);
-          ++issued;
-          if (++stage == S::kStages) stage = 0, phase ^= 1;
         }
+        ++issued;
+        if (++stage == S::kStages) stage = 0, phase ^= 1;
       }
-      // every stage comes back before the block ends: its copies have landed, and the products
-      // have sent their arrivals; after a failure the copies in flight get a bounded wait each
-      uint32_t quiet = 0;
-      if (!*failed) {
-        for (int i = 0; i < S::kStages; ++i) {
-          if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
-          if (++stage == S::kStages) stage = 0, phase ^= 1;
-        }
-      } else if (rank == 0) {
-        for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
-          if (stage == 0) phase ^= 1;
-          stage = stage == 0 ? S::kStages - 1 : stage - 1;
-          bar_wait(full + 8 * stage, phase, &quiet);
-        }
+    }
+    // every stage comes back before the block ends: its copies have landed, and the products
+    // have sent their arrivals; after a failure the copies in flight get a bounded wait each
+    uint32_t quiet = 0;
+    if (!*failed) {
+      for (int i = 0; i < S::kStages; ++i) {
+        if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
+        if (++stage == S::kStages) stage = 0, phase ^= 1;
+      }
+    } else if (rank == 0) {
+      for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
+        if (stage == 0) phase ^= 1;
+        stage = stage == 0 ? S::kStages - 1 : stage - 1;
+        bar_wait(full + 8 * stage, phase, &quiet);
       }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       constexpr uint32_t idesc = mma_desc(std::is_same<T, __nv_bfloat16>::value, 128 * kPair, NT, false);
+      const uint64_t ring = tile_k(smem);
       uint32_t stage = 0, phase = 0;
       bool go = true;
       Pieces it(s, worker);
@@ -707,21 +716,27 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
       for (uint32_t n = 0; go && it.next(&p); ++n) {
         const uint32_t buf = n % S::kBuffers, d = tmem + buf * S::kColumns;
         if (!bar_wait(drained + 8 * buf, ((n / S::kBuffers) & 1) ^ 1, failed)) break;
+        __syncwarp();
         tc_after_sync();
         for (int32_t k = p.k0; k < p.k1; ++k) {
           if (!(go = bar_wait(full + 8 * stage, phase, failed))) break;
+          __syncwarp();
           tc_after_sync();
-          const uint32_t at = smem + stage * S::kStage;
-          const uint64_t w = tile_k(at), g = tile_k(at + kWeightBytes), x = tile_k(at + S::kStage - S::kXBytes);
+          const uint64_t w = ring + stage * (S::kStage / 16), g = w + kWeightBytes / 16, x = w + (S::kStage - S::kXBytes) / 16;
+          const bool add = k > p.k0;
+          if (elect_one()) {
 #pragma unroll
-          for (int j = 0; j < kStep / 16; ++j) {
-            mma_ss<kPair>(d, w + 2 * j, x + 2 * j, idesc, k > p.k0 || j > 0);
-            if (kGate) mma_ss<kPair>(d + NT, g + 2 * j, x + 2 * j, idesc, k > p.k0 || j > 0);
+            for (int j = 0; j < kStep / 16; ++j) {
+              mma_ss<kPair>(d, w + 2 * j, x + 2 * j, idesc, add || j > 0);
+              if (kGate) mma_ss<kPair>(d + NT, g + 2 * j, x + 2 * j, idesc, add || j > 0);
+            }
+            mma_commit_pair(empty + 8 * stage);
           }
-          mma_commit_pair(empty + 8 * stage);
+          __syncwarp();
           if (++stage == S::kStages) stage = 0, phase ^= 1;
         }
-        mma_commit_pair(done + 8 * buf);
+        if (elect_one()) mma_commit_pair(done + 8 * buf);
+        __syncwarp();
       }
     }
     __syncwarp();
