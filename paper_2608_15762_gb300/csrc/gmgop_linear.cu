@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "../../include/gmgop.h"
@@ -846,14 +847,16 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 }
 
 int n_sm() {
-  static int count[64] = {};
+  static std::atomic<int> count[64];
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (!count[dev] && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) count[dev] = n;
-  return count[dev];
+  if ((n = count[dev].load(std::memory_order_relaxed)) == 0 &&
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
+    count[dev].store(n, std::memory_order_relaxed);
+  return n;
 }
 
-// How the tiles of a call with more than 128 rows are dealt out, and its workspace.
+// How the tiles of pairs are dealt out, and the workspace.
 Sched sched_for(const op_linear_t& a, int sms, size_t* work) {
   Sched s{};
   s.tiles_n = int32_t((a.n + 128 * kPair - 1) / (128 * kPair));
@@ -958,13 +961,13 @@ cudaError_t launch_split(const op_linear_t& a, int sms, void* work, cudaStream_t
   // much as the first (6,144 x 1,024, 16 rows, clusters of 6: 12 us, of 3: 7)
   L.tiles_n = int32_t((a.n + 127) / 128);
   const int64_t tiles = L.tiles_n * ((a.m + NT_ - 1) / NT_);
-  static int fits[64][9];   // clusters at once, by size; asked once per device
+  static std::atomic<int> fits[64][9];   // clusters at once, by size; asked once per device
   for (L.split = L.steps < 8 ? L.steps : 8; L.split > 1; --L.split) {
     at[0].val.clusterDim.x = (unsigned)L.split;
     cfg.gridDim = dim3((unsigned)(sms / L.split * L.split));
-    int n = dev < 64 ? fits[dev][L.split] : 0;
+    int n = dev < 64 ? fits[dev][L.split].load(std::memory_order_relaxed) : 0;
     if (n == 0 && cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) n = 0;
-    if (dev < 64) fits[dev][L.split] = n;
+    if (dev < 64) fits[dev][L.split].store(n, std::memory_order_relaxed);
     if (n >= tiles) break;
   }
   at[0].val.clusterDim.x = (unsigned)L.split;

@@ -248,8 +248,8 @@ class Rope:
     ``rope_freqs``, or its arguments."""
 
     def __init__(self, rotary: int, freqs=None, factor: float = 1.0, interleaved: bool = False, device="cuda", **kw):
-        if freqs is None:
-            freqs, factor = rope_freqs(rotary, **kw)
+        if freqs is None:   # (no rotation at all where rotary is 0)
+            freqs, factor = rope_freqs(rotary, **kw) if rotary else (np.zeros(0), factor)
         freqs = np.asarray(freqs, np.float64)
         _need(freqs.shape == (rotary // 2,) and rotary % 2 == 0, "freqs: one per pair")
         _need(bool(np.all((freqs >= 0) & (freqs < 2 * math.pi))), "freqs: 0 <= f < 2 pi")
@@ -413,6 +413,10 @@ class Workspace:
                 self.buf[:4096].zero_()
             self.ptr, self.size = self.buf.data_ptr(), self.buf.numel()
         return self.buf
+
+    def gave_up(self) -> int:
+        """Waits of ``linear`` that gave up (0 unless the GPU is at fault); synchronises."""
+        return 0 if self.buf is None else int(self.buf[:4].view(torch.int32).item())
 
 
 _WORK = {}

@@ -600,6 +600,61 @@ def test_a_step_of_requests_end_to_end():
 
 
 # ---------------------------------------------------------------------------
+# Offsets beyond 32 bits
+# ---------------------------------------------------------------------------
+
+def test_linear_and_rope_beyond_2_31_elements():
+    g = _gen(61)
+    m, n, k = 70_001, 32_768, 64
+    x, w = _rand(g, m, k), _rand(g, n, k, scale=1 / 8)
+    ws = P.Workspace()
+    y = P.linear(x, w, ws=ws)
+    assert y.numel() > 2 ** 31 and ws.gave_up() == 0
+    for part in (slice(0, 2), slice(65_530, 65_540), slice(m - 3, m)):
+        want, tol = R.linear(x[part], w)
+        R.within(y[part], want, tol)
+    heads = y.view(m, n // 128, 128)
+    pos = torch.arange(m, dtype=torch.int32, device="cuda")
+    last = heads[m - 2:].clone()
+    P.rope(P.Rope(128), heads, pos, out=heads)
+    want, tol = R.rope(last, pos[m - 2:], P.rope_freqs(128)[0])
+    R.within(heads[m - 2:], want, tol)
+
+
+def test_cache_beyond_2_31_elements():
+    """The last pages of a pool of more than 2^31 elements: appended to, copied, read."""
+    g = _gen(62)
+    hk, page, D, n_pages = 8, 64, 128, 17_000
+    pool = torch.empty(n_pages, 1, 2, hk, page, D, dtype=BF, device="cuda")
+    assert pool.numel() > 2 ** 31
+    c = P.PageCache(pool, n_seq=3, max_pages=6)
+    c.refs.fill_(1)                      # only pages at the far end, and one in front, are free
+    c.refs[n_pages - 8:] = 0
+    c.refs[3] = 0
+    c.grow(_ints([0]), _ints([150]))
+    assert c.table[0].tolist()[:3] == [3, n_pages - 8, n_pages - 7]
+    k, v = _rand(g, 150, hk, D), _rand(g, 150, hk, D)
+    none = torch.empty(150, 0, D, dtype=BF, device="cuda")
+    at = torch.arange(150, dtype=torch.int32, device="cuda")
+    P.rope_append(P.Rope(0), none, k, v, at, torch.zeros_like(at), c, 0)
+    c.fork(_ints([0]), _ints([1]))
+    c.grow(_ints([1, 0]), _ints([1, 1]))
+    new = [torch.cat((t, _rand(g, 1, hk, D))) for t in (k, v)]
+    P.rope_append(P.Rope(0), none[:1], new[0][150:], new[1][150:], _ints([150]), _ints([1]), c, 0)
+    q = _rand(g, 1, 16, D)
+    o, lse = P.attend(P.AttendPlan([1], [151], 16, hk, D, page, seq=[1]), q, c, 0, lse=True)
+    wo, to, wl, tl = R.attend(q, *new, 1, D ** -0.5)
+    R.within(o, wo, to)
+    R.within(lse, wl, tl)
+    assert c.code()[0] == P.PAGE_OK and c.table[1].tolist()[2] == n_pages - 6
+    c.free(_ints([0]))
+    c.compact()
+    assert c.status.tolist()[2] == 0 or int(c.refs[n_pages - 1]) == 0
+    o2 = P.attend(P.AttendPlan([1], [151], 16, hk, D, page, seq=[1]), q, c, 0)
+    assert torch.equal(o2, o)
+
+
+# ---------------------------------------------------------------------------
 # Together
 # ---------------------------------------------------------------------------
 
