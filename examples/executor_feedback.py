@@ -76,23 +76,29 @@ class Executor:
         kv = [o + n for o in old]
         plan = P.AttendPlan([n] * B, kv, H, Hk, D, self.page, seq=rows,
                             group_off=None if group is None else [0, B], prefix=None if group is None else [group])
-        for _ in range(20 * self.layers):   # keeps the GPU behind the host, so that events time operators and not launches
-            P.linear(self.ahead, self.ahead)
-        x = torch.randn(T, self.hidden, generator=self.gen, device="cuda").to(self.dtype)
+        first = torch.randn(T, self.hidden, generator=self.gen, device="cuda").to(self.dtype)
         pairs = float(sum(n * (t - n) + n * (n + 1) // 2 for t in kv))
         read = float(sum(kv) - (B - 1) * (group or 0))
-        for layer, w in enumerate(self.w):
-            def product(kind, a, weight, **kw):
-                m, k = a.shape
-                return self.call(kind, (float(m) * weight.shape[0] * k, 1.0), lambda: P.linear(a, weight, **kw))
 
-            qkv = product("qkv", norm(x), w["qkv"])
-            q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([H * D, Hk * D, Hk * D], 1))
-            q = self.call("rope", (float(T), 1.0), lambda: P.rope_append(self.rope, q, k, v, pos, seq, self.cache, layer))
-            o = self.call("attn", (pairs, read, 1.0), lambda: P.attend(plan, q, self.cache, layer))
-            x = product("oproj", o.flatten(1), w["o"], residual=x)
-            h = product("gateup", norm(x), w["up"], gate=w["gate"], act="silu")
-            x = product("down", h, w["down"], residual=x)
+        def product(kind, a, weight, **kw):
+            m, k = a.shape
+            return self.call(kind, (float(m) * weight.shape[0] * k, 1.0), lambda: P.linear(a, weight, **kw))
+
+        # twice: the first pass brings memory and code, the second is timed, behind enough other work that
+        # the host has issued it when the GPU comes to it
+        for timed in (False, True):
+            x, self.timed = first, []
+            for _ in range(20 * self.layers if timed else 0):
+                P.linear(self.ahead, self.ahead)
+            for layer, w in enumerate(self.w):
+                qkv = product("qkv", norm(x), w["qkv"])
+                q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([H * D, Hk * D, Hk * D], 1))
+                q = self.call("rope", (float(T), 1.0),
+                              lambda: P.rope_append(self.rope, q, k, v, pos, seq, self.cache, layer))
+                o = self.call("attn", (pairs, read, 1.0), lambda: P.attend(plan, q, self.cache, layer))
+                x = product("oproj", o.flatten(1), w["o"], residual=x)
+                h = product("gateup", norm(x), w["up"], gate=w["gate"], act="silu")
+                x = product("down", h, w["down"], residual=x)
         for r in rows:
             self.len[r] += n
         torch.cuda.synchronize()
