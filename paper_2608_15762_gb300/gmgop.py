@@ -344,11 +344,15 @@ def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=
     ptr = [None if a is None else a.ctypes.data for a in arr]
     d = _AttendDesc(q.size, n_heads, n_kv_heads, head_dim, page_tokens, 0 if pre is None else pre.size, *ptr)
     plan = _AttendPlan()
-    _check((_LIB or lib()).op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), None, 0), "op_attend_plan")
-    items = np.zeros(plan.plan_bytes // 4, np.int32)
-    _check((_LIB or lib()).op_attend_plan(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes),
-           "op_attend_plan")
-    return plan, items
+    items = np.empty(1 << 14, np.int32)      # most plans are shorter; longer ones are made again
+    call = (_LIB or lib()).op_attend_plan
+    rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
+    if rc == G.GMG_EWS:
+        _check(call(C.addressof(d), n_sm, C.addressof(plan), None, 0), "op_attend_plan")
+        items = np.empty(plan.plan_bytes // 4, np.int32)
+        rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
+    _check(rc, "op_attend_plan")
+    return plan, items[:plan.plan_bytes // 4].copy()
 
 
 class AttendPlan:
