@@ -618,6 +618,7 @@ struct Run {
 };
 
 constexpr int64_t kMinSteps = 6;   // of an item that is cut (16 requests behind 8,000 tokens: 2 25 us, 6 15, 8 15; 8 short ones: 6 11, 8 13)
+constexpr int64_t kItemSteps = 4;  // what an item costs beyond its steps (0: 96 requests behind 32,768 tokens 81 us, 4: 73)
 constexpr int64_t kJoinSteps = 8;  // what writing and joining a tile's partial results costs, in steps
 
 void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
@@ -653,7 +654,7 @@ void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
     }
   }
   int64_t steps = 0;
-  for (const Run& r : runs) steps += r.steps();
+  for (const Run& r : runs) steps += r.steps() + kItemSteps;
   const int64_t most = std::max(kMinSteps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
   // cut; then longest first, so that short items fill the end (equal ones keep their order:
   // tiles that read the same keys stay together)
