@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import math
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -58,6 +59,9 @@ class _Linear(C.Structure):
         (n, C.c_int64) for n in ("x_row", "w_row", "gate_row", "residual_row", "y_row")]
 
 
+# _Linear's bytes: packing them is quicker than filling a ctypes structure.
+_LINEAR = struct.Struct("@4i3q7P5q")
+assert _LINEAR.size == C.sizeof(_Linear)
 _LIB = None
 
 
@@ -374,6 +378,12 @@ class AttendPlan:
         with _on(stream):
             self.items = torch.from_numpy(items).to(dev)
         self._ptr = self.items.data_ptr() if items.size else None
+        self.work, self._kept = {}, []       # a workspace per stream that the plan has been used on
+
+    def new_work(self, handle):
+        self._kept.append(_aligned_empty(self.work_bytes, self.items.device))
+        self.work[handle] = self._kept[-1].data_ptr()
+        return self.work[handle]
 
 
 @_traced("op_attend")
@@ -383,20 +393,25 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
     after another) over the cache; with ``lse`` also log sum exp [tokens, heads], fp32."""
     if q.shape != plan.shape or q.dtype is not cache.dtype or q.device != cache.device:
         raise ValueError("q: [tokens, heads, head_dim] of the plan, the cache's type, on its GPU")
-    with _on(stream) if stream is not None else _HERE:
+    h = _handle(stream, cache._index)
+    work = plan.work.get(h)
+    if stream is None:
         out = _like(q, out, None)
         z = torch.empty(plan.shape[:2], dtype=torch.float32, device=q.device) if lse else None
-        work = torch.empty(plan.work_bytes, dtype=torch.uint8, device=q.device)
+        if work is None:
+            work = plan.new_work(h)
+    else:
+        with torch.cuda.stream(stream):
+            out = _like(q, out, None)
+            z = torch.empty(plan.shape[:2], dtype=torch.float32, device=q.device) if lse else None
+            if work is None:
+                work = plan.new_work(h)
     rc = (_LIB or lib()).op_attend(plan.ref, plan._ptr, cache.ref, layer, *_heads(q, "q"),
-                         plan.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
-                         None if z is None else z.data_ptr(), work.data_ptr(), plan.work_bytes,
-                         _handle(stream, cache._index))
+                                   plan.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
+                                   None if z is None else z.data_ptr(), work, plan.work_bytes, h)
     if rc:
         _fail(rc, "op_attend")
     return (out, z) if lse else out
-
-
-_HERE = contextlib.nullcontext()
 
 
 # ---------------------------------------------------------------------------
@@ -464,20 +479,23 @@ def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residu
     xp, xs = _rows(x, m, k, dt, dev, "x")
     wp, wrow = _rows(w, n, k, dt, dev, "w")
     yp, ys = _rows(out, m, n, dt, dev, "out")
-    gp, gs = (None, 0) if gate is None else _rows(gate, n, k, dt, dev, "gate")
-    rp, rs = (None, 0) if residual is None else _rows(residual, m, n, dt, dev, "residual")
-    a = _Linear(kind, how, 0 if gate is None else 1, 0, m, n, k, xp, wp, gp,
-                None if bias is None else _column(bias, n, dt, dev, "bias"),
-                None if gate_bias is None else _column(gate_bias, n, dt, dev, "gate_bias"), rp, yp, xs, wrow, gs, rs, ys)
-    ref = C.byref(a)
+    gp, gs = (0, 0) if gate is None else _rows(gate, n, k, dt, dev, "gate")
+    rp, rs = (0, 0) if residual is None else _rows(residual, m, n, dt, dev, "residual")
+    a = _LINEAR.pack(kind, how, 0 if gate is None else 1, 0, m, n, k, xp, wp, gp,
+                     0 if bias is None else _column(bias, n, dt, dev, "bias"),
+                     0 if gate_bias is None else _column(gate_bias, n, dt, dev, "gate_bias"), rp, yp, xs, wrow, gs, rs, ys)
     h = _handle(stream, index)
     if ws is None:
         ws = _WORK.get((index, h))
         if ws is None:
             ws = _WORK[(index, h)] = Workspace(dev)
+    if ws.ptr == 0:
+        ws.get(4096, stream)
     L = _LIB or lib()
-    ws.get(L.op_linear_work_bytes(ref), stream)
-    rc = L.op_linear(ref, ws.ptr, ws.size, h)
+    rc = L.op_linear(a, ws.ptr, ws.size, h)
+    if rc == G.GMG_EWS:      # it refuses a short workspace before it does anything
+        ws.get(L.op_linear_work_bytes(a), stream)
+        rc = L.op_linear(a, ws.ptr, ws.size, h)
     if rc:
         _fail(rc, "op_linear")
     return out
