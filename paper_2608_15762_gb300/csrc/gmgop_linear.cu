@@ -1,5 +1,15 @@
 // Product of a batch of rows with a weight, and its epilogue: bias, activation, gate,
 // residual.  The C ABI is declared in include/gmgop.h.
+//
+// Four kernels, by the number of rows of x and the tiles that there are (see few_tiles and
+// kFewRows), and one more for operands that bulk copies cannot read.  us a call, replayed on
+// weights beyond the L2 cache; in brackets the floor and what bounds it:
+//   1 x 4,096 x 4,096 (rows, columns of x, outputs)   9.9 (5.0: reading the weight, and the launch)
+//   16 x 4,096 x 12,288                              22.5 (15: reading the weight, 4.5 TB/s)
+//   77 x 1,000 x 1,111                                7.2 (0.4: launch, a chain of copy, product, sums)
+//   2,048 x 4,096 x 12,288 with a gate                264 (212: 5.05 rounds of tiles; tensor cores 72%
+//       busy: a tile's end is not hidden behind the next tile, as its two sums take all of TMEM)
+//   8,192 x 12,288 x 4,096 and a residual             436 (424: tensor cores, 88% busy; the power limit)
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -95,7 +105,8 @@ __device__ __forceinline__ void finish4(const op_linear_t& a, int64_t row, int64
 
 // A block of 256 threads takes 64 x 64 outputs, a thread 4 x 4, from tiles of 16
 // columns in shared memory.  It makes no assumption on alignment; bound by the fp32
-// multiply-adds of the ordinary cores.
+// multiply-adds of the ordinary cores (8,192 x 12,288 x 4,096 33.8 ms, 77 x 1,000 x 1,111
+// 138 us; the kernels below need rows on 16 bytes).
 constexpr int kTile = 64, kDepth = 16;
 
 template <class T, bool kGate>
@@ -282,7 +293,8 @@ constexpr int kTailMax = 1 << 30;      // steps dealt out, at most
 // A tile is 128 rows of the weight by up to 256 rows of x.  The blocks of a cluster take a share of
 // its steps each, leave their sums in shared memory, and then each adds up and finishes a
 // share of the rows, in the order of the blocks.  Bound by reading the weight: two blocks an
-// SM keep 200 KB of it on the way.
+// SM keep 200 KB of it on the way.  (A second launch that adds partial results from memory took
+// 2 to 3 us more, the last block adding them alone 40.)
 template <int NT, bool kGate>
 struct SplitShape {
   static constexpr int kXBytes = NT * kStep * 2;
@@ -975,7 +987,9 @@ cudaError_t launch_split(const op_linear_t& a, int sms, void* work, cudaStream_t
   return cudaLaunchKernelEx(&cfg, kernel, m.w, m.g, m.x, L);
 }
 
-// Whether a call is one of few tiles: those of pairs would leave more than half of the SMs idle.
+// Whether a call is one of few tiles: those of pairs would leave more than half of the SMs idle
+// (us, over a cluster / over pairs: 4,096 x 4,096 with 256 rows 16.3 / 24.1, 512 rows 18.9 / 24.9,
+// 1,024 rows, 64 tiles of pairs, 26.6 / 26.2; 12,288 x 4,096 with 256 rows, 48 tiles, 35.5 / 29.0).
 bool few_tiles(const op_linear_t& a, int sms) {
   return a.m <= 128 || 2 * ((a.n + 255) / 256) * ((a.m + 255) / 256) <= sms / kPair;
 }

