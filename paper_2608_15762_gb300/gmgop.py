@@ -5,7 +5,7 @@ epilogue (``linear``), rotary positions (``rope``, ``rope_append``), a paged cac
 (``PageCache``) and attention over shared prefixes (``AttendPlan``, ``attend``).
 Argument marshalling only; PyTorch provides device memory and streams.  Calls
 are asynchronous on the current stream, or on ``stream``, where their results'
-memory then belongs.  What the C ABI refuses raises ``GmgError``; tensors of the
+memory then belongs (and which their inputs' memory has to outlive).  What the C ABI refuses raises ``GmgError``; tensors of the
 wrong shape, type or device raise ``ValueError``.
 """
 from __future__ import annotations

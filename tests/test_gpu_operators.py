@@ -543,6 +543,43 @@ def test_attend_strides_streams_and_graph():
     assert torch.equal(y, want)
 
 
+def test_attend_heads_outside_tokens_and_wide_groups():
+    """Queries and results laid out head by head; 128 query heads on one key/value head."""
+    g = _gen(42)
+    for H, Hk, D in ((6, 2, 64), (128, 1, 128), (100, 1, 72)):
+        q_len, kv = [3, 1, 40], [77, 300, 41]
+        cache, keys, vals = _filled(g, kv, Hk, D, 32)
+        q = _rand(g, H, sum(q_len), D).transpose(0, 1)
+        out = torch.empty(H, sum(q_len), D, dtype=BF, device="cuda").transpose(0, 1)
+        plan = P.AttendPlan(q_len, kv, H, Hk, D, 32)
+        o, lse = P.attend(plan, q, cache, 1, out=out, lse=True)
+        at = 0
+        for b, n in enumerate(q_len):
+            wo, to, wl, tl = R.attend(q[at:at + n], keys[b], vals[b], n, D ** -0.5)
+            R.within(o[at:at + n], wo, to)
+            R.within(lse[at:at + n], wl, tl)
+            at += n
+
+
+def test_attend_one_plan_on_two_streams():
+    g = _gen(44)
+    kv = [900] * 6
+    cache, keys, vals = _filled(g, kv, 2, 64, 16)
+    plan = P.AttendPlan([1] * 6, kv, 16, 2, 64, 16)
+    assert plan.c.n_joins > 0
+    qs = [_rand(g, 6, 16, 64) for _ in range(2)]
+    want = [P.attend(plan, q, cache, 1) for q in qs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            got[i].append(P.attend(plan, qs[i], cache, 1, stream=st))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in got[i])
+
+
 def test_attend_table_with_missing_pages():
     """A page number outside the pool reads as no token's, never outside the pool's memory."""
     g = _gen(43)
