@@ -12,6 +12,7 @@ modification time alone.
 import hashlib
 import os
 import platform
+import shutil
 import subprocess
 import sys
 
@@ -25,6 +26,9 @@ HEADERS = ["gmg_layout.h", "gmg_access.h", "gmg_arb.h", "gmg_arbw.h", "gmg_arb_e
            os.path.join("..", "..", "include", "gmgest.h"), os.path.join("..", "..", "include", "gmground.h"),
            os.path.join("..", "..", "include", "gmgop.h"), "gmgop_host.h", "gmgop_ptx.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
+# The shared CUDA runtime, which PyTorch uses too: with one of its own in the library each had to
+# find the other's device state changed, 2 to 4 us a call that allocates its result.
+LINK = ["-cudart", "shared"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 
 
@@ -49,7 +53,7 @@ def stamp() -> str:
     for name in SOURCES + HEADERS:
         with open(os.path.join(CSRC, name), "rb") as f:
             h.update(name.encode() + b"\0" + f.read() + b"\0")
-    h.update(" ".join(ARCH + FLAGS).encode())
+    h.update(" ".join(ARCH + FLAGS + LINK).encode())
     h.update(_nvcc_version().encode())
     h.update(platform.machine().encode())
     return h.hexdigest()
@@ -86,7 +90,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if p.returncode != 0:
             raise RuntimeError("nvcc failed: " + " ".join(cmd))
     tmp = OUT + ".tmp%d" % os.getpid()
-    subprocess.check_call([nvcc()] + ARCH + ["-shared", "-o", tmp] + objs)
+    home = os.path.dirname(os.path.dirname(shutil.which(nvcc()) or nvcc()))
+    subprocess.check_call([nvcc()] + ARCH + LINK + ["-Xlinker", "-rpath," + os.path.join(home, "lib64"), "-shared", "-o",
+                                                    tmp] + objs)
     os.replace(tmp, OUT)
     with open(STAMP, "w") as f:
         f.write(want + "\n")
