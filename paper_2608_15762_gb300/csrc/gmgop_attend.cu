@@ -25,7 +25,7 @@
 //       the L2 cache (514 MB, 7.5 TB/s), then the start and end of 768 short items
 //   chunks of prompts, 8,691 queries behind 4,000   240, floor 107: the softmax warps' instructions
 //       (55% of the issue slots, two blocks an SM; the tensor cores are 41% busy)
-//   8 requests behind 500 shared tokens             11: two launches, a chain of four steps
+//   8 requests behind 500 shared tokens             9.7: a launch and a chain of eight steps
 // Two blocks an SM hide each other's waits; TMEM holds no third (O 128 columns, S and P 128).
 
 #include <cuda_bf16.h>
@@ -630,11 +630,23 @@ struct Run {
 };
 
 constexpr int64_t kMinSteps = 6;   // of an item that is cut (16 requests behind 8,000 tokens: 2 25 us, 6 15, 8 15; 8 short ones: 6 11, 8 13)
+// Up to so many steps a block takes alone, where one round of blocks is enough (us on the GPU / a call
+// from the host, joined and alone: 8 requests behind 500 tokens 11.4 / 16.5 and 9.7 / 12.8, 32 of up to
+// 616 tokens 13.9 / 17.0 and 11.8 / 13.1; with 16 steps one request of 1,000 tokens 11.8 and 14.0).
+constexpr int64_t kAloneSteps = 12;
 constexpr int64_t kItemSteps = 4;  // what an item costs beyond its steps (0: 96 requests behind 32,768 tokens 81 us, 4: 73)
 constexpr int64_t kJoinSteps = 8;  // what writing and joining a tile's partial results costs, in steps
 
 void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
   const int32_t group = d.n_heads / d.n_kv_heads, tile = kRows / group;
+  // a small step, which one round of blocks takes with a few steps each: apart and uncut, so that
+  // nothing is left to join
+  int64_t alone = 0, longest = 0;
+  for (int32_t b = 0; b < d.n_batch; ++b) {
+    alone += (d.q_len[b] + tile - 1) / tile;
+    if (d.q_len[b] > 0) longest = std::max<int64_t>(longest, (d.kv_len[b] + kKeys - 1) / kKeys);
+  }
+  const bool small = alone * d.n_kv_heads <= 2 * n_sm && longest <= kAloneSteps;
   std::vector<Run> runs;
   const int32_t ng = d.n_groups > 0 ? d.n_groups : 1;
   int32_t tok = 0;
@@ -651,7 +663,7 @@ void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
     // together, the prefix is read once a tile of all queries; apart, once a tile of each request's
     // (at the price of partial results to join: the steps that it saves have to outweigh them)
     const int64_t together = (tokens + tile - 1) / tile;
-    const bool pool = (apart - together) * (prefix / kKeys) > kJoinSteps * together + apart;
+    const bool pool = !small && (apart - together) * (prefix / kKeys) > kJoinSteps * together + apart;
     if (pool)
       for (int64_t t = 0; t < tokens; t += tile)
         runs.push_back(Run{int32_t(tok + t), int32_t(std::min<int64_t>(tile, tokens - t)), d.seq ? d.seq[lead] : lead, 0,
@@ -667,7 +679,7 @@ void plan_items(const op_attend_desc_t& d, int32_t n_sm, Work* w) {
   }
   int64_t steps = 0;
   for (const Run& r : runs) steps += r.steps() + kItemSteps;
-  const int64_t most = std::max(kMinSteps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
+  const int64_t most = std::max(small ? kAloneSteps : kMinSteps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
   // cut; then longest first, so that short items fill the end (equal ones keep their order:
   // tiles that read the same keys stay together)
   struct Cut {

@@ -699,7 +699,7 @@ def test_cache_beyond_2_31_elements():
 @pytest.mark.parametrize("H,Hk,D,page,dtype", [(8, 2, 128, 16, BF), (5, 1, 80, 64, HF), (6, 6, 64, 8, BF)])
 def test_attend_pooled_prefix_of_odd_lengths(pre, H, Hk, D, page, dtype):
     """Prefixes that end inside a step and a page, read once for all requests (the plan joins)."""
-    n = 40
+    n = 304 // Hk + 5                        # more than one round of blocks takes apart
     kv = [pre[0] + 1 + (13 * b) % 150 for b in range(n)]
     _, plan, *_ = _check_attend([1] * n, kv, H, Hk, D, page, dtype, groups=[0, n], prefix=pre)
     assert plan.c.n_joins >= n
