@@ -118,7 +118,8 @@ int op_rope(const op_rope_t* rope, int32_t dtype, int64_t n_tokens, int32_t n_he
 /* q_out[t] = q[t] rotated by pos[t]; k[t] rotated and v[t] are written to `layer` of
  * the cache, at token pos[t] of row seq[t].  A token whose row or page does not
  * exist (a negative seq marks padding) is rotated but not written; status[4]
- * counts those with seq >= 0.  n_heads may be 0.  Types are the cache's. */
+ * counts those with seq >= 0.  The page has to be the row's own, which op_grow
+ * sees to: what other rows share would be written too.  n_heads may be 0.  Types are the cache's. */
 int op_rope_append(const op_rope_t* rope, const op_cache_t* cache, int32_t layer, int64_t n_tokens, int32_t n_heads,
                    const void* q, int64_t q_tok, int64_t q_head, const void* k, int64_t k_tok, int64_t k_head,
                    const void* v, int64_t v_tok, int64_t v_head, const int32_t* pos, const int32_t* seq, void* q_out,

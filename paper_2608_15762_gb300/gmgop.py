@@ -143,9 +143,10 @@ def _list(t, device, what: str) -> int:
 class PageCache:
     """A paged cache of keys and values: pool [n_pages, n_layers, 2, n_kv_heads,
     page_tokens, head_dim] and, int32, table [n_seq, max_pages] (-1: no page), lens
-    [n_seq] and refs [n_pages].  What is not given starts empty.  The page calls take
-    int32 lists on the GPU and do not synchronise; ``code()`` does, and says how the
-    last one went."""
+    [n_seq] and refs [n_pages].  What is not given starts empty, but references are
+    counted from a given table (which has to come with its lens where rows are to grow).
+    The page calls take int32 lists on the GPU and do not synchronise; ``code()`` does,
+    and says how the last one went."""
 
     def __init__(self, pool, n_seq: int = 0, max_pages: int = 0, table=None, lens=None, refs=None):
         _need(pool.is_cuda and pool.dim() == 6 and pool.shape[2] == 2 and pool.is_contiguous(),
@@ -155,8 +156,11 @@ class PageCache:
             table = torch.full((n_seq, max_pages), -1, dtype=i32, device=dev)
         n_seq, max_pages = table.shape
         lens = torch.zeros(n_seq, dtype=i32, device=dev) if lens is None else lens
-        refs = torch.zeros(pool.shape[0], dtype=i32, device=dev) if refs is None else refs
         _need(table.dtype == i32 and table.is_contiguous() and table.device == dev, "table: contiguous int32")
+        if refs is None:
+            refs = torch.zeros(pool.shape[0], dtype=i32, device=dev)
+            used = table[(table >= 0) & (table < pool.shape[0])].long()
+            refs.index_add_(0, used, torch.ones_like(used, dtype=i32))
         _list(lens, dev, "lens")
         _list(refs, dev, "refs")
         _need(lens.numel() == n_seq and refs.numel() == pool.shape[0], "lens, refs: one entry a row, one a page")

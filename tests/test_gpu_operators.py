@@ -341,6 +341,15 @@ def test_pages_copy_every_byte():
     assert int((c.refs > 0).sum()) == int((c.refs[:4] > 0).sum())
 
 
+def test_references_are_counted_from_a_table():
+    pool = torch.zeros(9, 1, 2, 1, 8, 8, dtype=BF, device="cuda")
+    table = torch.tensor([[3, 5, -1], [3, 7, 5], [-1, 99, -1]], dtype=torch.int32, device="cuda")
+    c = P.PageCache(pool, table=table, lens=_ints([16, 24, 0]))
+    assert c.refs.tolist() == [0, 0, 0, 2, 0, 2, 0, 1, 0]
+    c.grow(_ints([0]), _ints([8]))
+    assert c.code() == (P.PAGE_OK, 0) and c.table[0].tolist() == [3, 5, 0]
+
+
 def test_page_calls_refuse_without_change():
     c = _labelled(10, 1, 1, 8, 8, 5, 4)
     c.grow(_ints([0, 1]), _ints([20, 9]))
