@@ -528,7 +528,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
 
 // Joins the parts of a query head: o = sum_i 2^(lse_i - L) o_i with L = log2 sum_i 2^lse_i.  A
 // warp takes one head of a token, a lane four elements; with more than 8 parts a block does: its
-// four warps every fourth part, and their sums are then added in order.
+// four warps every fourth part, and their sums are then added in order (us a call, a warp / a block:
+// one request of 32,000 tokens, 42 parts, 31.7 / 26.6; 96 requests of nine parts 72.6 / 72.2; 32 requests
+// of eight drafted tokens, few parts, 29.1 / 33.4).
 template <class T>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a) {
   __shared__ float4 sums[3][32];

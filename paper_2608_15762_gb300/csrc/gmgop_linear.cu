@@ -167,7 +167,7 @@ cudaError_t launch_any(const op_linear_t& a, cudaStream_t st) {
 
 // ---- few rows of x ---------------------------------------------------------
 
-// A warp (or four, where the weight has few rows) takes one row of the weight against up to
+// A warp (or four, where the weight has few and long rows) takes one row of the weight against up to
 // two rows of x: 16-byte loads, kAhead of them in flight, x from the L1 cache.  Bound by
 // reading the weight; no piece waits for another.
 constexpr int kFewRows = 2;
@@ -264,8 +264,10 @@ __global__ void __launch_bounds__(128) linear_few_kernel(op_linear_t a) {
 
 template <class T, int M, bool kGate>
 cudaError_t launch_few_rows(const op_linear_t& a, int sms, cudaStream_t st) {
-  // four warps a row of the weight while one each leaves an SM fewer than 16
-  if (a.n < (int64_t)sms * 16) linear_few_kernel<T, M, kGate, 4><<<(unsigned)a.n, 128, 0, st>>>(a);
+  // four warps a row of the weight while one each leaves an SM fewer than eight, and rows that give
+  // each several loads (us, one / four, rows x columns: 512 x 4,096 4.4 / 2.6, 1,024 x 12,288
+  // 10.9 / 8.6, 2,048 x 4,096 6.1 / 6.9, 2,048 x 1,024 2.9 / 4.8)
+  if (a.n < (int64_t)sms * 8 && a.k >= 2048) linear_few_kernel<T, M, kGate, 4><<<(unsigned)a.n, 128, 0, st>>>(a);
   else linear_few_kernel<T, M, kGate, 1><<<(unsigned)((a.n + 3) / 4), 128, 0, st>>>(a);
   return cudaGetLastError();
 }

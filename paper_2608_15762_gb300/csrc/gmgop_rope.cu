@@ -153,7 +153,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
 
 template <class T, int N, bool kInter>
 cudaError_t launch(const RopeArgs& a, bool append, cudaStream_t st) {
-  // enough blocks for every SM where there are few tokens: shares of a token's heads
+  // enough blocks for every SM where there are few tokens: shares of a token's heads (us, a block a
+  // token / shares, 32 + 8 + 8 heads: 16 tokens 4.5 / 3.1, 200 tokens 4.6 / 4.0, 500 5.5 / 5.1)
   const int64_t steps = int64_t(a.n_heads + 2 * a.n_kv) * ((a.dim + N - 1) / N);
   int64_t split = (152 * 4 + a.n_tokens - 1) / a.n_tokens;
   if (split > (steps + kThreads - 1) / kThreads) split = (steps + kThreads - 1) / kThreads;
