@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
   using S = Shape<DP>;
   extern __shared__ unsigned char raw[];
   __shared__ uint64_t bars[2 * S::kSlots + 7];
-  __shared__ uint32_t tmem_at, failed_word, keep_o, bad[2];
+  __shared__ uint32_t tmem_at, failed_word, keep_o, bad[2][2];   // bad: keys of even and of odd steps
   volatile uint32_t* failed = &failed_word;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   // all heads of an item, then the next item: the long ones start first
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
     bar_init(s_full, 1), bar_init(s_full + 8, 1);
     bar_init(p_ready, 4), bar_init(p_ready + 8, 4);
     bar_init(o_done, 1), bar_init(o_done + 8, 1);
-    failed_word = keep_o = bad[0] = bad[1] = 0;
+    failed_word = keep_o = bad[0][0] = bad[0][1] = bad[1][0] = bad[1][1] = 0;
     fence_bar_init();
   }
   if (warp == 7) tmem_alloc<1>(smem_addr(&tmem_at), S::kColumns);
@@ -401,6 +401,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
           for (int q = 0; q < 8; ++q) at[q] = uint4{};
         }
         if (k0 + kKeys > all_see && all_see < it.hi) {
+          // Words by step parity: a warp may be in the next step while another has yet to read this
+          // one's, but no further (S_{j+2} waits for every warp's P_j).
+          uint32_t* mine = bad[j & 1];
           constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
           for (int i = r; i < kKeys * S::kHalves; i += 128) {
             const int key = i % kKeys;
@@ -414,11 +417,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
 #pragma unroll
               for (int b = 0; b < 4; ++b) odd |= (w[b] & 0xffff) == (kExp & 0xffff) || w[b] >> 16 == kExp >> 16;
             }
-            if (odd) atomicOr(&bad[key >> 5], 1u << (key & 31));
+            if (odd) atomicOr(&mine[key >> 5], 1u << (key & 31));
           }
           part_sync(1, 128);
-          uint64_t found = (uint64_t)*reinterpret_cast<volatile uint32_t*>(&bad[1]) << 32 |
-                           *reinterpret_cast<volatile uint32_t*>(&bad[0]);
+          uint64_t found = (uint64_t)*reinterpret_cast<volatile uint32_t*>(&mine[1]) << 32 |
+                           *reinterpret_cast<volatile uint32_t*>(&mine[0]);
           if (found) {
             // Their share of O is added here, to the rows that see them; the products get zeros.
             if (j > 0) {
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
                 for (int q = 0; q < 8; ++q) at[q] = uint4{};
               }
             if (r == 0) {
-              bad[0] = bad[1] = 0;
+              mine[0] = mine[1] = 0;
               if (j == 0) keep_o = 1;
             }
             part_sync(1, 128);

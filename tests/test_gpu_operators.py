@@ -739,3 +739,50 @@ def test_executor_example():
     assert torch.equal(refs, ex.cache.refs) and int((refs > 0).sum()) == int((refs[:int((refs > 0).sum())] > 0).sum())
     assert all(len(s) for s in ex.samples.values()) and any("t = " in s for s in lines)
     assert r["best"] >= 0 and r["makespan"] > 0 and bool((r["desc"].dur >= 1).all())
+
+
+# ---------------------------------------------------------------------------
+# Values that are not finite, in steps that follow one another
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("D,dtype", [(128, BF), (64, HF)])
+def test_attend_values_that_are_not_finite_in_consecutive_steps(D, dtype):
+    """A head each, so that a tile's 128 queries end in two steps of keys or three, with values that are
+    not finite in the second, the third or all of them: only the rows that see one get it, and the
+    keys of one step are never taken for another's.  Many requests, so that the warps' pace differs."""
+    g = _gen(71)
+    n, page, H = 60, 16, 2
+    q_len = [128] * n
+    kv = [128 + (7 * b) % 100 for b in range(n)]
+    cache, keys, vals = _filled(g, kv, H, D, page, dtype)
+    q = _rand(g, sum(q_len), H, D, dtype=dtype)
+    want, tol, spoilt = [], [], torch.zeros(sum(q_len), H, D, dtype=torch.bool)
+    for b in range(n):
+        before = kv[b] - q_len[b]
+        clean = vals[b].clone()
+        # keys of the steps that the tile's queries end in: each step's, some steps' or one's
+        for step in range(before // 64 + 1, (kv[b] - 1) // 64 + 1):
+            if b % 3 == 1 and step % 2:
+                continue
+            for k in (64 * step + b % 5, 64 * step + 63 - b % 7)[:1 + b % 2]:
+                if before < k < kv[b]:
+                    h, d = k % H, (5 * k + b) % D
+                    cache.pool[int(cache.table[b, k // page]), 1, 1, h, k % page, d] = (math.nan, math.inf, -math.inf)[k % 3]
+                    clean[k, h, d] = 0
+                    spoilt[128 * b + k - before:128 * (b + 1), h, d] = True
+        w, t, _, _ = R.attend(q[128 * b:128 * (b + 1)], keys[b], clean, q_len[b], D ** -0.5)
+        want.append(w)
+        tol.append(t)
+    want, tol = torch.cat(want).cpu(), torch.cat(tol).cpu()
+    assert bool(spoilt.any()) and not bool(spoilt.all())
+    plan = P.AttendPlan(q_len, kv, H, H, D, page)
+    first = None
+    for _ in range(40):
+        o = P.attend(plan, q, cache, 1).cpu()
+        assert not bool(torch.isfinite(o[spoilt]).any())
+        o[spoilt] = want[spoilt].to(dtype)
+        if first is None:
+            R.within(o, want, tol)
+            first = o
+        assert torch.equal(o, first)
+    assert cache.status.tolist()[5] == 0
