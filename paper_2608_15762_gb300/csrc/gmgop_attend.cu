@@ -228,7 +228,6 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       // (this warp's copy before, three back, had all copies up to seven back consumed: the phase
       // before the one awaited is over, so the parity is not mistaken)
       if (!bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed)) break;
-      __syncwarp();
       const uint32_t bar = full + 8 * slot, dst = slots + slot * S::kSlot;
       if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * 128 * S::kHalves);
       for (int32_t k = from; k < to; k += box) {
@@ -240,11 +239,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
           for (int h = 0; h < S::kHalves; ++h) load_3d(dst + h * (kKeys * 128) + k * 128, &map_kv, h * 64, y, z, bar);
       }
     }
-    if (*failed && lane == 0) {   // the copies in flight still have to land: a bounded wait for each
+    if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
       uint32_t quiet = 0;
       for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - S::kSlots; b -= kCopiers)
-        bar_wait(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
-      bar_wait(q_full, 0, &quiet);
+        bar_pass(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
+      bar_pass(q_full, 0, &quiet);
     }
     __syncwarp();
   } else if (warp == 7) {
@@ -254,10 +253,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
     constexpr uint32_t desc_s = mma_desc(kBf16, kRows, kKeys, false), desc_o = mma_desc(kBf16, kRows, DP, true);
     const uint32_t with = desc_s | (a.negative ? kMinusA : 0u);
     const uint64_t q = tile_k(smem), k_ring = tile_k(slots), v_ring = tile_n(slots, kKeys * 128);
-    auto scores = [&](int j) {
+    auto scores = [&](int j, uint32_t behind, uint32_t parity) {   // behind: what S_j waits for besides K_j
       const int e = order_k(j), slot = e % S::kSlots;
-      if (!bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
-      __syncwarp();
+      if (!bar_wait_both(behind, parity, full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
       tc_after_sync();
       const uint64_t k = k_ring + slot * (S::kSlot / 16);
       const uint32_t d = tmem_s + (j & 1) * kKeys;
@@ -272,13 +270,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       __syncwarp();
       return true;
     };
-    bool go = bar_wait(q_full, 0, failed) && scores(0) && (n < 2 || scores(1));
+    bool go = scores(0, q_full, 0) && (n < 2 || scores(1, q_full, 0));
     for (int j = 0; go && j < n; ++j) {
       const int e = order_v(j, n), slot = e % S::kSlots;
-      if (!bar_wait(p_ready + 8 * (j & 1), (j >> 1) & 1, failed) ||
-          !bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed))
-        break;
-      __syncwarp();
+      if (!bar_wait_both(p_ready + 8 * (j & 1), (j >> 1) & 1, full + 8 * slot, (e / S::kSlots) & 1, failed)) break;
       tc_after_sync();
       const uint64_t v = v_ring + slot * (S::kSlot / 16);
       const uint32_t p = tmem_s + (j & 1) * kKeys;
@@ -291,11 +286,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       }
       __syncwarp();
       // S_{j+2} takes the place of P_j: once its product is done
-      if (j + 2 < n) go = bar_wait(o_done + 8 * (j & 1), (j >> 1) & 1, failed) && scores(j + 2);
+      if (j + 2 < n) go = scores(j + 2, o_done + 8 * (j & 1), (j >> 1) & 1);
     }
     // the last arrival that nothing else waits for
-    bar_wait(empty + 8 * ((2 * n - 1) % S::kSlots), ((2 * n - 1) / S::kSlots) & 1, failed);
-    __syncwarp();
+    bar_pass(empty + 8 * ((2 * n - 1) % S::kSlots), ((2 * n - 1) / S::kSlots) & 1, failed);
   } else {
     const int r = threadIdx.x;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
@@ -309,8 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
     float m = -INFINITY, l = 0.f;
     for (int j = 0; j < n; ++j) {
       const int32_t k0 = (first + j) * kKeys;
-      bar_wait(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
-      __syncwarp();
+      bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
       tc_after_sync();
       const uint32_t s_at = tmem_s + lanes + (j & 1) * kKeys;
       uint32_t lo[32], hi[32];
@@ -347,8 +340,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
         if (raise) m = here;
         l *= f;
         if (j > 0) {
-          bar_wait(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
-          __syncwarp();
+          bar_pass(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
           tc_after_sync();
 #pragma unroll 1
           for (int d = 0; d < DP; d += 32) {
@@ -390,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
         // Keys outside the item: whatever lies there must not meet the zeros of P.  So must
         // no value that is not finite and that some row does not see.
         const int e = order_v(j, n), slot = e % S::kSlots;
-        bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed);
+        bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
         unsigned char* v = base + S::kQ + slot * S::kSlot;
         const int below = it.lo > k0 ? it.lo - k0 : 0, upto = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
         for (int i = r; i < kKeys * S::kHalves; i += 128) {
@@ -425,8 +417,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
           if (found) {
             // Their share of O is added here, to the rows that see them; the products get zeros.
             if (j > 0) {
-              bar_wait(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
-              __syncwarp();
+              bar_pass(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
               tc_after_sync();
             }
 #pragma unroll 1
@@ -480,8 +471,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
       __syncwarp();
       if (lane == 0) bar_arrive(p_ready + 8 * (j & 1));
     }
-    bar_wait(o_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, failed);
-    __syncwarp();
+    bar_pass(o_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, failed);
     tc_after_sync();
     const bool in = tok < it.n_tok;
     const float inv = l == 0.f ? 0.f : 1.f / l;

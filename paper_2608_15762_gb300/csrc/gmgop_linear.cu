@@ -451,7 +451,6 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
     uint32_t stage = 0, phase = 0, issued = 0;
     for (int32_t k = k0; k < k1; ++k) {
       if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
-      __syncwarp();
       const uint32_t at = smem + stage * S::kStage, bar = full + 8 * stage;
       if (elect_one()) {
         bar_expect(bar, S::kStage);
@@ -465,7 +464,7 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
     // every stage comes back before the block ends; after a failure the copies in flight get a
     // bounded wait each
     uint32_t quiet = 0;
-    if (!*failed) {
+    if (!gave_up(failed)) {
       for (int i = 0; i < S::kStages; ++i) {
         if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
         if (++stage == S::kStages) stage = 0, phase ^= 1;
@@ -474,7 +473,7 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
       for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
         if (stage == 0) phase ^= 1;
         stage = stage == 0 ? S::kStages - 1 : stage - 1;
-        bar_wait(full + 8 * stage, phase, &quiet);
+        bar_pass(full + 8 * stage, phase, &quiet);
       }
     }
   } else if (warp == 1) {
@@ -483,7 +482,6 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
     uint32_t stage = 0, phase = 0;
     for (int32_t k = k0; k < k1; ++k) {
       if (!bar_wait(full + 8 * stage, phase, failed)) break;
-      __syncwarp();
       tc_after_sync();
       const uint64_t w = ring + stage * (S::kStage / 16), g = w + kWeightBytes / 16, x = w + (S::kStage - S::kXBytes) / 16;
       const bool add = k > k0;
@@ -501,8 +499,7 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const __grid_constant
     if (elect_one()) mma_commit(done);
   }
   __syncwarp();
-  bar_wait(done, 0, failed);   // every copy has landed and been read
-  __syncwarp();
+  bar_pass(done, 0, failed);   // every copy has landed and been read
   tc_after_sync();
   {
     // the sums, [row of x][row of the weight]; warps of one half of the block take every other 16 rows
@@ -690,7 +687,6 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
       const int32_t row_w = p.tile_n * (128 * kPair) + rank * 128, row_x = p.tile_m * NT + rank * (NT / kPair);
       for (int32_t k = p.k0; k < p.k1; ++k) {
         if (!(go = bar_wait(empty + 8 * stage, phase ^ 1, failed))) break;
-        __syncwarp();
         const uint32_t at = smem + stage * S::kStage;
         if (elect_one()) {
           // both blocks' copies count on the first block's barrier
@@ -707,7 +703,7 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
     // every stage comes back before the block ends: its copies have landed, and the products
     // have sent their arrivals; after a failure the copies in flight get a bounded wait each
     uint32_t quiet = 0;
-    if (!*failed) {
+    if (!gave_up(failed)) {
       for (int i = 0; i < S::kStages; ++i) {
         if (!bar_wait(empty + 8 * stage, phase ^ 1, failed)) break;
         if (++stage == S::kStages) stage = 0, phase ^= 1;
@@ -716,7 +712,7 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
       for (uint32_t i = 0; i < S::kStages && i < issued; ++i) {
         if (stage == 0) phase ^= 1;
         stage = stage == 0 ? S::kStages - 1 : stage - 1;
-        bar_wait(full + 8 * stage, phase, &quiet);
+        bar_pass(full + 8 * stage, phase, &quiet);
       }
     }
     __syncwarp();
@@ -731,11 +727,9 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
       for (uint32_t n = 0; go && it.next(&p); ++n) {
         const uint32_t buf = n % S::kBuffers, d = tmem + buf * S::kColumns;
         if (!bar_wait(drained + 8 * buf, ((n / S::kBuffers) & 1) ^ 1, failed)) break;
-        __syncwarp();
         tc_after_sync();
         for (int32_t k = p.k0; k < p.k1; ++k) {
           if (!(go = bar_wait(full + 8 * stage, phase, failed))) break;
-          __syncwarp();
           tc_after_sync();
           const uint64_t w = ring + stage * (S::kStage / 16), g = w + kWeightBytes / 16, x = w + (S::kStage - S::kXBytes) / 16;
           const bool add = k > p.k0;
@@ -774,8 +768,7 @@ __global__ void __cluster_dims__(kPair, 1, 1) __launch_bounds__(kRoles) linear_k
       if (in && a.bias) bias = up(static_cast<const T*>(a.bias)[col]);
       if (in && kGate && a.gate_bias) gate_bias = up(static_cast<const T*>(a.gate_bias)[col]);
       // a wait that gives up goes on with what it finds; the status says so
-      bar_wait(done + 8 * buf, (n / S::kBuffers) & 1, failed);
-      __syncwarp();
+      bar_pass(done + 8 * buf, (n / S::kBuffers) & 1, failed);
       tc_after_sync();
       const T* res = a.residual ? static_cast<const T*>(a.residual) + row0 * a.residual_row + col : nullptr;
       T* y = static_cast<T*>(a.y) + row0 * a.y_row + col;

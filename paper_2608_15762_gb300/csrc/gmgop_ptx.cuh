@@ -60,8 +60,8 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 
 // Waits for the phase of `parity` to complete; false if another wait of the block has
-// given up or this one did (after about two seconds).
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
+// given up or this one did (after about two seconds).  One lane's own answer.
+__device__ __forceinline__ bool bar_wait_lane(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
   if (bar_try(bar, parity)) return true;
   uint64_t began = 0;
   for (uint32_t i = 1;; ++i) {
@@ -78,6 +78,25 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     }
   }
 }
+
+// The same for a whole warp, of one answer: where a wait gives up, lanes may see it at different
+// times, and what follows takes the warp as a whole.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
+  return __all_sync(0xffffffffu, bar_wait_lane(bar, parity, failed));
+}
+// ... for two barriers, with one vote.
+__device__ __forceinline__ bool bar_wait_both(uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2,
+                                              volatile uint32_t* failed) {
+  const bool first = bar_wait_lane(bar, parity, failed), second = bar_wait_lane(bar2, parity2, failed);
+  return __all_sync(0xffffffffu, first && second);
+}
+// ... for a warp that goes on whatever the answer.
+__device__ __forceinline__ void bar_pass(uint32_t bar, uint32_t parity, volatile uint32_t* failed) {
+  bar_wait_lane(bar, parity, failed);
+  __syncwarp();
+}
+// Whether a wait of the block has given up, of one answer for the warp.
+__device__ __forceinline__ bool gave_up(volatile uint32_t* failed) { return __any_sync(0xffffffffu, *failed != 0); }
 
 __device__ __forceinline__ void fence_bar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 // Orders this thread's ordinary writes to shared memory before later asynchronous reads.

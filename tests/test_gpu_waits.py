@@ -1,0 +1,26 @@
+"""The operators' waits on the GPU are bounded: one that nothing ends gives up after about two seconds,
+with one answer for its warp, and ends the block's other waits."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+pytest.importorskip("torch")
+
+from paper_2608_15762_gb300 import build  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_wait_that_gives_up_has_one_answer_for_its_warp(tmp_path):
+    src, so = os.path.join(os.path.dirname(os.path.abspath(__file__)), "wait_check.cu"), str(tmp_path / "wait_check.so")
+    subprocess.check_call([build.nvcc()] + build.ARCH + build.FLAGS + ["-shared", "-o", so, src])
+    out = (C.c_int * 196)()
+    assert C.CDLL(so).wait_check(out) == 0
+    v = list(out)
+    assert v[:32] == [0] * 32 and v[32:64] == [1] * 32      # half of warp 0's lanes had their phase
+    assert v[64:128] == [1] * 64
+    assert v[128:192] == [0] * 64
+    assert v[192:194] == [1, 1]
+    assert 1900 <= v[194] <= 4000 and v[195] < 1000
