@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
                                                              const __grid_constant__ AttendArgs a) {
   using S = Shape<DP>;
   extern __shared__ unsigned char raw[];
-  __shared__ uint64_t bars[2 * S::kSlots + 7];
+  __shared__ uint64_t bars[2 * S::kSlots + 8];
   __shared__ uint32_t tmem_at, failed_word, keep_o, bad[2][2];   // bad: keys of even and of odd steps
   volatile uint32_t* failed = &failed_word;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
   unsigned char* base = raw + (smem - smem_addr(raw));
   const uint32_t slots = smem + S::kQ;
   const uint32_t full = smem_addr(bars), empty = full + 8 * S::kSlots, q_full = empty + 8 * S::kSlots,
-                 s_full = q_full + 8, p_ready = s_full + 16, o_done = p_ready + 16;
+                 s_full = q_full + 8, p_ready = s_full + 16, o_done = p_ready + 16, met = o_done + 16;
   // s_full, p_ready and o_done are two barriers each, for even and odd steps.  A wait tells a phase
   // from the one before it only, and every wait here has that one behind it: S_j is computed
   // after the product of step j - 2 is done.
@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
     bar_init(s_full, 1), bar_init(s_full + 8, 1);
     bar_init(p_ready, 4), bar_init(p_ready + 8, 4);
     bar_init(o_done, 1), bar_init(o_done + 8, 1);
+    bar_init(met, 4);
     failed_word = keep_o = bad[0][0] = bad[0][1] = bad[1][0] = bad[1][1] = 0;
     fence_bar_init();
   }
@@ -301,6 +302,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
     const int32_t end = it.pos0 + own + 1 < it.hi ? it.pos0 + own + 1 : it.hi;
     const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
     float m = -INFINITY, l = 0.f;
+    uint32_t meetings = 0;                // of the four warps: waits that are bounded, as all are
     for (int j = 0; j < n; ++j) {
       const int32_t k0 = (first + j) * kKeys;
       bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
@@ -411,9 +413,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
             }
             if (odd) atomicOr(&mine[key >> 5], 1u << (key & 31));
           }
-          part_sync(1, 128);
-          uint64_t found = (uint64_t)*reinterpret_cast<volatile uint32_t*>(&mine[1]) << 32 |
-                           *reinterpret_cast<volatile uint32_t*>(&mine[0]);
+          bar_meet(met, &meetings, failed);
+          // one answer for the warp (after a wait gave up, others may find otherwise)
+          const uint64_t found = __shfl_sync(0xffffffffu, (uint64_t)*reinterpret_cast<volatile uint32_t*>(&mine[1]) << 32 |
+                                                              *reinterpret_cast<volatile uint32_t*>(&mine[0]), 0);
           if (found) {
             // Their share of O is added here, to the rows that see them; the products get zeros.
             if (j > 0) {
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
               tmem_store32(tmem + lanes + d, o);
             }
             tmem_wait_store();
-            part_sync(1, 128);
+            bar_meet(met, &meetings, failed);
             for (int i = r; i < kKeys * S::kHalves; i += 128)
               if (found >> (i % kKeys) & 1) {
                 uint4* at = reinterpret_cast<uint4*>(v + (i / kKeys) * (kKeys * 128) + (i % kKeys) * 128);
@@ -462,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(const __grid_consta
               mine[0] = mine[1] = 0;
               if (j == 0) keep_o = 1;
             }
-            part_sync(1, 128);
+            bar_meet(met, &meetings, failed);
           }
         }
         fence_async();

@@ -66,6 +66,7 @@ __device__ __forceinline__ bool bar_wait_lane(uint32_t bar, uint32_t parity, vol
   uint64_t began = 0;
   for (uint32_t i = 1;; ++i) {
     if (bar_try(bar, parity)) return true;
+    if (i == 1 && *failed) return false;
     if ((i & 63) == 0) {
       if (*failed) return false;
       uint64_t now;
@@ -95,6 +96,14 @@ __device__ __forceinline__ void bar_pass(uint32_t bar, uint32_t parity, volatile
   bar_wait_lane(bar, parity, failed);
   __syncwarp();
 }
+// Meets the other warps that `bar` counts, one arrival each: what was written before it is seen behind
+// it.  *phase: the warp's meetings so far, modulo 2.
+__device__ __forceinline__ void bar_meet(uint32_t bar, uint32_t* phase, volatile uint32_t* failed) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) bar_arrive(bar);
+  bar_pass(bar, *phase, failed);
+  *phase ^= 1;
+}
 // Whether a wait of the block has given up, of one answer for the warp.
 __device__ __forceinline__ bool gave_up(volatile uint32_t* failed) { return __any_sync(0xffffffffu, *failed != 0); }
 
@@ -109,10 +118,6 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
-}
-// Barrier `id` of the block among `threads` threads.
-__device__ __forceinline__ void part_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
 // ---- bulk tensor copies ---------------------------------------------------

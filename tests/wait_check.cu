@@ -33,11 +33,48 @@ __global__ void wait_kernel(int* out) {
   if (t == 0) out[194] = int((t1 - t0) / 1000000), out[195] = int((t2 - t1) / 1000000);
 }
 
-extern "C" int wait_check(int* host) {
+// Four warps that meet: out[0] counts words of another warp's that were not seen behind a meeting; then
+// a meeting of five that a fifth never comes to: [1] gave up, [2] and [3] milliseconds of it and of
+// 100 meetings after it.
+__global__ void meet_kernel(int* out) {
+  __shared__ uint64_t bars[2];
+  __shared__ uint32_t failed_word;
+  __shared__ int word[128];
+  volatile uint32_t* failed = &failed_word;
+  const int t = threadIdx.x;
+  const uint32_t four = smem_addr(bars), five = four + 8;
+  if (t == 0) {
+    bar_init(four, 4), bar_init(five, 5);
+    failed_word = 0;
+    fence_bar_init();
+  }
+  __syncthreads();
+  uint32_t phase = 0;
+  for (int i = 1; i <= 1000; ++i) {
+    word[t] = i * 128 + t;
+    bar_meet(four, &phase, failed);
+    const int other = (t * 37 + i) & 127;
+    if (word[other] != i * 128 + other) atomicAdd(&out[0], 1);
+    bar_meet(four, &phase, failed);
+  }
+  if (gave_up(failed)) atomicAdd(&out[0], 1);
+  uint64_t t0, t1, t2;
+  phase = 0;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+  bar_meet(five, &phase, failed);
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+  for (int i = 0; i < 100; ++i) bar_meet(five, &phase, failed);
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t2));
+  const bool gone = gave_up(failed);
+  if (t == 0) out[1] = gone, out[2] = int((t1 - t0) / 1000000), out[3] = int((t2 - t1) / 1000000);
+}
+
+extern "C" int wait_check(int which, int* host) {
   int* out;
   if (cudaMalloc(&out, 196 * sizeof(int)) != cudaSuccess) return -1;
   cudaMemset(out, 0, 196 * sizeof(int));
-  wait_kernel<<<1, 64>>>(out);
+  if (which == 0) wait_kernel<<<1, 64>>>(out);
+  else meet_kernel<<<1, 128>>>(out);
   const cudaError_t e = cudaMemcpy(host, out, 196 * sizeof(int), cudaMemcpyDeviceToHost);
   cudaFree(out);
   return e == cudaSuccess ? 0 : -2;
