@@ -424,22 +424,26 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
 
 class Workspace:
     """A workspace of ``linear``: grown on demand, its head zeroed when it is made.
-    Calls that share one must be ordered (one stream)."""
+    Calls that share one must be ordered (one stream), replays of captured ones among them.
+    What it has outgrown stays allocated, as a captured call writes there whenever it is replayed;
+    it doubles at least, so that this is no more than the workspace itself."""
 
     def __init__(self, device="cuda"):
-        self.device, self.buf, self.ptr, self.size = device, None, 0, 0
+        self.device, self.buf, self.ptr, self.size, self._kept = device, None, 0, 0, []
 
     def get(self, nbytes: int, stream=None):
         if self.buf is None or self.size < nbytes:
+            if self.buf is not None:
+                self._kept.append(self.buf)
             with _on(stream):
-                self.buf = _aligned_empty(max(nbytes, 4096), self.device)
+                self.buf = _aligned_empty(max(nbytes, 2 * self.size, 4096), self.device)
                 self.buf[:4096].zero_()
             self.ptr, self.size = self.buf.data_ptr(), self.buf.numel()
         return self.buf
 
     def gave_up(self) -> int:
         """Waits of ``linear`` that gave up (0 unless the GPU is at fault); synchronises."""
-        return 0 if self.buf is None else int(self.buf[:4].view(torch.int32).item())
+        return sum(int(b[:4].view(torch.int32).item()) for b in self._kept + [self.buf] if b is not None)
 
 
 _WORK = {}

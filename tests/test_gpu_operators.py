@@ -786,3 +786,39 @@ def test_attend_values_that_are_not_finite_in_consecutive_steps(D, dtype):
             first = o
         assert torch.equal(o, first)
     assert cache.status.tolist()[5] == 0
+
+
+# ---------------------------------------------------------------------------
+# Workspaces and captured calls
+# ---------------------------------------------------------------------------
+
+def _work_bytes(m, k, n, gated=0):
+    import ctypes as C
+    a = P._Linear(P.BF16, 0, gated, 0, m, n, k, 256, 256, 256 if gated else 0, 0, 0, 0, 256, k, k, k if gated else 0, 0, n)
+    return P.lib().op_linear_work_bytes(C.addressof(a))
+
+
+def test_linear_captured_before_its_workspace_grew():
+    """The replay's partial sums go where they were captured to go, not to memory that others have now."""
+    g = _gen(81)
+    m, k, n = 1270, 2056, 4001                     # 80 tiles: four are dealt out by steps, and joined
+    x, w = _rand(g, m, k), _rand(g, n, k, scale=k ** -0.5)
+    need, more = _work_bytes(m, k, n), _work_bytes(2560, 4096, 4096)
+    assert 4096 < need < more
+    want, tol = R.linear(x, w)
+    ws = P.Workspace()
+    R.within(P.linear(x, w, ws=ws), want, tol)
+    out = torch.empty(m, n, dtype=BF, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.linear(x, w, out=out, ws=ws)
+    P.linear(_rand(g, 2560, 4096), _rand(g, 4096, 4096), ws=ws)
+    torch.cuda.synchronize()
+    others = [torch.full((need // 4,), 7.0, device="cuda") for _ in range(4)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        R.within(out, want, tol)
+    assert all(bool((t == 7).all()) for t in others) and ws.gave_up() == 0

@@ -213,3 +213,20 @@ def test_attend_plan_covers_every_key_once():
         kv = [prefix[k] + q[b] + r.choice([0, 0, 5, 70, 5000]) for k in range(len(prefix)) for b in range(groups[k], groups[k + 1])]
         _covered(q, kv, g * hk, hk, groups, prefix)
         _covered(q, [max(0, t - r.choice([0, 0, 3, 10 ** 6])) for t in kv], g * hk, hk)
+
+
+def test_a_workspace_keeps_what_it_has_outgrown():
+    """A captured call writes to the buffer that it was captured with whenever it is replayed."""
+    import gc
+    import weakref
+    ws = P.Workspace("cpu")
+    sizes = [4096, 5000, 20000, 20001, 10 ** 6]
+    held = []
+    for n in sizes:
+        held.append(weakref.ref(ws.get(n)))
+        assert ws.size >= n and ws.ptr % 256 == 0 and ws.ptr == ws.buf.data_ptr()
+    gc.collect()
+    assert all(h() is not None for h in held)
+    assert sum(b.numel() for b in {h().data_ptr(): h() for h in held}.values()) <= 2 * ws.size
+    held[0]()[:4] = 1                        # waits that gave up are counted wherever they were noted
+    assert ws.gave_up() == 0x01010101
