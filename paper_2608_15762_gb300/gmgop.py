@@ -129,6 +129,12 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _capturing(stream) -> bool:
+    """Whether the stream's calls are being captured into a graph."""
+    with _on(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _list(t, device, what: str) -> int:
     """The length of a list on the GPU."""
     if t.dtype is not _I32 or t.dim() != 1 or t.device != device or not t.is_contiguous():
@@ -365,7 +371,8 @@ def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=
 
 class AttendPlan:
     """The work of ``attend`` for requests of q_len new and kv_len cached tokens (the
-    new ones among them), for every layer of a step.  seq: their table rows (0, 1,
+    new ones among them), for every layer of a step (a graph captured with it serves these
+    lengths, and has a workspace of its own).  seq: their table rows (0, 1,
     ...).  group_off, prefix: requests group_off[g] .. group_off[g + 1] share their
     first prefix[g] tokens."""
 
@@ -384,8 +391,11 @@ class AttendPlan:
         self._ptr = self.items.data_ptr() if items.size else None
         self.work, self._kept = {}, []       # a workspace per stream that the plan has been used on
 
+    def empty_work(self):
+        return _aligned_empty(self.work_bytes, self.items.device)
+
     def new_work(self, handle):
-        self._kept.append(_aligned_empty(self.work_bytes, self.items.device))
+        self._kept.append(self.empty_work())
         self.work[handle] = self._kept[-1].data_ptr()
         return self.work[handle]
 
@@ -402,13 +412,19 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
     if stream is None:
         out = _like(q, out, None)
         z = torch.empty(plan.shape[:2], dtype=torch.float32, device=q.device) if lse else None
-        if work is None:
+        if torch.cuda.is_current_stream_capturing():
+            own = plan.empty_work()          # the graph's memory, free for its later calls
+            work = own.data_ptr()
+        elif work is None:
             work = plan.new_work(h)
     else:
         with torch.cuda.stream(stream):
             out = _like(q, out, None)
             z = torch.empty(plan.shape[:2], dtype=torch.float32, device=q.device) if lse else None
-            if work is None:
+            if torch.cuda.is_current_stream_capturing():
+                own = plan.empty_work()
+                work = own.data_ptr()
+            elif work is None:
                 work = plan.new_work(h)
     rc = (_LIB or lib()).op_attend(plan.ref, plan._ptr, cache.ref, layer, *_heads(q, "q"),
                                    plan.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
@@ -465,12 +481,30 @@ def _column(t, n, dt, dev, what: str):
     return t.data_ptr()
 
 
+def _captured_linear(a, ws, out, dev, stream, h):
+    """A call into a graph, whose replays may run beside the stream's other work, or another graph's.
+    (The head of the graph's own workspace is not zeroed: nobody can ask for its count.)"""
+    L = _LIB or lib()
+    need = L.op_linear_work_bytes(a)
+    if ws is not None and ws.size >= need:
+        ptr, size = ws.ptr, ws.size
+    else:
+        with _on(stream):
+            own = _aligned_empty(need, dev)
+        ptr, size = own.data_ptr(), need
+    rc = L.op_linear(a, ptr, size, h)
+    if rc:
+        _fail(rc, "op_linear")
+    return out
+
+
 @_traced("op_linear")
 def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residual=None, out=None,
            ws: Optional[Workspace] = None, stream=None):
     """act(x w^T + bias) + residual or, with a gate, act(x gate^T + gate_bias) * (x w^T +
     bias) + residual, for x [m, k], w and gate [n, k], biases [n], residual [m, n].
-    act: none, relu, silu, gelu.  out may be residual.  ws: kept per stream by default."""
+    act: none, relu, silu, gelu.  out may be residual.  ws: kept per stream by default; a captured
+    call has one in its graph's memory, unless it is given one that is large enough."""
     m, k = x.shape
     n, dt, dev, index = w.shape[0], x.dtype, x.device, x.get_device()
     kind, how = _TYPES.get(dt), ACTS.get(act)
@@ -493,6 +527,8 @@ def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residu
                      0 if bias is None else _column(bias, n, dt, dev, "bias"),
                      0 if gate_bias is None else _column(gate_bias, n, dt, dev, "gate_bias"), rp, yp, xs, wrow, gs, rs, ys)
     h = _handle(stream, index)
+    if (torch.cuda.is_current_stream_capturing() if stream is None else _capturing(stream)):
+        return _captured_linear(a, ws, out, dev, stream, h)
     if ws is None:
         ws = _WORK.get((index, h))
         if ws is None:

@@ -822,3 +822,61 @@ def test_linear_captured_before_its_workspace_grew():
         torch.cuda.synchronize()
         R.within(out, want, tol)
     assert all(bool((t == 7).all()) for t in others) and ws.gave_up() == 0
+
+
+def _captured(fn, stream):
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        out = fn()
+    return graph, out
+
+
+def _replayed_side_by_side(fns, wants):
+    """Graphs captured on one stream, then replayed on streams of their own, with eager calls beside them."""
+    capture = torch.cuda.Stream()
+    made = [_captured(fn, capture) for fn in fns]
+    streams = [torch.cuda.Stream() for _ in made]
+    torch.cuda.synchronize()
+    eager = []
+    for _ in range(30):
+        for (graph, _), st in zip(made, streams):
+            with torch.cuda.stream(st):
+                graph.replay()
+        with torch.cuda.stream(capture):
+            eager.append(fns[0]())
+    torch.cuda.synchronize()
+    for (_, out), want in zip(made, wants):
+        assert torch.equal(out, want)
+    assert all(torch.equal(t, wants[0]) for t in eager)
+
+
+def test_linear_graphs_of_one_stream_do_not_share_a_workspace():
+    g = _gen(82)
+    m, k, n = 1270, 2056, 4001
+    w = _rand(g, n, k, scale=k ** -0.5)
+    xs = [_rand(g, m, k) for _ in range(3)]
+    wants = [P.linear(x, w) for x in xs]
+    kept = {key: ws.size for key, ws in P._WORK.items()}
+    _replayed_side_by_side([lambda x=x: P.linear(x, w) for x in xs], wants)
+    new = set(P._WORK) - set(kept)
+    assert len(new) == 1 and P._WORK[new.pop()].gave_up() == 0      # the eager calls' stream, made outside a capture
+    # a workspace that is too small, or has not been used, is left as it is
+    ws = P.Workspace()
+    graph, out = _captured(lambda: P.linear(xs[0], w, ws=ws), torch.cuda.Stream())
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, wants[0]) and ws.buf is None and ws.gave_up() == 0
+
+
+def test_attend_graphs_of_one_plan_do_not_share_a_workspace():
+    g = _gen(83)
+    kv = [1500] * 6
+    cache, keys, vals = _filled(g, kv, 2, 64, 16)
+    plan = P.AttendPlan([1] * 6, kv, 16, 2, 64, 16)
+    assert plan.c.n_joins > 0
+    qs = [_rand(g, 6, 16, 64) for _ in range(3)]
+    wants = [P.attend(plan, q, cache, 1) for q in qs]
+    assert len(plan.work) == 1
+    _replayed_side_by_side([lambda q=q: P.attend(plan, q, cache, 1) for q in qs], wants)
+    assert len(plan.work) == 2
