@@ -48,8 +48,8 @@ extern "C" {
  *   status int32[8]: [0] GMG_PAGE_* of the last page call, [1] the entry of its
  *   lists that it concerns (GMG_PAGE_FULL: how many pages are missing), [2]
  *   pages moved (op_compact), [3] pages in use (op_compact), [4] tokens that
- *   op_rope_append had no page for, added up, [5] waits of op_attend that gave
- *   up (0 unless the GPU is at fault), added up. */
+ *   op_rope_append had no page for, added up, [5] blocks of op_attend with a wait
+ *   that gave up (0 unless the GPU is at fault: their output is not a result), added up. */
 typedef struct {
   void* pool;
   int32_t* table;
@@ -191,8 +191,9 @@ typedef struct {
 } op_linear_t;
 
 /* Bytes of the workspace (256-byte aligned; its first 4 KB zeroed once; calls that
- * share it must be ordered).  Its first int32 counts waits of op_linear that gave up
- * (0 unless the GPU is at fault).  0 on bad arguments. */
+ * share it must be ordered, replays of captured ones among them).  Its first int32 counts blocks
+ * of op_linear with a wait that gave up (0 unless the GPU is at fault: a call with such a block
+ * has returned 0, and what it wrote is not its result).  0 on bad arguments. */
 size_t op_linear_work_bytes(const op_linear_t* args);
 int op_linear(const op_linear_t* args, void* work, size_t work_bytes, gmg_stream_t stream);
 

@@ -458,11 +458,17 @@ class Workspace:
         return self.buf
 
     def gave_up(self) -> int:
-        """Waits of ``linear`` that gave up (0 unless the GPU is at fault); synchronises."""
+        """Blocks of ``linear`` with a wait that gave up (0 unless the GPU is at fault); synchronises."""
         return sum(int(b[:4].view(torch.int32).item()) for b in self._kept + [self.buf] if b is not None)
 
 
-_WORK = {}
+_WORK = {}      # the default workspaces, by GPU and stream
+
+
+def gave_up() -> int:
+    """Blocks of ``linear`` on its default workspaces with a wait that gave up (0 unless the GPU is at fault: what a
+    call with such a block wrote is not its result); synchronises."""
+    return sum(ws.gave_up() for ws in list(_WORK.values()))
 
 
 def _rows(t, n, k, dt, dev, what: str):

@@ -230,3 +230,15 @@ def test_a_workspace_keeps_what_it_has_outgrown():
     assert sum(b.numel() for b in {h().data_ptr(): h() for h in held}.values()) <= 2 * ws.size
     held[0]()[:4] = 1                        # waits that gave up are counted wherever they were noted
     assert ws.gave_up() == 0x01010101
+
+
+def test_waits_that_gave_up_on_default_workspaces_can_be_asked_for(monkeypatch):
+    made = {(0, h): P.Workspace("cpu") for h in (0, 7)}
+    monkeypatch.setattr(P, "_WORK", made)
+    assert P.gave_up() == 0
+    for ws in made.values():
+        ws.get(4096)
+    assert P.gave_up() == 0
+    made[(0, 7)].buf[:4] = 1
+    made[(0, 0)].buf[0] = 2
+    assert P.gave_up() == 0x01010103
