@@ -5,8 +5,9 @@ epilogue (``linear``), rotary positions (``rope``, ``rope_append``), a paged cac
 (``PageCache``) and attention over shared prefixes (``AttendPlan``, ``attend``).
 Argument marshalling only; PyTorch provides device memory and streams.  Calls
 are asynchronous on the current stream, or on ``stream``, where their results'
-memory then belongs (and which their inputs' memory has to outlive).  What the C ABI refuses raises ``GmgError``; tensors of the
-wrong shape, type or device raise ``ValueError``.
+memory then belongs (and which the memory of their inputs, plans and caches has to
+outlive).  Operands, plans, workspaces and stream are on the current GPU.  What the C ABI
+refuses raises ``GmgError``; tensors of the wrong shape, type or device raise ``ValueError``.
 """
 from __future__ import annotations
 
@@ -97,11 +98,17 @@ _traced = G._traced if G.NVTX else lambda name: lambda fn: fn
 _I32 = torch.int32
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _RAW = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _handle(stream, device_index):
-    """The stream's handle, by default that of the GPU's current stream."""
+    """The stream's handle, by default that of the current stream.  The library launches on the current
+    GPU, so operands and stream have to be there."""
+    if _current() != device_index:
+        raise ValueError("operands on GPU %d, which is not the current one" % device_index)
     if stream is not None:
+        if stream.device_index != device_index:
+            raise ValueError("stream: on the operands' GPU")
         return stream.cuda_stream
     if _RAW is not None:
         return _RAW(device_index)
@@ -272,7 +279,7 @@ class Rope:
         self.rotary, self.factor, self.interleaved = int(rotary), float(factor), bool(interleaved)
         self.freq = torch.from_numpy(turns.view(np.int64).copy()).to(device)
         self.c = _Rope(self.freq.data_ptr(), self.rotary, int(self.interleaved), self.factor)
-        self.ref = C.addressof(self.c)
+        self.ref, self.index = C.addressof(self.c), self.freq.get_device()
 
 
 def _heads(t, what: str):
@@ -305,6 +312,8 @@ def rope(plan: Rope, x, pos, backward: bool = False, out=None, stream=None):
     index = x.get_device()
     if index < 0 or _list(pos, x.device, "pos") != T:
         raise ValueError("x on a GPU, pos: one entry a token")
+    if plan.index != index:
+        raise ValueError("plan: on x's GPU")
     out = _like(x, out, stream)
     rc = (_LIB or lib()).op_rope(plan.ref, kind, T, H, D, ptr, s0, s1, pos.data_ptr(), 1 if backward else 0, *_heads(out, "out"),
                        _handle(stream, index))
@@ -323,6 +332,8 @@ def rope_append(plan: Rope, q, k, v, pos, seq, cache: PageCache, layer: int, out
         raise ValueError("q [tokens, heads, head_dim], k and v [tokens, n_kv_heads, head_dim]")
     if q.dtype is not dt or k.dtype is not dt or v.dtype is not dt or q.device != dev or k.device != dev or v.device != dev:
         raise ValueError("q, k, v: the cache's type, on its GPU")
+    if plan.index != cache._index:
+        raise ValueError("plan: on the cache's GPU")
     if _list(pos, dev, "pos") != T or _list(seq, dev, "seq") != T:
         raise ValueError("pos, seq: one entry a token")
     out = _like(q, out, stream)
@@ -388,7 +399,7 @@ class AttendPlan:
         self.work_bytes = int(self.c.work_bytes)
         with _on(stream):
             self.items = torch.from_numpy(items).to(dev)
-        self._ptr = self.items.data_ptr() if items.size else None
+        self._ptr, self.index = self.items.data_ptr() if items.size else None, self.items.get_device()
         self.work, self._kept = {}, []       # a workspace per stream that the plan has been used on
 
     def empty_work(self):
@@ -407,6 +418,8 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
     after another) over the cache; with ``lse`` also log sum exp [tokens, heads], fp32."""
     if q.shape != plan.shape or q.dtype is not cache.dtype or q.device != cache.device:
         raise ValueError("q: [tokens, heads, head_dim] of the plan, the cache's type, on its GPU")
+    if plan.index != cache._index:
+        raise ValueError("plan: on the cache's GPU")
     h = _handle(stream, cache._index)
     work = plan.work.get(h)
     if stream is None:
@@ -446,6 +459,7 @@ class Workspace:
 
     def __init__(self, device="cuda"):
         self.device, self.buf, self.ptr, self.size, self._kept = device, None, 0, 0, []
+        self.index = None                    # its GPU, once it has memory
 
     def get(self, nbytes: int, stream=None):
         if self.buf is None or self.size < nbytes:
@@ -454,7 +468,7 @@ class Workspace:
             with _on(stream):
                 self.buf = _aligned_empty(max(nbytes, 2 * self.size, 4096), self.device)
                 self.buf[:4096].zero_()
-            self.ptr, self.size = self.buf.data_ptr(), self.buf.numel()
+            self.ptr, self.size, self.index = self.buf.data_ptr(), self.buf.numel(), self.buf.get_device()
         return self.buf
 
     def gave_up(self) -> int:
@@ -492,7 +506,7 @@ def _captured_linear(a, ws, out, dev, stream, h):
     (The head of the graph's own workspace is not zeroed: nobody can ask for its count.)"""
     L = _LIB or lib()
     need = L.op_linear_work_bytes(a)
-    if ws is not None and ws.size >= need:
+    if ws is not None and ws.size >= need and ws.index == out.get_device():
         ptr, size = ws.ptr, ws.size
     else:
         with _on(stream):
@@ -541,6 +555,8 @@ def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residu
             ws = _WORK[(index, h)] = Workspace(dev)
     if ws.ptr == 0:
         ws.get(4096, stream)
+    if ws.index != index:
+        raise ValueError("ws: on x's GPU")
     L = _LIB or lib()
     rc = L.op_linear(a, ws.ptr, ws.size, h)
     if rc == G.GMG_EWS:      # it refuses a short workspace before it does anything

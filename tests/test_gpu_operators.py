@@ -880,3 +880,19 @@ def test_attend_graphs_of_one_plan_do_not_share_a_workspace():
     assert len(plan.work) == 1
     _replayed_side_by_side([lambda q=q: P.attend(plan, q, cache, 1) for q in qs], wants)
     assert len(plan.work) == 2
+
+
+def test_calls_refuse_plans_and_workspaces_of_other_devices():
+    g = _gen(84)
+    x, pos = _rand(g, 3, 2, 64), _ints([0, 1, 2])
+    cache = _cache(g, 4, 1, 2, 16, 64, 2, 2)
+    cpu = P.Rope(64, device="cpu")
+    ws = P.Workspace("cpu")
+    for call in (lambda: P.rope(cpu, x, pos), lambda: P.rope_append(cpu, x, x, x, pos, pos, cache, 0),
+                 lambda: P.linear(x[0], x[1], ws=ws)):
+        with pytest.raises(ValueError):
+            call()
+    plan = P.AttendPlan([3], [3], 2, 2, 64, 16)
+    plan.index = -1
+    with pytest.raises(ValueError):
+        P.attend(plan, x, cache, 0)

@@ -242,3 +242,102 @@ def test_waits_that_gave_up_on_default_workspaces_can_be_asked_for(monkeypatch):
     made[(0, 7)].buf[:4] = 1
     made[(0, 0)].buf[0] = 2
     assert P.gave_up() == 0x01010103
+
+
+class _On:
+    """What the binding asks of a tensor, of one that lies on GPU ``index``."""
+
+    def __init__(self, index, *shape, dtype):
+        import torch
+        self.shape, self.dtype, self.index = torch.Size(shape), dtype, index
+        self.device = torch.device("cuda", index) if index >= 0 else torch.device("cpu")
+
+    def get_device(self):
+        return self.index
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096
+
+
+class _Untouched:
+    def __getattr__(self, name):
+        def called(*a):
+            raise AssertionError("called " + name)
+        return called
+
+
+def test_calls_refuse_what_is_not_on_the_current_gpu(monkeypatch):
+    """Before anything is launched: the library must not be reached."""
+    import torch
+    P.lib()
+    monkeypatch.setattr(P, "_LIB", _Untouched())
+    monkeypatch.setattr(P, "lib", _Untouched())
+    monkeypatch.setattr(P, "_current", lambda: 0)
+    bf, i32 = torch.bfloat16, torch.int32
+
+    class Stream:
+        def __init__(self, index):
+            self.device_index, self.cuda_stream = index, 0
+
+    def plan(index, **kw):
+        p = object.__new__(P.Rope if not kw else P.AttendPlan)
+        p.index, p.ref = index, 256
+        for k, v in kw.items():
+            setattr(p, k, v)
+        return p
+
+    def cache(index):
+        c = object.__new__(P.PageCache)
+        c.device, c._index, c.dtype, c.n_kv_heads, c.head_dim = torch.device("cuda", index), index, bf, 2, 64
+        c.ref, c._work = 256, (256, 256)
+        return c
+
+    def heads(index, n=2):
+        return _On(index, 3, n, 64, dtype=bf)
+
+    def ints(index, n=3):
+        return _On(index, n, dtype=i32)
+
+    def attend_plan(index):
+        return plan(index, shape=(3, 2, 64), work={0: 256}, _ptr=256, head_dim=64, work_bytes=256)
+
+    def rope(at, of, stream=None):
+        P.rope(plan(of), heads(at), ints(at), out=heads(at), stream=stream)
+
+    def append(at, of, stream=None):
+        P.rope_append(plan(of), heads(at), heads(at), heads(at), ints(at), ints(at), cache(at), 0, out=heads(at), stream=stream)
+
+    def attend(at, of, stream=None):
+        P.attend(attend_plan(of), heads(at), cache(at), 0, out=heads(at), stream=stream)
+
+    def linear(at, of, stream=None):
+        ws = P.Workspace("cpu")
+        ws.get(4096)
+        ws.index = of
+        P.linear(_On(at, 4, 64, dtype=bf), _On(at, 8, 64, dtype=bf), out=_On(at, 4, 8, dtype=bf), ws=ws, stream=stream)
+
+    for call in (rope, append, attend, linear):
+        for args in ((1, 1), (1, 0), (0, 1), (0, -1), (0, 0, Stream(1))):
+            if call is attend and len(args) == 3 or call is linear and args != (1, 1):
+                continue                     # (these ask for the stream's capture first, which takes a GPU)
+            with pytest.raises(ValueError):
+                call(*args)
+    for call in (lambda c: c.free(ints(1, 2)), lambda c: c.fork(ints(1, 2), ints(1, 2)), lambda c: c.grow(ints(1, 2), ints(1, 2)),
+                 lambda c: c.compact()):
+        with pytest.raises(ValueError):
+            call(cache(1))
+    with pytest.raises(ValueError):
+        P._handle(Stream(1), 0)
+    assert P._handle(Stream(0), 0) == 0
