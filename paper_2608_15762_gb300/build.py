@@ -12,7 +12,6 @@ modification time alone.
 import hashlib
 import os
 import platform
-import shutil
 import subprocess
 import sys
 
@@ -26,9 +25,10 @@ HEADERS = ["gmg_layout.h", "gmg_access.h", "gmg_arb.h", "gmg_arbw.h", "gmg_arb_e
            os.path.join("..", "..", "include", "gmgest.h"), os.path.join("..", "..", "include", "gmground.h"),
            os.path.join("..", "..", "include", "gmgop.h"), "gmgop_host.h", "gmgop_ptx.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-# The shared CUDA runtime, which PyTorch uses too: with one of its own in the library each had to
-# find the other's device state changed, 2 to 4 us a call that allocates its result.
-LINK = ["-cudart", "shared"]
+# A CUDA runtime of the library's own: it loads without a toolkit on the machine, and what another
+# library's calls leave as the last error is neither reported nor taken here.  (Sharing PyTorch's
+# saves up to 2.5 us of the host's time in a small operator's call.)
+LINK = ["-cudart", "static"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 
 
@@ -90,9 +90,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if p.returncode != 0:
             raise RuntimeError("nvcc failed: " + " ".join(cmd))
     tmp = OUT + ".tmp%d" % os.getpid()
-    home = os.path.dirname(os.path.dirname(shutil.which(nvcc()) or nvcc()))
-    subprocess.check_call([nvcc()] + ARCH + LINK + ["-Xlinker", "-rpath," + os.path.join(home, "lib64"), "-shared", "-o",
-                                                    tmp] + objs)
+    subprocess.check_call([nvcc()] + ARCH + LINK + ["-shared", "-o", tmp] + objs)
     os.replace(tmp, OUT)
     with open(STAMP, "w") as f:
         f.write(want + "\n")

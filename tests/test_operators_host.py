@@ -341,3 +341,14 @@ def test_calls_refuse_what_is_not_on_the_current_gpu(monkeypatch):
     with pytest.raises(ValueError):
         P._handle(Stream(1), 0)
     assert P._handle(Stream(0), 0) == 0
+
+
+def test_the_library_needs_no_cuda_runtime_beside_it():
+    """It loads where no toolkit is installed, the simulator with it."""
+    import subprocess
+    import sys
+    code = ("import ctypes, sys\n"
+            "L = ctypes.CDLL(sys.argv[1])\n"
+            "assert L.gmg_strerror and L.op_linear\n"
+            "assert 'libcudart' not in open('/proc/self/maps').read()\n")
+    subprocess.check_call([sys.executable, "-c", code, G.LIB_PATH])
