@@ -45,8 +45,8 @@ extern "C" {
  *   pool [n_pages][n_layers][2 (K, V)][n_kv_heads][page_tokens][head_dim],
  *   16-byte aligned; page_tokens is 8, 16, 32, 64, 128 or 256, head_dim a
  *   multiple of 8 up to 128; bf16 or fp16.
- *   status int32[8]: [0] GMG_PAGE_* of the last page call, [1] the entry of its
- *   lists that it concerns (GMG_PAGE_FULL: how many pages are missing), [2]
+ *   status int32[8]: [0] GMG_PAGE_* of the last page call, [1] the first entry of its
+ *   lists that has a fault (of equal rows the second; GMG_PAGE_FULL: how many pages are missing), [2]
  *   pages moved (op_compact), [3] pages in use (op_compact), [4] tokens that
  *   op_rope_append had no page for, added up, [5] blocks of op_attend with a wait
  *   that gave up (0 unless the GPU is at fault: their output is not a result), added up. */

@@ -135,7 +135,7 @@ __device__ uint32_t free_bits(const op_cache_t& c, int64_t first) {
   return bits;
 }
 
-// Marks every listed row with its entry and reports rows that are out of range or
+// Marks every listed row with its first entry and reports rows that are out of range or
 // listed twice (the later entries find another's mark).  All threads of one block.
 __device__ void check_rows(const op_cache_t& c, const int32_t* rows, int32_t n, int32_t* mark, Faults f) {
   for (int32_t i = threadIdx.x; i < n; i += kPlanThreads) {
@@ -144,6 +144,16 @@ __device__ void check_rows(const op_cache_t& c, const int32_t* rows, int32_t n, 
     else mark[r] = i;
   }
   __syncthreads();
+  // of the entries of a row any may have left its mark: the others then take it down to the first
+  bool other = false;
+  for (int32_t i = threadIdx.x; i < n; i += kPlanThreads) {
+    const int32_t r = rows[i];
+    if (r >= 0 && r < c.n_seq && mark[r] != i) {
+      atomicMin(&mark[r], i);
+      other = true;
+    }
+  }
+  if (!__syncthreads_or(other)) return;
   for (int32_t i = threadIdx.x; i < n; i += kPlanThreads) {
     const int32_t r = rows[i];
     if (r >= 0 && r < c.n_seq && mark[r] != i) f.add(i, GMG_PAGE_TWICE);

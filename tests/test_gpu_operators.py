@@ -896,3 +896,32 @@ def test_calls_refuse_plans_and_workspaces_of_other_devices():
     plan.index = -1
     with pytest.raises(ValueError):
         P.attend(plan, x, cache, 0)
+
+
+@pytest.mark.parametrize("n_seq", [40, 3000])
+def test_a_row_listed_twice_is_reported_at_its_second_entry(n_seq):
+    """Whatever the order in which the threads run: the smallest entry that an earlier one equals."""
+    r = random.Random(n_seq)
+    c = _labelled(64, 1, 1, 8, 8, n_seq + 1, 20)
+    c.grow(_ints([n_seq]), _ints([5]))
+    for _ in range(12):
+        rows = r.sample(range(n_seq), n_seq // 2)
+        for _ in range(r.randint(1, 6)):
+            rows[r.randrange(len(rows))] = r.choice(rows)
+        seen, first = set(), None
+        for i, row in enumerate(rows):
+            if row in seen and first is None:
+                first = i
+            seen.add(row)
+        want = (P.PAGE_TWICE, first) if first is not None else None
+        for call in (lambda: c.free(_ints(rows)), lambda: c.grow(_ints(rows), _ints([0] * len(rows))),
+                     lambda: c.fork(_ints([n_seq] * len(rows)), _ints(rows), _ints([0] * len(rows)))):
+            call()
+            if want is not None:
+                assert c.code() == want
+            else:
+                assert c.code()[0] == P.PAGE_OK
+    c.grow(_ints([3, 5, 5, 3]), _ints([1, 1, 1, 1]))
+    assert c.code() == (P.PAGE_TWICE, 2)
+    c.free(_ints([7, 7]))
+    assert c.code() == (P.PAGE_TWICE, 1)
