@@ -101,15 +101,16 @@ int op_compact(const op_cache_t* cache, void* scratch, size_t scratch_bytes, gmg
  * (backward: a -> -a, the gradient's way back); the other elements pass.
  * Pairs are (2i, 2i + 1) if interleaved, else (i, i + rotary / 2).
  *   freq [rotary / 2] uint64: f_i / (2 pi) * 2^64, rounded, for 0 <= f_i < 2 pi.
- *   An angle is reduced by the wrap of a 64-bit product: its error does not
- *   grow beyond 2^-33 turns at any 32-bit position. */
+ *   An angle is reduced by the wrap of a 64-bit product, so that its error does not grow
+ *   with the position beyond |pos| 2^-65 turns, from the rounding of freq; its top 32 bits
+ *   are then rounded to fp32, up to 2^-26 turns (1e-7 radians). */
 typedef struct {
   const uint64_t* freq;
   int32_t rotary, interleaved;
   float factor;
 } op_rope_t;
 
-/* out[t][h] = x[t][h] rotated by pos[t] (int32); head_dim >= rotary, rotary even.
+/* out[t][h] = x[t][h] rotated by pos[t] (int32); head_dim >= rotary, rotary even, at most 256.
  * out may be x itself (same strides). */
 int op_rope(const op_rope_t* rope, int32_t dtype, int64_t n_tokens, int32_t n_heads, int32_t head_dim, const void* x,
             int64_t x_tok, int64_t x_head, const int32_t* pos, int32_t backward, void* out, int64_t out_tok,

@@ -2,8 +2,9 @@
 // The C ABI is declared in include/gmgop.h.
 //
 // An angle in turns is pos * f / (2 pi).  With f / (2 pi) as a 64-bit fraction, the
-// low 64 bits of the integer product are the angle's fraction of a turn, exactly:
-// no error grows with the position, and no table of angles is read.  One block
+// low 64 bits of the integer product are the angle's fraction of a turn: the fraction's
+// rounding, half a unit, is all that grows with the position, to 2^-34 turns at the last one,
+// and no table of angles is read.  The top 32 bits are kept and rounded to fp32, 2^-26 turns.  One block
 // serves one token (or a share of its heads): its threads take the sines and cosines
 // of the token's pairs into shared memory once, then every head uses them.
 //

@@ -263,6 +263,28 @@ def rope_freqs(rotary: int, base: float = 10000.0, scaling: str = "none", scale:
     return f * (keep + (1.0 - keep) / scale), 0.1 * math.log(scale) + 1.0
 
 
+def _pi(bits: int) -> int:
+    """pi 2^bits in whole numbers: 16 arctan(1/5) - 4 arctan(1/239), by their series."""
+    def arctan(x):
+        power = total = (1 << (bits + 16)) // x
+        n = 1
+        while power:
+            power //= -x * x
+            n += 2
+            total += power // n
+        return total
+    return (16 * arctan(5) - 4 * arctan(239)) >> 16
+
+
+_PI = _pi(256)
+
+
+def _turns(f: float) -> int:
+    """f / (2 pi) * 2^64, rounded (f is 64-bit: the quotient in 64 bits would be up to 2^10 off)."""
+    n, d = f.as_integer_ratio()
+    return min((n << (64 + 256)) // (d * _PI) + 1 >> 1, 2 ** 64 - 1)
+
+
 class Rope:
     """The frequencies of rotary positions, on the GPU: fractions of a turn per
     position in 64 bits.  freqs (64-bit, 0 <= f < 2 pi) and factor as from
@@ -274,8 +296,7 @@ class Rope:
         freqs = np.asarray(freqs, np.float64)
         _need(freqs.shape == (rotary // 2,) and rotary % 2 == 0, "freqs: one per pair")
         _need(bool(np.all((freqs >= 0) & (freqs < 2 * math.pi))), "freqs: 0 <= f < 2 pi")
-        # the top 53 bits in floating point, so that the fraction is f's rounding of 2^64 f / (2 pi)
-        turns = np.array([min(int(round(float(f) / (2 * math.pi) * 2.0 ** 64)), 2 ** 64 - 1) for f in freqs], np.uint64)
+        turns = np.array([_turns(float(f)) for f in freqs], np.uint64)
         self.rotary, self.factor, self.interleaved = int(rotary), float(factor), bool(interleaved)
         self.freq = torch.from_numpy(turns.view(np.int64).copy()).to(device)
         self.c = _Rope(self.freq.data_ptr(), self.rotary, int(self.interleaved), self.factor)

@@ -352,3 +352,16 @@ def test_the_library_needs_no_cuda_runtime_beside_it():
             "assert L.gmg_strerror and L.op_linear\n"
             "assert 'libcudart' not in open('/proc/self/maps').read()\n")
     subprocess.check_call([sys.executable, "-c", code, G.LIB_PATH])
+
+
+def test_rope_fractions_are_rounded_once():
+    """freq is f / (2 pi) * 2^64 to within half a unit, as the header says, for 64-bit f."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 80
+    pi = Decimal("3.1415926535897932384626433832795028841971693993751058209749445923078164062862089986")
+    top = float(np.nextafter(2 * np.pi, 0))
+    for f in (P.rope_freqs(128)[0], P.rope_freqs(96, base=5e5, scaling="parts", scale=8.0, length=8192)[0],
+              np.array([0.0, 1e-300, 5e-324, 1.0, 3.0, top])):
+        got = P.Rope(2 * len(f), freqs=f, device="cpu").freq.numpy().view(np.uint64)
+        for a, b in zip(got, f):
+            assert abs(int(a) - min(Decimal(float(b)) * 2 ** 64 / (2 * pi), Decimal(2 ** 64 - 1))) <= Decimal("0.5000001")
