@@ -141,8 +141,8 @@ int op_rope_append(const op_rope_t* rope, const op_cache_t* cache, int32_t layer
 typedef struct {
   int32_t n_batch, n_heads, n_kv_heads, head_dim, page_tokens;
   int32_t n_groups;           /* 0: no sharing (group_off and prefix not read) */
-  const int32_t* q_len;       /* host [n_batch] >= 0 */
-  const int32_t* kv_len;      /* host [n_batch] >= 0 */
+  const int32_t* q_len;       /* host [n_batch], 0 .. 2^30 */
+  const int32_t* kv_len;      /* host [n_batch], 0 .. 2^30 */
   const int32_t* seq;         /* host [n_batch] table rows; NULL: b */
   const int32_t* group_off;   /* host [n_groups + 1], 0 .. n_batch increasing */
   const int32_t* prefix;      /* host [n_groups] >= 0, at most each member's kv_len - q_len */

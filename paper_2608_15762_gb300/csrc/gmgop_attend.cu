@@ -51,6 +51,7 @@ constexpr int kKeys = 64;              // a step
 constexpr int kRows = 128;             // of a tile
 constexpr int kThreads = 256, kCopiers = 3;
 constexpr int32_t kSeesAll = 0x7f000000;
+constexpr int32_t kMaxLen = 1 << 30;   // of a request: no cache holds more, and lengths rounded up to steps stay in 32 bits
 
 struct Item {
   int32_t tok0, n_tok;                 // queries
@@ -599,6 +600,7 @@ bool desc_ok(const op_attend_desc_t* d) {
   int64_t total = 0;
   for (int32_t b = 0; b < d->n_batch; ++b) {
     if (d->q_len[b] < 0 || d->kv_len[b] < 0 || (d->seq && d->seq[b] < 0)) return false;
+    if (d->q_len[b] > kMaxLen || d->kv_len[b] > kMaxLen) return false;
     total += d->q_len[b];
   }
   if (total > 0x7fffffff / d->n_heads) return false;

@@ -365,3 +365,12 @@ def test_rope_fractions_are_rounded_once():
         got = P.Rope(2 * len(f), freqs=f, device="cpu").freq.numpy().view(np.uint64)
         for a, b in zip(got, f):
             assert abs(int(a) - min(Decimal(float(b)) * 2 ** 64 / (2 * pi), Decimal(2 ** 64 - 1))) <= Decimal("0.5000001")
+
+
+def test_attend_plan_refuses_lengths_that_no_cache_holds():
+    """Rounded up to whole steps or tiles they would pass 32 bits."""
+    for q, kv in (([1], [2 ** 31 - 1]), ([1], [2 ** 30 + 1]), ([0], [2 ** 31 - 1]), ([2 ** 30 + 1], [5])):
+        _refuses(q, kv, 1, 1, 64, 16)
+    plan, items = P.attend_items([1], [2 ** 30], 8, 1, 64, 256)
+    runs = sorted(items[:8 * plan.n_items].reshape(-1, 8)[:, 3:5].tolist())
+    assert runs[0][0] == 0 and runs[-1][1] == 2 ** 30 and all(a[1] == b[0] for a, b in zip(runs, runs[1:]))
