@@ -925,3 +925,136 @@ def test_a_row_listed_twice_is_reported_at_its_second_entry(n_seq):
     assert c.code() == (P.PAGE_TWICE, 2)
     c.free(_ints([7, 7]))
     assert c.code() == (P.PAGE_TWICE, 1)
+
+
+# ---------------------------------------------------------------------------
+# Products over pairs of blocks: more tiles than fill half of the SMs
+# ---------------------------------------------------------------------------
+
+def _pair_sizes():
+    # one round and a part, odd columns and rows; several tiles dealt out by steps and joined, odd and even;
+    # a last tile of one row and one column; columns of x that are no whole step
+    return [(1300, 520, 5001, False), (1270, 2056, 4001, True), (1537, 1544, 3500, False), (2305, 264, 2561, False),
+            (640, 4104, 6600, True), (20000, 72, 300, False)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("m,k,n,joined", _pair_sizes())
+def test_linear_over_pairs(m, k, n, joined, dtype):
+    g = _gen(m + k + n)
+    x, w, gate = _rand(g, m, k, dtype=dtype), _rand(g, n, k, dtype=dtype, scale=k ** -0.5), _rand(g, n, k, dtype=dtype, scale=k ** -0.5)
+    bias, gate_bias, res = _rand(g, n, dtype=dtype), _rand(g, n, dtype=dtype), _rand(g, m, n, dtype=dtype)
+    assert 2 * -(-n // 256) * -(-m // 256) > 76
+    if joined:
+        assert _work_bytes(m, k, n) > 4096 and _work_bytes(m, k, n, 1) > 4096
+    for kw in (dict(), dict(bias=bias, act="gelu", residual=res), dict(act="relu", residual=res), dict(bias=bias, act="silu"),
+               dict(gate=gate, act="silu"), dict(gate=gate, act="relu", bias=bias, gate_bias=gate_bias, residual=res),
+               dict(gate=gate, act="gelu", gate_bias=gate_bias), dict(gate=gate, act="none", bias=bias, residual=res)):
+        want, tol = R.linear(x, w, **kw)
+        ws = P.Workspace()
+        y = P.linear(x, w, ws=ws, **kw)
+        R.within(y, want, tol, "linear %s" % sorted(kw))
+        assert torch.equal(P.linear(x, w, ws=ws, **kw), y) and ws.gave_up() == 0
+
+
+@pytest.mark.parametrize("m,k,n", [(1300, 520, 5001), (1270, 2056, 4001)])
+def test_linear_over_pairs_strides_and_in_place(m, k, n):
+    g = _gen(m)
+    x, w, gate = _rand(g, m, k + 24)[:, 8:8 + k], _rand(g, n, k + 8, scale=k ** -0.5)[:, :k], _rand(g, n, k + 16, scale=k ** -0.5)[:, 8:8 + k]
+    out = torch.full((m, n + 9), 7.0, dtype=BF, device="cuda")
+    res = _rand(g, m, n + 3)[:, 1:n + 1]
+    for kw in (dict(act="silu", residual=res), dict(gate=gate, act="silu", residual=res)):
+        want, tol = R.linear(x, w, **kw)
+        P.linear(x, w, out=out[:, 5:n + 5], **kw)
+        R.within(out[:, 5:n + 5], want, tol)
+        assert bool((out[:, :5] == 7).all()) and bool((out[:, n + 5:] == 7).all())
+        y = res.clone()
+        P.linear(x, w, out=y, **dict(kw, residual=y))
+        R.within(y, want, tol)
+
+
+@pytest.mark.parametrize("m,k,n", [(1300, 520, 5001), (1270, 2056, 4001)])
+def test_linear_over_pairs_infinities_and_nan_stay_in_their_rows_and_columns(m, k, n):
+    g = _gen(n)
+    x, w = _rand(g, m, k), _rand(g, n, k, scale=k ** -0.5)
+    want, tol = R.linear(x, w)
+    rows, cols = (0, 255, 256, m - 1), (1, 127, 128, n - 1)
+    for i, r in enumerate(rows):
+        x[r, (5 * i) % k] = (math.nan, math.inf)[i % 2]
+    for i, c in enumerate(cols):
+        w[c, (k - 1 - i)] = (math.nan, -math.inf)[i % 2]
+    y = P.linear(x, w)
+    clean = torch.ones(m, n, dtype=torch.bool, device="cuda")
+    clean[list(rows)] = False
+    clean[:, list(cols)] = False
+    assert not bool(torch.isfinite(y[list(rows)]).any()) and not bool(torch.isfinite(y[:, list(cols)]).any())
+    R.within(y[clean], want[clean], tol[clean])
+
+
+def test_linear_clusters_of_every_tile():
+    """Fewer tiles: each height of a tile, gated and not, with every activation and both types."""
+    g = _gen(91)
+    for i, m in enumerate((3, 16, 17, 31, 32, 33, 64, 65, 128, 129, 255, 256, 257)):
+        k, n, dtype = 1032 + 8 * i, 384 + 37 * i, (BF, HF)[i % 2]
+        x, w, gate = _rand(g, m, k, dtype=dtype), _rand(g, n, k, dtype=dtype, scale=k ** -0.5), _rand(g, n, k, dtype=dtype, scale=k ** -0.5)
+        bias, res = _rand(g, n, dtype=dtype), _rand(g, m, n, dtype=dtype)
+        for act in sorted(P.ACTS):
+            for kw in (dict(bias=bias, act=act, residual=res), dict(gate=gate, act=act, gate_bias=bias, residual=res)):
+                want, tol = R.linear(x, w, **kw)
+                R.within(P.linear(x, w, **kw), want, tol, "%d rows, %s" % (m, sorted(kw)))
+
+
+# ---------------------------------------------------------------------------
+# What a table without a page, and a compaction, come to
+# ---------------------------------------------------------------------------
+
+def test_attend_missing_pages_read_as_zeros():
+    g = _gen(43)
+    for D, page, n in ((64, 16, 64), (128, 8, 200)):
+        cache, keys, vals = _filled(g, [n], 1, D, page)
+        gone = {1: 10 ** 6, 2: -1, 5: len(cache.refs), (n - 1) // page: -2 ** 31}
+        for j, p in gone.items():
+            if j < -(-n // page):
+                cache.table[0, j] = p
+                keys[0][j * page:(j + 1) * page] = 0
+                vals[0][j * page:(j + 1) * page] = 0
+        q = _rand(g, 3, 2, D)
+        o, lse = P.attend(P.AttendPlan([3], [n], 2, 1, D, page), q, cache, 1, lse=True)
+        wo, to, wl, tl = R.attend(q, keys[0], vals[0], 3, D ** -0.5)
+        R.within(o, wo, to)
+        R.within(lse, wl, tl)
+
+
+def test_compact_moves_the_last_pages_of_a_large_pool():
+    g = _gen(92)
+    hk, page, D, n_pages = 8, 64, 128, 17_000
+    pool = torch.empty(n_pages, 1, 2, hk, page, D, dtype=BF, device="cuda")
+    c = P.PageCache(pool, n_seq=3, max_pages=6)
+    c.refs.fill_(1)
+    c.refs[n_pages - 8:] = 0
+    c.refs[3] = 0
+    c.grow(_ints([0]), _ints([150]))         # pages 3, n - 8, n - 7
+    c.grow(_ints([1]), _ints([10]))          # n - 6
+    assert c.table[:2, :3].tolist() == [[3, n_pages - 8, n_pages - 7], [n_pages - 6, -1, -1]]
+    for p in (3, n_pages - 8, n_pages - 7, n_pages - 6):
+        pool[p] = _rand(g, 1, 2, hk, page, D)
+    held, still = pool[n_pages - 6].clone(), pool[n_pages - 9].clone()
+    c.free(_ints([0]))
+    c.compact()
+    assert c.status.tolist()[:4] == [P.PAGE_OK, 0, 1, n_pages - 8]
+    assert c.table.tolist() == [[-1] * 6, [3] + [-1] * 5, [-1] * 6] and c.lens.tolist() == [0, 10, 0]
+    refs = c.refs.tolist()
+    assert refs[:n_pages - 8] == [1] * (n_pages - 8) and refs[n_pages - 8:] == [0] * 8
+    assert torch.equal(pool[3], held) and torch.equal(pool[n_pages - 9], still)
+    # two pages move, in order
+    c.grow(_ints([0, 2]), _ints([64, 128]))
+    assert c.table[:, :2].tolist() == [[n_pages - 8, -1], [3, -1], [n_pages - 7, n_pages - 6]]
+    for p in (n_pages - 7, n_pages - 6):
+        pool[p] = _rand(g, 1, 2, hk, page, D)
+    held = [pool[n_pages - 7].clone(), pool[n_pages - 6].clone()]
+    c.free(_ints([0, 1]))
+    c.compact()
+    assert c.status.tolist()[:4] == [P.PAGE_OK, 0, 2, n_pages - 7]
+    assert c.table[2, :2].tolist() == [3, n_pages - 8]
+    assert torch.equal(pool[3], held[0]) and torch.equal(pool[n_pages - 8], held[1])
+    assert c.refs[n_pages - 9:].tolist() == [1, 1] + [0] * 7
