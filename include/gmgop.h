@@ -18,7 +18,8 @@
  * GMG_EWS for a short or misaligned buffer, GMG_ECUDA for a failed launch.
  * Strides are in elements; the innermost dimension of a tensor is contiguous
  * and no tensor's elements overlap.  Sums, softmax statistics and angles are
- * held in 32 bits or more and rounded once, to the output's type.
+ * held in 32 bits or more and rounded once, to the output's type; op_attend's
+ * probabilities are rounded to the values' type before, for their product.
  */
 #ifndef GMGOP_H
 #define GMGOP_H

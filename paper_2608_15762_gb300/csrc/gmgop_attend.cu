@@ -12,6 +12,8 @@
 // S_{j+1} is computed while the softmax works on S_j.  The reference m need not be the exact
 // running maximum, as it cancels: O is rescaled only where a score exceeds m by more than
 // 2^8, so p stays below 2^8 (times 2^7 for fp16, whose small p would lose bits below 2^-14).
+// P is rounded to the values' type because the tensor cores take it so (their sum l is of the
+// unrounded ones): the error against 64 bits is 1.4 times that of probabilities in 32 bits.
 //
 // Queries that share a prefix lie next to each other, so a tile of rows reaches over their
 // requests and every page of the prefix is read once a tile.  Long runs of keys are cut into
@@ -20,12 +22,12 @@
 //
 // What bounds it, and what it measured (us a call, replayed; floor: bytes at 6.67 TB/s or products
 // at 1,946 TFLOP/s):
-//   32 requests of 6,000 tokens, one query each    119, floor 113: reading the cache
-//   96 requests behind 32,768 shared tokens         73, floor 40: three tiles read the prefix from
+//   32 requests of 6,000 tokens, one query each    125, floor 118: reading the cache
+//   96 requests behind 32,768 shared tokens         74, floor 40: three tiles read the prefix from
 //       the L2 cache (514 MB, 7.5 TB/s), then the start and end of 768 short items
-//   chunks of prompts, 8,691 queries behind 4,000   240, floor 107: the softmax warps' instructions
-//       (55% of the issue slots, two blocks an SM; the tensor cores are 41% busy)
-//   8 requests behind 500 shared tokens             9.7: a launch and a chain of eight steps
+//   chunks of prompts, 8,691 queries behind 4,000   242, floor 107: the softmax warps' instructions and
+//       each step's waits (54% of the issue slots, two blocks an SM; the tensor cores are 41% busy)
+//   8 requests behind 500 shared tokens             9.9: a launch and a chain of eight steps
 // Two blocks an SM hide each other's waits; TMEM holds no third (O 128 columns, S and P 128).
 
 #include <cuda_bf16.h>

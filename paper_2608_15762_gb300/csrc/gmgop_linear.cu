@@ -4,10 +4,11 @@
 // Four kernels, by the number of rows of x and the tiles that there are (see few_tiles and
 // kFewRows), and one more for operands that bulk copies cannot read.  us a call, replayed on
 // weights beyond the L2 cache; in brackets the floor and what bounds it:
-//   1 x 4,096 x 4,096 (rows, columns of x, outputs)   9.9 (5.0: reading the weight, and the launch)
+//   1 x 4,096 x 4,096 (rows, columns of x, outputs)   9.8 (5.0: the launch and the loads in flight; memory is at
+//       35% of its rate: five blocks an SM, 82 registers a thread, so that 1,024 blocks are 1.35 rounds)
 //   16 x 4,096 x 12,288                              22.5 (15: reading the weight, 4.5 TB/s)
 //   77 x 1,000 x 1,111                                7.2 (0.4: launch, a chain of copy, product, sums)
-//   2,048 x 4,096 x 12,288 with a gate                264 (212: 5.05 rounds of tiles; tensor cores 72%
+//   2,048 x 4,096 x 12,288 with a gate                260 (212: 5.05 rounds of tiles; tensor cores 72%
 //       busy: a tile's end is not hidden behind the next tile, as its two sums take all of TMEM)
 //   8,192 x 12,288 x 4,096 and a residual             436 (424: tensor cores, 88% busy; the power limit)
 
@@ -32,7 +33,8 @@ __device__ __forceinline__ float up(__half v) { return __half2float(v); }
 __device__ __forceinline__ void down(float v, __nv_bfloat16* o) { *o = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void down(float v, __half* o) { *o = __float2half_rn(v); }
 
-// The activations, in fp32.
+// The activations, in fp32.  (silu's exponential is the fast one: its error, a few units of 2^-24 and
+// 2^-24 of the argument, is far below the output's rounding to 16 bits.)
 template <int kAct>
 __device__ __forceinline__ float act_of(float v) {
   if (kAct == GMG_OP_RELU) return v < 0.f ? 0.f : v;   // keeps a NaN
@@ -168,8 +170,9 @@ cudaError_t launch_any(const op_linear_t& a, cudaStream_t st) {
 // ---- few rows of x ---------------------------------------------------------
 
 // A warp (or four, where the weight has few and long rows) takes one row of the weight against up to
-// two rows of x: 16-byte loads, kAhead of them in flight, x from the L1 cache.  Bound by
-// reading the weight; no piece waits for another.
+// two rows of x: 16-byte loads, kAhead of them in flight, x from the L1 cache.  No piece waits for
+// another; bound by the loads that the resident blocks keep in flight (35% of the memory's rate and
+// 22% of the issue slots for 4,096 x 4,096).
 constexpr int kFewRows = 2;
 // ... and two rows of x only with a weight of few rows (us, here / below: 6,144 x 1,024 7.2 / 8.1,
 // 1,024 x 12,288 10.0 / 12.7, 12,288 x 4,096 29.9 / 24; one row 22.6 there).
@@ -295,7 +298,7 @@ constexpr int kTailMax = 1 << 30;      // steps dealt out, at most
 // A tile is 128 rows of the weight by up to 256 rows of x.  The blocks of a cluster take a share of
 // its steps each, leave their sums in shared memory, and then each adds up and finishes a
 // share of the rows, in the order of the blocks.  Bound by reading the weight: two blocks an
-// SM keep 200 KB of it on the way.  (A second launch that adds partial results from memory took
+// SM keep 200 KB of it on the way (gated products of 17 to 32 rows 144, two stages of 36 a block).  (A second launch that adds partial results from memory took
 // 2 to 3 us more, the last block adding them alone 40.)
 template <int NT, bool kGate>
 struct SplitShape {

@@ -9,7 +9,8 @@
 // of the token's pairs into shared memory once, then every head uses them.
 //
 // Bound by memory: 32,768 tokens of 32 + 8 + 8 heads of 128 into a cache 123 us, 6.5 TB/s
-// (floor 121); 16 tokens 2.8 us, a launch; 1,537 x 20 heads of 80, fp32, 7.2 us (floor 3.0).
+// (floor 121).  16 tokens 2.8 us, a launch; 1,537 x 20 heads of 80, fp32, 7.2 us (floor 3.0): the launch
+// and a block's chain of position, frequencies, sines and only then its first load of x.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
