@@ -158,6 +158,7 @@ class PageCache:
     page_tokens, head_dim] and, int32, table [n_seq, max_pages] (-1: no page), lens
     [n_seq] and refs [n_pages].  What is not given starts empty, but references are
     counted from a given table (which has to come with its lens where rows are to grow).
+    It is set up on the current stream, which calls on others have to wait for.
     The page calls take int32 lists on the GPU and do not synchronise; ``code()`` does,
     and says how the last one went."""
 
