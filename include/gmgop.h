@@ -10,7 +10,9 @@
  *   op_free, op_fork, op_grow, op_compact   pages of the cache
  *   op_rope, op_rope_append                 rotary positions, into the cache
  *   op_attend_plan, op_attend               attention over shared prefixes
+ *   op_rope_append8, op_attend8_plan, op_attend8    the same on a cache in 8 bits
  *   op_linear                               product with its epilogue
+ *   op_norm                                 norms around a block, with its gate and residual
  *
  * All pointers are device pointers unless stated; calls are asynchronous on
  * `stream`, allocate nothing, and return 0 or a negative GMG_E* code
@@ -37,6 +39,7 @@ extern "C" {
 #define GMG_OP_F32 0
 #define GMG_OP_BF16 1
 #define GMG_OP_F16 2
+#define GMG_OP_E4M3 3     /* caches only */
 
 /* A paged cache of keys and values.  Request row s holds tokens 0 ..
  * lens[s] - 1; token t is slot t % page_tokens of page table[s * max_pages +
@@ -60,6 +63,15 @@ typedef struct {
   int32_t dtype, n_pages, n_layers, n_kv_heads, page_tokens, head_dim;
   int32_t n_seq, max_pages;
 } op_cache_t;
+
+/* A cache in 8 bits (dtype GMG_OP_E4M3; page_tokens at least 16, head_dim a multiple of 16): half the
+ * bytes.  A page of the pool is, page_bytes after the one before it,
+ *   codes [n_layers][2 (K, V)][n_kv_heads][page_tokens][head_dim], e4m3, then
+ *   scales [n_layers][2][n_kv_heads][page_tokens / 16], fp32, one for 16 tokens of a head;
+ *   page_bytes = their sum, up to a whole 128 bytes.
+ * A value is code * scale.  Scales are from 2^-60 to 2^60; one outside is read as the nearer bound
+ * (NaN as the lower).  Page calls move codes and scales. */
+size_t op_page8_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t page_tokens, int32_t head_dim); /* 0 on bad arguments */
 
 #define GMG_PAGE_OK 0
 #define GMG_PAGE_FULL 1   /* fewer free pages than needed */
@@ -127,6 +139,22 @@ int op_rope_append(const op_rope_t* rope, const op_cache_t* cache, int32_t layer
                    const void* v, int64_t v_tok, int64_t v_head, const int32_t* pos, const int32_t* seq, void* q_out,
                    int64_t o_tok, int64_t o_head, gmg_stream_t stream);
 
+/* The same into a cache in 8 bits; q, k, v and q_out of type dtype (bf16 or fp16).  Of every block
+ * of 16 tokens, layer, K or V and head that the call writes to:
+ *   need = the least power of two with (largest finite |new value|) / need <= 448, from 2^-60 to 2^60;
+ *   the scale becomes need where the call writes the block's first token, else the larger of need
+ *   and what it was; tokens before the first one written keep their values, rounded again where the
+ *   scale has grown (tokens behind it are no longer valid, as where a row is cut back and grown again);
+ *   a new value's code is (k rotated or v) / scale, rounded once, to nearest even; infinities become
+ *   +-448, NaN stays.
+ * Tokens of one row that lie in one block come one after another in the lists, in increasing order,
+ * within 32 entries (some that are not written, as padding, may lie between): else what that block
+ * holds is not defined. */
+int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, int32_t layer, int32_t dtype, int64_t n_tokens,
+                    int32_t n_heads, const void* q, int64_t q_tok, int64_t q_head, const void* k, int64_t k_tok,
+                    int64_t k_head, const void* v, int64_t v_tok, int64_t v_head, const int32_t* pos,
+                    const int32_t* seq, void* q_out, int64_t o_tok, int64_t o_head, gmg_stream_t stream);
+
 /* Attention of a batch of requests over a paged cache.  Request b has
  * q_len[b] queries, the last of its kv_len[b] cached tokens: query i sits at
  * position kv_len[b] - q_len[b] + i and sees the keys at or before it (none, if
@@ -174,6 +202,19 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
               const void* q, int64_t q_tok, int64_t q_head, float scale, void* out, int64_t out_tok, int64_t out_head,
               float* lse, void* work, size_t work_bytes, gmg_stream_t stream);
 
+/* The same over a cache in 8 bits, for q and out of type dtype (bf16 or fp16); n_heads /
+ * n_kv_heads at most 64.  Codes are exact in the products, probabilities (times the values'
+ * scales) rounded to fp16 for theirs. */
+typedef struct {
+  op_attend_plan_t p;
+} op_attend8_plan_t;
+
+int op_attend8_plan(const op_attend_desc_t* desc, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,
+                    size_t item_bytes);
+int op_attend8(const op_attend8_plan_t* plan, const int32_t* d_items, const op_cache_t* cache, int32_t layer,
+               int32_t dtype, const void* q, int64_t q_tok, int64_t q_head, float scale, void* out, int64_t out_tok,
+               int64_t out_head, float* lse, void* work, size_t work_bytes, gmg_stream_t stream);
+
 /* y = act(x w^T + bias) + residual, or, with a gate,
  * y = act(x gate^T + gate_bias) * (x w^T + bias) + residual.
  * x [m][k], w and gate [n][k], residual and y [m][n], bias and gate_bias [n], all of
@@ -198,6 +239,30 @@ typedef struct {
  * has returned 0, and what it wrote is not its result).  0 on bad arguments. */
 size_t op_linear_work_bytes(const op_linear_t* args);
 int op_linear(const op_linear_t* args, void* work, size_t work_bytes, gmg_stream_t stream);
+
+/* Norms around a block: with its result y [m][n] and the residual stream x [m][n],
+ *   N(v; w, b) = (v - mean) / sqrt(mean((v - mean)^2) + eps) * (w + shift) + b, mean 0 for GMG_NORM_RMS,
+ *   r = x + scale * gate * (after ? N(y; y_weight, y_bias) : y),   h = N(r; weight, bias);
+ * without y, h = N(x; weight, bias).  All in fp32, h from the unrounded r.
+ * x and r are of type stream_dtype (dtype or fp32), all else of type dtype (bf16, fp16 or fp32).
+ * Weights and biases [n] may be NULL (1 and 0, whatever shift), gate (1), and one of r and h.  gate: one for each channel
+ * (gate_row 0, gate_col 1), each row (gate_col 0) or each element (gate_col 1).  r may be x, and
+ * h or r may be y (same type and strides).  m, n >= 0, n at most GMG_NORM_MOST. */
+#define GMG_NORM_RMS 0
+#define GMG_NORM_LAYER 1
+#define GMG_NORM_MOST 32768
+
+typedef struct {
+  int32_t dtype, stream_dtype, kind, after;
+  int64_t m, n;
+  const void *x, *y, *gate, *y_weight, *y_bias, *weight, *bias;
+  void *r, *h;
+  int64_t x_row, y_row, gate_row, gate_col, r_row, h_row; /* row strides, >= the row's length; gate_col 0 or 1 */
+  float scale, eps, shift;
+  int32_t reserved;
+} op_norm_t;
+
+int op_norm(const op_norm_t* args, gmg_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,660 @@
+// Attention over a paged cache in 8 bits, with a scale for each block of 16 tokens and head.  The C
+// ABI is declared in include/gmgop.h.
+//
+// A work item is up to 64 rows (queries of consecutive tokens, all query heads of one key/value
+// head: row = token * heads + head) against a run of keys, 128 a step.  The products are turned
+// round: keys fill the tensor core's 128 lanes and rows are columns, so that a step of few rows
+// (a decode step has 4 to 8) costs few columns, few exponentials and few registers:
+//   S^T [128 keys][rows] = K Q^T,   O^T [128 dims][rows] += V^T P^T.
+// A thread of the softmax holds one key, so the scales of its block are numbers of its own.
+// Codes become fp16 on the way, which holds e4m3 exactly: keys go into TMEM, values into shared
+// memory.  Q (times a power of two that brings the tile's largest to 2^13, so that bf16's 8 bits
+// lie in fp16's range) and P are fp16 too.
+// One block takes one item:
+//   warps 4 to 6   copies: page by page into a ring of 128-key slots, K_0 K_1 V_0 K_2 V_1 ...
+//   warp 7         products
+//   warps 0 to 3   K_{j+1} to fp16, the softmax of S_j, V_j to fp16
+// With value scales v_j, P holds w = exp2(s + log2 v - m) and the sum takes w / v: one exponent
+// for both, so that P uses fp16's range whatever the scales, and O has them right.  The reference
+// m is of the w and need not be the exact running maximum: it is raised where a w would exceed
+// 2^8 times it (times 2^7 for fp16's small numbers).
+// P is rounded to fp16 because the tensor cores take it so (the sum is of the unrounded): 2^-12.
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <new>
+#include <type_traits>
+
+#include "../../include/gmgop.h"
+#include "gmg_once.h"
+#include "gmgop_attend.cuh"
+#include "gmgop_host.h"
+#include "gmgop_ptx.cuh"
+
+namespace gop {
+namespace {
+
+constexpr int kKeys = 128;             // a step
+constexpr int kRows = 64;              // of a tile
+constexpr int kThreads = 256, kCopiers = 3;
+constexpr float kBias = 7.f;           // p is at most 2^(8 + kBias)
+constexpr float kNone = -1e30f;        // the reference of a row that has seen nothing
+constexpr uint32_t kTurnedA = 1u << 15;   // A lies with its rows (M) contiguous
+
+struct Args8 {
+  AttendArgs a;
+  const void* q;
+  int64_t q_tok, q_head;
+  const unsigned char* pool;
+  int64_t page_bytes, scale_at;        // of a page; of the layer's scales in it
+};
+
+template <int DP>
+struct Shape {
+  static constexpr int kHalves = DP / 64;
+  static constexpr int kQ = kHalves * kRows * 128;
+  static constexpr int kP = kKeys * 128;
+  static constexpr int kV = kHalves * kKeys * 128;
+  static constexpr int kSlot = kKeys * DP;
+  static constexpr int kSlots = 49152 / kSlot;
+  static constexpr int kMiscAt = kQ + kP + kV + kSlots * kSlot;
+  static constexpr int kSmem = kMiscAt + 1024;
+  static constexpr int kColumns = 256;   // of TMEM: O^T 64, S^T twice 64, K 64 (fp16, two a column)
+};
+
+template <int DP>
+struct Misc {
+  float neg_m[kRows];                  // minus the rows' references
+  int32_t first_nan[128];              // by dimension: the first key whose value is NaN where rows see different keys
+  uint64_t bars[2 * Shape<DP>::kSlots + 5];
+  uint32_t tmem_at, failed, flag[2];   // flag: the step (+ 1) that raises a reference
+};
+static_assert(sizeof(Misc<128>) <= 1024 && sizeof(Misc<64>) <= 1024, "fits behind the ring");
+
+// Two e4m3 to two fp16, exactly.
+__device__ __forceinline__ uint32_t wide2(uint16_t v) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
+  return r;
+}
+__device__ __forceinline__ void wide16(uint4 v, uint32_t* o) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = wide2((uint16_t)w[i]);
+    o[2 * i + 1] = wide2((uint16_t)(w[i] >> 16));
+  }
+}
+
+// 16 codes of a row of a slot, where the copy has put them.
+template <int DP>
+__device__ __forceinline__ uint4* codes_at(unsigned char* slot, int row, int c) {
+  const int x = DP == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3);
+  return reinterpret_cast<uint4*>(slot + row * DP + x * 16);
+}
+
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+
+// Order of floats as that of int32.
+__device__ __forceinline__ int32_t ordered(float v) {
+  const int32_t i = __float_as_int(v);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+
+// Two numbers of a row of Q times `by`, as fp16.
+__device__ __forceinline__ uint32_t to_q(__nv_bfloat16, uint32_t v, float by) {
+  return pack(__half(), __uint_as_float(v << 16) * by, __uint_as_float(v & 0xffff0000u) * by);
+}
+__device__ __forceinline__ uint32_t to_q(__half, uint32_t v, float by) { return by < 0.f ? v ^ 0x80008000u : v; }
+
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_constant__ CUtensorMap map_kv,
+                                                              const __grid_constant__ Args8 g) {
+  using S = Shape<DP>;
+  extern __shared__ __align__(1024) unsigned char base[];
+  const AttendArgs& a = g.a;
+  unsigned char *const p_mem = base + S::kQ, *const v_mem = p_mem + S::kP, *const ring = v_mem + S::kV;
+  Misc<DP>& misc = *reinterpret_cast<Misc<DP>*>(base + S::kMiscAt);
+  volatile uint32_t* failed = &misc.failed;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
+  // all heads of an item, then the next item: the long ones start first
+  const int32_t item = blockIdx.x / a.n_kv, hk = blockIdx.x - item * a.n_kv;
+  const Item it = a.items[item];
+  const int32_t rows = it.n_tok * a.group;
+  const int32_t first = it.lo / kKeys, n = it.hi > it.lo ? (it.hi + kKeys - 1) / kKeys - first : 0;
+
+  if (n == 0) {   // queries that see nothing
+    for (int r = threadIdx.x; r < rows; r += kThreads) {
+      const int64_t t = it.tok0 + r / a.group;
+      const int32_t h = hk * a.group + r % a.group;
+      T* o = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+      for (int d = 0; d < a.dim; d += 8) *reinterpret_cast<uint4*>(o + d) = uint4{};
+      if (a.lse) a.lse[t * a.n_heads + h] = -INFINITY;
+    }
+    return;
+  }
+
+  const int n_c = (rows + 15) / 16;     // columns, 16 at a time
+  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, k_ready = empty + 8 * S::kSlots,
+                 s_full = k_ready + 8, v_ready = s_full + 8, o_done = v_ready + 8, met = o_done + 8;
+  // Each of these barriers' phases is awaited by all that arrive at the next one before they do, so
+  // a wait's parity tells its phase from the one before it, which is over.
+  if (warp == 4 && lane == 0) {
+    prefetch_map(&map_kv);
+    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 4);
+    bar_init(k_ready, 4), bar_init(s_full, 1), bar_init(v_ready, 4), bar_init(o_done, 1), bar_init(met, 4);
+    misc.failed = misc.flag[0] = misc.flag[1] = 0;
+    fence_bar_init();
+  }
+  if (threadIdx.x < 128) misc.first_nan[threadIdx.x] = 0x7fffffff;
+  if (threadIdx.x < kRows) misc.neg_m[threadIdx.x] = -kNone;
+  if (warp == 7) tmem_alloc<1>(smem_addr(&misc.tmem_at), S::kColumns);
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + 64, tmem_k = tmem + 192;
+
+  if (warp >= 4 && warp < 4 + kCopiers) {
+    const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
+    const uint32_t slots = smem_addr(ring);
+    // the page numbers come 32 at a time, the next 32 on their way
+    const int shift = __ffs(a.page_tokens) - 1;
+    const int32_t last = (it.hi - 1) >> shift;
+    int32_t at0 = first * kKeys >> shift;
+    auto look_up = [&](int32_t i) {
+      const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
+      return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
+    };
+    int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
+    int e = warp - 4;
+    for (; e < 2 * n; e += kCopiers) {
+      // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
+      const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
+      const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
+      const int slot = e % S::kSlots;
+      const int32_t k0 = (first + j) * kKeys;
+      const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
+      if (is_v && (k0 >> shift) - at0 >= 32) {   // K is at most three steps ahead of V, 24 pages
+        at0 += 32;
+        now = next;
+        next = look_up(at0 + 32 + lane);
+      }
+      if (!bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed)) break;
+      const uint32_t bar = full + 8 * slot, dst = slots + slot * S::kSlot;
+      if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * DP);
+      for (int32_t k = from; k < to; k += box) {
+        const int32_t rel = ((k0 + k) >> shift) - at0;
+        const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
+        const int32_t y = ((a.plane + is_v) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
+        if (elect_one()) load_3d(dst + k * DP, &map_kv, 0, y, page, bar);
+      }
+    }
+    if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
+      uint32_t quiet = 0;
+      for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - S::kSlots; b -= kCopiers)
+        bar_pass(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
+    }
+    __syncwarp();
+  } else if (warp == 7) {
+    // the whole warp goes along; one lane issues
+    const uint32_t desc_s = mma_desc(false, kKeys, 16 * n_c, false), desc_o = mma_desc(false, 128, 16 * n_c, true) | kTurnedA;
+    const uint64_t q = tile_k(smem_addr(base)), p = tile_n(smem_addr(p_mem), kKeys * 128),
+                   v = tile_n(smem_addr(v_mem), kKeys * 128);
+    auto scores = [&](int j) {
+      if (!bar_wait(k_ready, j & 1, failed)) return false;
+      tc_after_sync();
+      const uint32_t d = tmem_s + (j & 1) * kRows;
+      if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+          mma_ts(d, tmem_k + 8 * i, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), desc_s, i > 0);
+        mma_commit(s_full);
+      }
+      __syncwarp();
+      return true;
+    };
+    int asked = 0, done = 0;            // S and O that are on their way
+    bool go = scores(0);
+    asked += go;
+    for (int j = 0; go && j < n; ++j) {
+      if (j + 1 < n) {
+        if (!scores(j + 1)) break;
+        ++asked;
+      }
+      if (!bar_wait(v_ready, j & 1, failed)) break;
+      tc_after_sync();
+      if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < kKeys / 16; ++i)
+          mma_ss<1>(tmem, v + i * (16 * 128 / 16), p + i * (16 * 128 / 16), desc_o, j > 0 || i > 0);
+        mma_commit(o_done);
+      }
+      __syncwarp();
+      ++done;
+    }
+    uint32_t quiet = 0;
+    if (asked > 0) bar_pass(s_full, (asked - 1) & 1, &quiet);
+    if (done > 0) bar_pass(o_done, (done - 1) & 1, &quiet);
+  } else {
+    const int r = threadIdx.x;           // the key of a step, and the dimension of O^T
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    uint32_t meetings = 0;
+    float by = 1.f, unit = 1.f;          // Q is scaled by `by`; |1 / by|
+    {
+      // Q to shared memory, 16 bytes a step: consecutive threads along a row
+      constexpr int kEach = kRows * DP / 8 / 128;
+      uint4 v[kEach];
+      uint32_t top = 0;                  // of |q| where finite, its bits
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int x = r + 128 * i, row = x / (DP / 8), c = x % (DP / 8);
+        v[i] = uint4{};
+        if (row < rows && c * 8 < a.dim) {
+          const int32_t tok = row / a.group;
+          v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
+                                                 (hk * a.group + row - tok * a.group) * g.q_head + c * 8);
+        }
+        if (std::is_same<T, __nv_bfloat16>::value) {
+          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = w[k] & 0x7fff, hi = (w[k] >> 16) & 0x7fff;
+            if (lo < 0x7f80 && lo > top) top = lo;
+            if (hi < 0x7f80 && hi > top) top = hi;
+          }
+        }
+      }
+      if (std::is_same<T, __nv_bfloat16>::value) {
+        top = __reduce_max_sync(0xffffffffu, top);
+        uint32_t* tops = reinterpret_cast<uint32_t*>(p_mem);
+        if (lane == 0) tops[warp] = top;
+        bar_meet(met, &meetings, failed);
+        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        const int e = max(min(140 - (int)(top >> 7), 126), -114);   // 2^13 over the largest's power of two
+        by = __int_as_float((e + 127) << 23);
+        unit = __int_as_float((127 - e) << 23);
+      }
+      if (a.negative) by = -by;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int x = r + 128 * i, row = x / (DP / 8), c = x % (DP / 8);
+        if (row >= 16 * n_c) continue;
+        uint4 o;
+        o.x = to_q(T(), v[i].x, by), o.y = to_q(T(), v[i].y, by), o.z = to_q(T(), v[i].z, by), o.w = to_q(T(), v[i].w, by);
+        *reinterpret_cast<uint4*>(base + (c / 8) * (kRows * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16) = o;
+      }
+      fence_async();
+    }
+    const int shift = __ffs(a.page_tokens) - 1;
+    const float c_all = a.scale2 * unit;
+    auto page_of = [&](int32_t key) {
+      return key >= it.lo && key < it.hi ? a.table[int64_t(it.row) * a.max_pages + (key >> shift)] : -1;
+    };
+    // the scales of this key's block; of a page that is none 1 (its codes are zeros)
+    auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
+      *ks = *vs = 1.f;
+      if (page < 0 || page >= a.n_pages) return;
+      const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
+      const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
+      *ks = __ldg(s + at);
+      *vs = __ldg(s + a.n_kv * blocks + at);
+    };
+    auto put_keys = [&](int j) {
+      const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
+      bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
+#pragma unroll
+      for (int h = 0; h < S::kHalves; ++h) {
+        uint32_t o[32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) wide16(*codes_at<DP>(ring + slot * S::kSlot, r, 4 * h + c), o + 8 * c);
+        tmem_store32(tmem_k + lanes + 32 * h, o);
+      }
+      tmem_wait_store();
+      tc_before_sync();
+      __syncwarp();
+      if (lane == 0) bar_arrive(empty + 8 * slot), bar_arrive(k_ready);
+    };
+    const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
+    int32_t key = first * kKeys + r;
+    float ks, vs;
+    scales_of(page_of(key), key, &ks, &vs);
+    int32_t page_next = page_of(key + kKeys);
+    put_keys(0);
+    uint64_t l2[kRows / 2];              // of this key's share of every row's sum
+#pragma unroll
+    for (int i = 0; i < kRows / 2; ++i) l2[i] = 0;
+    for (int j = 0; j < n; ++j, key += kKeys) {
+      const int32_t k0 = (first + j) * kKeys;
+      float ks_next, vs_next;
+      scales_of(page_next, key + kKeys, &ks_next, &vs_next);
+      page_next = page_of(key + 2 * kKeys);
+      bar_pass(s_full, j & 1, failed);
+      tc_after_sync();
+      if (j + 1 < n) put_keys(j + 1);
+      // S_j: x = s c + log2 v - m
+      const float vs_in = fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
+      const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f), lv = log2f(vs_in);
+      const uint32_t s_at = tmem_s + lanes + (j & 1) * kRows;
+      const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kKeys > all_see;
+      // rows that see this key: those of its token and later ones
+      uint64_t sees = ~0ull;
+      if (masked) {
+        const int64_t before = key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group;
+        sees = !in || before >= 64 ? 0 : ~0ull << before;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < n_c) {
+          uint32_t s[16];
+          tmem_load16(s_at + 16 * q, s);
+          float4 m[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) m[i] = reinterpret_cast<const float4*>(misc.neg_m)[4 * q + i];
+          tmem_wait_load();
+          tmem_loaded(s);
+          const float* mf = reinterpret_cast<const float*>(m);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float x = fmaf(__uint_as_float(s[i]), c, lv + mf[i]);
+            if (!masked || (sees >> (16 * q + i) & 1)) top = fmaxf(top, x);
+          }
+        }
+      if (__any_sync(0xffffffffu, top > 8.f) && lane == 0) misc.flag[j & 1] = j + 1;
+      bar_meet(met, &meetings, failed);
+      if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&misc.flag[j & 1]), 0) == j + 1u) {
+        // a reference is raised: the columns' maxima over the keys, in P's place
+        if (j > 0) {
+          bar_pass(o_done, (j - 1) & 1, failed);
+          tc_after_sync();
+        }
+        float* tops = reinterpret_cast<float*>(p_mem);   // [4][kRows], then the factors [kRows]
+#pragma unroll 1
+        for (int q = 0; q < n_c; ++q) {
+          uint32_t s[16];
+          tmem_load16(s_at + 16 * q, s);
+          tmem_wait_load();
+          tmem_loaded(s);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float x = fmaf(__uint_as_float(s[i]), c, lv);
+            if (!(x == x) || (masked && !(sees >> (16 * q + i) & 1))) x = -INFINITY;
+            const int32_t most = __reduce_max_sync(0xffffffffu, ordered(x));
+            if (lane == i) tops[warp * kRows + 16 * q + i] = __int_as_float(most ^ ((most >> 31) & 0x7fffffff));
+          }
+        }
+        bar_meet(met, &meetings, failed);
+        if (r < 16 * n_c) {
+          const float was = -misc.neg_m[r];
+          const float most = fmaxf(fmaxf(tops[r], tops[kRows + r]), fmaxf(tops[2 * kRows + r], tops[3 * kRows + r]));
+          const float now = most > was + 8.f ? most : was;
+          misc.neg_m[r] = -now;
+          tops[4 * kRows + r] = now == was ? 1.f : exp2f(was - now);
+        }
+        bar_meet(met, &meetings, failed);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < n_c) {
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(f + 4 * i) = reinterpret_cast<const float4*>(tops)[kRows + 4 * q + i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float x, y;
+              halves(l2[8 * q + i], &x, &y);
+              l2[8 * q + i] = two(x * f[2 * i], y * f[2 * i + 1]);
+            }
+            if (j > 0) {
+              uint32_t o[16];
+              tmem_load16(tmem + lanes + 16 * q, o);
+              tmem_wait_load();
+              tmem_loaded(o);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[i]);
+              tmem_store16(tmem + lanes + 16 * q, o);
+            }
+          }
+        tmem_wait_store();
+        bar_meet(met, &meetings, failed);
+      }
+      if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // P and V are read
+      const uint64_t c2 = two(c, c), lv2 = two(lv + kBias, lv + kBias), inv2 = two(1.f / vs_in, 1.f / vs_in);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < n_c) {
+          uint32_t s[16], p[8];
+          tmem_load16(s_at + 16 * q, s);
+          float4 m[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) m[i] = reinterpret_cast<const float4*>(misc.neg_m)[4 * q + i];
+          tmem_wait_load();
+          tmem_loaded(s);
+          const float* mf = reinterpret_cast<const float*>(m);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float x, y;
+            halves(fma2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, add2(two(mf[2 * i], mf[2 * i + 1]), lv2)),
+                   &x, &y);
+            if (masked) {
+              if (!(sees >> (16 * q + 2 * i) & 1)) x = -INFINITY;
+              if (!(sees >> (16 * q + 2 * i + 1) & 1)) y = -INFINITY;
+            }
+            x = exp2_fast(x), y = exp2_fast(y);
+            l2[8 * q + i] = fma2(two(x, y), inv2, l2[8 * q + i]);
+            p[i] = pack(__half(), x, y);
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4*>(p_mem + r * 128 + ((2 * q + i) ^ (r & 7)) * 16) =
+                uint4{p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]};
+        }
+      {
+        const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
+        bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
+#pragma unroll
+        for (int c16 = 0; c16 < DP / 16; ++c16) {
+          uint4 v = *codes_at<DP>(ring + slot * S::kSlot, r, c16);
+          if (masked) {
+            // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN
+            // that some row does not see; those that see it get theirs at the end.
+            if (!in) v = uint4{};
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) {
+                for (int b = 0; b < 4; ++b)
+                  if ((w[i] >> (8 * b) & 0x7f) == 0x7f) {
+                    atomicMin(&misc.first_nan[16 * c16 + 4 * i + b], key);
+                    w[i] &= ~(0xffu << (8 * b));
+                  }
+              }
+          }
+          uint32_t o[8];
+          wide16(v, o);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4*>(v_mem + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + i) % 8) ^ (r & 7)) * 16) =
+                uint4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+        }
+        fence_async();
+        tc_before_sync();
+        __syncwarp();
+        if (lane == 0) bar_arrive(empty + 8 * slot), bar_arrive(v_ready);
+      }
+      ks = ks_next, vs = vs_next;
+    }
+    bar_pass(o_done, (n - 1) & 1, failed);
+    tc_after_sync();
+    // the rows' sums over the keys, in P's place: [4][kRows], then 1 / sum
+    float* sums = reinterpret_cast<float*>(p_mem);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < n_c) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) halves(l2[8 * q + i], &x[2 * i], &x[2 * i + 1]);
+        // lane i ends with column i / 2: each step keeps half of the columns
+#pragma unroll
+        for (int d = 16, k = 8; k; d /= 2, k /= 2) {
+          const bool upper = lane & d;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < k) {
+              const float give = upper ? x[i] : x[i + k];
+              const float keep = upper ? x[i + k] : x[i];
+              x[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+            }
+        }
+        x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
+        if (!(lane & 1)) sums[warp * kRows + 16 * q + lane / 2] = x[0];
+      }
+    bar_meet(met, &meetings, failed);
+    if (r < rows) {
+      const float l = (sums[r] + sums[kRows + r]) + (sums[2 * kRows + r] + sums[3 * kRows + r]);
+      const float lse2 = l == 0.f ? -INFINITY : -misc.neg_m[r] - kBias + log2f(l);
+      sums[4 * kRows + r] = l == 0.f ? 0.f : 1.f / l;
+      if (it.part >= 0) {
+        a.part_lse[hk * a.part_rows + it.part + r] = lse2;
+      } else if (a.lse) {
+        const int32_t tok = r / a.group;
+        a.lse[(int64_t)(it.tok0 + tok) * a.n_heads + hk * a.group + r - tok * a.group] = lse2 * 0.69314718055994531f;
+      }
+    }
+    bar_meet(met, &meetings, failed);
+    const int32_t nan_at = misc.first_nan[r];
+    int32_t tok = 0, h = 0;
+#pragma unroll 1
+    for (int q = 0; q < n_c; ++q) {
+      uint32_t o[16];
+      tmem_load16(tmem + lanes + 16 * q, o);
+      tmem_wait_load();
+      tmem_loaded(o);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = 16 * q + i;
+        if (row < rows && r < a.dim) {
+          const float inv = sums[4 * kRows + row];
+          float v = inv == 0.f ? 0.f : __uint_as_float(o[i]) * inv;
+          if (nan_at <= it.pos0 + tok) v = NAN;
+          if (it.part >= 0) {
+            __stcg(a.part_o + (hk * a.part_rows + it.part + row) * a.dim + r, v);
+          } else {
+            T* out = static_cast<T*>(a.out) + (it.tok0 + tok) * a.o_tok + (hk * a.group + h) * a.o_head + r;
+            const uint32_t both = pack(T(), v, v);
+            *reinterpret_cast<unsigned short*>(out) = (unsigned short)both;
+          }
+        }
+        if (++h == a.group) h = 0, ++tok;
+      }
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  if (warp == 7) tmem_free<1>(tmem, S::kColumns);
+  if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
+}
+
+constexpr Cutting kCutting = {kKeys, kRows, 4, 8, 3, 5};
+
+template <class T, int DP>
+cudaError_t launch(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
+  static gsim::OncePerDevice once;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
+  auto kernel = attend8_kernel<T, DP>;
+  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP>::kSmem); })) return cudaErrorInvalidValue;
+  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(kv, g);
+  if (p.n_joins > 0) {
+    const int64_t heads = (int64_t)p.join_tokens * p.n_heads;
+    attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>(heads, 1024)), 128, 0, st>>>(g.a);
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace
+}  // namespace gop
+
+using namespace gop;
+
+extern "C" {
+
+int op_attend8_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,
+                    size_t item_bytes) try {
+  if (!desc_ok(d, kRows) || d->head_dim % 16 || d->page_tokens < 16 || !plan || n_sm < 1) return GMG_EINVAL;
+  Work w;
+  plan_items(*d, n_sm, kCutting, &w);
+  return fill_plan(d, w, &plan->p, items, item_bytes);
+} catch (const std::bad_alloc&) {
+  return GMG_ENOMEM;
+}
+
+int op_attend8(const op_attend8_plan_t* plan8, const int32_t* d_items, const op_cache_t* cache, int32_t layer,
+               int32_t dtype, const void* q, int64_t q_tok, int64_t q_head, float scale, void* out, int64_t out_tok,
+               int64_t out_head, float* lse, void* work, size_t work_bytes, gmg_stream_t stream) {
+  if (!plan8 || !cache8_ok(cache) || layer < 0 || layer >= cache->n_layers) return GMG_EINVAL;
+  const op_attend_plan_t* plan = &plan8->p;
+  if (plan->head_dim != cache->head_dim || plan->n_kv_heads != cache->n_kv_heads ||
+      plan->page_tokens != cache->page_tokens || plan->max_seq >= cache->n_seq ||
+      plan->max_kv > int64_t(cache->max_pages) * cache->page_tokens)
+    return GMG_EINVAL;
+  if (dtype != GMG_OP_BF16 && dtype != GMG_OP_F16) return GMG_EINVAL;
+  if (plan->n_tokens == 0) return GMG_OK;
+  if (!d_items || (reinterpret_cast<uintptr_t>(d_items) & 15) || !q || !out || !aligned(q, q_tok, q_head, 2) ||
+      !aligned(out, out_tok, out_head, 2) || !(scale == scale))
+    return GMG_EINVAL;
+  if (!work || (reinterpret_cast<uintptr_t>(work) & 255) || work_bytes < plan->work_bytes) return GMG_EWS;
+  const int64_t rows = int64_t(cache->n_layers) * 2 * cache->n_kv_heads * cache->page_tokens;   // of a page
+  if (rows > 0x7fffffff) return GMG_ERANGE;
+  Args8 g{};
+  AttendArgs& a = g.a;
+  a.items = reinterpret_cast<const Item*>(d_items);
+  a.joins = reinterpret_cast<const Join*>(a.items + plan->n_items);
+  a.table = cache->table;
+  a.status = cache->status;
+  a.max_pages = cache->max_pages;
+  a.page_tokens = cache->page_tokens;
+  a.n_pages = cache->n_pages;
+  a.plane = layer * 2;
+  a.n_heads = plan->n_heads;
+  a.n_kv = plan->n_kv_heads;
+  a.group = plan->n_heads / plan->n_kv_heads;
+  a.dim = plan->head_dim;
+  // a scale of 0 gives every key one weight, as a tiny one does, whose product with -inf is -inf
+  a.scale2 = fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-30f);
+  a.negative = scale < 0.f;
+  a.out = out, a.o_tok = out_tok, a.o_head = out_head;
+  a.lse = lse;
+  a.part_rows = plan->part_rows;
+  a.part_o = reinterpret_cast<float*>(work);
+  a.part_lse = a.part_o + plan->part_rows * plan->n_kv_heads * plan->head_dim;
+  g.q = q, g.q_tok = q_tok, g.q_head = q_head;
+  g.pool = static_cast<const unsigned char*>(cache->pool);
+  g.page_bytes = page8_bytes(*cache);
+  g.scale_at = page8_scales(*cache) + int64_t(layer) * 2 * cache->n_kv_heads * (cache->page_tokens / 16) * 4;
+  CUtensorMap map_kv;
+  const int64_t size[3] = {cache->head_dim, rows, cache->n_pages}, stride[2] = {cache->head_dim, g.page_bytes};
+  const int32_t dp = cache->head_dim <= 64 ? 64 : 128;
+  const int32_t box[3] = {dp, std::min(cache->page_tokens, kKeys), 1};
+  if (!make_map8(&map_kv, 3, cache->pool, size, stride, box)) return GMG_ECUDA;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (dtype == GMG_OP_BF16)
+    e = dp == 64 ? launch<__nv_bfloat16, 64>(*plan, map_kv, g, st) : launch<__nv_bfloat16, 128>(*plan, map_kv, g, st);
+  else
+    e = dp == 64 ? launch<__half, 64>(*plan, map_kv, g, st) : launch<__half, 128>(*plan, map_kv, g, st);
+  return e == cudaSuccess ? GMG_OK : GMG_ECUDA;
+}
+
+}  // extern "C"

@@ -77,7 +77,10 @@ size_t layout(const op_cache_t& c, char* base, Scratch* s) {
   return o;
 }
 
+bool any_cache_ok(const op_cache_t* c) { return cache_ok(c) || cache8_ok(c); }
+
 size_t page_bytes(const op_cache_t& c) {
+  if (c.dtype == GMG_OP_E4M3) return size_t(page8_bytes(c));
   return size_t(c.n_layers) * 2 * c.n_kv_heads * c.page_tokens * c.head_dim * 2;
 }
 
@@ -472,7 +475,7 @@ __global__ void __launch_bounds__(kThreads) compact_apply_kernel(op_cache_t c, s
 }
 
 int check(const op_cache_t* c, int32_t n, void* scratch, size_t scratch_bytes, Scratch* s) {
-  if (!cache_ok(c) || n < 0 || n > c->n_seq) return GMG_EINVAL;
+  if (!any_cache_ok(c) || n < 0 || n > c->n_seq) return GMG_EINVAL;
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_bytes < layout(*c, nullptr, nullptr))
     return GMG_EWS;
   layout(*c, static_cast<char*>(scratch), s);
@@ -492,7 +495,17 @@ using namespace gop;
 
 extern "C" {
 
-size_t op_page_scratch_bytes(const op_cache_t* cache) { return cache_ok(cache) ? layout(*cache, nullptr, nullptr) : 0; }
+size_t op_page8_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t page_tokens, int32_t head_dim) {
+  op_cache_t c{};
+  c.table = c.lens = c.refs = c.status = reinterpret_cast<int32_t*>(256);
+  c.pool = c.table;   // (the rest is not looked at)
+  c.dtype = GMG_OP_E4M3;
+  c.n_pages = c.n_seq = c.max_pages = 1;
+  c.n_layers = n_layers, c.n_kv_heads = n_kv_heads, c.page_tokens = page_tokens, c.head_dim = head_dim;
+  return cache8_ok(&c) ? size_t(page8_bytes(c)) : 0;
+}
+
+size_t op_page_scratch_bytes(const op_cache_t* cache) { return any_cache_ok(cache) ? layout(*cache, nullptr, nullptr) : 0; }
 
 int op_free(const op_cache_t* cache, const int32_t* seq, int32_t n, void* scratch, size_t scratch_bytes,
             gmg_stream_t stream) {

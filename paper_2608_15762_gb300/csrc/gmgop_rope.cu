@@ -19,12 +19,12 @@
 
 #include "../../include/gmgop.h"
 #include "gmgop_host.h"
+#include "gmgop_rope.cuh"
 
 namespace gop {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kMaxPairs = 128;   // rotary <= 256
 
 struct RopeArgs {
   const uint64_t* freq;
@@ -40,56 +40,6 @@ struct RopeArgs {
   int64_t page_stride, layer_at;  // elements: from page to page, of the layer's keys in a page
 };
 
-__device__ __forceinline__ float up(float v) { return v; }
-__device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float up(__half v) { return __half2float(v); }
-__device__ __forceinline__ void down(float v, float* o) { *o = v; }
-__device__ __forceinline__ void down(float v, __nv_bfloat16* o) { *o = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void down(float v, __half* o) { *o = __float2half_rn(v); }
-
-template <class T, int N>
-struct alignas(sizeof(T) * N) Vec {
-  T v[N];
-};
-
-// One head: N elements of type T a step, aligned to N elements.  Pairs of the half
-// layout take a step of the first half and one of the second, interleaved ones a step.
-template <class T, int N, bool kInter>
-__device__ __forceinline__ void turn_step(const T* x, T* y, int32_t step, int32_t half, const float2* cs) {
-  using V = Vec<T, N>;
-  if (kInter) {
-    if (N == 1) {   // unaligned: a pair a step
-      const float u = up(x[2 * step]), w = up(x[2 * step + 1]);
-      const float2 t = cs[step];
-      down(u * t.x - w * t.y, &y[2 * step]);
-      down(u * t.y + w * t.x, &y[2 * step + 1]);
-    } else {
-      const V a = *reinterpret_cast<const V*>(x + step * N);
-      V b;
-#pragma unroll
-      for (int j = 0; j < N / 2; ++j) {
-        const float u = up(a.v[2 * j]), w = up(a.v[2 * j + 1]);
-        const float2 t = cs[step * (N / 2) + j];
-        down(u * t.x - w * t.y, &b.v[2 * j]);
-        down(u * t.y + w * t.x, &b.v[2 * j + 1]);
-      }
-      *reinterpret_cast<V*>(y + step * N) = b;
-    }
-  } else {
-    const V a = *reinterpret_cast<const V*>(x + step * N), b = *reinterpret_cast<const V*>(x + half + step * N);
-    V c, d;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float u = up(a.v[j]), w = up(b.v[j]);
-      const float2 t = cs[step * N + j];
-      down(u * t.x - w * t.y, &c.v[j]);
-      down(u * t.y + w * t.x, &d.v[j]);
-    }
-    *reinterpret_cast<V*>(y + step * N) = c;
-    *reinterpret_cast<V*>(y + half + step * N) = d;
-  }
-}
-
 template <class T, int N, bool kInter, bool kAppend>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
   using V = Vec<T, N>;
@@ -97,12 +47,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
   const int64_t t = blockIdx.x;
   const int32_t pos = a.pos[t];
   for (int32_t i = threadIdx.x; i < a.half; i += kThreads) {
-    const uint64_t turn = a.freq[i] * (uint64_t)(int64_t)pos;
-    // the top 32 bits, signed: half turns in [-1, 1)
-    const float x = (float)(int32_t)(turn >> 32) * 4.656612873077393e-10f;   // 2^-31
-    float s, c;
-    sincospif(x, &s, &c);
-    cs[i] = make_float2(c * a.factor, s * a.factor * a.sign);
+    cs[i] = turn_of(a.freq[i], pos, a.factor, a.factor * a.sign);
   }
   T *key = nullptr, *value = nullptr;   // this token's slot of head 0 in the cache
   if (kAppend) {

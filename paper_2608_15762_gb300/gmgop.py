@@ -1,8 +1,10 @@
 """Thin Python binding of the decoder-layer operators in ``include/gmgop.h``.
 
 The operators are what an executor runs of a placed graph: products with their
-epilogue (``linear``), rotary positions (``rope``, ``rope_append``), a paged cache
-(``PageCache``) and attention over shared prefixes (``AttendPlan``, ``attend``).
+epilogue (``linear``), the norms around a block (``norm``), rotary positions (``rope``,
+``rope_append``), a paged cache (``PageCache``) and attention over shared prefixes (``AttendPlan``,
+``attend``), the last three also for a cache in 8 bits (``rope_append8``, ``PageCache8``, ``AttendPlan8``,
+``attend8``).
 Argument marshalling only; PyTorch provides device memory and streams.  Calls
 are asynchronous on the current stream, or on ``stream``, where their results'
 memory then belongs (and which the memory of their inputs, plans and caches has to
@@ -24,9 +26,10 @@ from . import gmgsim as G
 from .gmgsim import GmgError, _aligned_empty, _check
 
 EXPORTED = ("op_page_scratch_bytes", "op_free", "op_fork", "op_grow", "op_compact", "op_rope", "op_rope_append",
-            "op_attend_plan", "op_attend", "op_linear_work_bytes", "op_linear")
+            "op_attend_plan", "op_attend", "op_linear_work_bytes", "op_linear", "op_page8_bytes", "op_rope_append8",
+            "op_attend8_plan", "op_attend8", "op_norm")
 
-F32, BF16, F16 = 0, 1, 2
+F32, BF16, F16, E4M3 = 0, 1, 2, 3
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 PAGE_OK, PAGE_FULL, PAGE_SEQ, PAGE_TWICE, PAGE_LONG, PAGE_USED = range(6)
 
@@ -60,9 +63,19 @@ class _Linear(C.Structure):
         (n, C.c_int64) for n in ("x_row", "w_row", "gate_row", "residual_row", "y_row")]
 
 
+class _Norm(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "stream_dtype", "kind", "after")] + [
+        (n, C.c_int64) for n in ("m", "n")] + [
+        (n, C.c_void_p) for n in ("x", "y", "gate", "y_weight", "y_bias", "weight", "bias", "r", "h")] + [
+        (n, C.c_int64) for n in ("x_row", "y_row", "gate_row", "gate_col", "r_row", "h_row")] + [
+        (n, C.c_float) for n in ("scale", "eps", "shift")] + [("reserved", C.c_int32)]
+
+
 # _Linear's bytes: packing them is quicker than filling a ctypes structure.
 _LINEAR = struct.Struct("@4i3q7P5q")
 assert _LINEAR.size == C.sizeof(_Linear)
+_NORM = struct.Struct("@4i2q9P6q3fi")
+assert _NORM.size == C.sizeof(_Norm)
 _LIB = None
 
 
@@ -83,6 +96,11 @@ def lib():
             "op_attend": ([vp, vp, vp, i32, vp, i64, i64, f32, vp, i64, i64, vp, vp, sz, vp], C.c_int),
             "op_linear_work_bytes": ([vp], sz),
             "op_linear": ([vp, vp, sz, vp], C.c_int),
+            "op_page8_bytes": ([i32] * 4, sz),
+            "op_rope_append8": ([vp, vp, i32, i32, i64, i32] + [vp, i64, i64] * 3 + [vp, vp, vp, i64, i64, vp], C.c_int),
+            "op_attend8_plan": ([vp, i32, vp, vp, sz], C.c_int),
+            "op_attend8": ([vp, vp, vp, i32, i32, vp, i64, i64, f32, vp, i64, i64, vp, vp, sz, vp], C.c_int),
+            "op_norm": ([vp, vp], C.c_int),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -165,6 +183,10 @@ class PageCache:
     def __init__(self, pool, n_seq: int = 0, max_pages: int = 0, table=None, lens=None, refs=None):
         _need(pool.is_cuda and pool.dim() == 6 and pool.shape[2] == 2 and pool.is_contiguous(),
               "pool: contiguous, [n_pages, n_layers, 2, n_kv_heads, page_tokens, head_dim], on a GPU")
+        p = pool.shape
+        self._set_up(pool, _dtype(pool), p[1], p[3], p[4], p[5], n_seq, max_pages, table, lens, refs)
+
+    def _set_up(self, pool, kind, n_layers, n_kv_heads, page_tokens, head_dim, n_seq, max_pages, table, lens, refs):
         dev, i32 = pool.device, torch.int32
         if table is None:
             table = torch.full((n_seq, max_pages), -1, dtype=i32, device=dev)
@@ -180,11 +202,10 @@ class PageCache:
         _need(lens.numel() == n_seq and refs.numel() == pool.shape[0], "lens, refs: one entry a row, one a page")
         self.pool, self.table, self.lens, self.refs = pool, table, lens, refs
         self.status = torch.zeros(8, dtype=i32, device=dev)
-        p = pool.shape
-        self.n_layers, self.n_kv_heads, self.page_tokens, self.head_dim = p[1], p[3], p[4], p[5]
+        self.n_layers, self.n_kv_heads, self.page_tokens, self.head_dim = n_layers, n_kv_heads, page_tokens, head_dim
         self.device, self.dtype, self._index = dev, pool.dtype, pool.get_device()
         self.c = _Cache(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(), self.status.data_ptr(),
-                        _dtype(pool), p[0], p[1], p[3], p[4], p[5], n_seq, max_pages)
+                        kind, pool.shape[0], n_layers, n_kv_heads, page_tokens, head_dim, n_seq, max_pages)
         self.ref = C.addressof(self.c)
         nbytes = (_LIB or lib()).op_page_scratch_bytes(self.ref)
         if nbytes == 0:
@@ -233,6 +254,31 @@ class PageCache:
         rc = (_LIB or lib()).op_compact(self.ref, *self._work, _handle(stream, self._index))
         if rc:
             _fail(rc, "op_compact")
+
+
+def page8_bytes(n_layers: int, n_kv_heads: int, page_tokens: int, head_dim: int) -> int:
+    """Bytes of a page of a ``PageCache8``."""
+    n = (_LIB or lib()).op_page8_bytes(n_layers, n_kv_heads, page_tokens, head_dim)
+    _need(n > 0, "a page of 16 to 256 tokens (a power of two), heads of 16 to 128 elements (a multiple of 16)")
+    return n
+
+
+class PageCache8(PageCache):
+    """A paged cache in 8 bits: pool uint8 [n_pages, page8_bytes(...)], each page ``codes``
+    [n_layers, 2, n_kv_heads, page_tokens, head_dim], e4m3, and then ``scales`` [n_layers, 2,
+    n_kv_heads, page_tokens / 16], fp32, one for 16 tokens of a head: a value is its code times its scale.
+    Both are views of the pool, over all pages.  The rest, and the page calls, are ``PageCache``'s."""
+
+    def __init__(self, pool, n_layers: int, n_kv_heads: int, page_tokens: int, head_dim: int, n_seq: int = 0,
+                 max_pages: int = 0, table=None, lens=None, refs=None):
+        nbytes = page8_bytes(n_layers, n_kv_heads, page_tokens, head_dim)
+        _need(pool.is_cuda and pool.dtype is torch.uint8 and pool.dim() == 2 and pool.shape[1] == nbytes and
+              pool.is_contiguous(), "pool: contiguous uint8, [n_pages, %d], on a GPU" % nbytes)
+        self._set_up(pool, E4M3, n_layers, n_kv_heads, page_tokens, head_dim, n_seq, max_pages, table, lens, refs)
+        planes = n_layers * 2 * n_kv_heads
+        n, m = planes * page_tokens * head_dim, planes * (page_tokens // 16) * 4
+        self.codes = pool[:, :n].view(torch.float8_e4m3fn).unflatten(1, (n_layers, 2, n_kv_heads, page_tokens, head_dim))
+        self.scales = pool[:, n:n + m].view(torch.float32).unflatten(1, (n_layers, 2, n_kv_heads, page_tokens // 16))
 
 
 # ---------------------------------------------------------------------------
@@ -366,6 +412,33 @@ def rope_append(plan: Rope, q, k, v, pos, seq, cache: PageCache, layer: int, out
     return out
 
 
+@_traced("op_rope_append8")
+def rope_append8(plan: Rope, q, k, v, pos, seq, cache: PageCache8, layer: int, out=None, stream=None):
+    """``rope_append`` into a cache in 8 bits, from q, k and v in bf16 or fp16.  A block of 16 tokens gets the
+    least power of two as its scale with which its largest value is at most 448; what it held before its first
+    token of this call is rounded again where the scale grows.  Tokens of one row that lie in one block follow
+    one another in the lists, in increasing order and (padding between them included) within 32 entries."""
+    T, H, D = q.shape
+    kv, dt, dev, kind = (T, cache.n_kv_heads, D), q.dtype, cache.device, _TYPES.get(q.dtype)
+    if cache.dtype is not torch.uint8:
+        raise ValueError("cache: in 8 bits")
+    if D != cache.head_dim or k.shape != kv or v.shape != kv:
+        raise ValueError("q [tokens, heads, head_dim], k and v [tokens, n_kv_heads, head_dim]")
+    if not kind or k.dtype is not dt or v.dtype is not dt or q.device != dev or k.device != dev or v.device != dev:
+        raise ValueError("q, k, v: of one type, bf16 or fp16, on the cache's GPU")
+    if plan.index != cache._index:
+        raise ValueError("plan: on the cache's GPU")
+    if _list(pos, dev, "pos") != T or _list(seq, dev, "seq") != T:
+        raise ValueError("pos, seq: one entry a token")
+    out = _like(q, out, stream)
+    rc = (_LIB or lib()).op_rope_append8(plan.ref, cache.ref, layer, kind, T, H, *_heads(q, "q"), *_heads(k, "k"),
+                                         *_heads(v, "v"), pos.data_ptr(), seq.data_ptr(), *_heads(out, "out"),
+                                         _handle(stream, cache._index))
+    if rc:
+        _fail(rc, "op_rope_append8")
+    return out
+
+
 # ---------------------------------------------------------------------------
 # Attention
 # ---------------------------------------------------------------------------
@@ -380,8 +453,9 @@ def _n_sm(device) -> int:
 
 
 def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=None, group_off=None, prefix=None,
-                 n_sm: int = 152):
-    """(plan, its int32 array on the host): the work of ``attend`` for these lengths."""
+                 n_sm: int = 152, bits: int = 16):
+    """(plan, its int32 array on the host): the work of ``attend`` (bits 8: ``attend8``) for these lengths."""
+    name = "op_attend_plan" if bits == 16 else "op_attend8_plan"
     arr = [None if a is None else np.ascontiguousarray(a, np.int32) for a in (q_len, kv_len, seq, group_off, prefix)]
     q, kv, sq, off, pre = arr
     _need(q.ndim == 1 and kv.shape == q.shape and (sq is None or sq.shape == q.shape),
@@ -392,13 +466,13 @@ def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=
     d = _AttendDesc(q.size, n_heads, n_kv_heads, head_dim, page_tokens, 0 if pre is None else pre.size, *ptr)
     plan = _AttendPlan()
     items = np.empty(1 << 14, np.int32)      # most plans are shorter; longer ones are made again
-    call = (_LIB or lib()).op_attend_plan
+    call = getattr(_LIB or lib(), name)
     rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
     if rc == G.GMG_EWS:
-        _check(call(C.addressof(d), n_sm, C.addressof(plan), None, 0), "op_attend_plan")
+        _check(call(C.addressof(d), n_sm, C.addressof(plan), None, 0), name)
         items = np.empty(plan.plan_bytes // 4, np.int32)
         rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
-    _check(rc, "op_attend_plan")
+    _check(rc, name)
     return plan, items[:plan.plan_bytes // 4].copy()
 
 
@@ -409,12 +483,14 @@ class AttendPlan:
     ...).  group_off, prefix: requests group_off[g] .. group_off[g + 1] share their
     first prefix[g] tokens."""
 
+    bits = 16
+
     def __init__(self, q_len: Sequence[int], kv_len: Sequence[int], n_heads: int, n_kv_heads: int, head_dim: int,
                  page_tokens: int, seq: Optional[Sequence[int]] = None, group_off: Optional[Sequence[int]] = None,
                  prefix: Optional[Sequence[int]] = None, device="cuda", stream=None):
         dev = torch.device(device)
         self.c, items = attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq, group_off, prefix,
-                                     _n_sm(dev))
+                                     _n_sm(dev), self.bits)
         self.ref = C.addressof(self.c)
         self.n_tokens, self.n_heads, self.head_dim = int(self.c.n_tokens), n_heads, head_dim
         self.shape = (self.n_tokens, n_heads, head_dim)
@@ -433,6 +509,12 @@ class AttendPlan:
         return self.work[handle]
 
 
+class AttendPlan8(AttendPlan):
+    """An ``AttendPlan`` for ``attend8``: at most 64 query heads for each key/value head."""
+
+    bits = 8
+
+
 @_traced("op_attend")
 def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[float] = None, out=None, lse=False,
            stream=None):
@@ -440,6 +522,26 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
     after another) over the cache; with ``lse`` also log sum exp [tokens, heads], fp32."""
     if q.shape != plan.shape or q.dtype is not cache.dtype or q.device != cache.device:
         raise ValueError("q: [tokens, heads, head_dim] of the plan, the cache's type, on its GPU")
+    if plan.bits != 16:
+        raise ValueError("plan: an AttendPlan")
+    return _attend((_LIB or lib()).op_attend, (), plan, q, cache, layer, scale, out, lse, stream)
+
+
+@_traced("op_attend8")
+def attend8(plan: AttendPlan8, q, cache: PageCache8, layer: int, scale: Optional[float] = None, out=None, lse=False,
+            stream=None):
+    """``attend`` over a cache in 8 bits, for q in bf16 or fp16 (the result's type)."""
+    kind = _TYPES.get(q.dtype)
+    if cache.dtype is not torch.uint8:
+        raise ValueError("cache: in 8 bits")
+    if q.shape != plan.shape or not kind or q.device != cache.device:
+        raise ValueError("q: [tokens, heads, head_dim] of the plan, bf16 or fp16, on the cache's GPU")
+    if plan.bits != 8:
+        raise ValueError("plan: an AttendPlan8")
+    return _attend((_LIB or lib()).op_attend8, (kind,), plan, q, cache, layer, scale, out, lse, stream)
+
+
+def _attend(call, kind, plan, q, cache, layer, scale, out, lse, stream):
     if plan.index != cache._index:
         raise ValueError("plan: on the cache's GPU")
     h = _handle(stream, cache._index)
@@ -461,11 +563,11 @@ def attend(plan: AttendPlan, q, cache: PageCache, layer: int, scale: Optional[fl
                 work = own.data_ptr()
             elif work is None:
                 work = plan.new_work(h)
-    rc = (_LIB or lib()).op_attend(plan.ref, plan._ptr, cache.ref, layer, *_heads(q, "q"),
-                                   plan.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
-                                   None if z is None else z.data_ptr(), work, plan.work_bytes, h)
+    rc = call(plan.ref, plan._ptr, cache.ref, layer, *kind, *_heads(q, "q"),
+              plan.head_dim ** -0.5 if scale is None else scale, *_heads(out, "out"),
+              None if z is None else z.data_ptr(), work, plan.work_bytes, h)
     if rc:
-        _fail(rc, "op_attend")
+        _fail(rc, call.__name__)
     return (out, z) if lse else out
 
 
@@ -587,3 +689,79 @@ def linear(x, w, bias=None, act: str = "none", gate=None, gate_bias=None, residu
     if rc:
         _fail(rc, "op_linear")
     return out
+
+
+# ---------------------------------------------------------------------------
+# Norms
+# ---------------------------------------------------------------------------
+
+NORMS = {"rms": 0, "layer": 1}
+
+
+def _matrix(t, m, n, dt, dev, what: str):
+    """(pointer, stride of a row) of a matrix [m, n] of type dt."""
+    if t.shape != (m, n) or t.dtype is not dt or t.device != dev:
+        raise ValueError("%s: [%d, %d], %s, on x's GPU" % (what, m, n, dt))
+    s = t.stride()
+    if s[1] != 1 and n > 1:
+        raise ValueError("%s: rows contiguous" % what)
+    return t.data_ptr(), s[0] if m > 1 or s[0] > n else n
+
+
+def _gate(t, m, n, dt, dev):
+    """(pointer, stride of a row, of a column) of a gate [n], [m, 1] or [m, n]."""
+    if t.dtype is not dt or t.device != dev:
+        raise ValueError("gate: %s, on x's GPU" % dt)
+    if t.shape == (n,) and t.is_contiguous():
+        return t.data_ptr(), 0, 1
+    if t.shape == (m, 1) and t.stride(0) >= 1:
+        return t.data_ptr(), t.stride(0), 0
+    if t.shape == (m, n):
+        return (*_matrix(t, m, n, dt, dev, "gate"), 1)
+    raise ValueError("gate: [%d], [%d, 1] or [%d, %d]" % (n, m, m, n))
+
+
+@_traced("op_norm")
+def norm(x, w=None, bias=None, kind: str = "rms", eps: float = 1e-6, shift: float = 0.0, y=None, after: bool = False,
+         y_w=None, y_bias=None, gate=None, scale: float = 1.0, out=None, x_out=None, only_x: bool = False, stream=None):
+    """The norms around a block, kind rms or layer: N(v; w, b) = (v - mean) / sqrt(mean((v - mean)^2) + eps)
+    * (w + shift) + b, mean 0 for rms.
+
+    Without y: N(x; w, bias), of x's type or, where x is fp32, w's.  With the block's result y [m, n], whose
+    type the weights, the gate and the first result have (x may be fp32): (N(r; w, bias), r) for
+    r = x + scale * gate * z, z = N(y; y_w, y_bias) if ``after``, else y; ``only_x``: r alone.
+    gate: [n], [m, 1] or [m, n].  out and x_out take the results; x_out may be x, and either may be y."""
+    m, n = x.shape
+    dev, index, how = x.device, x.get_device(), NORMS.get(kind)
+    dt = y.dtype if y is not None else w.dtype if w is not None else bias.dtype if bias is not None else (
+        out.dtype if out is not None else x.dtype)
+    code, wide = _TYPES.get(dt), _TYPES.get(x.dtype)
+    if code is None or (wide != code and wide != F32) or how is None or index < 0:
+        raise ValueError("x: fp32 or the others' type (fp32, bf16 or fp16), on a GPU; kind: one of %s" % ", ".join(NORMS))
+    if y is None and (after or gate is not None or x_out is not None or only_x or y_w is not None or y_bias is not None):
+        raise ValueError("after, gate, x_out, only_x, y_w, y_bias: with y")
+    if only_x and (w is not None or bias is not None or out is not None):
+        raise ValueError("only_x: without w, bias and out")
+    if not after and (y_w is not None or y_bias is not None):
+        raise ValueError("y_w, y_bias: with after")
+    if stream is None:
+        h = torch.empty((m, n), dtype=dt, device=dev) if out is None and not only_x else out
+        r = torch.empty((m, n), dtype=x.dtype, device=dev) if y is not None and x_out is None else x_out
+    else:
+        with torch.cuda.stream(stream):
+            h = torch.empty((m, n), dtype=dt, device=dev) if out is None and not only_x else out
+            r = torch.empty((m, n), dtype=x.dtype, device=dev) if y is not None and x_out is None else x_out
+    xp, xs = _matrix(x, m, n, x.dtype, dev, "x")
+    yp, ys = (0, 0) if y is None else _matrix(y, m, n, dt, dev, "y")
+    gp, gr, gc = (0, 0, 0) if gate is None else _gate(gate, m, n, dt, dev)
+    hp, hs = (0, 0) if h is None else _matrix(h, m, n, dt, dev, "out")
+    rp, rs = (0, 0) if r is None else _matrix(r, m, n, x.dtype, dev, "x_out")
+    a = _NORM.pack(code, wide, how, 1 if after else 0, m, n, xp, yp, gp,
+                   0 if y_w is None else _column(y_w, n, dt, dev, "y_w"),
+                   0 if y_bias is None else _column(y_bias, n, dt, dev, "y_bias"),
+                   0 if w is None else _column(w, n, dt, dev, "w"), 0 if bias is None else _column(bias, n, dt, dev, "bias"),
+                   rp, hp, xs, ys, gr, gc, rs, hs, scale, eps, shift, 0)
+    rc = (_LIB or lib()).op_norm(a, _handle(stream, index))
+    if rc:
+        _fail(rc, "op_norm")
+    return h if y is None else r if only_x else (h, r)
