@@ -207,6 +207,7 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
  * scales) rounded to fp16 for theirs. */
 typedef struct {
   op_attend_plan_t p;
+  int32_t most_rows, reserved;  /* query heads times queries of the largest item, of a key/value head */
 } op_attend8_plan_t;
 
 int op_attend8_plan(const op_attend_desc_t* desc, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,

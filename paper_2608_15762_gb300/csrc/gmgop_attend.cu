@@ -454,7 +454,7 @@ constexpr int64_t kAloneSteps = 12;
 constexpr int64_t kItemSteps = 4;  // what an item costs beyond its steps (0: 96 requests behind 32,768 tokens 81 us, 4: 73)
 constexpr int64_t kJoinSteps = 8;  // what writing and joining a tile's partial results costs, in steps
 
-constexpr Cutting kCutting = {kKeys, kRows, kMinSteps, kAloneSteps, kItemSteps, kJoinSteps};
+constexpr Cutting kCutting = {kKeys, kRows, kMinSteps, kAloneSteps, kItemSteps, kJoinSteps, false};
 
 template <class T, int DP>
 cudaError_t launch(const op_attend_plan_t& p, const CUtensorMap& q, const CUtensorMap& kv, const AttendArgs& a, cudaStream_t st) {

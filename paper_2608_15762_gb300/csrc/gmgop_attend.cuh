@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <functional>
 #include <vector>
 
 #include "../../include/gmgop.h"
@@ -208,7 +209,39 @@ struct Cutting {
   int64_t alone_steps;   // up to so many a block takes alone, where one round of blocks is enough
   int64_t item_steps;    // what an item costs beyond its steps
   int64_t join_steps;    // what writing and joining a tile's partial results costs
+  bool balanced;         // cut so that the blocks' rounds come out even, not only into as many items as blocks run at once
 };
+
+// Of some lengths up to `most`, the one with which blocks that start one after another, the longest first, on
+// `slots` places end first.
+template <class F>
+int64_t even_cut(const std::vector<Run>& runs, const F& steps_of, int32_t heads, int32_t slots, int64_t most, const Cutting& cut) {
+  int64_t best = most, best_end = -1;
+  std::vector<int64_t> sizes, places;
+  for (int64_t k = 1; k <= 6; ++k) {
+    const int64_t most_k = std::max(cut.min_steps, (most + k - 1) / k);
+    sizes.clear();
+    bool joins = false;
+    for (const Run& r : runs) {
+      const int64_t n = steps_of(r), parts = std::max<int64_t>(1, (n + most_k - 1) / most_k);
+      joins |= parts > 1 || r.pooled;
+      for (int64_t p = 0; p < parts; ++p) sizes.push_back(n * (p + 1) / parts - n * p / parts + cut.item_steps);
+    }
+    if ((int64_t)sizes.size() * heads > 40 * slots) break;       // (so many come out even by themselves)
+    std::sort(sizes.begin(), sizes.end(), std::greater<int64_t>());
+    places.assign(slots, 0);                                     // when they are free, as a heap
+    for (const int64_t n : sizes)
+      for (int32_t h = 0; h < heads; ++h) {
+        std::pop_heap(places.begin(), places.end(), std::greater<int64_t>());
+        places.back() += n;
+        std::push_heap(places.begin(), places.end(), std::greater<int64_t>());
+      }
+    const int64_t end = *std::max_element(places.begin(), places.end()) + (joins ? cut.join_steps : 0);
+    if (best_end < 0 || end < best_end) best = most_k, best_end = end;
+    if (most_k == cut.min_steps) break;
+  }
+  return best;
+}
 
 inline void plan_items(const op_attend_desc_t& d, int32_t n_sm, const Cutting& cut, Work* w) {
   const int32_t keys = cut.keys, group = d.n_heads / d.n_kv_heads, tile = cut.rows / group;
@@ -253,7 +286,8 @@ inline void plan_items(const op_attend_desc_t& d, int32_t n_sm, const Cutting& c
   }
   int64_t steps = 0;
   for (const Run& r : runs) steps += steps_of(r) + cut.item_steps;
-  const int64_t most = std::max(small ? cut.alone_steps : cut.min_steps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
+  int64_t most = std::max(small ? cut.alone_steps : cut.min_steps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
+  if (cut.balanced && !small) most = even_cut(runs, steps_of, d.n_kv_heads, 2 * n_sm, most, cut);
   // cut; then longest first, so that short items fill the end (equal ones keep their order:
   // tiles that read the same keys stay together)
   struct Cut {

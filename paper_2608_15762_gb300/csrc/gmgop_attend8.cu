@@ -11,14 +11,15 @@
 // memory.  Q (times a power of two that brings the tile's largest to 2^13, so that bf16's 8 bits
 // lie in fp16's range) and P are fp16 too.
 // One block takes one item:
-//   warps 4 to 6   copies: page by page into a ring of 128-key slots, K_0 K_1 V_0 K_2 V_1 ...
-//   warp 7         products
-//   warps 0 to 3   K_{j+1} to fp16, the softmax of S_j, V_j to fp16
+//   warps 0 to 3    the softmax of S_j; in tiles of 64 rows of half of them, and K_{j+1} to fp16
+//   warps 4 to 7    V_j to fp16, and K_{j+2}; in tiles of 64 rows the softmax of the others instead
+//   warps 8 to 10   copies: page by page into a ring of 128-key slots, K_0 K_1 V_0 K_2 V_1 ...
+//   warp 11         products
 // With value scales v_j, P holds w = exp2(s + log2 v - m) and the sum takes w / v: one exponent
 // for both, so that P uses fp16's range whatever the scales, and O has them right.  The reference
 // m is of the w and need not be the exact running maximum: it is raised where a w would exceed
-// 2^8 times it (times 2^7 for fp16's small numbers).
-// P is rounded to fp16 because the tensor cores take it so (the sum is of the unrounded): 2^-12.
+// 2^11 times it (times 2^4 for fp16's small numbers).
+// P is rounded to fp16 because the tensor cores take it so (the sum is of the unrounded): 2^-11.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -40,9 +41,9 @@ namespace gop {
 namespace {
 
 constexpr int kKeys = 128;             // a step
-constexpr int kRows = 64;              // of a tile
-constexpr int kThreads = 256, kCopiers = 3;
-constexpr float kBias = 7.f;           // p is at most 2^(8 + kBias)
+constexpr int kFew = 32, kMany = 64;   // rows of a tile: what a kernel has room for
+constexpr int kThreads = 384, kCopiers = 3;
+constexpr float kBias = 4.f, kMost = 11.f;   // a weight is at most 2^(kMost + kBias)
 constexpr float kNone = -1e30f;        // the reference of a row that has seen nothing
 constexpr uint32_t kTurnedA = 1u << 15;   // A lies with its rows (M) contiguous
 
@@ -54,27 +55,31 @@ struct Args8 {
   int64_t page_bytes, scale_at;        // of a page; of the layer's scales in it
 };
 
-template <int DP>
+template <int DP, int kRows>
 struct Shape {
   static constexpr int kHalves = DP / 64;
   static constexpr int kQ = kHalves * kRows * 128;
-  static constexpr int kP = kKeys * 128;
+  static constexpr int kP = kKeys * kRows * 2;
   static constexpr int kV = kHalves * kKeys * 128;
   static constexpr int kSlot = kKeys * DP;
-  static constexpr int kSlots = 49152 / kSlot;
+  static constexpr int kSlots = (kRows == kFew ? 65536 : 49152) / kSlot;
   static constexpr int kMiscAt = kQ + kP + kV + kSlots * kSlot;
   static constexpr int kSmem = kMiscAt + 1024;
-  static constexpr int kColumns = 256;   // of TMEM: O^T 64, S^T twice 64, K 64 (fp16, two a column)
+  // TMEM: O^T, S^T twice, then K (fp16, two a column) once or, for few rows, twice
+  static constexpr int kColumns = 256, kS = kRows, kK = 3 * kRows, kKeep = kRows == kFew ? 2 : 1;
+  static_assert(kSmem <= 115712 && kK + kKeep * 64 <= kColumns, "two blocks an SM");
 };
 
-template <int DP>
+template <int DP, int kRows>
 struct Misc {
   float neg_m[kRows];                  // minus the rows' references
-  int32_t first_nan[128];              // by dimension: the first key whose value is NaN where rows see different keys
-  uint64_t bars[2 * Shape<DP>::kSlots + 5];
-  uint32_t tmem_at, failed, flag[2];   // flag: the step (+ 1) that raises a reference
+  int32_t top[kRows];                  // their largest weights where they are raised, as ordered integers
+  uint32_t first_nan[32];              // by dimension, a byte: the first query that sees a NaN where rows see different keys
+  uint64_t bars[2 * Shape<DP, kRows>::kSlots + 10];
+  uint32_t tmem_at, failed, flag[4];   // flag: the step (+ 1) that raises a reference, by half of the rows and step parity
 };
-static_assert(sizeof(Misc<128>) <= 1024 && sizeof(Misc<64>) <= 1024, "fits behind the ring");
+static_assert(sizeof(Misc<128, kMany>) <= 1024 && sizeof(Misc<64, kMany>) <= 1024 && sizeof(Misc<64, kFew>) <= 1024,
+              "fits behind the ring");
 
 // Two e4m3 to two fp16, exactly.
 __device__ __forceinline__ uint32_t wide2(uint16_t v) {
@@ -89,6 +94,11 @@ __device__ __forceinline__ void wide16(uint4 v, uint32_t* o) {
     o[2 * i] = wide2((uint16_t)w[i]);
     o[2 * i + 1] = wide2((uint16_t)(w[i] >> 16));
   }
+}
+
+// As tile_n, of 32 rows (N) in 64 bytes and the 64-byte swizzle; the next 8 columns 512 on.
+__device__ __forceinline__ uint64_t tile_n64(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
 }
 
 // 16 codes of a row of a slot, where the copy has put them.
@@ -106,11 +116,25 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* v) {
       : "memory");
 }
 
-// Order of floats as that of int32.
+__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(addr));
+}
+
+// Order of floats as that of int32, and back.
 __device__ __forceinline__ int32_t ordered(float v) {
   const int32_t i = __float_as_int(v);
   return i ^ ((i >> 31) & 0x7fffffff);
 }
+__device__ __forceinline__ float from_ordered(int32_t i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+constexpr int32_t kLeast = INT32_MIN;
+
+// Registers of a warp group's threads: what the copies and products leave, the softmax has.
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // Two numbers of a row of Q times `by`, as fp16.
 __device__ __forceinline__ uint32_t to_q(__nv_bfloat16, uint32_t v, float by) {
@@ -118,14 +142,16 @@ __device__ __forceinline__ uint32_t to_q(__nv_bfloat16, uint32_t v, float by) {
 }
 __device__ __forceinline__ uint32_t to_q(__half, uint32_t v, float by) { return by < 0.f ? v ^ 0x80008000u : v; }
 
-template <class T, int DP>
+template <class T, int DP, int kRows>
 __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_constant__ CUtensorMap map_kv,
                                                               const __grid_constant__ Args8 g) {
-  using S = Shape<DP>;
+  using S = Shape<DP, kRows>;
+  constexpr bool kHalved = kRows == kMany;   // the softmax of a tile's halves by different warps
   extern __shared__ __align__(1024) unsigned char base[];
   const AttendArgs& a = g.a;
   unsigned char *const p_mem = base + S::kQ, *const v_mem = p_mem + S::kP, *const ring = v_mem + S::kV;
-  Misc<DP>& misc = *reinterpret_cast<Misc<DP>*>(base + S::kMiscAt);
+  using M = Misc<DP, kRows>;
+  M& misc = *reinterpret_cast<M*>(base + S::kMiscAt);
   volatile uint32_t* failed = &misc.failed;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   // all heads of an item, then the next item: the long ones start first
@@ -146,119 +172,143 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
   }
 
   const int n_c = (rows + 15) / 16;     // columns, 16 at a time
-  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, k_ready = empty + 8 * S::kSlots,
-                 s_full = k_ready + 8, v_ready = s_full + 8, o_done = v_ready + 8, met = o_done + 8;
-  // Each of these barriers' phases is awaited by all that arrive at the next one before they do, so
-  // a wait's parity tells its phase from the one before it, which is over.
-  if (warp == 4 && lane == 0) {
+  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, q_ready = empty + 8 * S::kSlots,
+                 k_ready = q_ready + 8, s_full = k_ready + 16, v_ready = s_full + 16, o_done = v_ready + 8,
+                 met = o_done + 8, all_met = met + 16;
+  // k_ready and s_full are two barriers each, for even and odd steps, as K_{j+1} and S_{j+1} may come before
+  // all have waited for those of step j.  What arrives at a barrier's phase after next needs that all have
+  // waited for this one, so a wait tells its phase from the one before it.
+  if (warp == 8 && lane == 0) {
     prefetch_map(&map_kv);
     for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 4);
-    bar_init(k_ready, 4), bar_init(s_full, 1), bar_init(v_ready, 4), bar_init(o_done, 1), bar_init(met, 4);
-    misc.failed = misc.flag[0] = misc.flag[1] = 0;
+    bar_init(q_ready, 8), bar_init(k_ready, 4), bar_init(k_ready + 8, 4), bar_init(s_full, 1), bar_init(s_full + 8, 1), bar_init(v_ready, 8);
+    bar_init(o_done, 1), bar_init(met, 4), bar_init(met + 8, 4), bar_init(all_met, 8);
+    misc.failed = misc.flag[0] = misc.flag[1] = misc.flag[2] = misc.flag[3] = 0;
     fence_bar_init();
   }
-  if (threadIdx.x < 128) misc.first_nan[threadIdx.x] = 0x7fffffff;
-  if (threadIdx.x < kRows) misc.neg_m[threadIdx.x] = -kNone;
-  if (warp == 7) tmem_alloc<1>(smem_addr(&misc.tmem_at), S::kColumns);
+  if (threadIdx.x < kRows) misc.neg_m[threadIdx.x] = -kNone, misc.top[threadIdx.x] = kLeast;
+  if (threadIdx.x < 32) misc.first_nan[threadIdx.x] = 0xffffffffu;
+  if (warp == 11) tmem_alloc<1>(smem_addr(&misc.tmem_at), S::kColumns);
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + 64, tmem_k = tmem + 192;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + S::kS, tmem_k = tmem + S::kK;
 
-  if (warp >= 4 && warp < 4 + kCopiers) {
-    const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
-    const uint32_t slots = smem_addr(ring);
-    // the page numbers come 32 at a time, the next 32 on their way
-    const int shift = __ffs(a.page_tokens) - 1;
-    const int32_t last = (it.hi - 1) >> shift;
-    int32_t at0 = first * kKeys >> shift;
-    auto look_up = [&](int32_t i) {
-      const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
-      return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
-    };
-    int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
-    int e = warp - 4;
-    for (; e < 2 * n; e += kCopiers) {
-      // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
-      const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
-      const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
-      const int slot = e % S::kSlots;
-      const int32_t k0 = (first + j) * kKeys;
-      const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
-      if (is_v && (k0 >> shift) - at0 >= 32) {   // K is at most three steps ahead of V, 24 pages
-        at0 += 32;
-        now = next;
-        next = look_up(at0 + 32 + lane);
+  if (warp >= 8) {
+    fewer_registers<32>();
+    if (warp < 8 + kCopiers) {
+      const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
+      const uint32_t slots = smem_addr(ring);
+      // the page numbers come 32 at a time, the next 32 on their way
+      const int shift = __ffs(a.page_tokens) - 1;
+      const int32_t last = (it.hi - 1) >> shift;
+      int32_t at0 = first * kKeys >> shift;
+      auto look_up = [&](int32_t i) {
+        const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
+        return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
+      };
+      int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
+      int e = warp - 8;
+      for (; e < 2 * n; e += kCopiers) {
+        // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
+        const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
+        const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
+        const int slot = e % S::kSlots;
+        const int32_t k0 = (first + j) * kKeys;
+        const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
+        if (is_v && (k0 >> shift) - at0 >= 32) {   // K is at most three steps ahead of V, 24 pages
+          at0 += 32;
+          now = next;
+          next = look_up(at0 + 32 + lane);
+        }
+        if (!bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed)) break;
+        const uint32_t bar = full + 8 * slot, dst = slots + slot * S::kSlot;
+        if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * DP);
+        for (int32_t k = from; k < to; k += box) {
+          const int32_t rel = ((k0 + k) >> shift) - at0;
+          const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
+          const int32_t y = ((a.plane + is_v) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
+          if (elect_one()) load_3d(dst + k * DP, &map_kv, 0, y, page, bar);
+        }
       }
-      if (!bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed)) break;
-      const uint32_t bar = full + 8 * slot, dst = slots + slot * S::kSlot;
-      if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * DP);
-      for (int32_t k = from; k < to; k += box) {
-        const int32_t rel = ((k0 + k) >> shift) - at0;
-        const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
-        const int32_t y = ((a.plane + is_v) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
-        if (elect_one()) load_3d(dst + k * DP, &map_kv, 0, y, page, bar);
+      if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
+        uint32_t quiet = 0;
+        for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - S::kSlots; b -= kCopiers)
+          bar_pass(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
       }
-    }
-    if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
+      __syncwarp();
+    } else {
+      // the whole warp goes along; one lane issues
+      const uint32_t desc_s = mma_desc(false, kKeys, 16 * n_c, false), desc_o = mma_desc(false, 128, 16 * n_c, true) | kTurnedA;
+      const uint64_t q = tile_k(smem_addr(base)), p = kHalved ? tile_n(smem_addr(p_mem), kKeys * 128) : tile_n64(smem_addr(p_mem)),
+                     v = tile_n(smem_addr(v_mem), kKeys * 128);
+      auto scores = [&](int j) {
+        if (!bar_wait(k_ready + 8 * (j & 1), (j >> 1) & 1, failed)) return false;
+        tc_after_sync();
+        const uint32_t d = tmem_s + (j & 1) * kRows, k = tmem_k + j % S::kKeep * 64;
+        if (elect_one()) {
+#pragma unroll
+          for (int i = 0; i < DP / 16; ++i)
+            mma_ts(d, k + 8 * i, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), desc_s, i > 0);
+          mma_commit(s_full + 8 * (j & 1));
+        }
+        __syncwarp();
+        return true;
+      };
+      int asked = 0, done = 0;            // S and O that are on their way
+      bool go = bar_wait(q_ready, 0, failed) && scores(0);
+      asked += go;
+      for (int j = 0; go && j < n; ++j) {
+        if (j + 1 < n) {
+          if (!scores(j + 1)) break;
+          ++asked;
+        }
+        if (!bar_wait(v_ready, j & 1, failed)) break;
+        tc_after_sync();
+        if (elect_one()) {
+#pragma unroll
+          for (int i = 0; i < kKeys / 16; ++i)
+            mma_ss<1>(tmem, v + i * (16 * 128 / 16), p + i * (16 * kRows * 2 / 16), desc_o, j > 0 || i > 0);
+          mma_commit(o_done);
+        }
+        __syncwarp();
+        ++done;
+      }
       uint32_t quiet = 0;
-      for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - S::kSlots; b -= kCopiers)
-        bar_pass(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
+      if (asked > 0) bar_pass(s_full + 8 * ((asked - 1) & 1), ((asked - 1) >> 1) & 1, &quiet);
+      if (done > 0) bar_pass(o_done, (done - 1) & 1, &quiet);
     }
-    __syncwarp();
-  } else if (warp == 7) {
-    // the whole warp goes along; one lane issues
-    const uint32_t desc_s = mma_desc(false, kKeys, 16 * n_c, false), desc_o = mma_desc(false, 128, 16 * n_c, true) | kTurnedA;
-    const uint64_t q = tile_k(smem_addr(base)), p = tile_n(smem_addr(p_mem), kKeys * 128),
-                   v = tile_n(smem_addr(v_mem), kKeys * 128);
-    auto scores = [&](int j) {
-      if (!bar_wait(k_ready, j & 1, failed)) return false;
-      tc_after_sync();
-      const uint32_t d = tmem_s + (j & 1) * kRows;
-      if (elect_one()) {
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
-          mma_ts(d, tmem_k + 8 * i, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), desc_s, i > 0);
-        mma_commit(s_full);
-      }
-      __syncwarp();
-      return true;
-    };
-    int asked = 0, done = 0;            // S and O that are on their way
-    bool go = scores(0);
-    asked += go;
-    for (int j = 0; go && j < n; ++j) {
-      if (j + 1 < n) {
-        if (!scores(j + 1)) break;
-        ++asked;
-      }
-      if (!bar_wait(v_ready, j & 1, failed)) break;
-      tc_after_sync();
-      if (elect_one()) {
-#pragma unroll
-        for (int i = 0; i < kKeys / 16; ++i)
-          mma_ss<1>(tmem, v + i * (16 * 128 / 16), p + i * (16 * 128 / 16), desc_o, j > 0 || i > 0);
-        mma_commit(o_done);
-      }
-      __syncwarp();
-      ++done;
-    }
-    uint32_t quiet = 0;
-    if (asked > 0) bar_pass(s_full, (asked - 1) & 1, &quiet);
-    if (done > 0) bar_pass(o_done, (done - 1) & 1, &quiet);
   } else {
-    const int r = threadIdx.x;           // the key of a step, and the dimension of O^T
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    more_registers<104>();
+    const int half = warp / 4, r = threadIdx.x & 127;   // the key of a step, and the dimension of O^T
+    // this half's columns, 16 at a time
+    const int q0 = half ? (n_c + 1) / 2 : 0, q_n = !kHalved ? (half ? 0 : n_c) : half ? n_c / 2 : (n_c + 1) / 2;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, met_half = met + 8 * half;
     uint32_t meetings = 0;
+    const int shift = __ffs(a.page_tokens) - 1;
+    auto page_of = [&](int32_t key) {
+      return key >= it.lo && key < it.hi ? a.table[int64_t(it.row) * a.max_pages + (key >> shift)] : -1;
+    };
+    // the scales of this key's block; of a page that is none 1 (its codes are zeros)
+    auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
+      *ks = *vs = 1.f;
+      if (page < 0 || page >= a.n_pages) return;
+      const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
+      const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
+      *ks = __ldg(s + at);
+      *vs = __ldg(s + a.n_kv * blocks + at);
+    };
+    int32_t key = first * kKeys + r;
+    int32_t page_now = page_of(key), page_next = page_of(key + kKeys);
     float by = 1.f, unit = 1.f;          // Q is scaled by `by`; |1 / by|
     {
       // Q to shared memory, 16 bytes a step: consecutive threads along a row
-      constexpr int kEach = kRows * DP / 8 / 128;
+      constexpr int kEach = kRows * DP / 8 / 256;
       uint4 v[kEach];
       uint32_t top = 0;                  // of |q| where finite, its bits
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int x = r + 128 * i, row = x / (DP / 8), c = x % (DP / 8);
+        const int x = threadIdx.x + 256 * i, row = x / (DP / 8), c = x % (DP / 8);
         v[i] = uint4{};
         if (row < rows && c * 8 < a.dim) {
           const int32_t tok = row / a.group;
@@ -279,8 +329,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
         top = __reduce_max_sync(0xffffffffu, top);
         uint32_t* tops = reinterpret_cast<uint32_t*>(p_mem);
         if (lane == 0) tops[warp] = top;
-        bar_meet(met, &meetings, failed);
-        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        uint32_t first_meeting = 0;
+        bar_meet(all_met, &first_meeting, failed);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, tops[i]);
         const int e = max(min(140 - (int)(top >> 7), 126), -114);   // 2^13 over the largest's power of two
         by = __int_as_float((e + 127) << 23);
         unit = __int_as_float((127 - e) << 23);
@@ -288,28 +340,19 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
       if (a.negative) by = -by;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int x = r + 128 * i, row = x / (DP / 8), c = x % (DP / 8);
+        const int x = threadIdx.x + 256 * i, row = x / (DP / 8), c = x % (DP / 8);
         if (row >= 16 * n_c) continue;
         uint4 o;
         o.x = to_q(T(), v[i].x, by), o.y = to_q(T(), v[i].y, by), o.z = to_q(T(), v[i].z, by), o.w = to_q(T(), v[i].w, by);
         *reinterpret_cast<uint4*>(base + (c / 8) * (kRows * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16) = o;
       }
       fence_async();
+      __syncwarp();
+      if (lane == 0) bar_arrive(q_ready);
     }
-    const int shift = __ffs(a.page_tokens) - 1;
     const float c_all = a.scale2 * unit;
-    auto page_of = [&](int32_t key) {
-      return key >= it.lo && key < it.hi ? a.table[int64_t(it.row) * a.max_pages + (key >> shift)] : -1;
-    };
-    // the scales of this key's block; of a page that is none 1 (its codes are zeros)
-    auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
-      *ks = *vs = 1.f;
-      if (page < 0 || page >= a.n_pages) return;
-      const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
-      const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
-      *ks = __ldg(s + at);
-      *vs = __ldg(s + a.n_kv * blocks + at);
-    };
+    float ks, vs;
+    scales_of(page_now, key, &ks, &vs);
     auto put_keys = [&](int j) {
       const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
       bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
@@ -318,180 +361,213 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
         uint32_t o[32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) wide16(*codes_at<DP>(ring + slot * S::kSlot, r, 4 * h + c), o + 8 * c);
-        tmem_store32(tmem_k + lanes + 32 * h, o);
+        tmem_store32(tmem_k + j % S::kKeep * 64 + lanes + 32 * h, o);
       }
       tmem_wait_store();
       tc_before_sync();
       __syncwarp();
-      if (lane == 0) bar_arrive(empty + 8 * slot), bar_arrive(k_ready);
+      if (lane == 0) bar_arrive(empty + 8 * slot), bar_arrive(k_ready + 8 * (j & 1));
+    };
+    // V_j to shared memory.  `some`: not every row sees every key
+    auto put_values = [&](int j, bool in, auto some) {
+      constexpr bool kSome = decltype(some)::value;
+      const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
+      bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
+#pragma unroll
+      for (int c16 = 0; c16 < DP / 16; ++c16) {
+        uint4 v = *codes_at<DP>(ring + slot * S::kSlot, r, c16);
+        if (kSome) {
+          // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN
+          // that some row does not see; those that see it get theirs at the end.
+          if (!in) v = uint4{};
+          uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+          const uint32_t query = key <= it.pos0 ? 0 : min(key - it.pos0, 254);
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i) {
+            if (!(((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) continue;
+            for (int b = 0; b < 4; ++b)
+              if ((w[i] >> (8 * b) & 0x7f) == 0x7f) {
+                uint32_t* word = &misc.first_nan[4 * c16 + i];
+                uint32_t was = *reinterpret_cast<volatile uint32_t*>(word);
+                while ((was >> (8 * b) & 0xff) > query) {   // (ends: the byte only falls)
+                  const uint32_t found = atomicCAS(word, was, (was & ~(0xffu << (8 * b))) | query << (8 * b));
+                  if (found == was) break;
+                  was = found;
+                }
+                w[i] &= ~(0xffu << (8 * b));
+              }
+          }
+        }
+        uint32_t o[8];
+        wide16(v, o);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          *reinterpret_cast<uint4*>(v_mem + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + i) % 8) ^ (r & 7)) * 16) =
+              uint4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(empty + 8 * slot);
     };
     const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
-    int32_t key = first * kKeys + r;
-    float ks, vs;
-    scales_of(page_of(key), key, &ks, &vs);
-    int32_t page_next = page_of(key + kKeys);
-    put_keys(0);
-    uint64_t l2[kRows / 2];              // of this key's share of every row's sum
+    if (half == (kHalved ? 0 : 1)) {
+      put_keys(0);
+      if (!kHalved && n > 1) put_keys(1);
+    }
+    uint64_t l2[16];                     // of this key's share of the sums of this half's rows
 #pragma unroll
-    for (int i = 0; i < kRows / 2; ++i) l2[i] = 0;
+    for (int i = 0; i < 16; ++i) l2[i] = 0;
     for (int j = 0; j < n; ++j, key += kKeys) {
       const int32_t k0 = (first + j) * kKeys;
-      float ks_next, vs_next;
-      scales_of(page_next, key + kKeys, &ks_next, &vs_next);
-      page_next = page_of(key + 2 * kKeys);
-      bar_pass(s_full, j & 1, failed);
-      tc_after_sync();
-      if (j + 1 < n) put_keys(j + 1);
-      // S_j: x = s c + log2 v - m
-      const float vs_in = fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
-      const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f), lv = log2f(vs_in);
-      const uint32_t s_at = tmem_s + lanes + (j & 1) * kRows;
       const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kKeys > all_see;
-      // rows that see this key: those of its token and later ones
-      uint64_t sees = ~0ull;
-      if (masked) {
-        const int64_t before = key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group;
-        sees = !in || before >= 64 ? 0 : ~0ull << before;
+      float ks_next = 1.f, vs_next = 1.f;
+      if (kHalved || half == 0) {
+        scales_of(page_next, key + kKeys, &ks_next, &vs_next);
+        page_next = page_of(key + 2 * kKeys);
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (q < n_c) {
-          uint32_t s[16];
-          tmem_load16(s_at + 16 * q, s);
-          float4 m[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) m[i] = reinterpret_cast<const float4*>(misc.neg_m)[4 * q + i];
+      if (half == 0) {
+        bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
+        tc_after_sync();
+        if (kHalved && j + 1 < n) put_keys(j + 1);
+      } else {
+        if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // V is read
+        if (masked) put_values(j, in, std::true_type());
+        else put_values(j, in, std::false_type());
+        if (!kHalved) {
+          fence_async();
+          __syncwarp();
+          if (lane == 0) bar_arrive(v_ready);
+          if (j + 2 < n) {
+            bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);   // K_j is read
+            tc_after_sync();
+            put_keys(j + 2);
+          }
+          continue;
+        }
+        if (q_n > 0) bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
+        tc_after_sync();
+      }
+      if (q_n > 0) {
+        // x = s c + log2 v - m, of two rows a register pair
+        const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
+        const float lv0 = __log2f(fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f)), lv = lv0 + kBias;
+        const uint32_t s_at = tmem_s + lanes + (j & 1) * kRows + 16 * q0;
+        // rows that see this key: those of its token and later ones
+        uint32_t sees = ~0u;
+        if (masked) {
+          const int64_t before = (key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group) - 16 * q0;
+          sees = !in || before >= 32 ? 0 : before <= 0 ? ~0u : ~0u << before;
+        }
+        uint32_t s[32];
+        auto exponents = [&]() {         // over s; returns the largest
+          tmem_load16(s_at, s);
+          if (q_n > 1) tmem_load16(s_at + 16, s + 16);
           tmem_wait_load();
           tmem_loaded(s);
-          const float* mf = reinterpret_cast<const float*>(m);
+          const uint64_t c2 = two(c, c), lv2 = two(lv, lv);
+          float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float x = fmaf(__uint_as_float(s[i]), c, lv + mf[i]);
-            if (!masked || (sees >> (16 * q + i) & 1)) top = fmaxf(top, x);
-          }
-        }
-      if (__any_sync(0xffffffffu, top > 8.f) && lane == 0) misc.flag[j & 1] = j + 1;
-      bar_meet(met, &meetings, failed);
-      if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&misc.flag[j & 1]), 0) == j + 1u) {
-        // a reference is raised: the columns' maxima over the keys, in P's place
-        if (j > 0) {
-          bar_pass(o_done, (j - 1) & 1, failed);
-          tc_after_sync();
-        }
-        float* tops = reinterpret_cast<float*>(p_mem);   // [4][kRows], then the factors [kRows]
-#pragma unroll 1
-        for (int q = 0; q < n_c; ++q) {
-          uint32_t s[16];
-          tmem_load16(s_at + 16 * q, s);
-          tmem_wait_load();
-          tmem_loaded(s);
+          for (int q = 0; q < 2; ++q)
+            if (q < q_n) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float x = fmaf(__uint_as_float(s[i]), c, lv);
-            if (!(x == x) || (masked && !(sees >> (16 * q + i) & 1))) x = -INFINITY;
-            const int32_t most = __reduce_max_sync(0xffffffffu, ordered(x));
-            if (lane == i) tops[warp * kRows + 16 * q + i] = __int_as_float(most ^ ((most >> 31) & 0x7fffffff));
-          }
-        }
-        bar_meet(met, &meetings, failed);
-        if (r < 16 * n_c) {
-          const float was = -misc.neg_m[r];
-          const float most = fmaxf(fmaxf(tops[r], tops[kRows + r]), fmaxf(tops[2 * kRows + r], tops[3 * kRows + r]));
-          const float now = most > was + 8.f ? most : was;
-          misc.neg_m[r] = -now;
-          tops[4 * kRows + r] = now == was ? 1.f : exp2f(was - now);
-        }
-        bar_meet(met, &meetings, failed);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q < n_c) {
-            float f[16];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(f + 4 * i) = reinterpret_cast<const float4*>(tops)[kRows + 4 * q + i];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float x, y;
-              halves(l2[8 * q + i], &x, &y);
-              l2[8 * q + i] = two(x * f[2 * i], y * f[2 * i + 1]);
+              for (int i = 0; i < 4; ++i) {
+                const float4 m = reinterpret_cast<const float4*>(misc.neg_m)[4 * (q0 + q) + i];
+                float x, y, z, w;
+                uint32_t* at = s + 16 * q + 4 * i;
+                halves(fma2(two(__uint_as_float(at[0]), __uint_as_float(at[1])), c2, add2(two(m.x, m.y), lv2)), &x, &y);
+                halves(fma2(two(__uint_as_float(at[2]), __uint_as_float(at[3])), c2, add2(two(m.z, m.w), lv2)), &z, &w);
+                at[0] = __float_as_uint(x), at[1] = __float_as_uint(y), at[2] = __float_as_uint(z), at[3] = __float_as_uint(w);
+              }
             }
-            if (j > 0) {
+          if (masked)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(sees >> i & 1)) s[i] = 0xff800000u;
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (q < q_n)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) most[i & 1] = max3(most[i & 1], s[16 * q + 2 * i], s[16 * q + 2 * i + 1]);
+          return fmaxf(most[0], most[1]);
+        };
+        uint32_t* flag = &misc.flag[2 * half + (j & 1)];
+        if (__any_sync(0xffffffffu, exponents() > kMost + kBias) && lane == 0) *flag = j + 1;
+        bar_meet(met_half, &meetings, failed);
+        if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(flag), 0) == j + 1u) {
+          // a reference is raised: the columns' maxima over the keys
+#pragma unroll 1
+          for (int q = 0; q < q_n; ++q) {
+            uint32_t t[16];
+            tmem_load16(s_at + 16 * q, t);
+            tmem_wait_load();
+            tmem_loaded(t);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float x = fmaf(__uint_as_float(t[i]), c, lv);
+              if (!(x == x) || !(sees >> (16 * q + i) & 1)) x = -INFINITY;
+              const int32_t most = __reduce_max_sync(0xffffffffu, ordered(x));
+              if (lane == i) atomicMax(&misc.top[16 * (q0 + q) + i], most);
+            }
+          }
+          bar_meet(met_half, &meetings, failed);
+          // what a raised reference takes from the sums and from O (there is nothing yet in the first step)
+          auto factor = [&](int col) {
+            const float was = -misc.neg_m[col], most = from_ordered(misc.top[col]) - kBias;
+            return most > was + kMost ? exp2_fast(was - most) : 1.f;
+          };
+          if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);
+          tc_after_sync();
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (q < q_n && j > 0) {
               uint32_t o[16];
-              tmem_load16(tmem + lanes + 16 * q, o);
+              tmem_load16(tmem + lanes + 16 * (q0 + q), o);
               tmem_wait_load();
               tmem_loaded(o);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f[i]);
-              tmem_store16(tmem + lanes + 16 * q, o);
-            }
-          }
-        tmem_wait_store();
-        bar_meet(met, &meetings, failed);
-      }
-      if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // P and V are read
-      const uint64_t c2 = two(c, c), lv2 = two(lv + kBias, lv + kBias), inv2 = two(1.f / vs_in, 1.f / vs_in);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (q < n_c) {
-          uint32_t s[16], p[8];
-          tmem_load16(s_at + 16 * q, s);
-          float4 m[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) m[i] = reinterpret_cast<const float4*>(misc.neg_m)[4 * q + i];
-          tmem_wait_load();
-          tmem_loaded(s);
-          const float* mf = reinterpret_cast<const float*>(m);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float x, y;
-            halves(fma2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, add2(two(mf[2 * i], mf[2 * i + 1]), lv2)),
-                   &x, &y);
-            if (masked) {
-              if (!(sees >> (16 * q + 2 * i) & 1)) x = -INFINITY;
-              if (!(sees >> (16 * q + 2 * i + 1) & 1)) y = -INFINITY;
-            }
-            x = exp2_fast(x), y = exp2_fast(y);
-            l2[8 * q + i] = fma2(two(x, y), inv2, l2[8 * q + i]);
-            p[i] = pack(__half(), x, y);
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<uint4*>(p_mem + r * 128 + ((2 * q + i) ^ (r & 7)) * 16) =
-                uint4{p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]};
-        }
-      {
-        const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
-        bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
-#pragma unroll
-        for (int c16 = 0; c16 < DP / 16; ++c16) {
-          uint4 v = *codes_at<DP>(ring + slot * S::kSlot, r, c16);
-          if (masked) {
-            // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN
-            // that some row does not see; those that see it get theirs at the end.
-            if (!in) v = uint4{};
-            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) {
-                for (int b = 0; b < 4; ++b)
-                  if ((w[i] >> (8 * b) & 0x7f) == 0x7f) {
-                    atomicMin(&misc.first_nan[16 * c16 + 4 * i + b], key);
-                    w[i] &= ~(0xffu << (8 * b));
-                  }
+              for (int i = 0; i < 8; ++i) {
+                const float f = factor(16 * (q0 + q) + 2 * i), h = factor(16 * (q0 + q) + 2 * i + 1);
+                float x, y;
+                halves(l2[8 * q + i], &x, &y);
+                l2[8 * q + i] = two(x * f, y * h);
+                o[2 * i] = __float_as_uint(__uint_as_float(o[2 * i]) * f);
+                o[2 * i + 1] = __float_as_uint(__uint_as_float(o[2 * i + 1]) * h);
               }
+              tmem_store16(tmem + lanes + 16 * (q0 + q), o);
+            }
+          tmem_wait_store();
+          bar_meet(met_half, &meetings, failed);
+          if (r < 16 * q_n) {
+            const int col = 16 * q0 + r;
+            const float was = -misc.neg_m[col], most = from_ordered(misc.top[col]) - kBias;
+            if (most > was + kMost) misc.neg_m[col] = -most;
+            misc.top[col] = kLeast;
           }
-          uint32_t o[8];
-          wide16(v, o);
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<uint4*>(v_mem + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + i) % 8) ^ (r & 7)) * 16) =
-                uint4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+          bar_meet(met_half, &meetings, failed);
+          exponents();
         }
-        fence_async();
-        tc_before_sync();
-        __syncwarp();
-        if (lane == 0) bar_arrive(empty + 8 * slot), bar_arrive(v_ready);
+        if (half == 0 && j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // P is read
+        const float inv = exp2_fast(-lv0);
+        const uint64_t inv2 = two(inv, inv);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (q < q_n) {
+            uint32_t p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float x = exp2_fast(__uint_as_float(s[16 * q + 2 * i])), y = exp2_fast(__uint_as_float(s[16 * q + 2 * i + 1]));
+              l2[8 * q + i] = fma2(two(x, y), inv2, l2[8 * q + i]);
+              p[i] = pack(__half(), x, y);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              *reinterpret_cast<uint4*>(p_mem + r * (2 * kRows) + ((2 * (q0 + q) + i) ^ (kHalved ? r & 7 : (r >> 1) & 3)) * 16) =
+                  uint4{p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]};
+          }
       }
+      fence_async();
+      tc_before_sync();
+      __syncwarp();
+      if (lane == 0) bar_arrive(v_ready);
       ks = ks_next, vs = vs_next;
     }
     bar_pass(o_done, (n - 1) & 1, failed);
@@ -499,8 +575,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
     // the rows' sums over the keys, in P's place: [4][kRows], then 1 / sum
     float* sums = reinterpret_cast<float*>(p_mem);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (q < n_c) {
+    for (int q = 0; q < 2; ++q)
+      if (q < q_n) {
         float x[16];
 #pragma unroll
         for (int i = 0; i < 8; ++i) halves(l2[8 * q + i], &x[2 * i], &x[2 * i + 1]);
@@ -517,69 +593,77 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
             }
         }
         x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
-        if (!(lane & 1)) sums[warp * kRows + 16 * q + lane / 2] = x[0];
+        if (!(lane & 1)) sums[(warp & 3) * kRows + 16 * (q0 + q) + lane / 2] = x[0];
       }
-    bar_meet(met, &meetings, failed);
-    if (r < rows) {
-      const float l = (sums[r] + sums[kRows + r]) + (sums[2 * kRows + r] + sums[3 * kRows + r]);
-      const float lse2 = l == 0.f ? -INFINITY : -misc.neg_m[r] - kBias + log2f(l);
-      sums[4 * kRows + r] = l == 0.f ? 0.f : 1.f / l;
+    bar_meet(met_half, &meetings, failed);
+    const int row = 16 * q0 + r;
+    if (r < 16 * q_n && row < rows) {
+      const float l = (sums[row] + sums[kRows + row]) + (sums[2 * kRows + row] + sums[3 * kRows + row]);
+      const float lse2 = l == 0.f ? -INFINITY : -misc.neg_m[row] - kBias + log2f(l);
+      sums[4 * kRows + row] = l == 0.f ? 0.f : 1.f / l;
       if (it.part >= 0) {
-        a.part_lse[hk * a.part_rows + it.part + r] = lse2;
+        a.part_lse[hk * a.part_rows + it.part + row] = lse2;
       } else if (a.lse) {
-        const int32_t tok = r / a.group;
-        a.lse[(int64_t)(it.tok0 + tok) * a.n_heads + hk * a.group + r - tok * a.group] = lse2 * 0.69314718055994531f;
+        const int32_t tok = row / a.group;
+        a.lse[(int64_t)(it.tok0 + tok) * a.n_heads + hk * a.group + row - tok * a.group] = lse2 * 0.69314718055994531f;
       }
     }
-    bar_meet(met, &meetings, failed);
-    const int32_t nan_at = misc.first_nan[r];
-    int32_t tok = 0, h = 0;
+    bar_meet(met_half, &meetings, failed);
+    // a row after the other, a dimension a thread
+    const int nan_at = misc.first_nan[r / 4] >> (8 * (r % 4)) & 0xff;
+    int32_t tok = 16 * q0 / a.group, h = 16 * q0 - tok * a.group;
+    float* part = a.part_o + (hk * a.part_rows + it.part + 16 * q0) * a.dim + r;
+    T* out = static_cast<T*>(a.out) + (it.tok0 + tok) * a.o_tok + (hk * a.group + h) * a.o_head + r;
+    const int64_t next_tok = a.o_tok - (a.group - 1) * a.o_head;
+    const int last_row = rows < 16 * (q0 + q_n) ? rows : 16 * (q0 + q_n);
 #pragma unroll 1
-    for (int q = 0; q < n_c; ++q) {
-      uint32_t o[16];
-      tmem_load16(tmem + lanes + 16 * q, o);
+    for (int at = 16 * q0; at < last_row; at += 8) {
+      uint32_t o[8];
+      tmem_load8(tmem + lanes + at, o);
+      const float4 i0 = *reinterpret_cast<const float4*>(sums + 4 * kRows + at), i1 = *reinterpret_cast<const float4*>(sums + 4 * kRows + at + 4);
+      const float inv[8] = {i0.x, i0.y, i0.z, i0.w, i1.x, i1.y, i1.z, i1.w};
       tmem_wait_load();
       tmem_loaded(o);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = 16 * q + i;
-        if (row < rows && r < a.dim) {
-          const float inv = sums[4 * kRows + row];
-          float v = inv == 0.f ? 0.f : __uint_as_float(o[i]) * inv;
-          if (nan_at <= it.pos0 + tok) v = NAN;
-          if (it.part >= 0) {
-            __stcg(a.part_o + (hk * a.part_rows + it.part + row) * a.dim + r, v);
-          } else {
-            T* out = static_cast<T*>(a.out) + (it.tok0 + tok) * a.o_tok + (hk * a.group + h) * a.o_head + r;
-            const uint32_t both = pack(T(), v, v);
-            *reinterpret_cast<unsigned short*>(out) = (unsigned short)both;
-          }
+      for (int i = 0; i < 8; ++i) {
+        if (at + i < last_row && r < a.dim) {
+          float v = inv[i] == 0.f ? 0.f : __uint_as_float(o[i]) * inv[i];
+          if (nan_at <= tok) v = NAN;
+          if (it.part >= 0) __stcg(part, v);
+          else *reinterpret_cast<unsigned short*>(out) = (unsigned short)pack(T(), v, v);
         }
-        if (++h == a.group) h = 0, ++tok;
+        part += a.dim;
+        if (++h == a.group) h = 0, ++tok, out += next_tok;
+        else out += a.o_head;
       }
     }
   }
   __syncwarp();
   tc_before_sync();
   __syncthreads();
-  if (warp == 7) tmem_free<1>(tmem, S::kColumns);
+  if (warp == 11) tmem_free<1>(tmem, S::kColumns);
   if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
 }
 
-constexpr Cutting kCutting = {kKeys, kRows, 4, 8, 3, 5};
+constexpr Cutting kCutting = {kKeys, kMany, 4, 8, 3, 5, true};
 
-template <class T, int DP>
-cudaError_t launch(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
+template <class T, int DP, int kRows>
+cudaError_t launch_rows(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
   static gsim::OncePerDevice once;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
-  auto kernel = attend8_kernel<T, DP>;
-  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP>::kSmem); })) return cudaErrorInvalidValue;
-  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(kv, g);
-  if (p.n_joins > 0) {
-    const int64_t heads = (int64_t)p.join_tokens * p.n_heads;
-    attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>(heads, 1024)), 128, 0, st>>>(g.a);
-  }
+  auto kernel = attend8_kernel<T, DP, kRows>;
+  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP, kRows>::kSmem); })) return cudaErrorInvalidValue;
+  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP, kRows>::kSmem, st>>>(kv, g);
+  return cudaGetLastError();
+}
+
+template <class T, int DP>
+cudaError_t launch(const op_attend_plan_t& p, int32_t most_rows, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
+  const cudaError_t e = most_rows <= kFew ? launch_rows<T, DP, kFew>(p, kv, g, st) : launch_rows<T, DP, kMany>(p, kv, g, st);
+  if (e != cudaSuccess || p.n_joins == 0) return e;
+  const int64_t heads = (int64_t)p.join_tokens * p.n_heads;
+  attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>(heads, 1024)), 128, 0, st>>>(g.a);
   return cudaGetLastError();
 }
 
@@ -592,10 +676,14 @@ extern "C" {
 
 int op_attend8_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,
                     size_t item_bytes) try {
-  if (!desc_ok(d, kRows) || d->head_dim % 16 || d->page_tokens < 16 || !plan || n_sm < 1) return GMG_EINVAL;
+  if (!desc_ok(d, kMany) || d->head_dim % 16 || d->page_tokens < 16 || !plan || n_sm < 1) return GMG_EINVAL;
   Work w;
   plan_items(*d, n_sm, kCutting, &w);
-  return fill_plan(d, w, &plan->p, items, item_bytes);
+  int32_t most = 0;
+  for (const Item& it : w.items) most = std::max(most, it.n_tok * (d->n_heads / d->n_kv_heads));
+  const int rc = fill_plan(d, w, &plan->p, items, item_bytes);
+  if (rc == GMG_OK) plan->most_rows = most;
+  return rc;
 } catch (const std::bad_alloc&) {
   return GMG_ENOMEM;
 }
@@ -651,9 +739,9 @@ int op_attend8(const op_attend8_plan_t* plan8, const int32_t* d_items, const op_
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (dtype == GMG_OP_BF16)
-    e = dp == 64 ? launch<__nv_bfloat16, 64>(*plan, map_kv, g, st) : launch<__nv_bfloat16, 128>(*plan, map_kv, g, st);
+    e = dp == 64 ? launch<__nv_bfloat16, 64>(*plan, plan8->most_rows, map_kv, g, st) : launch<__nv_bfloat16, 128>(*plan, plan8->most_rows, map_kv, g, st);
   else
-    e = dp == 64 ? launch<__half, 64>(*plan, map_kv, g, st) : launch<__half, 128>(*plan, map_kv, g, st);
+    e = dp == 64 ? launch<__half, 64>(*plan, plan8->most_rows, map_kv, g, st) : launch<__half, 128>(*plan, plan8->most_rows, map_kv, g, st);
   return e == cudaSuccess ? GMG_OK : GMG_ECUDA;
 }
 

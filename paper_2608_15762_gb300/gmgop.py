@@ -56,6 +56,10 @@ class _AttendPlan(C.Structure):
         ("n_tokens", C.c_int64), ("part_rows", C.c_int64), ("plan_bytes", C.c_size_t), ("work_bytes", C.c_size_t)]
 
 
+class _AttendPlan8(C.Structure):
+    _fields_ = _AttendPlan._fields_ + [("most_rows", C.c_int32), ("reserved", C.c_int32)]
+
+
 class _Linear(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "act", "gated", "reserved")] + [
         (n, C.c_int64) for n in ("m", "n", "k")] + [
@@ -464,7 +468,7 @@ def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=
           "group_off: one entry more than prefix")
     ptr = [None if a is None else a.ctypes.data for a in arr]
     d = _AttendDesc(q.size, n_heads, n_kv_heads, head_dim, page_tokens, 0 if pre is None else pre.size, *ptr)
-    plan = _AttendPlan()
+    plan = _AttendPlan() if bits == 16 else _AttendPlan8()
     items = np.empty(1 << 14, np.int32)      # most plans are shorter; longer ones are made again
     call = getattr(_LIB or lib(), name)
     rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
