@@ -101,6 +101,18 @@ __device__ __forceinline__ uint64_t tile_n64(uint32_t addr) {
   return (uint64_t)((addr & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
 }
 
+// Loads that stay where they are written, ahead of their use.
+__device__ __forceinline__ float load_now(const float* p) {
+  float v;
+  asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ int32_t load_now(const int32_t* p) {
+  int32_t v;
+  asm volatile("ld.global.nc.s32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+
 // 16 codes of a row of a slot, where the copy has put them.
 template <int DP>
 __device__ __forceinline__ uint4* codes_at(unsigned char* slot, int row, int c) {
@@ -141,6 +153,570 @@ __device__ __forceinline__ uint32_t to_q(__nv_bfloat16, uint32_t v, float by) {
   return pack(__half(), __uint_as_float(v << 16) * by, __uint_as_float(v & 0xffff0000u) * by);
 }
 __device__ __forceinline__ uint32_t to_q(__half, uint32_t v, float by) { return by < 0.f ? v ^ 0x80008000u : v; }
+
+// Queries that see nothing.
+template <class T>
+__device__ void sees_nothing(const AttendArgs& a, const Item& it, int32_t hk, int32_t rows) {
+  for (int r = threadIdx.x; r < rows; r += blockDim.x) {
+    const int64_t t = it.tok0 + r / a.group;
+    const int32_t h = hk * a.group + r % a.group;
+    T* o = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+    for (int d = 0; d < a.dim; d += 8) *reinterpret_cast<uint4*>(o + d) = uint4{};
+    if (a.lse) a.lse[t * a.n_heads + h] = -INFINITY;
+  }
+}
+
+// A copying warp: every kCopiers-th slot of K_0 K_1 V_0 K_2 V_1 ..., page by page, rows of kRow bytes.
+template <int kRow, int kSlots>
+__device__ __forceinline__ void copy_pages(const CUtensorMap& map, const AttendArgs& a, const Item& it, int32_t hk, int32_t first,
+                                           int32_t n, int e, int lane, uint32_t slots, uint32_t full, uint32_t empty,
+                                           volatile uint32_t* failed) {
+  const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
+  // the page numbers come 32 at a time, the next 32 on their way
+  const int shift = __ffs(a.page_tokens) - 1;
+  const int32_t last = (it.hi - 1) >> shift;
+  int32_t at0 = first * kKeys >> shift;
+  auto look_up = [&](int32_t i) {
+    const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
+    return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
+  };
+  int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
+  for (; e < 2 * n; e += kCopiers) {
+    // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
+    const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
+    const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
+    const int slot = e % kSlots;
+    const int32_t k0 = (first + j) * kKeys;
+    const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
+    if (is_v && (k0 >> shift) - at0 >= 32) {   // K is at most three steps ahead of V, 24 pages
+      at0 += 32;
+      now = next;
+      next = look_up(at0 + 32 + lane);
+    }
+    if (!bar_wait(empty + 8 * slot, ((e / kSlots) & 1) ^ 1, failed)) break;
+    const uint32_t bar = full + 8 * slot, dst = slots + slot * (kKeys * kRow);
+    if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * kRow);
+    for (int32_t k = from; k < to; k += box) {
+      const int32_t rel = ((k0 + k) >> shift) - at0;
+      const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
+      const int32_t y = ((a.plane + is_v) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
+      if (elect_one()) load_3d(dst + k * kRow, &map, 0, y, page, bar);
+    }
+  }
+  if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
+    uint32_t quiet = 0;
+    for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - kSlots; b -= kCopiers)
+      bar_pass(full + 8 * (b % kSlots), (b / kSlots) & 1, &quiet);
+  }
+  __syncwarp();
+}
+
+// Codes that are NaN become zeros; first_nan, a byte a dimension, falls to the first query that sees one.
+__device__ __forceinline__ void drop_nan(uint4* v, uint32_t* first_nan, uint32_t query) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (!(((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) continue;
+    for (int b = 0; b < 4; ++b)
+      if ((w[i] >> (8 * b) & 0x7f) == 0x7f) {
+        uint32_t was = *reinterpret_cast<volatile uint32_t*>(first_nan + i);
+        while ((was >> (8 * b) & 0xff) > query) {   // (ends: the byte only falls)
+          const uint32_t found = atomicCAS(first_nan + i, was, (was & ~(0xffu << (8 * b))) | query << (8 * b));
+          if (found == was) break;
+          was = found;
+        }
+        w[i] &= ~(0xffu << (8 * b));
+      }
+  }
+}
+
+// The warp's sums of 16 columns, two a register pair: lane 2 i has column i's in the end.
+__device__ __forceinline__ void column_sums(const uint64_t* l2, float* out, int lane) {
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) halves(l2[i], &x[2 * i], &x[2 * i + 1]);
+  // each step keeps half of the columns
+#pragma unroll
+  for (int d = 16, k = 8; k; d /= 2, k /= 2) {
+    const bool upper = lane & d;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < k) {
+        const float give = upper ? x[i] : x[i + k];
+        const float keep = upper ? x[i + k] : x[i];
+        x[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+      }
+  }
+  x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
+  if (!(lane & 1)) out[lane / 2] = x[0];
+}
+
+// A row's sum l of the weights against reference m (log2): 1 / l to inv[row], its log-sum-exp where it goes.
+template <class T>
+__device__ __forceinline__ void finish_row(const AttendArgs& a, const Item& it, int32_t hk, int32_t row, float l, float m, float* inv) {
+  const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+  inv[row] = l == 0.f ? 0.f : 1.f / l;
+  if (it.part >= 0) {
+    a.part_lse[hk * a.part_rows + it.part + row] = lse2;
+  } else if (a.lse) {
+    const int32_t tok = row / a.group;
+    a.lse[(int64_t)(it.tok0 + tok) * a.n_heads + hk * a.group + row - tok * a.group] = lse2 * 0.69314718055994531f;
+  }
+}
+
+// Where a thread's dimension of one row after the other goes.
+template <class T>
+struct Rows {
+  float* part;
+  T* out;
+  int64_t next_tok;
+  int32_t tok, h;
+  __device__ Rows(const AttendArgs& a, const Item& it, int32_t hk, int32_t row, int32_t dim) {
+    tok = row / a.group, h = row - tok * a.group;
+    part = a.part_o + (hk * a.part_rows + it.part + row) * a.dim + dim;
+    out = static_cast<T*>(a.out) + (it.tok0 + tok) * a.o_tok + (hk * a.group + h) * a.o_head + dim;
+    next_tok = a.o_tok - (a.group - 1) * a.o_head;
+  }
+  __device__ void put(const AttendArgs&, const Item& it, float v, float inv, int nan_at) {
+    v = inv == 0.f ? 0.f : v * inv;
+    if (nan_at <= tok) v = NAN;
+    if (it.part >= 0) __stcg(part, v);
+    else *reinterpret_cast<unsigned short*>(out) = (unsigned short)pack(T(), v, v);
+  }
+  __device__ void next(const AttendArgs& a) {
+    part += a.dim;
+    if (++h == a.group) h = 0, ++tok, out += next_tok;
+    else out += a.o_head;
+  }
+};
+
+template <class T>
+__device__ __forceinline__ T from_bits(uint32_t v) {
+  const unsigned short s = (unsigned short)v;
+  return *reinterpret_cast<const T*>(&s);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: codes straight into the products
+// ---------------------------------------------------------------------------
+
+// Numbers of more bits than a code has, as a sum of codes: x = t_0 + t_1 / 16 + t_2 / 256, each the
+// nearest to 16 times what the ones before it leave.  Two terms hold bf16 exactly (as far as 2^-14, of
+// 2^8 at most), three 12 bits and more (as far as 2^-18).
+constexpr int kFewRows = 16;
+constexpr int kTermsP = 3;
+constexpr float kBiasFew = 6.f, kMostFew = 2.75f;   // a weight is at most 2^8.75 < 448
+
+template <class T>
+struct TermsQ {
+  static constexpr int kN = std::is_same<T, __nv_bfloat16>::value ? 2 : 3;
+};
+
+template <class T>
+struct FewShape {
+  static constexpr int kTerms = TermsQ<T>::kN;
+  static constexpr int kQ = 6144, kP = kTermsP * kKeys * 16;   // Q: terms of 16 rows of 128 bytes
+  static constexpr int kSlot = kKeys * 128, kSlots = 6;
+  static constexpr int kRingAt = (kQ + kP + 1023) / 1024 * 1024;
+  static constexpr int kMiscAt = kRingAt + kSlots * kSlot;
+  static constexpr int kSmem = kMiscAt + 1024;
+  static constexpr int kThreads = 256;
+  static constexpr int kColumns = 256, kS = 64, kSTwo = 64;    // of TMEM: O^T, then S^T twice
+  static_assert(kSmem <= 115712, "two blocks an SM");
+};
+
+struct FewMisc {
+  float neg_m[kFewRows];
+  int32_t top[kFewRows];
+  uint32_t first_nan[32];
+  uint64_t bars[2 * 6 + 8];
+  uint32_t tmem_at, failed, flag[2];
+};
+static_assert(sizeof(FewMisc) <= 1024, "fits behind the ring");
+
+// D (+)= A B^T for 32 codes of A and B.
+__device__ __forceinline__ void mma8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+// e4m3 both (types 0), fp32 sums.
+__host__ __device__ constexpr uint32_t mma8_desc(int m, int n, bool a_rows, bool b_rows) {
+  return (1u << 4) | ((a_rows ? 1u : 0u) << 15) | ((b_rows ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+// No swizzle, rows (N) contiguous, 16 of a column in 16 bytes: eight columns after each other; the next eight are
+// `deeper` bytes on, the next 16 rows `further`.
+__device__ __forceinline__ uint64_t tile_n16(uint32_t addr, uint32_t deeper, uint32_t further) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(deeper >> 4) << 16) | ((uint64_t)(further >> 4) << 32) | (1ull << 46);
+}
+
+__device__ __forceinline__ uint16_t codes2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// The next term of x and y: its codes; x and y become 16 times what it leaves.
+__device__ __forceinline__ uint16_t next_term(uint64_t* xy) {
+  float x, y;
+  halves(*xy, &x, &y);
+  const uint16_t c = codes2(x, y);
+  const uint32_t h = wide2(c);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  *xy = fma2(two(f.x, f.y), two(-16.f, -16.f), fma2(*xy, two(16.f, 16.f), 0ull));
+  return c;
+}
+
+template <class T>
+__global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(const __grid_constant__ CUtensorMap map_kv,
+                                                                             const __grid_constant__ Args8 g) {
+  using S = FewShape<T>;
+  extern __shared__ __align__(1024) unsigned char base[];
+  const AttendArgs& a = g.a;
+  unsigned char* const p_mem = base + S::kQ;
+  FewMisc& misc = *reinterpret_cast<FewMisc*>(base + S::kMiscAt);
+  volatile uint32_t* failed = &misc.failed;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
+  const int32_t item = blockIdx.x / a.n_kv, hk = blockIdx.x - item * a.n_kv;
+  const Item it = a.items[item];
+  const int32_t rows = it.n_tok * a.group;
+  const int32_t first = it.lo / kKeys, n = it.hi > it.lo ? (it.hi + kKeys - 1) / kKeys - first : 0;
+
+  if (n == 0) {   // queries that see nothing
+    sees_nothing<T>(a, it, hk, rows);
+    return;
+  }
+
+  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, q_ready = empty + 8 * S::kSlots,
+                 s_full = q_ready + 8, p_ready = s_full + 8, o_done = p_ready + 8, met = o_done + 8;
+  // S_{j+1} is computed when P_{j-1} is there, after all have waited for S_{j-1}: two phases may be complete that
+  // nobody has waited for, so s_full is two barriers (the second behind the others).
+  const uint32_t s_full_odd = met + 8;
+  if (warp == 4 && lane == 0) {
+    prefetch_map(&map_kv);
+    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+    bar_init(q_ready, 4), bar_init(s_full, 1), bar_init(s_full_odd, 1), bar_init(p_ready, 4), bar_init(o_done, 1), bar_init(met, 4);
+    misc.failed = misc.flag[0] = misc.flag[1] = 0;
+    fence_bar_init();
+  }
+  if (threadIdx.x < kFewRows) misc.neg_m[threadIdx.x] = -kNone, misc.top[threadIdx.x] = kLeast;
+  if (threadIdx.x < 32) misc.first_nan[threadIdx.x] = 0xffffffffu;
+  if (warp == 7) tmem_alloc<1>(smem_addr(&misc.tmem_at), S::kColumns);
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + S::kS;
+
+  if (warp >= 4 && warp < 4 + kCopiers) {
+    copy_pages<128, S::kSlots>(map_kv, a, it, hk, first, n, warp - 4, lane, smem_addr(base + S::kRingAt), full, empty, failed);
+  } else if (warp == 7) {
+    constexpr uint32_t desc_s = mma8_desc(kKeys, kFewRows * S::kTerms, false, false),
+                       desc_o = mma8_desc(128, kFewRows * kTermsP, true, true);
+    const uint64_t q = tile_k(smem_addr(base)), p = tile_n16(smem_addr(p_mem), 128, kKeys * 16);
+    const uint64_t k_ring = tile_k(smem_addr(base + S::kRingAt)), v_ring = tile_n(smem_addr(base + S::kRingAt), kKeys * 128);
+    const int k_steps = (a.dim + 31) / 32;
+    auto scores = [&](int j) {
+      const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
+      if (!bar_wait(full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
+      tc_after_sync();
+      const uint64_t k = k_ring + slot * (S::kSlot / 16);
+      const uint32_t d = tmem_s + (j & 1) * S::kSTwo;
+      if (elect_one()) {
+        for (int i = 0; i < k_steps; ++i) mma8_ss(d, k + 2 * i, q + 2 * i, desc_s, i > 0);
+        mma_commit(empty + 8 * slot);
+        mma_commit(j & 1 ? s_full_odd : s_full);
+      }
+      __syncwarp();
+      return true;
+    };
+    int asked = 0, done = 0;
+    bool go = bar_wait(q_ready, 0, failed) && scores(0);
+    asked += go;
+    for (int j = 0; go && j < n; ++j) {
+      if (j + 1 < n) {
+        if (!scores(j + 1)) break;
+        ++asked;
+      }
+      const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
+      if (!bar_wait_both(p_ready, j & 1, full + 8 * slot, (e / S::kSlots) & 1, failed)) break;
+      tc_after_sync();
+      const uint64_t v = v_ring + slot * (S::kSlot / 16);
+      if (elect_one()) {
+#pragma unroll
+        for (int i = 0; i < kKeys / 32; ++i) mma8_ss(tmem, v + i * (32 * 128 / 16), p + i * (32 * 16 / 16), desc_o, j > 0 || i > 0);
+        mma_commit(empty + 8 * slot);
+        mma_commit(o_done);
+      }
+      __syncwarp();
+      ++done;
+    }
+    uint32_t quiet = 0;
+    if (asked > 0) bar_pass((asked - 1) & 1 ? s_full_odd : s_full, ((asked - 1) >> 1) & 1, &quiet);
+    if (done > 0) bar_pass(o_done, (done - 1) & 1, &quiet);
+  } else {
+    const int r = threadIdx.x;           // the key of a step, and the dimension of O^T
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    uint32_t meetings = 0;
+    const int shift = __ffs(a.page_tokens) - 1;
+    auto page_of = [&](int32_t key) {
+      return key >= it.lo && key < it.hi ? load_now(a.table + int64_t(it.row) * a.max_pages + (key >> shift)) : -1;
+    };
+    auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
+      *ks = *vs = 1.f;
+      if (page < 0 || page >= a.n_pages) return;
+      const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
+      const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
+      *ks = load_now(s + at);
+      *vs = load_now(s + a.n_kv * blocks + at);
+    };
+    int32_t key = first * kKeys + r;
+    const int32_t page_now = page_of(key);
+    int32_t page_next = page_of(key + kKeys);
+    float unit;                          // of Q's terms
+    {
+      // a row's 8 elements a step, to its terms: codes of row `term * 16 + row`
+      constexpr int kEach = kFewRows * 16 / 128;
+      uint4 v[kEach];
+      uint32_t top = 0;
+      auto raise = [&](uint32_t x) {
+        constexpr uint32_t kInf = std::is_same<T, __nv_bfloat16>::value ? 0x7f80 : 0x7c00;
+        if (x < kInf && x > top) top = x;
+      };
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int x = r + 128 * i, row = x / 16, c = x % 16;
+        v[i] = uint4{};
+        if (row < rows && c * 8 < a.dim) {
+          const int32_t tok = row / a.group;
+          v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
+                                                 (hk * a.group + row - tok * a.group) * g.q_head + c * 8);
+        }
+        for (const uint32_t w : {v[i].x, v[i].y, v[i].z, v[i].w}) raise(w & 0x7fff), raise(w >> 16 & 0x7fff);
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      uint32_t* tops = reinterpret_cast<uint32_t*>(p_mem);
+      if (lane == 0) tops[warp] = top;
+      bar_meet(met, &meetings, failed);
+      top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+      // the tile's largest to between 2^7 and 2^8
+      const float most = up(from_bits<T>(top));
+      const int e = max(min(134 - (int)(__float_as_uint(most) >> 23), 126), -120);
+      float by = __int_as_float((e + 127) << 23);
+      unit = __int_as_float((127 - e) << 23);
+      if (a.negative) by = -by;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int x = r + 128 * i, row = x / 16, c = x % 16;
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        uint64_t xy[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x0 = unpack(T(), w[k], 0) * by, x1 = unpack(T(), w[k], 1) * by;
+          xy[k] = two(fmaf(x0, 0.f, x0), fmaf(x1, 0.f, x1));   // (infinities to NaN: there is no code for them)
+        }
+#pragma unroll
+        for (int t = 0; t < S::kTerms; ++t) {
+          uint32_t o[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t lo = next_term(&xy[2 * k]), hi = next_term(&xy[2 * k + 1]);
+            o[k] = lo | hi << 16;
+          }
+          const int at = t * kFewRows + row;
+          *reinterpret_cast<uint2*>(base + at * 128 + ((c / 2) ^ (at & 7)) * 16 + (c & 1) * 8) = uint2{o[0], o[1]};
+        }
+      }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) bar_arrive(q_ready);
+    }
+    const float c_all = a.scale2 * unit;
+    float ks, vs;
+    scales_of(page_now, key, &ks, &vs);
+    const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
+    uint64_t l2[8];                      // of this key's share of the rows' sums
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l2[i] = 0;
+    for (int j = 0; j < n; ++j, key += kKeys) {
+      const int32_t k0 = (first + j) * kKeys;
+      const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kKeys > all_see;
+      float ks_next, vs_next;
+      scales_of(page_next, key + kKeys, &ks_next, &vs_next);
+      page_next = page_of(key + 2 * kKeys);
+      const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
+      const float lv0 = __log2f(fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f)), lv = lv0 + kBiasFew;
+      uint32_t sees = 0xffffu;           // rows that see this key: those of its token and later ones
+      if (masked) {
+        const int64_t before = key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group;
+        sees = !in || before >= 16 ? 0 : 0xffffu << before;
+      }
+      bar_pass(j & 1 ? s_full_odd : s_full, (j >> 1) & 1, failed);
+      tc_after_sync();
+      const uint32_t s_at = tmem_s + lanes + (j & 1) * S::kSTwo;
+      uint64_t x[8];                     // scores, then exponents, of two rows each
+      auto sums = [&]() {
+        uint32_t t[S::kTerms][16];
+#pragma unroll
+        for (int k = 0; k < S::kTerms; ++k) tmem_load16(s_at + 16 * k, t[k]);
+        tmem_wait_load();
+#pragma unroll
+        for (int k = 0; k < S::kTerms; ++k) tmem_loaded(t[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] = two(__uint_as_float(t[S::kTerms - 1][2 * i]), __uint_as_float(t[S::kTerms - 1][2 * i + 1]));
+#pragma unroll
+          for (int k = S::kTerms - 2; k >= 0; --k)
+            x[i] = fma2(x[i], two(0.0625f, 0.0625f), two(__uint_as_float(t[k][2 * i]), __uint_as_float(t[k][2 * i + 1])));
+        }
+      };
+      auto exponents = [&]() {
+        sums();
+        float most = -INFINITY;
+        const uint64_t c2 = two(c, c), lv2 = two(lv, lv);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 m = reinterpret_cast<const float2*>(misc.neg_m)[i];
+          x[i] = fma2(x[i], c2, add2(two(m.x, m.y), lv2));
+          float u, w;
+          halves(x[i], &u, &w);
+          if (masked) {
+            if (!(sees >> (2 * i) & 1)) u = -INFINITY;
+            if (!(sees >> (2 * i + 1) & 1)) w = -INFINITY;
+            x[i] = two(u, w);
+          }
+          most = max3(most, __float_as_uint(u), __float_as_uint(w));
+        }
+        return most;
+      };
+      if (__any_sync(0xffffffffu, exponents() > kMostFew + kBiasFew) && lane == 0) misc.flag[j & 1] = j + 1;
+      bar_meet(met, &meetings, failed);
+      if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&misc.flag[j & 1]), 0) == j + 1u) {
+        // a reference is raised: the columns' maxima over the keys
+        sums();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float u, w;
+          halves(x[i / 2], &u, &w);
+          float y = fmaf(i & 1 ? w : u, c, lv);
+          if (!(y == y) || !(sees >> i & 1)) y = -INFINITY;
+          const int32_t most = __reduce_max_sync(0xffffffffu, ordered(y));
+          if (lane == i) atomicMax(&misc.top[i], most);
+        }
+        bar_meet(met, &meetings, failed);
+        if (j > 0) {
+          // what the raised references take from the sums and from O's terms
+          bar_pass(o_done, (j - 1) & 1, failed);
+          tc_after_sync();
+          uint64_t f[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float v[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float was = -misc.neg_m[2 * i + k], most = from_ordered(misc.top[2 * i + k]) - kBiasFew;
+              v[k] = most > was ? exp2_fast(was - most) : 1.f;
+            }
+            f[i] = two(v[0], v[1]);
+            l2[i] = fma2(l2[i], f[i], 0ull);
+          }
+#pragma unroll 1
+          for (int k = 0; k < kTermsP; ++k) {
+            uint32_t o[16];
+            tmem_load16(tmem + lanes + 16 * k, o);
+            tmem_wait_load();
+            tmem_loaded(o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float u, w;
+              halves(fma2(two(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1])), f[i], 0ull), &u, &w);
+              o[2 * i] = __float_as_uint(u), o[2 * i + 1] = __float_as_uint(w);
+            }
+            tmem_store16(tmem + lanes + 16 * k, o);
+          }
+          tmem_wait_store();
+        }
+        bar_meet(met, &meetings, failed);
+        if (r < kFewRows) {
+          const float was = -misc.neg_m[r], most = from_ordered(misc.top[r]) - kBiasFew;
+          if (most > was) misc.neg_m[r] = -most;
+          misc.top[r] = kLeast;
+        }
+        bar_meet(met, &meetings, failed);
+        exponents();
+      }
+      const float inv = exp2_fast(-lv0);
+      uint32_t p[kTermsP][4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float u, w;
+        halves(x[i], &u, &w);
+        uint64_t left = two(exp2_fast(u), exp2_fast(w));
+        l2[i] = fma2(left, two(inv, inv), l2[i]);
+#pragma unroll
+        for (int k = 0; k < kTermsP; ++k) {
+          const uint32_t both = next_term(&left);
+          p[k][i / 2] = i & 1 ? p[k][i / 2] | both << 16 : both;
+        }
+      }
+      if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // P is read
+#pragma unroll
+      for (int k = 0; k < kTermsP; ++k)
+        *reinterpret_cast<uint4*>(p_mem + k * (kKeys * 16) + r * 16) = uint4{p[k][0], p[k][1], p[k][2], p[k][3]};
+      if (masked) {
+        // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN that some row
+        // does not see; those that see it get theirs at the end.
+        const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
+        bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
+        const uint32_t query = key <= it.pos0 ? 0 : min(key - it.pos0, 254);
+#pragma unroll 1
+        for (int c16 = 0; c16 < 8; ++c16) {
+          uint4* at = codes_at<128>(base + S::kRingAt + slot * S::kSlot, r, c16);
+          uint4 v = in ? *at : uint4{};
+          drop_nan(&v, misc.first_nan + 4 * c16, query);
+          *at = v;
+        }
+      }
+      fence_async();
+      tc_before_sync();
+      __syncwarp();
+      if (lane == 0) bar_arrive(p_ready);
+      ks = ks_next, vs = vs_next;
+    }
+    bar_pass(o_done, (n - 1) & 1, failed);
+    tc_after_sync();
+    // the rows' sums over the keys, in P's place: [4][16], then 1 / sum
+    float* total = reinterpret_cast<float*>(p_mem);
+    column_sums(l2, total + warp * kFewRows, lane);
+    bar_meet(met, &meetings, failed);
+    if (r < rows) finish_row<T>(a, it, hk, r, ((total[r] + total[kFewRows + r]) + (total[2 * kFewRows + r] + total[3 * kFewRows + r])),
+                                -misc.neg_m[r] - kBiasFew, total + 4 * kFewRows);
+    bar_meet(met, &meetings, failed);
+    // a row after the other, a dimension a thread
+    uint32_t o[kTermsP][16];
+#pragma unroll
+    for (int k = 0; k < kTermsP; ++k) tmem_load16(tmem + lanes + 16 * k, o[k]);
+    tmem_wait_load();
+#pragma unroll
+    for (int k = 0; k < kTermsP; ++k) tmem_loaded(o[k]);
+    Rows<T> at(a, it, hk, 0, r);
+    const int nan_at = misc.first_nan[r / 4] >> (8 * (r % 4)) & 0xff;
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) {
+      float v = __uint_as_float(o[kTermsP - 1][i]);
+#pragma unroll
+      for (int k = kTermsP - 2; k >= 0; --k) v = fmaf(v, 0.0625f, __uint_as_float(o[k][i]));
+      if (i < rows && r < a.dim) at.put(a, it, v, total[4 * kFewRows + i], nan_at);
+      at.next(a);
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  if (warp == 7) tmem_free<1>(tmem, S::kColumns);
+  if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
+}
 
 template <class T, int DP, int kRows>
 __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_constant__ CUtensorMap map_kv,
@@ -287,7 +863,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
     uint32_t meetings = 0;
     const int shift = __ffs(a.page_tokens) - 1;
     auto page_of = [&](int32_t key) {
-      return key >= it.lo && key < it.hi ? a.table[int64_t(it.row) * a.max_pages + (key >> shift)] : -1;
+      return key >= it.lo && key < it.hi ? load_now(a.table + int64_t(it.row) * a.max_pages + (key >> shift)) : -1;
     };
     // the scales of this key's block; of a page that is none 1 (its codes are zeros)
     auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
@@ -295,8 +871,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
       if (page < 0 || page >= a.n_pages) return;
       const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
       const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
-      *ks = __ldg(s + at);
-      *vs = __ldg(s + a.n_kv * blocks + at);
+      *ks = load_now(s + at);
+      *vs = load_now(s + a.n_kv * blocks + at);
     };
     int32_t key = first * kKeys + r;
     int32_t page_now = page_of(key), page_next = page_of(key + kKeys);
@@ -658,9 +1234,20 @@ cudaError_t launch_rows(const op_attend_plan_t& p, const CUtensorMap& kv, const 
   return cudaGetLastError();
 }
 
+template <class T>
+cudaError_t launch_few(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
+  static gsim::OncePerDevice once;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
+  auto kernel = attend8_few_kernel<T>;
+  if (!once.done(dev, [&] { return allow_smem(kernel, FewShape<T>::kSmem); })) return cudaErrorInvalidValue;
+  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), FewShape<T>::kThreads, FewShape<T>::kSmem, st>>>(kv, g);
+  return cudaGetLastError();
+}
+
 template <class T, int DP>
 cudaError_t launch(const op_attend_plan_t& p, int32_t most_rows, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
-  const cudaError_t e = most_rows <= kFew ? launch_rows<T, DP, kFew>(p, kv, g, st) : launch_rows<T, DP, kMany>(p, kv, g, st);
+  const cudaError_t e = most_rows <= kFewRows ? launch_few<T>(p, kv, g, st) : launch_rows<T, DP, kMany>(p, kv, g, st);
   if (e != cudaSuccess || p.n_joins == 0) return e;
   const int64_t heads = (int64_t)p.join_tokens * p.n_heads;
   attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>(heads, 1024)), 128, 0, st>>>(g.a);
@@ -733,7 +1320,7 @@ int op_attend8(const op_attend8_plan_t* plan8, const int32_t* d_items, const op_
   g.scale_at = page8_scales(*cache) + int64_t(layer) * 2 * cache->n_kv_heads * (cache->page_tokens / 16) * 4;
   CUtensorMap map_kv;
   const int64_t size[3] = {cache->head_dim, rows, cache->n_pages}, stride[2] = {cache->head_dim, g.page_bytes};
-  const int32_t dp = cache->head_dim <= 64 ? 64 : 128;
+  const int32_t dp = plan8->most_rows <= kFewRows || cache->head_dim > 64 ? 128 : 64;
   const int32_t box[3] = {dp, std::min(cache->page_tokens, kKeys), 1};
   if (!make_map8(&map_kv, 3, cache->pool, size, stride, box)) return GMG_ECUDA;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
