@@ -128,6 +128,11 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* v) {
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_load4(uint32_t addr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(addr));
+}
 __device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t* v) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
@@ -166,11 +171,28 @@ __device__ void sees_nothing(const AttendArgs& a, const Item& it, int32_t hk, in
   }
 }
 
-// A copying warp: every kCopiers-th slot of K_0 K_1 V_0 K_2 V_1 ..., page by page, rows of kRow bytes.
+// Scales of eight steps, as the copying warps bring them: a step's blocks of 16 keys, K's and then V's.  The copies
+// are at most three steps ahead of the softmax, so a step's place is read before it is written again.
+constexpr int kScaleSteps = 8;
+struct ScaleRing {
+  float s[kScaleSteps][2][kKeys / 16];
+};
+__device__ __forceinline__ void copy_word(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+// An arrival on `bar` when this thread's copies so far are done.
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+constexpr int kFullCount = 33;        // arrivals at a slot's barrier: of its bytes, and of each lane's scales
+
+// A copying warp: every kCopiers-th slot of K_0 K_1 V_0 K_2 V_1 ..., page by page, rows of kRow bytes;
+// with K_j the scales of step j.
 template <int kRow, int kSlots>
-__device__ __forceinline__ void copy_pages(const CUtensorMap& map, const AttendArgs& a, const Item& it, int32_t hk, int32_t first,
+__device__ __forceinline__ void copy_pages(const CUtensorMap& map, const Args8& g, const Item& it, int32_t hk, int32_t first,
                                            int32_t n, int e, int lane, uint32_t slots, uint32_t full, uint32_t empty,
-                                           volatile uint32_t* failed) {
+                                           ScaleRing& scales, volatile uint32_t* failed) {
+  const AttendArgs& a = g.a;
   const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
   // the page numbers come 32 at a time, the next 32 on their way
   const int shift = __ffs(a.page_tokens) - 1;
@@ -181,6 +203,10 @@ __device__ __forceinline__ void copy_pages(const CUtensorMap& map, const AttendA
     return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
   };
   int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
+  auto page_at = [&](int32_t rel) {
+    const int32_t x = __shfl_sync(0xffffffffu, now, rel & 31), y = __shfl_sync(0xffffffffu, next, rel & 31);
+    return rel < 32 ? x : y;
+  };
   for (; e < 2 * n; e += kCopiers) {
     // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
     const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
@@ -197,11 +223,25 @@ __device__ __forceinline__ void copy_pages(const CUtensorMap& map, const AttendA
     const uint32_t bar = full + 8 * slot, dst = slots + slot * (kKeys * kRow);
     if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * kRow);
     for (int32_t k = from; k < to; k += box) {
-      const int32_t rel = ((k0 + k) >> shift) - at0;
-      const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
+      const int32_t page = page_at(((k0 + k) >> shift) - at0);
       const int32_t y = ((a.plane + is_v) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
       if (elect_one()) load_3d(dst + k * kRow, &map, 0, y, page, bar);
     }
+    if (!is_v) {
+      const int32_t k = k0 + (lane & 7) * 16, v = lane >> 3 & 1;
+      const int32_t page = page_at((k >> shift) - at0);
+      float* at = &scales.s[j & (kScaleSteps - 1)][v][lane & 7];
+      if (lane < 16) {
+        if (page < a.n_pages && k < it.hi) {
+          const int32_t blocks = a.page_tokens / 16;
+          copy_word(smem_addr(at), g.pool + page * g.page_bytes + g.scale_at +
+                                       4 * (int64_t(v * a.n_kv + hk) * blocks + (k & (a.page_tokens - 1)) / 16));
+        } else {
+          *at = 1.f;
+        }
+      }
+    }
+    copies_arrive(bar);
   }
   if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
     uint32_t quiet = 0;
@@ -230,11 +270,12 @@ __device__ __forceinline__ void drop_nan(uint4* v, uint32_t* first_nan, uint32_t
   }
 }
 
-// The warp's sums of 16 columns, two a register pair: lane 2 i has column i's in the end.
-__device__ __forceinline__ void column_sums(const uint64_t* l2, float* out, int lane) {
+// 16 columns over the warp's lanes (two a register pair), summed or their largest: lane 2 i has column i's in the end.
+template <class F>
+__device__ __forceinline__ void over_lanes(const uint64_t* pairs, float* out, int lane, F join) {
   float x[16];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) halves(l2[i], &x[2 * i], &x[2 * i + 1]);
+  for (int i = 0; i < 8; ++i) halves(pairs[i], &x[2 * i], &x[2 * i + 1]);
   // each step keeps half of the columns
 #pragma unroll
   for (int d = 16, k = 8; k; d /= 2, k /= 2) {
@@ -244,11 +285,14 @@ __device__ __forceinline__ void column_sums(const uint64_t* l2, float* out, int 
       if (i < k) {
         const float give = upper ? x[i] : x[i + k];
         const float keep = upper ? x[i + k] : x[i];
-        x[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+        x[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, d));
       }
   }
-  x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
+  x[0] = join(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
   if (!(lane & 1)) out[lane / 2] = x[0];
+}
+__device__ __forceinline__ void column_sums(const uint64_t* l2, float* out, int lane) {
+  over_lanes(l2, out, lane, [](float a, float b) { return a + b; });
 }
 
 // A row's sum l of the weights against reference m (log2): 1 / l to inv[row], its log-sum-exp where it goes.
@@ -302,37 +346,42 @@ __device__ __forceinline__ T from_bits(uint32_t v) {
 
 // Numbers of more bits than a code has, as a sum of codes: x = t_0 + t_1 / 16 + t_2 / 256, each the
 // nearest to 16 times what the ones before it leave.  Two terms hold bf16 exactly (as far as 2^-14, of
-// 2^8 at most), three 12 bits and more (as far as 2^-18).
+// 2^8 at most), three 12 bits and more (as far as 2^-18), four 16 (2^-22).
 constexpr int kFewRows = 16;
-constexpr int kTermsP = 3;
-constexpr float kBiasFew = 6.f, kMostFew = 2.75f;   // a weight is at most 2^8.75 < 448
+constexpr float kBiasFew = 4.f, kMostFew = 4.75f;   // a weight is at most 2^8.75 < 448
 
 template <class T>
 struct TermsQ {
   static constexpr int kN = std::is_same<T, __nv_bfloat16>::value ? 2 : 3;
 };
+// Of P, whose numbers below 2^-18 (2^-22) times the largest are lost: bf16's results have 8 bits, fp16's 11.
+template <class T>
+struct TermsP {
+  static constexpr int kN = std::is_same<T, __nv_bfloat16>::value ? 3 : 4;
+};
 
 template <class T>
 struct FewShape {
   static constexpr int kTerms = TermsQ<T>::kN;
+  static constexpr int kTermsP = TermsP<T>::kN;
   static constexpr int kQ = 6144, kP = kTermsP * kKeys * 16;   // Q: terms of 16 rows of 128 bytes
   static constexpr int kSlot = kKeys * 128, kSlots = 6;
   static constexpr int kRingAt = (kQ + kP + 1023) / 1024 * 1024;
   static constexpr int kMiscAt = kRingAt + kSlots * kSlot;
-  static constexpr int kSmem = kMiscAt + 1024;
+  static constexpr int kSmem = kMiscAt + 2048;
   static constexpr int kThreads = 256;
   static constexpr int kColumns = 256, kS = 64, kSTwo = 64;    // of TMEM: O^T, then S^T twice
   static_assert(kSmem <= 115712, "two blocks an SM");
 };
 
 struct FewMisc {
-  float neg_m[kFewRows];
-  int32_t top[kFewRows];
+  ScaleRing scales;
+  float top[4][kFewRows];              // the warps' largest weights where references are raised
   uint32_t first_nan[32];
   uint64_t bars[2 * 6 + 8];
   uint32_t tmem_at, failed, flag[2];
 };
-static_assert(sizeof(FewMisc) <= 1024, "fits behind the ring");
+static_assert(sizeof(FewMisc) <= 2048, "fits behind the ring");
 
 // D (+)= A B^T for 32 codes of A and B.
 __device__ __forceinline__ void mma8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
@@ -373,6 +422,7 @@ template <class T>
 __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(const __grid_constant__ CUtensorMap map_kv,
                                                                              const __grid_constant__ Args8 g) {
   using S = FewShape<T>;
+  constexpr int kTermsP = S::kTermsP;
   extern __shared__ __align__(1024) unsigned char base[];
   const AttendArgs& a = g.a;
   unsigned char* const p_mem = base + S::kQ;
@@ -396,12 +446,11 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
   const uint32_t s_full_odd = met + 8;
   if (warp == 4 && lane == 0) {
     prefetch_map(&map_kv);
-    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, kFullCount), bar_init(empty + 8 * i, 1);
     bar_init(q_ready, 4), bar_init(s_full, 1), bar_init(s_full_odd, 1), bar_init(p_ready, 4), bar_init(o_done, 1), bar_init(met, 4);
     misc.failed = misc.flag[0] = misc.flag[1] = 0;
     fence_bar_init();
   }
-  if (threadIdx.x < kFewRows) misc.neg_m[threadIdx.x] = -kNone, misc.top[threadIdx.x] = kLeast;
   if (threadIdx.x < 32) misc.first_nan[threadIdx.x] = 0xffffffffu;
   if (warp == 7) tmem_alloc<1>(smem_addr(&misc.tmem_at), S::kColumns);
   tc_before_sync();
@@ -410,7 +459,8 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
   const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + S::kS;
 
   if (warp >= 4 && warp < 4 + kCopiers) {
-    copy_pages<128, S::kSlots>(map_kv, a, it, hk, first, n, warp - 4, lane, smem_addr(base + S::kRingAt), full, empty, failed);
+    copy_pages<128, S::kSlots>(map_kv, g, it, hk, first, n, warp - 4, lane, smem_addr(base + S::kRingAt), full, empty, misc.scales,
+                               failed);
   } else if (warp == 7) {
     constexpr uint32_t desc_s = mma8_desc(kKeys, kFewRows * S::kTerms, false, false),
                        desc_o = mma8_desc(128, kFewRows * kTermsP, true, true);
@@ -459,21 +509,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
     const int r = threadIdx.x;           // the key of a step, and the dimension of O^T
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     uint32_t meetings = 0;
-    const int shift = __ffs(a.page_tokens) - 1;
-    auto page_of = [&](int32_t key) {
-      return key >= it.lo && key < it.hi ? load_now(a.table + int64_t(it.row) * a.max_pages + (key >> shift)) : -1;
-    };
-    auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
-      *ks = *vs = 1.f;
-      if (page < 0 || page >= a.n_pages) return;
-      const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
-      const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
-      *ks = load_now(s + at);
-      *vs = load_now(s + a.n_kv * blocks + at);
-    };
     int32_t key = first * kKeys + r;
-    const int32_t page_now = page_of(key);
-    int32_t page_next = page_of(key + kKeys);
     float unit;                          // of Q's terms
     {
       // a row's 8 elements a step, to its terms: codes of row `term * 16 + row`
@@ -533,20 +569,16 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       if (lane == 0) bar_arrive(q_ready);
     }
     const float c_all = a.scale2 * unit;
-    float ks, vs;
-    scales_of(page_now, key, &ks, &vs);
     const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
     uint64_t l2[8];                      // of this key's share of the rows' sums
 #pragma unroll
     for (int i = 0; i < 8; ++i) l2[i] = 0;
+    uint64_t neg_m[8];                   // minus the rows' references; all threads have the same
+#pragma unroll
+    for (int i = 0; i < 8; ++i) neg_m[i] = two(-kNone, -kNone);
     for (int j = 0; j < n; ++j, key += kKeys) {
       const int32_t k0 = (first + j) * kKeys;
       const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kKeys > all_see;
-      float ks_next, vs_next;
-      scales_of(page_next, key + kKeys, &ks_next, &vs_next);
-      page_next = page_of(key + 2 * kKeys);
-      const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
-      const float lv0 = __log2f(fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f)), lv = lv0 + kBiasFew;
       uint32_t sees = 0xffffu;           // rows that see this key: those of its token and later ones
       if (masked) {
         const int64_t before = key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group;
@@ -555,6 +587,9 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       bar_pass(j & 1 ? s_full_odd : s_full, (j >> 1) & 1, failed);
       tc_after_sync();
       const uint32_t s_at = tmem_s + lanes + (j & 1) * S::kSTwo;
+      const float ks = misc.scales.s[j & (kScaleSteps - 1)][0][r / 16], vs = misc.scales.s[j & (kScaleSteps - 1)][1][r / 16];
+      const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
+      const float lv0 = __log2f(fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f)), lv = lv0 + kBiasFew;
       uint64_t x[8];                     // scores, then exponents, of two rows each
       auto sums = [&]() {
         uint32_t t[S::kTerms][16];
@@ -577,8 +612,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
         const uint64_t c2 = two(c, c), lv2 = two(lv, lv);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float2 m = reinterpret_cast<const float2*>(misc.neg_m)[i];
-          x[i] = fma2(x[i], c2, add2(two(m.x, m.y), lv2));
+          x[i] = fma2(x[i], c2, add2(neg_m[i], lv2));
           float u, w;
           halves(x[i], &u, &w);
           if (masked) {
@@ -593,34 +627,37 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       if (__any_sync(0xffffffffu, exponents() > kMostFew + kBiasFew) && lane == 0) misc.flag[j & 1] = j + 1;
       bar_meet(met, &meetings, failed);
       if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&misc.flag[j & 1]), 0) == j + 1u) {
-        // a reference is raised: the columns' maxima over the keys
+        // references are raised: the columns' maxima over the keys
         sums();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 8; ++i) {
           float u, w;
-          halves(x[i / 2], &u, &w);
-          float y = fmaf(i & 1 ? w : u, c, lv);
-          if (!(y == y) || !(sees >> i & 1)) y = -INFINITY;
-          const int32_t most = __reduce_max_sync(0xffffffffu, ordered(y));
-          if (lane == i) atomicMax(&misc.top[i], most);
+          halves(x[i], &u, &w);
+          u = fmaf(u, c, lv), w = fmaf(w, c, lv);
+          if (!(u == u) || !(sees >> (2 * i) & 1)) u = -INFINITY;
+          if (!(w == w) || !(sees >> (2 * i + 1) & 1)) w = -INFINITY;
+          x[i] = two(u, w);
         }
+        over_lanes(x, misc.top[warp], lane, [](float u, float w) { return fmaxf(u, w); });
         bar_meet(met, &meetings, failed);
+        uint64_t f[8];                   // what they take from the sums and from O's terms
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float u, w;
+          halves(neg_m[i], &u, &w);
+          float tops[2] = {-u, -w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 t = *reinterpret_cast<const float2*>(&misc.top[k][2 * i]);
+            tops[0] = fmaxf(tops[0], t.x - kBiasFew), tops[1] = fmaxf(tops[1], t.y - kBiasFew);
+          }
+          neg_m[i] = two(-tops[0], -tops[1]);
+          f[i] = two(-u == tops[0] ? 1.f : exp2_fast(-u - tops[0]), -w == tops[1] ? 1.f : exp2_fast(-w - tops[1]));
+          l2[i] = fma2(l2[i], f[i], 0ull);
+        }
         if (j > 0) {
-          // what the raised references take from the sums and from O's terms
           bar_pass(o_done, (j - 1) & 1, failed);
           tc_after_sync();
-          uint64_t f[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float v[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float was = -misc.neg_m[2 * i + k], most = from_ordered(misc.top[2 * i + k]) - kBiasFew;
-              v[k] = most > was ? exp2_fast(was - most) : 1.f;
-            }
-            f[i] = two(v[0], v[1]);
-            l2[i] = fma2(l2[i], f[i], 0ull);
-          }
 #pragma unroll 1
           for (int k = 0; k < kTermsP; ++k) {
             uint32_t o[16];
@@ -637,13 +674,6 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
           }
           tmem_wait_store();
         }
-        bar_meet(met, &meetings, failed);
-        if (r < kFewRows) {
-          const float was = -misc.neg_m[r], most = from_ordered(misc.top[r]) - kBiasFew;
-          if (most > was) misc.neg_m[r] = -most;
-          misc.top[r] = kLeast;
-        }
-        bar_meet(met, &meetings, failed);
         exponents();
       }
       const float inv = exp2_fast(-lv0);
@@ -682,33 +712,45 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       tc_before_sync();
       __syncwarp();
       if (lane == 0) bar_arrive(p_ready);
-      ks = ks_next, vs = vs_next;
     }
     bar_pass(o_done, (n - 1) & 1, failed);
     tc_after_sync();
     // the rows' sums over the keys, in P's place: [4][16], then 1 / sum
     float* total = reinterpret_cast<float*>(p_mem);
     column_sums(l2, total + warp * kFewRows, lane);
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (lane == i) {
+          float u, w;
+          halves(neg_m[i], &u, &w);
+          misc.top[0][2 * i] = -u, misc.top[0][2 * i + 1] = -w;
+        }
+    }
     bar_meet(met, &meetings, failed);
-    if (r < rows) finish_row<T>(a, it, hk, r, ((total[r] + total[kFewRows + r]) + (total[2 * kFewRows + r] + total[3 * kFewRows + r])),
-                                -misc.neg_m[r] - kBiasFew, total + 4 * kFewRows);
+    if (r < rows)
+      finish_row<T>(a, it, hk, r, (total[r] + total[kFewRows + r]) + (total[2 * kFewRows + r] + total[3 * kFewRows + r]),
+                    misc.top[0][r] - kBiasFew, total + 4 * kFewRows);
     bar_meet(met, &meetings, failed);
     // a row after the other, a dimension a thread
-    uint32_t o[kTermsP][16];
-#pragma unroll
-    for (int k = 0; k < kTermsP; ++k) tmem_load16(tmem + lanes + 16 * k, o[k]);
-    tmem_wait_load();
-#pragma unroll
-    for (int k = 0; k < kTermsP; ++k) tmem_loaded(o[k]);
     Rows<T> at(a, it, hk, 0, r);
     const int nan_at = misc.first_nan[r / 4] >> (8 * (r % 4)) & 0xff;
+#pragma unroll 1
+    for (int row = 0; row < rows; row += 4) {
+      uint32_t o[kTermsP][4];
 #pragma unroll
-    for (int i = 0; i < kFewRows; ++i) {
-      float v = __uint_as_float(o[kTermsP - 1][i]);
+      for (int k = 0; k < kTermsP; ++k) tmem_load4(tmem + lanes + 16 * k + row, o[k]);
+      tmem_wait_load();
 #pragma unroll
-      for (int k = kTermsP - 2; k >= 0; --k) v = fmaf(v, 0.0625f, __uint_as_float(o[k][i]));
-      if (i < rows && r < a.dim) at.put(a, it, v, total[4 * kFewRows + i], nan_at);
-      at.next(a);
+      for (int k = 0; k < kTermsP; ++k) tmem_loaded(o[k]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v = __uint_as_float(o[kTermsP - 1][i]);
+#pragma unroll
+        for (int k = kTermsP - 2; k >= 0; --k) v = fmaf(v, 0.0625f, __uint_as_float(o[k][i]));
+        if (row + i < rows && r < a.dim) at.put(a, it, v, total[4 * kFewRows + row + i], nan_at);
+        at.next(a);
+      }
     }
   }
   __syncwarp();
