@@ -203,11 +203,11 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
               float* lse, void* work, size_t work_bytes, gmg_stream_t stream);
 
 /* The same over a cache in 8 bits, for q and out of type dtype (bf16 or fp16); n_heads /
- * n_kv_heads at most 64.  Codes are exact in the products, probabilities (times the values'
- * scales) rounded to fp16 for theirs. */
+ * n_kv_heads at most 128.  Codes and q are exact in the products, probabilities (times the values'
+ * scales) rounded to 11 bits or more for theirs. */
 typedef struct {
   op_attend_plan_t p;
-  int32_t most_rows, reserved;  /* query heads times queries of the largest item, of a key/value head */
+  int32_t few, reserved;        /* whether its items have few rows (query heads times queries of a key/value head) */
 } op_attend8_plan_t;
 
 int op_attend8_plan(const op_attend_desc_t* desc, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,

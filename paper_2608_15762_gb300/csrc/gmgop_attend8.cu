@@ -1,26 +1,23 @@
 // Attention over a paged cache in 8 bits, with a scale for each block of 16 tokens and head.  The C
 // ABI is declared in include/gmgop.h.
 //
-// A work item is up to 64 rows (queries of consecutive tokens, all query heads of one key/value
-// head: row = token * heads + head) against a run of keys, 128 a step.  The products are turned
-// round: keys fill the tensor core's 128 lanes and rows are columns, so that a step of few rows
-// (a decode step has 4 to 8) costs few columns, few exponentials and few registers:
-//   S^T [128 keys][rows] = K Q^T,   O^T [128 dims][rows] += V^T P^T.
-// A thread of the softmax holds one key, so the scales of its block are numbers of its own.
-// Codes become fp16 on the way, which holds e4m3 exactly: keys go into TMEM, values into shared
-// memory.  Q (times a power of two that brings the tile's largest to 2^13, so that bf16's 8 bits
-// lie in fp16's range) and P are fp16 too.
-// One block takes one item:
-//   warps 0 to 3    the softmax of S_j; in tiles of 64 rows of half of them, and K_{j+1} to fp16
-//   warps 4 to 7    V_j to fp16, and K_{j+2}; in tiles of 64 rows the softmax of the others instead
-//   warps 8 to 10   copies: page by page into a ring of 128-key slots, K_0 K_1 V_0 K_2 V_1 ...
-//   warp 11         products
-// With value scales v_j, P holds w = exp2(s + log2 v - m) and the sum takes w / v: one exponent
-// for both, so that P uses fp16's range whatever the scales, and O has them right.  The reference
+// With value scales v_j, P holds w = exp2(s + log2 v - m) and a row's sum takes w / v: one exponent
+// for both, so that P uses its type's range whatever the scales, and O has them right.  The reference
 // m is of the w and need not be the exact running maximum: it is raised where a w would exceed
-// 2^11 times it (times 2^4 for fp16's small numbers).
-// P is rounded to fp16 because the tensor cores take it so (the sum is of the unrounded): 2^-11.
-
+// a power of two times it.
+//
+// Tiles of up to 16 rows (queries of consecutive tokens, all query heads of one key/value head:
+// row = token * heads + head), a decode step's, turn the products round:
+//   S^T [128 keys][rows] = K Q^T,   O^T [128 dims][rows] += V^T P^T.
+// Keys fill the tensor core's 128 lanes and rows are columns, so that a step of few rows costs few columns,
+// exponentials and registers, and K and V are read once, as the codes that they are, by fp8 products.
+// What the codes meet is split into several of them: Q exactly, P to 12 bits or more.
+//
+// Tiles of more rows, up to 128, lie with their rows on the lanes, against 64 keys a step; K and V
+// become fp16, which holds e4m3 exactly, on their way through shared memory, and Q (times a power of
+// two, so that bf16's 8 bits lie in fp16's range) and P are fp16: P's rounding, 2^-11, is
+// what the tensor cores take.
+//
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -40,12 +37,8 @@
 namespace gop {
 namespace {
 
-constexpr int kKeys = 128;             // a step
-constexpr int kFew = 32, kMany = 64;   // rows of a tile: what a kernel has room for
-constexpr int kThreads = 384, kCopiers = 3;
-constexpr float kBias = 4.f, kMost = 11.f;   // a weight is at most 2^(kMost + kBias)
+constexpr int kCopiers = 3;
 constexpr float kNone = -1e30f;        // the reference of a row that has seen nothing
-constexpr uint32_t kTurnedA = 1u << 15;   // A lies with its rows (M) contiguous
 
 struct Args8 {
   AttendArgs a;
@@ -54,32 +47,6 @@ struct Args8 {
   const unsigned char* pool;
   int64_t page_bytes, scale_at;        // of a page; of the layer's scales in it
 };
-
-template <int DP, int kRows>
-struct Shape {
-  static constexpr int kHalves = DP / 64;
-  static constexpr int kQ = kHalves * kRows * 128;
-  static constexpr int kP = kKeys * kRows * 2;
-  static constexpr int kV = kHalves * kKeys * 128;
-  static constexpr int kSlot = kKeys * DP;
-  static constexpr int kSlots = (kRows == kFew ? 65536 : 49152) / kSlot;
-  static constexpr int kMiscAt = kQ + kP + kV + kSlots * kSlot;
-  static constexpr int kSmem = kMiscAt + 1024;
-  // TMEM: O^T, S^T twice, then K (fp16, two a column) once or, for few rows, twice
-  static constexpr int kColumns = 256, kS = kRows, kK = 3 * kRows, kKeep = kRows == kFew ? 2 : 1;
-  static_assert(kSmem <= 115712 && kK + kKeep * 64 <= kColumns, "two blocks an SM");
-};
-
-template <int DP, int kRows>
-struct Misc {
-  float neg_m[kRows];                  // minus the rows' references
-  int32_t top[kRows];                  // their largest weights where they are raised, as ordered integers
-  uint32_t first_nan[32];              // by dimension, a byte: the first query that sees a NaN where rows see different keys
-  uint64_t bars[2 * Shape<DP, kRows>::kSlots + 10];
-  uint32_t tmem_at, failed, flag[4];   // flag: the step (+ 1) that raises a reference, by half of the rows and step parity
-};
-static_assert(sizeof(Misc<128, kMany>) <= 1024 && sizeof(Misc<64, kMany>) <= 1024 && sizeof(Misc<64, kFew>) <= 1024,
-              "fits behind the ring");
 
 // Two e4m3 to two fp16, exactly.
 __device__ __forceinline__ uint32_t wide2(uint16_t v) {
@@ -94,23 +61,6 @@ __device__ __forceinline__ void wide16(uint4 v, uint32_t* o) {
     o[2 * i] = wide2((uint16_t)w[i]);
     o[2 * i + 1] = wide2((uint16_t)(w[i] >> 16));
   }
-}
-
-// As tile_n, of 32 rows (N) in 64 bytes and the 64-byte swizzle; the next 8 columns 512 on.
-__device__ __forceinline__ uint64_t tile_n64(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
-}
-
-// Loads that stay where they are written, ahead of their use.
-__device__ __forceinline__ float load_now(const float* p) {
-  float v;
-  asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ int32_t load_now(const int32_t* p) {
-  int32_t v;
-  asm volatile("ld.global.nc.s32 %0, [%1];" : "=r"(v) : "l"(p));
-  return v;
 }
 
 // 16 codes of a row of a slot, where the copy has put them.
@@ -133,20 +83,6 @@ __device__ __forceinline__ void tmem_load4(uint32_t addr, uint32_t* v) {
                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
                : "r"(addr));
 }
-__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t* v) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-               : "r"(addr));
-}
-
-// Order of floats as that of int32, and back.
-__device__ __forceinline__ int32_t ordered(float v) {
-  const int32_t i = __float_as_int(v);
-  return i ^ ((i >> 31) & 0x7fffffff);
-}
-__device__ __forceinline__ float from_ordered(int32_t i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
-constexpr int32_t kLeast = INT32_MIN;
-
 // Registers of a warp group's threads: what the copies and products leave, the softmax has.
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -171,9 +107,10 @@ __device__ void sees_nothing(const AttendArgs& a, const Item& it, int32_t hk, in
   }
 }
 
-// Scales of eight steps, as the copying warps bring them: a step's blocks of 16 keys, K's and then V's.  The copies
-// are at most three steps ahead of the softmax, so a step's place is read before it is written again.
+// Scales of eight steps, as the copying warps bring them: a step's blocks of 16 keys, K's and then V's.  With the
+// slots that there are a step's place is read before the copies are eight steps further.
 constexpr int kScaleSteps = 8;
+template <int kKeys>
 struct ScaleRing {
   float s[kScaleSteps][2][kKeys / 16];
 };
@@ -188,10 +125,10 @@ constexpr int kFullCount = 33;        // arrivals at a slot's barrier: of its by
 
 // A copying warp: every kCopiers-th slot of K_0 K_1 V_0 K_2 V_1 ..., page by page, rows of kRow bytes;
 // with K_j the scales of step j.
-template <int kRow, int kSlots>
+template <int kKeys, int kRow, int kSlots>
 __device__ __forceinline__ void copy_pages(const CUtensorMap& map, const Args8& g, const Item& it, int32_t hk, int32_t first,
                                            int32_t n, int e, int lane, uint32_t slots, uint32_t full, uint32_t empty,
-                                           ScaleRing& scales, volatile uint32_t* failed) {
+                                           ScaleRing<kKeys>& scales, volatile uint32_t* failed) {
   const AttendArgs& a = g.a;
   const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
   // the page numbers come 32 at a time, the next 32 on their way
@@ -228,10 +165,11 @@ __device__ __forceinline__ void copy_pages(const CUtensorMap& map, const Args8& 
       if (elect_one()) load_3d(dst + k * kRow, &map, 0, y, page, bar);
     }
     if (!is_v) {
-      const int32_t k = k0 + (lane & 7) * 16, v = lane >> 3 & 1;
+      constexpr int kBlocks = kKeys / 16;
+      const int32_t k = k0 + lane % kBlocks * 16, v = lane / kBlocks & 1;
       const int32_t page = page_at((k >> shift) - at0);
-      float* at = &scales.s[j & (kScaleSteps - 1)][v][lane & 7];
-      if (lane < 16) {
+      float* at = &scales.s[j & (kScaleSteps - 1)][v][lane % kBlocks];
+      if (lane < 2 * kBlocks) {
         if (page < a.n_pages && k < it.hi) {
           const int32_t blocks = a.page_tokens / 16;
           copy_word(smem_addr(at), g.pool + page * g.page_bytes + g.scale_at +
@@ -252,7 +190,8 @@ __device__ __forceinline__ void copy_pages(const CUtensorMap& map, const Args8& 
 }
 
 // Codes that are NaN become zeros; first_nan, a byte a dimension, falls to the first query that sees one.
-__device__ __forceinline__ void drop_nan(uint4* v, uint32_t* first_nan, uint32_t query) {
+__device__ __forceinline__ bool drop_nan(uint4* v, uint32_t* first_nan, uint32_t query) {
+  bool any = false;
   uint32_t* w = reinterpret_cast<uint32_t*>(v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -266,8 +205,10 @@ __device__ __forceinline__ void drop_nan(uint4* v, uint32_t* first_nan, uint32_t
           was = found;
         }
         w[i] &= ~(0xffu << (8 * b));
+        any = true;
       }
   }
+  return any;
 }
 
 // 16 columns over the warp's lanes (two a register pair), summed or their largest: lane 2 i has column i's in the end.
@@ -347,7 +288,7 @@ __device__ __forceinline__ T from_bits(uint32_t v) {
 // Numbers of more bits than a code has, as a sum of codes: x = t_0 + t_1 / 16 + t_2 / 256, each the
 // nearest to 16 times what the ones before it leave.  Two terms hold bf16 exactly (as far as 2^-14, of
 // 2^8 at most), three 12 bits and more (as far as 2^-18), four 16 (2^-22).
-constexpr int kFewRows = 16;
+constexpr int kFewKeys = 128, kFewRows = 16;   // of a step, of a tile
 constexpr float kBiasFew = 4.f, kMostFew = 4.75f;   // a weight is at most 2^8.75 < 448
 
 template <class T>
@@ -364,8 +305,8 @@ template <class T>
 struct FewShape {
   static constexpr int kTerms = TermsQ<T>::kN;
   static constexpr int kTermsP = TermsP<T>::kN;
-  static constexpr int kQ = 6144, kP = kTermsP * kKeys * 16;   // Q: terms of 16 rows of 128 bytes
-  static constexpr int kSlot = kKeys * 128, kSlots = 6;
+  static constexpr int kQ = 6144, kP = kTermsP * kFewKeys * 16;   // Q: terms of 16 rows of 128 bytes
+  static constexpr int kSlot = kFewKeys * 128, kSlots = 6;
   static constexpr int kRingAt = (kQ + kP + 1023) / 1024 * 1024;
   static constexpr int kMiscAt = kRingAt + kSlots * kSlot;
   static constexpr int kSmem = kMiscAt + 2048;
@@ -375,7 +316,7 @@ struct FewShape {
 };
 
 struct FewMisc {
-  ScaleRing scales;
+  ScaleRing<kFewKeys> scales;
   float top[4][kFewRows];              // the warps' largest weights where references are raised
   uint32_t first_nan[32];
   uint64_t bars[2 * 6 + 8];
@@ -432,7 +373,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
   const int32_t item = blockIdx.x / a.n_kv, hk = blockIdx.x - item * a.n_kv;
   const Item it = a.items[item];
   const int32_t rows = it.n_tok * a.group;
-  const int32_t first = it.lo / kKeys, n = it.hi > it.lo ? (it.hi + kKeys - 1) / kKeys - first : 0;
+  const int32_t first = it.lo / kFewKeys, n = it.hi > it.lo ? (it.hi + kFewKeys - 1) / kFewKeys - first : 0;
 
   if (n == 0) {   // queries that see nothing
     sees_nothing<T>(a, it, hk, rows);
@@ -459,13 +400,13 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
   const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + S::kS;
 
   if (warp >= 4 && warp < 4 + kCopiers) {
-    copy_pages<128, S::kSlots>(map_kv, g, it, hk, first, n, warp - 4, lane, smem_addr(base + S::kRingAt), full, empty, misc.scales,
+    copy_pages<kFewKeys, 128, S::kSlots>(map_kv, g, it, hk, first, n, warp - 4, lane, smem_addr(base + S::kRingAt), full, empty, misc.scales,
                                failed);
   } else if (warp == 7) {
-    constexpr uint32_t desc_s = mma8_desc(kKeys, kFewRows * S::kTerms, false, false),
+    constexpr uint32_t desc_s = mma8_desc(kFewKeys, kFewRows * S::kTerms, false, false),
                        desc_o = mma8_desc(128, kFewRows * kTermsP, true, true);
-    const uint64_t q = tile_k(smem_addr(base)), p = tile_n16(smem_addr(p_mem), 128, kKeys * 16);
-    const uint64_t k_ring = tile_k(smem_addr(base + S::kRingAt)), v_ring = tile_n(smem_addr(base + S::kRingAt), kKeys * 128);
+    const uint64_t q = tile_k(smem_addr(base)), p = tile_n16(smem_addr(p_mem), 128, kFewKeys * 16);
+    const uint64_t k_ring = tile_k(smem_addr(base + S::kRingAt)), v_ring = tile_n(smem_addr(base + S::kRingAt), kFewKeys * 128);
     const int k_steps = (a.dim + 31) / 32;
     auto scores = [&](int j) {
       const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
@@ -495,7 +436,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       const uint64_t v = v_ring + slot * (S::kSlot / 16);
       if (elect_one()) {
 #pragma unroll
-        for (int i = 0; i < kKeys / 32; ++i) mma8_ss(tmem, v + i * (32 * 128 / 16), p + i * (32 * 16 / 16), desc_o, j > 0 || i > 0);
+        for (int i = 0; i < kFewKeys / 32; ++i) mma8_ss(tmem, v + i * (32 * 128 / 16), p + i * (32 * 16 / 16), desc_o, j > 0 || i > 0);
         mma_commit(empty + 8 * slot);
         mma_commit(o_done);
       }
@@ -509,7 +450,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
     const int r = threadIdx.x;           // the key of a step, and the dimension of O^T
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     uint32_t meetings = 0;
-    int32_t key = first * kKeys + r;
+    int32_t key = first * kFewKeys + r;
     float unit;                          // of Q's terms
     {
       // a row's 8 elements a step, to its terms: codes of row `term * 16 + row`
@@ -576,9 +517,9 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
     uint64_t neg_m[8];                   // minus the rows' references; all threads have the same
 #pragma unroll
     for (int i = 0; i < 8; ++i) neg_m[i] = two(-kNone, -kNone);
-    for (int j = 0; j < n; ++j, key += kKeys) {
-      const int32_t k0 = (first + j) * kKeys;
-      const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kKeys > all_see;
+    for (int j = 0; j < n; ++j, key += kFewKeys) {
+      const int32_t k0 = (first + j) * kFewKeys;
+      const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kFewKeys > all_see;
       uint32_t sees = 0xffffu;           // rows that see this key: those of its token and later ones
       if (masked) {
         const int64_t before = key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group;
@@ -693,7 +634,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // P is read
 #pragma unroll
       for (int k = 0; k < kTermsP; ++k)
-        *reinterpret_cast<uint4*>(p_mem + k * (kKeys * 16) + r * 16) = uint4{p[k][0], p[k][1], p[k][2], p[k][3]};
+        *reinterpret_cast<uint4*>(p_mem + k * (kFewKeys * 16) + r * 16) = uint4{p[k][0], p[k][1], p[k][2], p[k][3]};
       if (masked) {
         // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN that some row
         // does not see; those that see it get theirs at the end.
@@ -760,16 +701,51 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
   if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
 }
 
-template <class T, int DP, int kRows>
+
+// ---------------------------------------------------------------------------
+// Many rows: codes to fp16 on the way
+// ---------------------------------------------------------------------------
+
+//   warps 0 to 3    the softmax: a thread holds one row
+//   warps 4 to 7    K and V from slots of codes to slots of fp16
+//   warps 8 to 10   copies: page by page into a ring of 64-key slots, K_0 K_1 V_0 K_2 V_1 ...
+//   warp 11         products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
+constexpr int kKeys = 64, kRows = 128;   // of a step, of a tile
+constexpr int kThreads = 384;
+constexpr float kBias = 7.f, kMost = 8.f;   // a weight is at most 2^(kMost + kBias), in fp16's range
+
+template <int DP>
+struct Shape {
+  static constexpr int kQ = kRows * DP * 2;
+  static constexpr int kSlot = kKeys * DP * 2, kSlots = 49152 / kSlot;         // of fp16
+  static constexpr int kCodes = kKeys * DP, kCodeSlots = 4;
+  static constexpr int kCodesAt = kQ + kSlots * kSlot;
+  static constexpr int kMiscAt = kCodesAt + kCodeSlots * kCodes;
+  static constexpr int kSmem = kMiscAt + 1024;
+  static constexpr int kColumns = 256;                    // of TMEM: O, then two buffers of S
+  static_assert(kSmem <= 115712, "two blocks an SM");
+};
+
+template <int DP>
+struct Misc {
+  float2 step[kScaleSteps][4];         // of a step's blocks of 16 keys: what a score is multiplied by, log2 v
+  ScaleRing<kKeys> scales;
+  uint32_t first_nan[32];              // by dimension, a byte: the first query that sees a NaN where rows see different keys
+  uint64_t bars[2 * Shape<DP>::kSlots + 2 * Shape<DP>::kCodeSlots + 9];
+  uint32_t tmem_at, failed, any_nan, unit;
+};
+static_assert(sizeof(Misc<128>) <= 1024 && sizeof(Misc<64>) <= 1024, "fits behind the slots");
+
+__device__ __forceinline__ float in_range(float scale) { return fminf(fmaxf(scale, 8.6736174e-19f), 1.1529215e18f); }   // 2^-60 .. 2^60
+
+template <class T, int DP>
 __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_constant__ CUtensorMap map_kv,
                                                               const __grid_constant__ Args8 g) {
-  using S = Shape<DP, kRows>;
-  constexpr bool kHalved = kRows == kMany;   // the softmax of a tile's halves by different warps
+  using S = Shape<DP>;
   extern __shared__ __align__(1024) unsigned char base[];
   const AttendArgs& a = g.a;
-  unsigned char *const p_mem = base + S::kQ, *const v_mem = p_mem + S::kP, *const ring = v_mem + S::kV;
-  using M = Misc<DP, kRows>;
-  M& misc = *reinterpret_cast<M*>(base + S::kMiscAt);
+  unsigned char *const ring = base + S::kQ, *const code_ring = base + S::kCodesAt;
+  Misc<DP>& misc = *reinterpret_cast<Misc<DP>*>(base + S::kMiscAt);
   volatile uint32_t* failed = &misc.failed;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   // all heads of an item, then the next item: the long ones start first
@@ -778,163 +754,102 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
   const int32_t rows = it.n_tok * a.group;
   const int32_t first = it.lo / kKeys, n = it.hi > it.lo ? (it.hi + kKeys - 1) / kKeys - first : 0;
 
-  if (n == 0) {   // queries that see nothing
-    for (int r = threadIdx.x; r < rows; r += kThreads) {
-      const int64_t t = it.tok0 + r / a.group;
-      const int32_t h = hk * a.group + r % a.group;
-      T* o = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
-      for (int d = 0; d < a.dim; d += 8) *reinterpret_cast<uint4*>(o + d) = uint4{};
-      if (a.lse) a.lse[t * a.n_heads + h] = -INFINITY;
-    }
+  if (n == 0) {
+    sees_nothing<T>(a, it, hk, rows);
     return;
   }
 
-  const int n_c = (rows + 15) / 16;     // columns, 16 at a time
-  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, q_ready = empty + 8 * S::kSlots,
-                 k_ready = q_ready + 8, s_full = k_ready + 16, v_ready = s_full + 16, o_done = v_ready + 8,
-                 met = o_done + 8, all_met = met + 16;
-  // k_ready and s_full are two barriers each, for even and odd steps, as K_{j+1} and S_{j+1} may come before
-  // all have waited for those of step j.  What arrives at a barrier's phase after next needs that all have
-  // waited for this one, so a wait tells its phase from the one before it.
+  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, code_full = empty + 8 * S::kSlots,
+                 code_empty = code_full + 8 * S::kCodeSlots, q_ready = code_empty + 8 * S::kCodeSlots, s_full = q_ready + 8,
+                 p_ready = s_full + 16, o_done = p_ready + 16, all_met = o_done + 16;
+  // s_full, p_ready and o_done are two barriers each, for even and odd steps.  A wait tells a phase
+  // from the one before it only, and every wait here has that one behind it: S_j is computed
+  // after the product of step j - 2 is done.
   if (warp == 8 && lane == 0) {
     prefetch_map(&map_kv);
-    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 4);
-    bar_init(q_ready, 8), bar_init(k_ready, 4), bar_init(k_ready + 8, 4), bar_init(s_full, 1), bar_init(s_full + 8, 1), bar_init(v_ready, 8);
-    bar_init(o_done, 1), bar_init(met, 4), bar_init(met + 8, 4), bar_init(all_met, 8);
-    misc.failed = misc.flag[0] = misc.flag[1] = misc.flag[2] = misc.flag[3] = 0;
+    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 4), bar_init(empty + 8 * i, 1);
+    for (int i = 0; i < S::kCodeSlots; ++i) bar_init(code_full + 8 * i, kFullCount), bar_init(code_empty + 8 * i, 4);
+    bar_init(q_ready, 8), bar_init(all_met, 8);
+    for (int i = 0; i < 2; ++i) bar_init(s_full + 8 * i, 1), bar_init(p_ready + 8 * i, 4), bar_init(o_done + 8 * i, 1);
+    misc.failed = misc.any_nan = 0;
     fence_bar_init();
   }
-  if (threadIdx.x < kRows) misc.neg_m[threadIdx.x] = -kNone, misc.top[threadIdx.x] = kLeast;
   if (threadIdx.x < 32) misc.first_nan[threadIdx.x] = 0xffffffffu;
   if (warp == 11) tmem_alloc<1>(smem_addr(&misc.tmem_at), S::kColumns);
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + S::kS, tmem_k = tmem + S::kK;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, misc.tmem_at, 0), tmem_s = tmem + 128;
+  const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
 
   if (warp >= 8) {
-    fewer_registers<32>();
+    fewer_registers<40>();
     if (warp < 8 + kCopiers) {
-      const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
-      const uint32_t slots = smem_addr(ring);
-      // the page numbers come 32 at a time, the next 32 on their way
-      const int shift = __ffs(a.page_tokens) - 1;
-      const int32_t last = (it.hi - 1) >> shift;
-      int32_t at0 = first * kKeys >> shift;
-      auto look_up = [&](int32_t i) {
-        const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
-        return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
-      };
-      int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
-      int e = warp - 8;
-      for (; e < 2 * n; e += kCopiers) {
-        // the e-th copy: K of step (e + 1) / 2 if e is 0 or odd (and not the last), else V
-        const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
-        const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
-        const int slot = e % S::kSlots;
-        const int32_t k0 = (first + j) * kKeys;
-        const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
-        if (is_v && (k0 >> shift) - at0 >= 32) {   // K is at most three steps ahead of V, 24 pages
-          at0 += 32;
-          now = next;
-          next = look_up(at0 + 32 + lane);
-        }
-        if (!bar_wait(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed)) break;
-        const uint32_t bar = full + 8 * slot, dst = slots + slot * S::kSlot;
-        if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * DP);
-        for (int32_t k = from; k < to; k += box) {
-          const int32_t rel = ((k0 + k) >> shift) - at0;
-          const int32_t page = rel < 32 ? __shfl_sync(0xffffffffu, now, rel) : __shfl_sync(0xffffffffu, next, rel - 32);
-          const int32_t y = ((a.plane + is_v) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
-          if (elect_one()) load_3d(dst + k * DP, &map_kv, 0, y, page, bar);
-        }
-      }
-      if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
-        uint32_t quiet = 0;
-        for (int b = e - kCopiers; b >= 0 && b > e - kCopiers - S::kSlots; b -= kCopiers)
-          bar_pass(full + 8 * (b % S::kSlots), (b / S::kSlots) & 1, &quiet);
-      }
-      __syncwarp();
+      copy_pages<kKeys, DP, S::kCodeSlots>(map_kv, g, it, hk, first, n, warp - 8, lane, smem_addr(code_ring), code_full, code_empty,
+                                           misc.scales, failed);
     } else {
       // the whole warp goes along; one lane issues
-      const uint32_t desc_s = mma_desc(false, kKeys, 16 * n_c, false), desc_o = mma_desc(false, 128, 16 * n_c, true) | kTurnedA;
-      const uint64_t q = tile_k(smem_addr(base)), p = kHalved ? tile_n(smem_addr(p_mem), kKeys * 128) : tile_n64(smem_addr(p_mem)),
-                     v = tile_n(smem_addr(v_mem), kKeys * 128);
-      auto scores = [&](int j) {
-        if (!bar_wait(k_ready + 8 * (j & 1), (j >> 1) & 1, failed)) return false;
+      constexpr uint32_t desc_s = mma_desc(false, kRows, kKeys, false), desc_o = mma_desc(false, kRows, DP, true);
+      const uint64_t q = tile_k(smem_addr(base)), k_ring = tile_k(smem_addr(ring)), v_ring = tile_n(smem_addr(ring), kKeys * 128);
+      auto scores = [&](int j, uint32_t behind, uint32_t parity) {   // behind: what S_j waits for besides K_j
+        const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
+        if (!bar_wait_both(behind, parity, full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
         tc_after_sync();
-        const uint32_t d = tmem_s + (j & 1) * kRows, k = tmem_k + j % S::kKeep * 64;
+        const uint64_t k = k_ring + slot * (S::kSlot / 16);
+        const uint32_t d = tmem_s + (j & 1) * kKeys;
         if (elect_one()) {
 #pragma unroll
           for (int i = 0; i < DP / 16; ++i)
-            mma_ts(d, k + 8 * i, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), desc_s, i > 0);
+            mma_ss<1>(d, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), k + (i / 4) * (kKeys * 128 / 16) + 2 * (i % 4), desc_s, i > 0);
+          mma_commit(empty + 8 * slot);
           mma_commit(s_full + 8 * (j & 1));
         }
         __syncwarp();
         return true;
       };
       int asked = 0, done = 0;            // S and O that are on their way
-      bool go = bar_wait(q_ready, 0, failed) && scores(0);
+      bool go = scores(0, q_ready, 0);
       asked += go;
+      if (go && n > 1) go = scores(1, q_ready, 0), asked += go;
       for (int j = 0; go && j < n; ++j) {
-        if (j + 1 < n) {
-          if (!scores(j + 1)) break;
-          ++asked;
-        }
-        if (!bar_wait(v_ready, j & 1, failed)) break;
+        const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
+        if (!bar_wait_both(p_ready + 8 * (j & 1), (j >> 1) & 1, full + 8 * slot, (e / S::kSlots) & 1, failed)) break;
         tc_after_sync();
+        const uint64_t v = v_ring + slot * (S::kSlot / 16);
+        const uint32_t p = tmem_s + (j & 1) * kKeys;
         if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < kKeys / 16; ++i)
-            mma_ss<1>(tmem, v + i * (16 * 128 / 16), p + i * (16 * kRows * 2 / 16), desc_o, j > 0 || i > 0);
-          mma_commit(o_done);
+          for (int i = 0; i < kKeys / 16; ++i) mma_ts(tmem, p + i * 8, v + i * (16 * 128 / 16), desc_o, j > 0 || i > 0);
+          mma_commit(empty + 8 * slot);
+          mma_commit(o_done + 8 * (j & 1));
         }
         __syncwarp();
         ++done;
+        // S_{j+2} takes the place of P_j: once its product is done
+        if (j + 2 < n) go = scores(j + 2, o_done + 8 * (j & 1), (j >> 1) & 1), asked += go;
       }
       uint32_t quiet = 0;
       if (asked > 0) bar_pass(s_full + 8 * ((asked - 1) & 1), ((asked - 1) >> 1) & 1, &quiet);
-      if (done > 0) bar_pass(o_done, (done - 1) & 1, &quiet);
+      if (done > 0) bar_pass(o_done + 8 * ((done - 1) & 1), ((done - 1) >> 1) & 1, &quiet);
     }
   } else {
-    more_registers<104>();
-    const int half = warp / 4, r = threadIdx.x & 127;   // the key of a step, and the dimension of O^T
-    // this half's columns, 16 at a time
-    const int q0 = half ? (n_c + 1) / 2 : 0, q_n = !kHalved ? (half ? 0 : n_c) : half ? n_c / 2 : (n_c + 1) / 2;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, met_half = met + 8 * half;
-    uint32_t meetings = 0;
-    const int shift = __ffs(a.page_tokens) - 1;
-    auto page_of = [&](int32_t key) {
-      return key >= it.lo && key < it.hi ? load_now(a.table + int64_t(it.row) * a.max_pages + (key >> shift)) : -1;
-    };
-    // the scales of this key's block; of a page that is none 1 (its codes are zeros)
-    auto scales_of = [&](int32_t page, int32_t key, float* ks, float* vs) {
-      *ks = *vs = 1.f;
-      if (page < 0 || page >= a.n_pages) return;
-      const float* s = reinterpret_cast<const float*>(g.pool + page * g.page_bytes + g.scale_at);
-      const int32_t blocks = a.page_tokens / 16, at = hk * blocks + (key & (a.page_tokens - 1)) / 16;
-      *ks = load_now(s + at);
-      *vs = load_now(s + a.n_kv * blocks + at);
-    };
-    int32_t key = first * kKeys + r;
-    int32_t page_now = page_of(key), page_next = page_of(key + kKeys);
+    // Q to shared memory, 16 bytes a step: consecutive threads along a row
     float by = 1.f, unit = 1.f;          // Q is scaled by `by`; |1 / by|
     {
-      // Q to shared memory, 16 bytes a step: consecutive threads along a row
       constexpr int kEach = kRows * DP / 8 / 256;
-      uint4 v[kEach];
-      uint32_t top = 0;                  // of |q| where finite, its bits
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
+      auto load = [&](int i) {
         const int x = threadIdx.x + 256 * i, row = x / (DP / 8), c = x % (DP / 8);
-        v[i] = uint4{};
-        if (row < rows && c * 8 < a.dim) {
-          const int32_t tok = row / a.group;
-          v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
-                                                 (hk * a.group + row - tok * a.group) * g.q_head + c * 8);
-        }
-        if (std::is_same<T, __nv_bfloat16>::value) {
-          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        if (row >= rows || c * 8 >= a.dim) return uint4{};
+        const int32_t tok = row / a.group;
+        return *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
+                                               (hk * a.group + row - tok * a.group) * g.q_head + c * 8);
+      };
+      if (std::is_same<T, __nv_bfloat16>::value) {
+        uint32_t top = 0;                // of |q| where finite, its bits
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const uint4 v = load(i);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const uint32_t lo = w[k] & 0x7fff, hi = (w[k] >> 16) & 0x7fff;
@@ -942,317 +857,197 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
             if (hi < 0x7f80 && hi > top) top = hi;
           }
         }
-      }
-      if (std::is_same<T, __nv_bfloat16>::value) {
         top = __reduce_max_sync(0xffffffffu, top);
-        uint32_t* tops = reinterpret_cast<uint32_t*>(p_mem);
+        uint32_t* tops = reinterpret_cast<uint32_t*>(misc.step);
         if (lane == 0) tops[warp] = top;
-        uint32_t first_meeting = 0;
-        bar_meet(all_met, &first_meeting, failed);
+        uint32_t meetings = 0;
+        bar_meet(all_met, &meetings, failed);
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, tops[i]);
         const int e = max(min(140 - (int)(top >> 7), 126), -114);   // 2^13 over the largest's power of two
         by = __int_as_float((e + 127) << 23);
         unit = __int_as_float((127 - e) << 23);
+        bar_meet(all_met, &meetings, failed);
       }
       if (a.negative) by = -by;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int x = threadIdx.x + 256 * i, row = x / (DP / 8), c = x % (DP / 8);
-        if (row >= 16 * n_c) continue;
+        const uint4 v = load(i);
         uint4 o;
-        o.x = to_q(T(), v[i].x, by), o.y = to_q(T(), v[i].y, by), o.z = to_q(T(), v[i].z, by), o.w = to_q(T(), v[i].w, by);
+        o.x = to_q(T(), v.x, by), o.y = to_q(T(), v.y, by), o.z = to_q(T(), v.z, by), o.w = to_q(T(), v.w, by);
         *reinterpret_cast<uint4*>(base + (c / 8) * (kRows * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16) = o;
       }
       fence_async();
       __syncwarp();
       if (lane == 0) bar_arrive(q_ready);
     }
-    const float c_all = a.scale2 * unit;
-    float ks, vs;
-    scales_of(page_now, key, &ks, &vs);
-    auto put_keys = [&](int j) {
-      const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
-      bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
-#pragma unroll
-      for (int h = 0; h < S::kHalves; ++h) {
-        uint32_t o[32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) wide16(*codes_at<DP>(ring + slot * S::kSlot, r, 4 * h + c), o + 8 * c);
-        tmem_store32(tmem_k + j % S::kKeep * 64 + lanes + 32 * h, o);
-      }
-      tmem_wait_store();
-      tc_before_sync();
-      __syncwarp();
-      if (lane == 0) bar_arrive(empty + 8 * slot), bar_arrive(k_ready + 8 * (j & 1));
-    };
-    // V_j to shared memory.  `some`: not every row sees every key
-    auto put_values = [&](int j, bool in, auto some) {
-      constexpr bool kSome = decltype(some)::value;
-      const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
-      bar_pass(full + 8 * slot, (e / S::kSlots) & 1, failed);
-#pragma unroll
-      for (int c16 = 0; c16 < DP / 16; ++c16) {
-        uint4 v = *codes_at<DP>(ring + slot * S::kSlot, r, c16);
-        if (kSome) {
-          // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN
-          // that some row does not see; those that see it get theirs at the end.
-          if (!in) v = uint4{};
-          uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-          const uint32_t query = key <= it.pos0 ? 0 : min(key - it.pos0, 254);
-#pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            if (!(((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) continue;
-            for (int b = 0; b < 4; ++b)
-              if ((w[i] >> (8 * b) & 0x7f) == 0x7f) {
-                uint32_t* word = &misc.first_nan[4 * c16 + i];
-                uint32_t was = *reinterpret_cast<volatile uint32_t*>(word);
-                while ((was >> (8 * b) & 0xff) > query) {   // (ends: the byte only falls)
-                  const uint32_t found = atomicCAS(word, was, (was & ~(0xffu << (8 * b))) | query << (8 * b));
-                  if (found == was) break;
-                  was = found;
-                }
-                w[i] &= ~(0xffu << (8 * b));
-              }
-          }
+    if (warp >= 4) {
+      fewer_registers<72>();
+      const int r = threadIdx.x & 63, part = (threadIdx.x - 128) / 64;   // a key, half of its dimensions
+      const float c_all = a.scale2 * unit;
+      for (int e = 0; e < 2 * n; ++e) {
+        const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
+        const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
+        const int slot = e % S::kSlots, code_slot = e % S::kCodeSlots;
+        const int32_t k0 = (first + j) * kKeys, key = k0 + r;
+        bar_pass(code_full + 8 * code_slot, (e / S::kCodeSlots) & 1, failed);
+        if (!is_v && threadIdx.x - 128 < 4) {
+          const int b = threadIdx.x - 128;
+          const float ks = misc.scales.s[j & (kScaleSteps - 1)][0][b], vs = misc.scales.s[j & (kScaleSteps - 1)][1][b];
+          misc.step[j & (kScaleSteps - 1)][b] = float2{c_all * in_range(ks), __log2f(in_range(vs))};
         }
-        uint32_t o[8];
-        wide16(v, o);
+        bar_pass(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed);
+        unsigned char *from = code_ring + code_slot * S::kCodes, *to = ring + slot * S::kSlot;
+        const bool masked = is_v && (k0 < it.lo || k0 + kKeys > all_see);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          *reinterpret_cast<uint4*>(v_mem + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + i) % 8) ^ (r & 7)) * 16) =
-              uint4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
-      }
-      __syncwarp();
-      if (lane == 0) bar_arrive(empty + 8 * slot);
-    };
-    const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
-    if (half == (kHalved ? 0 : 1)) {
-      put_keys(0);
-      if (!kHalved && n > 1) put_keys(1);
-    }
-    uint64_t l2[16];                     // of this key's share of the sums of this half's rows
+        for (int i = 0; i < DP / 32; ++i) {
+          const int c16 = part * (DP / 32) + i;
+          uint4 v = *codes_at<DP>(from, r, c16);
+          if (masked) {
+            // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN that
+            // some row does not see; those that see it get theirs at the end.
+            if (key < it.lo || key >= it.hi) v = uint4{};
+            if (drop_nan(&v, misc.first_nan + 4 * c16, key <= it.pos0 ? 0 : min(key - it.pos0, 254))) misc.any_nan = 1;
+          }
+          uint32_t o[8];
+          wide16(v, o);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) l2[i] = 0;
-    for (int j = 0; j < n; ++j, key += kKeys) {
-      const int32_t k0 = (first + j) * kKeys;
-      const bool in = key >= it.lo && key < it.hi, masked = k0 < it.lo || k0 + kKeys > all_see;
-      float ks_next = 1.f, vs_next = 1.f;
-      if (kHalved || half == 0) {
-        scales_of(page_next, key + kKeys, &ks_next, &vs_next);
-        page_next = page_of(key + 2 * kKeys);
+          for (int k = 0; k < 2; ++k)
+            *reinterpret_cast<uint4*>(to + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + k) % 8) ^ (r & 7)) * 16) =
+                uint4{o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]};
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) bar_arrive(code_empty + 8 * code_slot), bar_arrive(full + 8 * slot);
       }
-      if (half == 0) {
+    } else {
+      more_registers<128>();
+      const int r = threadIdx.x;
+      const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+      const int32_t tok = r / a.group;
+      // the keys that this row sees end here; rows beyond the tile's see what the last one does
+      const int32_t own = tok < it.n_tok ? tok : it.n_tok - 1;
+      const int32_t end = it.pos0 + own + 1 < it.hi ? it.pos0 + own + 1 : it.hi;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n; ++j) {
+        const int32_t k0 = (first + j) * kKeys;
         bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
         tc_after_sync();
-        if (kHalved && j + 1 < n) put_keys(j + 1);
-      } else {
-        if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // V is read
-        if (masked) put_values(j, in, std::true_type());
-        else put_values(j, in, std::false_type());
-        if (!kHalved) {
-          fence_async();
-          __syncwarp();
-          if (lane == 0) bar_arrive(v_ready);
-          if (j + 2 < n) {
-            bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);   // K_j is read
+        const uint32_t s_at = tmem_s + lanes + (j & 1) * kKeys;
+        uint32_t s[64];
+        tmem_load32(s_at, s);
+        tmem_load32(s_at + 32, s + 32);
+        float2 block[4];                 // of 16 keys
+#pragma unroll
+        for (int b = 0; b < 4; ++b) block[b] = misc.step[j & (kScaleSteps - 1)][b];
+        tmem_wait_load();
+        tmem_loaded(s);
+        // the weights' exponents, without the reference; -inf for what this row does not see
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float x, y;
+          const float2 b = block[i / 8];
+          halves(fma2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), two(b.x, b.x), two(b.y, b.y)), &x, &y);
+          s[2 * i] = __float_as_uint(x), s[2 * i + 1] = __float_as_uint(y);
+        }
+        if (k0 < it.lo || k0 + kKeys > all_see) {
+          const int below = it.lo > k0 ? it.lo - k0 : 0, upto = end - k0 < 0 ? 0 : end - k0 < kKeys ? end - k0 : kKeys;
+          const uint64_t sees = upto <= below ? 0 : (upto == 64 ? ~0ull : (1ull << upto) - 1) & ~((1ull << below) - 1);
+#pragma unroll
+          for (int i = 0; i < 64; ++i)
+            if (!(sees >> i & 1)) s[i] = 0xff800000u;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mx[i & 3] = max3(mx[i & 3], s[2 * i], s[2 * i + 1]);
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        const bool raise = top > m + kMost || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xffffffffu, raise)) {
+          const float f = raise ? (m == -INFINITY ? 0.f : exp2_fast(m - top)) : 1.f;
+          if (raise) m = top;
+          l *= f;
+          if (j > 0) {
+            bar_pass(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);
             tc_after_sync();
-            put_keys(j + 2);
-          }
-          continue;
-        }
-        if (q_n > 0) bar_pass(s_full + 8 * (j & 1), (j >> 1) & 1, failed);
-        tc_after_sync();
-      }
-      if (q_n > 0) {
-        // x = s c + log2 v - m, of two rows a register pair
-        const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
-        const float lv0 = __log2f(fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f)), lv = lv0 + kBias;
-        const uint32_t s_at = tmem_s + lanes + (j & 1) * kRows + 16 * q0;
-        // rows that see this key: those of its token and later ones
-        uint32_t sees = ~0u;
-        if (masked) {
-          const int64_t before = (key <= it.pos0 ? 0 : int64_t(key - it.pos0) * a.group) - 16 * q0;
-          sees = !in || before >= 32 ? 0 : before <= 0 ? ~0u : ~0u << before;
-        }
-        uint32_t s[32];
-        auto exponents = [&]() {         // over s; returns the largest
-          tmem_load16(s_at, s);
-          if (q_n > 1) tmem_load16(s_at + 16, s + 16);
-          tmem_wait_load();
-          tmem_loaded(s);
-          const uint64_t c2 = two(c, c), lv2 = two(lv, lv);
-          float most[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (q < q_n) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float4 m = reinterpret_cast<const float4*>(misc.neg_m)[4 * (q0 + q) + i];
-                float x, y, z, w;
-                uint32_t* at = s + 16 * q + 4 * i;
-                halves(fma2(two(__uint_as_float(at[0]), __uint_as_float(at[1])), c2, add2(two(m.x, m.y), lv2)), &x, &y);
-                halves(fma2(two(__uint_as_float(at[2]), __uint_as_float(at[3])), c2, add2(two(m.z, m.w), lv2)), &z, &w);
-                at[0] = __float_as_uint(x), at[1] = __float_as_uint(y), at[2] = __float_as_uint(z), at[3] = __float_as_uint(w);
-              }
-            }
-          if (masked)
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(sees >> i & 1)) s[i] = 0xff800000u;
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (q < q_n)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) most[i & 1] = max3(most[i & 1], s[16 * q + 2 * i], s[16 * q + 2 * i + 1]);
-          return fmaxf(most[0], most[1]);
-        };
-        uint32_t* flag = &misc.flag[2 * half + (j & 1)];
-        if (__any_sync(0xffffffffu, exponents() > kMost + kBias) && lane == 0) *flag = j + 1;
-        bar_meet(met_half, &meetings, failed);
-        if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(flag), 0) == j + 1u) {
-          // a reference is raised: the columns' maxima over the keys
 #pragma unroll 1
-          for (int q = 0; q < q_n; ++q) {
-            uint32_t t[16];
-            tmem_load16(s_at + 16 * q, t);
-            tmem_wait_load();
-            tmem_loaded(t);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float x = fmaf(__uint_as_float(t[i]), c, lv);
-              if (!(x == x) || !(sees >> (16 * q + i) & 1)) x = -INFINITY;
-              const int32_t most = __reduce_max_sync(0xffffffffu, ordered(x));
-              if (lane == i) atomicMax(&misc.top[16 * (q0 + q) + i], most);
-            }
-          }
-          bar_meet(met_half, &meetings, failed);
-          // what a raised reference takes from the sums and from O (there is nothing yet in the first step)
-          auto factor = [&](int col) {
-            const float was = -misc.neg_m[col], most = from_ordered(misc.top[col]) - kBias;
-            return most > was + kMost ? exp2_fast(was - most) : 1.f;
-          };
-          if (j > 0) bar_pass(o_done, (j - 1) & 1, failed);
-          tc_after_sync();
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (q < q_n && j > 0) {
+            for (int d = 0; d < DP; d += 16) {
               uint32_t o[16];
-              tmem_load16(tmem + lanes + 16 * (q0 + q), o);
+              tmem_load16(tmem + lanes + d, o);
               tmem_wait_load();
               tmem_loaded(o);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float f = factor(16 * (q0 + q) + 2 * i), h = factor(16 * (q0 + q) + 2 * i + 1);
-                float x, y;
-                halves(l2[8 * q + i], &x, &y);
-                l2[8 * q + i] = two(x * f, y * h);
-                o[2 * i] = __float_as_uint(__uint_as_float(o[2 * i]) * f);
-                o[2 * i + 1] = __float_as_uint(__uint_as_float(o[2 * i + 1]) * h);
-              }
-              tmem_store16(tmem + lanes + 16 * (q0 + q), o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_store16(tmem + lanes + d, o);
             }
-          tmem_wait_store();
-          bar_meet(met_half, &meetings, failed);
-          if (r < 16 * q_n) {
-            const int col = 16 * q0 + r;
-            const float was = -misc.neg_m[col], most = from_ordered(misc.top[col]) - kBias;
-            if (most > was + kMost) misc.neg_m[col] = -most;
-            misc.top[col] = kLeast;
+            tmem_wait_store();
           }
-          bar_meet(met_half, &meetings, failed);
-          exponents();
         }
-        if (half == 0 && j > 0) bar_pass(o_done, (j - 1) & 1, failed);   // P is read
-        const float inv = exp2_fast(-lv0);
-        const uint64_t inv2 = two(inv, inv);
+        const float shift = m == -INFINITY ? 0.f : kBias - m;
+        const uint64_t shift2 = two(shift, shift);
+        uint32_t p[32];
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-          if (q < q_n) {
-            uint32_t p[8];
+        for (int b = 0; b < 4; ++b) {
+          uint64_t sum[2] = {};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float x = exp2_fast(__uint_as_float(s[16 * q + 2 * i])), y = exp2_fast(__uint_as_float(s[16 * q + 2 * i + 1]));
-              l2[8 * q + i] = fma2(two(x, y), inv2, l2[8 * q + i]);
-              p[i] = pack(__half(), x, y);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              *reinterpret_cast<uint4*>(p_mem + r * (2 * kRows) + ((2 * (q0 + q) + i) ^ (kHalved ? r & 7 : (r >> 1) & 3)) * 16) =
-                  uint4{p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]};
+          for (int i = 8 * b; i < 8 * b + 8; ++i) {
+            float x, y;
+            halves(add2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), shift2), &x, &y);
+            x = exp2_fast(x), y = exp2_fast(y);
+            sum[i & 1] = add2(sum[i & 1], two(x, y));
+            p[i] = pack(__half(), x, y);
           }
-      }
-      fence_async();
-      tc_before_sync();
-      __syncwarp();
-      if (lane == 0) bar_arrive(v_ready);
-      ks = ks_next, vs = vs_next;
-    }
-    bar_pass(o_done, (n - 1) & 1, failed);
-    tc_after_sync();
-    // the rows' sums over the keys, in P's place: [4][kRows], then 1 / sum
-    float* sums = reinterpret_cast<float*>(p_mem);
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-      if (q < q_n) {
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) halves(l2[8 * q + i], &x[2 * i], &x[2 * i + 1]);
-        // lane i ends with column i / 2: each step keeps half of the columns
-#pragma unroll
-        for (int d = 16, k = 8; k; d /= 2, k /= 2) {
-          const bool upper = lane & d;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < k) {
-              const float give = upper ? x[i] : x[i + k];
-              const float keep = upper ? x[i + k] : x[i];
-              x[i] = keep + __shfl_xor_sync(0xffffffffu, give, d);
-            }
+          float x, y;
+          halves(add2(sum[0], sum[1]), &x, &y);
+          l = fmaf(x + y, exp2_fast(-block[b].y), l);
         }
-        x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
-        if (!(lane & 1)) sums[(warp & 3) * kRows + 16 * (q0 + q) + lane / 2] = x[0];
+        tmem_store32(s_at, p);
+        tmem_wait_store();
+        tc_before_sync();
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_ready + 8 * (j & 1));
       }
-    bar_meet(met_half, &meetings, failed);
-    const int row = 16 * q0 + r;
-    if (r < 16 * q_n && row < rows) {
-      const float l = (sums[row] + sums[kRows + row]) + (sums[2 * kRows + row] + sums[3 * kRows + row]);
-      const float lse2 = l == 0.f ? -INFINITY : -misc.neg_m[row] - kBias + log2f(l);
-      sums[4 * kRows + row] = l == 0.f ? 0.f : 1.f / l;
-      if (it.part >= 0) {
-        a.part_lse[hk * a.part_rows + it.part + row] = lse2;
-      } else if (a.lse) {
-        const int32_t tok = row / a.group;
-        a.lse[(int64_t)(it.tok0 + tok) * a.n_heads + hk * a.group + row - tok * a.group] = lse2 * 0.69314718055994531f;
+      bar_pass(o_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1, failed);
+      tc_after_sync();
+      const bool in = tok < it.n_tok, any_nan = *reinterpret_cast<volatile uint32_t*>(&misc.any_nan);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float lse2 = l == 0.f ? -INFINITY : m - kBias + log2f(l);
+      const int32_t h = hk * a.group + r - tok * a.group;
+      const int64_t t = it.tok0 + tok;
+      const int64_t part = hk * a.part_rows + it.part + r;
+      T* out = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+      float* part_o = a.part_o + part * a.dim;
+      if (in) {
+        if (it.part >= 0) a.part_lse[part] = lse2;
+        else if (a.lse) a.lse[t * a.n_heads + h] = lse2 * 0.69314718055994531f;
       }
-    }
-    bar_meet(met_half, &meetings, failed);
-    // a row after the other, a dimension a thread
-    const int nan_at = misc.first_nan[r / 4] >> (8 * (r % 4)) & 0xff;
-    int32_t tok = 16 * q0 / a.group, h = 16 * q0 - tok * a.group;
-    float* part = a.part_o + (hk * a.part_rows + it.part + 16 * q0) * a.dim + r;
-    T* out = static_cast<T*>(a.out) + (it.tok0 + tok) * a.o_tok + (hk * a.group + h) * a.o_head + r;
-    const int64_t next_tok = a.o_tok - (a.group - 1) * a.o_head;
-    const int last_row = rows < 16 * (q0 + q_n) ? rows : 16 * (q0 + q_n);
 #pragma unroll 1
-    for (int at = 16 * q0; at < last_row; at += 8) {
-      uint32_t o[8];
-      tmem_load8(tmem + lanes + at, o);
-      const float4 i0 = *reinterpret_cast<const float4*>(sums + 4 * kRows + at), i1 = *reinterpret_cast<const float4*>(sums + 4 * kRows + at + 4);
-      const float inv[8] = {i0.x, i0.y, i0.z, i0.w, i1.x, i1.y, i1.z, i1.w};
-      tmem_wait_load();
-      tmem_loaded(o);
+      for (int d = 0; d < a.dim; d += 16) {
+        uint32_t o[16];
+        tmem_load16(tmem + lanes + d, o);
+        tmem_wait_load();
+        tmem_loaded(o);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (at + i < last_row && r < a.dim) {
-          float v = inv[i] == 0.f ? 0.f : __uint_as_float(o[i]) * inv[i];
-          if (nan_at <= tok) v = NAN;
-          if (it.part >= 0) __stcg(part, v);
-          else *reinterpret_cast<unsigned short*>(out) = (unsigned short)pack(T(), v, v);
+        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(l == 0.f ? 0.f : __uint_as_float(o[i]) * inv);
+        if (any_nan)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if ((int)(misc.first_nan[(d + i) / 4] >> (8 * (i % 4)) & 0xff) <= tok) o[i] = 0x7fc00000u;
+        if (in && it.part >= 0) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) __stcg(reinterpret_cast<uint4*>(part_o + d + i), uint4{o[i], o[i + 1], o[i + 2], o[i + 3]});
+        } else if (in) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 8) {
+            uint4 v;
+            v.x = pack(T(), __uint_as_float(o[i]), __uint_as_float(o[i + 1]));
+            v.y = pack(T(), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+            v.z = pack(T(), __uint_as_float(o[i + 4]), __uint_as_float(o[i + 5]));
+            v.w = pack(T(), __uint_as_float(o[i + 6]), __uint_as_float(o[i + 7]));
+            *reinterpret_cast<uint4*>(out + d + i) = v;
+          }
         }
-        part += a.dim;
-        if (++h == a.group) h = 0, ++tok, out += next_tok;
-        else out += a.o_head;
+        __syncwarp();
       }
     }
   }
@@ -1263,16 +1058,26 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
   if (threadIdx.x == 0 && *failed) atomicAdd(&a.status[5], 1);
 }
 
-constexpr Cutting kCutting = {kKeys, kMany, 4, 8, 3, 5, true};
+// A plan is for one of the kernels: the one whose steps and items take less time (in clocks; the many rows' steps are of
+// 64 keys).
+constexpr Cutting kCuttingFew = {kFewKeys, kFewRows, 4, 8, 3, 5, true}, kCuttingMany = {kKeys, kRows, 6, 12, 4, 8, true};
+constexpr int64_t kFewClocks = 1900, kManyClocks = 1300;
 
-template <class T, int DP, int kRows>
-cudaError_t launch_rows(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
+int64_t steps_of(const Work& w, const Cutting& cut) {
+  int64_t steps = 0;
+  for (const Item& it : w.items)
+    steps += cut.item_steps + (it.hi > it.lo ? (it.hi + cut.keys - 1) / cut.keys - it.lo / cut.keys : 0);
+  return steps;
+}
+
+template <class T, int DP>
+cudaError_t launch_many(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
   static gsim::OncePerDevice once;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
-  auto kernel = attend8_kernel<T, DP, kRows>;
-  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP, kRows>::kSmem); })) return cudaErrorInvalidValue;
-  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP, kRows>::kSmem, st>>>(kv, g);
+  auto kernel = attend8_kernel<T, DP>;
+  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP>::kSmem); })) return cudaErrorInvalidValue;
+  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(kv, g);
   return cudaGetLastError();
 }
 
@@ -1288,8 +1093,8 @@ cudaError_t launch_few(const op_attend_plan_t& p, const CUtensorMap& kv, const A
 }
 
 template <class T, int DP>
-cudaError_t launch(const op_attend_plan_t& p, int32_t most_rows, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
-  const cudaError_t e = most_rows <= kFewRows ? launch_few<T>(p, kv, g, st) : launch_rows<T, DP, kMany>(p, kv, g, st);
+cudaError_t launch(const op_attend_plan_t& p, bool few, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
+  const cudaError_t e = few ? launch_few<T>(p, kv, g, st) : launch_many<T, DP>(p, kv, g, st);
   if (e != cudaSuccess || p.n_joins == 0) return e;
   const int64_t heads = (int64_t)p.join_tokens * p.n_heads;
   attend_join_kernel<T><<<dim3((unsigned)p.n_joins, (unsigned)std::min<int64_t>(heads, 1024)), 128, 0, st>>>(g.a);
@@ -1305,13 +1110,16 @@ extern "C" {
 
 int op_attend8_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,
                     size_t item_bytes) try {
-  if (!desc_ok(d, kMany) || d->head_dim % 16 || d->page_tokens < 16 || !plan || n_sm < 1) return GMG_EINVAL;
-  Work w;
-  plan_items(*d, n_sm, kCutting, &w);
-  int32_t most = 0;
-  for (const Item& it : w.items) most = std::max(most, it.n_tok * (d->n_heads / d->n_kv_heads));
-  const int rc = fill_plan(d, w, &plan->p, items, item_bytes);
-  if (rc == GMG_OK) plan->most_rows = most;
+  if (!desc_ok(d, kRows) || d->head_dim % 16 || d->page_tokens < 16 || !plan || n_sm < 1) return GMG_EINVAL;
+  Work few, many;
+  plan_items(*d, n_sm, kCuttingMany, &many);
+  bool is_few = d->n_heads / d->n_kv_heads <= kFewRows;
+  if (is_few) {
+    plan_items(*d, n_sm, kCuttingFew, &few);
+    is_few = steps_of(few, kCuttingFew) * kFewClocks <= steps_of(many, kCuttingMany) * kManyClocks;
+  }
+  const int rc = fill_plan(d, is_few ? few : many, &plan->p, items, item_bytes);
+  if (rc == GMG_OK) plan->few = is_few, plan->reserved = 0;
   return rc;
 } catch (const std::bad_alloc&) {
   return GMG_ENOMEM;
@@ -1362,15 +1170,15 @@ int op_attend8(const op_attend8_plan_t* plan8, const int32_t* d_items, const op_
   g.scale_at = page8_scales(*cache) + int64_t(layer) * 2 * cache->n_kv_heads * (cache->page_tokens / 16) * 4;
   CUtensorMap map_kv;
   const int64_t size[3] = {cache->head_dim, rows, cache->n_pages}, stride[2] = {cache->head_dim, g.page_bytes};
-  const int32_t dp = plan8->most_rows <= kFewRows || cache->head_dim > 64 ? 128 : 64;
-  const int32_t box[3] = {dp, std::min(cache->page_tokens, kKeys), 1};
+  const int32_t dp = plan8->few || cache->head_dim > 64 ? 128 : 64;
+  const int32_t box[3] = {dp, std::min(cache->page_tokens, plan8->few ? kFewKeys : kKeys), 1};
   if (!make_map8(&map_kv, 3, cache->pool, size, stride, box)) return GMG_ECUDA;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (dtype == GMG_OP_BF16)
-    e = dp == 64 ? launch<__nv_bfloat16, 64>(*plan, plan8->most_rows, map_kv, g, st) : launch<__nv_bfloat16, 128>(*plan, plan8->most_rows, map_kv, g, st);
+    e = dp == 64 ? launch<__nv_bfloat16, 64>(*plan, plan8->few, map_kv, g, st) : launch<__nv_bfloat16, 128>(*plan, plan8->few, map_kv, g, st);
   else
-    e = dp == 64 ? launch<__half, 64>(*plan, plan8->most_rows, map_kv, g, st) : launch<__half, 128>(*plan, plan8->most_rows, map_kv, g, st);
+    e = dp == 64 ? launch<__half, 64>(*plan, plan8->few, map_kv, g, st) : launch<__half, 128>(*plan, plan8->few, map_kv, g, st);
   return e == cudaSuccess ? GMG_OK : GMG_ECUDA;
 }
 

@@ -57,7 +57,7 @@ class _AttendPlan(C.Structure):
 
 
 class _AttendPlan8(C.Structure):
-    _fields_ = _AttendPlan._fields_ + [("most_rows", C.c_int32), ("reserved", C.c_int32)]
+    _fields_ = _AttendPlan._fields_ + [("few", C.c_int32), ("reserved", C.c_int32)]
 
 
 class _Linear(C.Structure):
@@ -514,7 +514,7 @@ class AttendPlan:
 
 
 class AttendPlan8(AttendPlan):
-    """An ``AttendPlan`` for ``attend8``: at most 64 query heads for each key/value head."""
+    """An ``AttendPlan`` for ``attend8``."""
 
     bits = 8
 
