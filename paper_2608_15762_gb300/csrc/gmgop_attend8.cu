@@ -13,10 +13,10 @@
 // exponentials and registers, and K and V are read once, as the codes that they are, by fp8 products.
 // What the codes meet is split into several of them: Q exactly, P to 12 bits or more.
 //
-// Tiles of more rows, up to 128, lie with their rows on the lanes, against 64 keys a step; K and V
-// become fp16, which holds e4m3 exactly, on their way through shared memory, and Q (times a power of
-// two, so that bf16's 8 bits lie in fp16's range) and P are fp16: P's rounding, 2^-11, is
-// what the tensor cores take.
+// Tiles of more rows, up to 128, lie with their rows on the lanes, against 64 keys a step.  K is taken as the
+// codes that it is here too, by Q's.  V becomes fp16, which holds e4m3 exactly, on its way through shared
+// memory, which costs fewer instructions than splitting P would; P is fp16: its rounding, 2^-11, is what the
+// tensor cores take.
 //
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -88,12 +88,6 @@ template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-
-// Two numbers of a row of Q times `by`, as fp16.
-__device__ __forceinline__ uint32_t to_q(__nv_bfloat16, uint32_t v, float by) {
-  return pack(__half(), __uint_as_float(v << 16) * by, __uint_as_float(v & 0xffff0000u) * by);
-}
-__device__ __forceinline__ uint32_t to_q(__half, uint32_t v, float by) { return by < 0.f ? v ^ 0x80008000u : v; }
 
 // Queries that see nothing.
 template <class T>
@@ -281,6 +275,17 @@ __device__ __forceinline__ T from_bits(uint32_t v) {
   return *reinterpret_cast<const T*>(&s);
 }
 
+// Eight elements of a row of Q, from an address that there is (what is none is the caller's to drop): the loads of a
+// thread stay free of branches, so that none waits for another.
+template <class T>
+__device__ __forceinline__ uint4 q_piece(const Args8& g, const Item& it, int32_t hk, int32_t rows, int32_t row, int32_t piece,
+                                         uint32_t per_group) {
+  row = min(row, rows - 1);
+  const int32_t tok = row * per_group >> 16;
+  return *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
+                                         (hk * g.a.group + row - tok * g.a.group) * g.q_head + min(piece * 8, g.a.dim - 8));
+}
+
 // ---------------------------------------------------------------------------
 // Few rows: codes straight into the products
 // ---------------------------------------------------------------------------
@@ -455,6 +460,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
     {
       // a row's 8 elements a step, to its terms: codes of row `term * 16 + row`
       constexpr int kEach = kFewRows * 16 / 128;
+      const uint32_t per_group = 65536 / a.group + 1;   // row * per_group >> 16 is row / group
       uint4 v[kEach];
       uint32_t top = 0;
       auto raise = [&](uint32_t x) {
@@ -462,14 +468,10 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
         if (x < kInf && x > top) top = x;
       };
 #pragma unroll
+      for (int i = 0; i < kEach; ++i) v[i] = q_piece<T>(g, it, hk, rows, (r + 128 * i) / 16, (r + 128 * i) % 16, per_group);
+#pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int x = r + 128 * i, row = x / 16, c = x % 16;
-        v[i] = uint4{};
-        if (row < rows && c * 8 < a.dim) {
-          const int32_t tok = row / a.group;
-          v[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
-                                                 (hk * a.group + row - tok * a.group) * g.q_head + c * 8);
-        }
+        if (r / 16 + 8 * i >= rows || r % 16 * 8 >= a.dim) v[i] = uint4{};
         for (const uint32_t w : {v[i].x, v[i].y, v[i].z, v[i].w}) raise(w & 0x7fff), raise(w >> 16 & 0x7fff);
       }
       top = __reduce_max_sync(0xffffffffu, top);
@@ -707,45 +709,192 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
 // ---------------------------------------------------------------------------
 
 //   warps 0 to 3    the softmax: a thread holds one row
-//   warps 4 to 7    K and V from slots of codes to slots of fp16
-//   warps 8 to 10   copies: page by page into a ring of 64-key slots, K_0 K_1 V_0 K_2 V_1 ...
+//   warps 4, 5      keys from slots of codes to slots of fp16; warps 6, 7 values
+//   warps 8, 9      copies: the pages of 64 keys, or values, a slot
 //   warp 11         products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
 constexpr int kKeys = 64, kRows = 128;   // of a step, of a tile
 constexpr int kThreads = 384;
 constexpr float kBias = 7.f, kMost = 8.f;   // a weight is at most 2^(kMost + kBias), in fp16's range
 
-template <int DP>
+template <class T, int DP>
 struct Shape {
-  static constexpr int kQ = kRows * DP * 2;
-  static constexpr int kSlot = kKeys * DP * 2, kSlots = 49152 / kSlot;         // of fp16
-  static constexpr int kCodes = kKeys * DP, kCodeSlots = 4;
-  static constexpr int kCodesAt = kQ + kSlots * kSlot;
-  static constexpr int kMiscAt = kCodesAt + kCodeSlots * kCodes;
+  static constexpr int kTerms = TermsQ<T>::kN;
+  static constexpr int kTerm = kRows * DP, kQ = kTerms * kTerm;
+  static constexpr int kWide = kKeys * DP * 2, kWideSlots = 2;                       // V in fp16
+  static constexpr int kCodes = kKeys * DP, kCodeSlots = DP == 64 ? 4 : kTerms == 2 ? 3 : 2;   // of K, and of V
+  static constexpr int kWideAt = kQ, kCodesAt = kWideAt + kWideSlots * kWide;
+  static constexpr int kMiscAt = kCodesAt + 2 * kCodeSlots * kCodes;
   static constexpr int kSmem = kMiscAt + 1024;
   static constexpr int kColumns = 256;                    // of TMEM: O, then two buffers of S
   static_assert(kSmem <= 115712, "two blocks an SM");
 };
 
-template <int DP>
+// The larger of two pairs of magnitudes.
+__device__ __forceinline__ uint32_t most_of(__nv_bfloat16, uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t most_of(__half, uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Full and empty, by slot.
+template <int N>
+struct Ring {
+  uint64_t full[N], empty[N];
+};
+
+template <class T, int DP>
 struct Misc {
-  float2 step[kScaleSteps][4];         // of a step's blocks of 16 keys: what a score is multiplied by, log2 v
   ScaleRing<kKeys> scales;
   uint32_t first_nan[32];              // by dimension, a byte: the first query that sees a NaN where rows see different keys
-  uint64_t bars[2 * Shape<DP>::kSlots + 2 * Shape<DP>::kCodeSlots + 9];
-  uint32_t tmem_at, failed, any_nan, unit;
+  signed char q_scale[kRows];          // the power of two that a row of Q is multiplied by
+  Ring<Shape<T, DP>::kCodeSlots> codes_k, codes_v;
+  Ring<Shape<T, DP>::kWideSlots> wide;
+  uint64_t q_ready, s_full[2], p_ready[2], o_done[2];
+  uint32_t tmem_at, failed, any_nan;
 };
-static_assert(sizeof(Misc<128>) <= 1024 && sizeof(Misc<64>) <= 1024, "fits behind the slots");
+static_assert(sizeof(Misc<__half, 128>) <= 1024 && sizeof(Misc<__half, 64>) <= 1024, "fits behind the slots");
+
+// As tile_k, in rows of 64 bytes and the 64-byte swizzle.
+__device__ __forceinline__ uint64_t tile_k64(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | (1ull << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
+}
+// The next term of x and y, itself: its codes; x and y become what it leaves.
+__device__ __forceinline__ uint16_t next_code(uint64_t* xy) {
+  float x, y;
+  halves(*xy, &x, &y);
+  const uint16_t c = codes2(x, y);
+  const uint32_t h = wide2(c);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  *xy = two(x - f.x, y - f.y);
+  return c;
+}
+
+// The slots of a ring in order: a wait tells its phase from the one before it, which the same wait has had before.
+template <int N>
+struct Turn {
+  uint32_t full, empty;
+  int slot = 0;
+  uint32_t parity = 0;                 // of the full one; an empty one is awaited with the other
+  __device__ explicit Turn(Ring<N>& r) : full(smem_addr(r.full)), empty(smem_addr(r.empty)) {}
+  __device__ uint32_t full_bar() const { return full + 8 * slot; }
+  __device__ uint32_t empty_bar() const { return empty + 8 * slot; }
+  __device__ void next() {
+    if (++slot == N) slot = 0, parity ^= 1;
+  }
+};
 
 __device__ __forceinline__ float in_range(float scale) { return fminf(fmaxf(scale, 8.6736174e-19f), 1.1529215e18f); }   // 2^-60 .. 2^60
+
+// A copying warp: K (with the scales), or V, page by page.
+template <int DP, int kSlots, bool kKeysToo>
+__device__ __forceinline__ void copy_tiles(const CUtensorMap& map, const Args8& g, const Item& it, int32_t hk, int32_t first,
+                                           int32_t n, int lane, uint32_t slots, Ring<kSlots>& ring, ScaleRing<kKeys>& scales,
+                                           volatile uint32_t* failed) {
+  const AttendArgs& a = g.a;
+  const int32_t box = a.page_tokens < kKeys ? a.page_tokens : kKeys;   // keys a copy
+  // the page numbers come 32 at a time, the next 32 on their way
+  const int shift = __ffs(a.page_tokens) - 1;
+  const int32_t last = (it.hi - 1) >> shift;
+  int32_t at0 = first * kKeys >> shift;
+  auto look_up = [&](int32_t i) {
+    const int32_t page = i <= last ? a.table[int64_t(it.row) * a.max_pages + i] : -1;
+    return page >= 0 && page < a.n_pages ? page : a.n_pages;   // no such page: read as zeros
+  };
+  int32_t now = look_up(at0 + lane), next = look_up(at0 + 32 + lane);
+  Turn<kSlots> turn(ring);
+  int j = 0;
+  for (; j < n; ++j) {
+    const int32_t k0 = (first + j) * kKeys;
+    const int32_t from = it.lo > k0 ? (it.lo - k0) / box * box : 0, to = it.hi - k0 < kKeys ? it.hi - k0 : kKeys;
+    if ((k0 >> shift) - at0 >= 32) {
+      at0 += 32;
+      now = next;
+      next = look_up(at0 + 32 + lane);
+    }
+    if (!bar_wait(turn.empty_bar(), turn.parity ^ 1, failed)) break;
+    const uint32_t bar = turn.full_bar(), dst = slots + turn.slot * (kKeys * DP);
+    if (elect_one()) bar_expect(bar, (to - from + box - 1) / box * box * DP);
+    for (int32_t k = from; k < to; k += box) {
+      // (a step has at most four pages, so it does not reach beyond the 32 before the next ones move up)
+      const int32_t page = __shfl_sync(0xffffffffu, now, ((k0 + k) >> shift) - at0);
+      const int32_t y = ((a.plane + !kKeysToo) * a.n_kv + hk) * a.page_tokens + ((k0 + k) & (a.page_tokens - 1));
+      if (elect_one()) load_3d(dst + k * DP, &map, 0, y, page, bar);
+    }
+    if (kKeysToo) {
+      const int32_t k = k0 + (lane & 3) * 16, v = lane >> 2 & 1;
+      const int32_t page = __shfl_sync(0xffffffffu, now, ((k >> shift) - at0) & 31);
+      float* at = &scales.s[j & (kScaleSteps - 1)][v][lane & 3];
+      if (lane < 8) {
+        if (page < a.n_pages && k < it.hi) {
+          const int32_t blocks = a.page_tokens / 16;
+          copy_word(smem_addr(at), g.pool + page * g.page_bytes + g.scale_at +
+                                       4 * (int64_t(v * a.n_kv + hk) * blocks + (k & (a.page_tokens - 1)) / 16));
+        } else {
+          *at = 1.f;
+        }
+      }
+      copies_arrive(bar);
+    }
+    turn.next();
+  }
+  if (gave_up(failed)) {   // the copies in flight still have to land: a bounded wait for each
+    uint32_t quiet = 0;
+    for (int b = j - 1; b >= 0 && b >= j - kSlots; --b) bar_pass(smem_addr(&ring.full[b % kSlots]), (b / kSlots) & 1, &quiet);
+  }
+  __syncwarp();
+}
+
+// Four warps: V's codes to fp16, a thread half of a key's.
+template <class T, int DP>
+__device__ __forceinline__ void widen(unsigned char* codes, unsigned char* wide, Misc<T, DP>& misc, const Item& it, int32_t first,
+                                      int32_t n, int32_t all_see) {
+  volatile uint32_t* failed = &misc.failed;
+  const int r = threadIdx.x & 63, part = threadIdx.x >> 6 & 1;
+  Turn<Shape<T, DP>::kCodeSlots> from(misc.codes_v);
+  Turn<Shape<T, DP>::kWideSlots> to(misc.wide);
+  for (int j = 0; j < n; ++j) {
+    const int32_t k0 = (first + j) * kKeys, key = k0 + r;
+    bar_pass(from.full_bar(), from.parity, failed);
+    bar_pass(to.empty_bar(), to.parity ^ 1, failed);
+    unsigned char *x = codes + from.slot * (kKeys * DP), *y = wide + to.slot * (kKeys * DP * 2);
+    const bool masked = k0 < it.lo || k0 + kKeys > all_see;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+      const int c16 = part * (DP / 32) + i;
+      uint4 v = *codes_at<DP>(x, r, c16);
+      if (masked) {
+        // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN that
+        // some row does not see; those that see it get theirs at the end.
+        if (key < it.lo || key >= it.hi) v = uint4{};
+        if (drop_nan(&v, misc.first_nan + 4 * c16, key <= it.pos0 ? 0 : min(key - it.pos0, 254))) misc.any_nan = 1;
+      }
+      uint32_t o[8];
+      wide16(v, o);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        *reinterpret_cast<uint4*>(y + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + k) % 8) ^ (r & 7)) * 16) =
+            uint4{o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]};
+    }
+    fence_async();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(from.empty_bar()), bar_arrive(to.full_bar());
+    from.next();
+    to.next();
+  }
+}
 
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_constant__ CUtensorMap map_kv,
                                                               const __grid_constant__ Args8 g) {
-  using S = Shape<DP>;
+  using S = Shape<T, DP>;
   extern __shared__ __align__(1024) unsigned char base[];
   const AttendArgs& a = g.a;
-  unsigned char *const ring = base + S::kQ, *const code_ring = base + S::kCodesAt;
-  Misc<DP>& misc = *reinterpret_cast<Misc<DP>*>(base + S::kMiscAt);
+  Misc<T, DP>& misc = *reinterpret_cast<Misc<T, DP>*>(base + S::kMiscAt);
   volatile uint32_t* failed = &misc.failed;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   // all heads of an item, then the next item: the long ones start first
@@ -759,17 +908,19 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
     return;
   }
 
-  const uint32_t full = smem_addr(misc.bars), empty = full + 8 * S::kSlots, code_full = empty + 8 * S::kSlots,
-                 code_empty = code_full + 8 * S::kCodeSlots, q_ready = code_empty + 8 * S::kCodeSlots, s_full = q_ready + 8,
-                 p_ready = s_full + 16, o_done = p_ready + 16, all_met = o_done + 16;
+  const uint32_t q_ready = smem_addr(&misc.q_ready), s_full = smem_addr(misc.s_full), p_ready = smem_addr(misc.p_ready),
+                 o_done = smem_addr(misc.o_done);
   // s_full, p_ready and o_done are two barriers each, for even and odd steps.  A wait tells a phase
   // from the one before it only, and every wait here has that one behind it: S_j is computed
   // after the product of step j - 2 is done.
   if (warp == 8 && lane == 0) {
     prefetch_map(&map_kv);
-    for (int i = 0; i < S::kSlots; ++i) bar_init(full + 8 * i, 4), bar_init(empty + 8 * i, 1);
-    for (int i = 0; i < S::kCodeSlots; ++i) bar_init(code_full + 8 * i, kFullCount), bar_init(code_empty + 8 * i, 4);
-    bar_init(q_ready, 8), bar_init(all_met, 8);
+    for (int i = 0; i < S::kCodeSlots; ++i) {
+      bar_init(smem_addr(&misc.codes_k.full[i]), kFullCount), bar_init(smem_addr(&misc.codes_k.empty[i]), 1);
+      bar_init(smem_addr(&misc.codes_v.full[i]), 1), bar_init(smem_addr(&misc.codes_v.empty[i]), 4);
+    }
+    for (int i = 0; i < S::kWideSlots; ++i) bar_init(smem_addr(&misc.wide.full[i]), 4), bar_init(smem_addr(&misc.wide.empty[i]), 1);
+    bar_init(q_ready, 8);
     for (int i = 0; i < 2; ++i) bar_init(s_full + 8 * i, 1), bar_init(p_ready + 8 * i, 4), bar_init(o_done + 8 * i, 1);
     misc.failed = misc.any_nan = 0;
     fence_bar_init();
@@ -784,27 +935,37 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
 
   if (warp >= 8) {
     fewer_registers<40>();
-    if (warp < 8 + kCopiers) {
-      copy_pages<kKeys, DP, S::kCodeSlots>(map_kv, g, it, hk, first, n, warp - 8, lane, smem_addr(code_ring), code_full, code_empty,
-                                           misc.scales, failed);
-    } else {
+    if (warp < 10) {
+      if (warp == 8)
+        copy_tiles<DP, S::kCodeSlots, true>(map_kv, g, it, hk, first, n, lane, smem_addr(base + S::kCodesAt), misc.codes_k,
+                                            misc.scales, failed);
+      else
+        copy_tiles<DP, S::kCodeSlots, false>(map_kv, g, it, hk, first, n, lane,
+                                             smem_addr(base + S::kCodesAt + S::kCodeSlots * S::kCodes), misc.codes_v, misc.scales,
+                                             failed);
+    } else if (warp == 11) {
       // the whole warp goes along; one lane issues
-      constexpr uint32_t desc_s = mma_desc(false, kRows, kKeys, false), desc_o = mma_desc(false, kRows, DP, true);
-      const uint64_t q = tile_k(smem_addr(base)), k_ring = tile_k(smem_addr(ring)), v_ring = tile_n(smem_addr(ring), kKeys * 128);
+      constexpr uint32_t desc_s = mma8_desc(kRows, kKeys, false, false), desc_o = mma_desc(false, kRows, DP, true);
+      const uint32_t k_at = smem_addr(base + S::kCodesAt);
+      const uint64_t q = DP == 64 ? tile_k64(smem_addr(base)) : tile_k(smem_addr(base)),
+                     k_ring = DP == 64 ? tile_k64(k_at) : tile_k(k_at), v_ring = tile_n(smem_addr(base + S::kWideAt), kKeys * 128);
+      Turn<S::kCodeSlots> kt(misc.codes_k);
+      Turn<S::kWideSlots> vt(misc.wide);
       auto scores = [&](int j, uint32_t behind, uint32_t parity) {   // behind: what S_j waits for besides K_j
-        const int e = j == 0 ? 0 : 2 * j - 1, slot = e % S::kSlots;
-        if (!bar_wait_both(behind, parity, full + 8 * slot, (e / S::kSlots) & 1, failed)) return false;
+        if (!bar_wait_both(behind, parity, kt.full_bar(), kt.parity, failed)) return false;
         tc_after_sync();
-        const uint64_t k = k_ring + slot * (S::kSlot / 16);
+        const uint64_t k = k_ring + kt.slot * (S::kCodes / 16);
         const uint32_t d = tmem_s + (j & 1) * kKeys;
         if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < DP / 16; ++i)
-            mma_ss<1>(d, q + (i / 4) * (kRows * 128 / 16) + 2 * (i % 4), k + (i / 4) * (kKeys * 128 / 16) + 2 * (i % 4), desc_s, i > 0);
-          mma_commit(empty + 8 * slot);
+          for (int t = 0; t < S::kTerms; ++t)
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) mma8_ss(d, q + t * (S::kTerm / 16) + 2 * i, k + 2 * i, desc_s, t > 0 || i > 0);
+          mma_commit(kt.empty_bar());
           mma_commit(s_full + 8 * (j & 1));
         }
         __syncwarp();
+        kt.next();
         return true;
       };
       int asked = 0, done = 0;            // S and O that are on their way
@@ -812,18 +973,18 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
       asked += go;
       if (go && n > 1) go = scores(1, q_ready, 0), asked += go;
       for (int j = 0; go && j < n; ++j) {
-        const int e = j == n - 1 ? 2 * n - 1 : 2 * j + 2, slot = e % S::kSlots;
-        if (!bar_wait_both(p_ready + 8 * (j & 1), (j >> 1) & 1, full + 8 * slot, (e / S::kSlots) & 1, failed)) break;
+        if (!bar_wait_both(p_ready + 8 * (j & 1), (j >> 1) & 1, vt.full_bar(), vt.parity, failed)) break;
         tc_after_sync();
-        const uint64_t v = v_ring + slot * (S::kSlot / 16);
+        const uint64_t v = v_ring + vt.slot * (S::kWide / 16);
         const uint32_t p = tmem_s + (j & 1) * kKeys;
         if (elect_one()) {
 #pragma unroll
           for (int i = 0; i < kKeys / 16; ++i) mma_ts(tmem, p + i * 8, v + i * (16 * 128 / 16), desc_o, j > 0 || i > 0);
-          mma_commit(empty + 8 * slot);
+          mma_commit(vt.empty_bar());
           mma_commit(o_done + 8 * (j & 1));
         }
         __syncwarp();
+        vt.next();
         ++done;
         // S_{j+2} takes the place of P_j: once its product is done
         if (j + 2 < n) go = scores(j + 2, o_done + 8 * (j & 1), (j >> 1) & 1), asked += go;
@@ -833,50 +994,58 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
       if (done > 0) bar_pass(o_done + 8 * ((done - 1) & 1), ((done - 1) >> 1) & 1, &quiet);
     }
   } else {
-    // Q to shared memory, 16 bytes a step: consecutive threads along a row
-    float by = 1.f, unit = 1.f;          // Q is scaled by `by`; |1 / by|
     {
-      constexpr int kEach = kRows * DP / 8 / 256;
-      auto load = [&](int i) {
-        const int x = threadIdx.x + 256 * i, row = x / (DP / 8), c = x % (DP / 8);
-        if (row >= rows || c * 8 >= a.dim) return uint4{};
-        const int32_t tok = row / a.group;
-        return *reinterpret_cast<const uint4*>(static_cast<const T*>(g.q) + (it.tok0 + tok) * g.q_tok +
-                                               (hk * a.group + row - tok * a.group) * g.q_head + c * 8);
-      };
-      if (std::is_same<T, __nv_bfloat16>::value) {
-        uint32_t top = 0;                // of |q| where finite, its bits
+      // Q's terms to shared memory, 8 elements a step: consecutive threads along a row, which is first multiplied by the
+      // power of two that brings its largest to between 2^7 and 2^8
+      // (four at a time, the next four on their way: a block goes through this code once, and more of it would
+      // be fetched for longer than it runs)
+      constexpr int kLanes = DP / 8, kEach = kRows * kLanes / 256, kApart = 256 / kLanes;
+      const int c = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+      const uint32_t per_group = 65536 / a.group + 1;   // row * per_group >> 16 is row / group, for rows below 128
+      auto piece = [&](int i) { return q_piece<T>(g, it, hk, rows, row0 + i * kApart, c, per_group); };
+      uint4 ahead[4];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          const uint4 v = load(i);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      for (int i = 0; i < 4; ++i) ahead[i] = piece(i);
+#pragma unroll 1
+      for (int i0 = 0; i0 < kEach && i0 * kApart < rows; i0 += 4) {
+        uint4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ahead[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ahead[i] = piece(i0 + 4 + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = row0 + (i0 + i) * kApart;
+          if (row >= rows || c * 8 >= a.dim) v[i] = uint4{};
+          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+          // of |q| (a row that holds an infinity is NaN in the end, whatever its scale)
+          uint32_t both = most_of(T(), most_of(T(), w[0] & 0x7fff7fff, w[1] & 0x7fff7fff), most_of(T(), w[2] & 0x7fff7fff, w[3] & 0x7fff7fff));
+#pragma unroll
+          for (int d = kLanes / 2; d; d /= 2) both = most_of(T(), both, __shfl_xor_sync(0xffffffffu, both, d));
+          const float most = fmaxf(unpack(T(), both, 0), unpack(T(), both, 1));
+          const int e = max(min(134 - (int)(__float_as_uint(most) >> 23), 126), -120);
+          if (c == 0) misc.q_scale[row] = (signed char)e;
+          float by = __int_as_float((e + 127) << 23);
+          if (a.negative) by = -by;
+          uint64_t xy[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = w[k] & 0x7fff, hi = (w[k] >> 16) & 0x7fff;
-            if (lo < 0x7f80 && lo > top) top = lo;
-            if (hi < 0x7f80 && hi > top) top = hi;
+            const float x0 = unpack(T(), w[k], 0) * by, x1 = unpack(T(), w[k], 1) * by;
+            xy[k] = two(fmaf(x0, 0.f, x0), fmaf(x1, 0.f, x1));   // (infinities to NaN: there is no code for them)
           }
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-        uint32_t* tops = reinterpret_cast<uint32_t*>(misc.step);
-        if (lane == 0) tops[warp] = top;
-        uint32_t meetings = 0;
-        bar_meet(all_met, &meetings, failed);
+          // 16 bytes of a row, where the products look for them: the swizzle of rows of DP bytes
+          unsigned char* at = base + row * DP + ((c / 2) ^ (DP == 64 ? row >> 1 & 3 : row & 7)) * 16 + (c & 1) * 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, tops[i]);
-        const int e = max(min(140 - (int)(top >> 7), 126), -114);   // 2^13 over the largest's power of two
-        by = __int_as_float((e + 127) << 23);
-        unit = __int_as_float((127 - e) << 23);
-        bar_meet(all_met, &meetings, failed);
+          for (int t = 0; t < S::kTerms; ++t) {
+            uint32_t o[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t lo = next_code(&xy[2 * k]), hi = next_code(&xy[2 * k + 1]);
+              o[k] = lo | hi << 16;
+            }
+            *reinterpret_cast<uint2*>(at + t * S::kTerm) = uint2{o[0], o[1]};
+          }
       }
-      if (a.negative) by = -by;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int x = threadIdx.x + 256 * i, row = x / (DP / 8), c = x % (DP / 8);
-        const uint4 v = load(i);
-        uint4 o;
-        o.x = to_q(T(), v.x, by), o.y = to_q(T(), v.y, by), o.z = to_q(T(), v.z, by), o.w = to_q(T(), v.w, by);
-        *reinterpret_cast<uint4*>(base + (c / 8) * (kRows * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16) = o;
       }
       fence_async();
       __syncwarp();
@@ -884,46 +1053,13 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
     }
     if (warp >= 4) {
       fewer_registers<72>();
-      const int r = threadIdx.x & 63, part = (threadIdx.x - 128) / 64;   // a key, half of its dimensions
-      const float c_all = a.scale2 * unit;
-      for (int e = 0; e < 2 * n; ++e) {
-        const bool is_v = e == 2 * n - 1 || (e > 0 && e % 2 == 0);
-        const int j = e == 2 * n - 1 ? n - 1 : is_v ? e / 2 - 1 : (e + 1) / 2;
-        const int slot = e % S::kSlots, code_slot = e % S::kCodeSlots;
-        const int32_t k0 = (first + j) * kKeys, key = k0 + r;
-        bar_pass(code_full + 8 * code_slot, (e / S::kCodeSlots) & 1, failed);
-        if (!is_v && threadIdx.x - 128 < 4) {
-          const int b = threadIdx.x - 128;
-          const float ks = misc.scales.s[j & (kScaleSteps - 1)][0][b], vs = misc.scales.s[j & (kScaleSteps - 1)][1][b];
-          misc.step[j & (kScaleSteps - 1)][b] = float2{c_all * in_range(ks), __log2f(in_range(vs))};
-        }
-        bar_pass(empty + 8 * slot, ((e / S::kSlots) & 1) ^ 1, failed);
-        unsigned char *from = code_ring + code_slot * S::kCodes, *to = ring + slot * S::kSlot;
-        const bool masked = is_v && (k0 < it.lo || k0 + kKeys > all_see);
-#pragma unroll
-        for (int i = 0; i < DP / 32; ++i) {
-          const int c16 = part * (DP / 32) + i;
-          uint4 v = *codes_at<DP>(from, r, c16);
-          if (masked) {
-            // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN that
-            // some row does not see; those that see it get theirs at the end.
-            if (key < it.lo || key >= it.hi) v = uint4{};
-            if (drop_nan(&v, misc.first_nan + 4 * c16, key <= it.pos0 ? 0 : min(key - it.pos0, 254))) misc.any_nan = 1;
-          }
-          uint32_t o[8];
-          wide16(v, o);
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<uint4*>(to + (c16 / 4) * (kKeys * 128) + r * 128 + (((2 * c16 + k) % 8) ^ (r & 7)) * 16) =
-                uint4{o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]};
-        }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) bar_arrive(code_empty + 8 * code_slot), bar_arrive(full + 8 * slot);
-      }
+      widen<T, DP>(base + S::kCodesAt + S::kCodeSlots * S::kCodes, base + S::kWideAt, misc, it, first, n, all_see);
     } else {
       more_registers<128>();
       const int r = threadIdx.x;
+      bar_pass(q_ready, 0, failed);      // (the rows' scales are others' work)
+      // (rows beyond the tile's hold whatever was there: their scores count as nothing)
+      const float c_all = r < rows ? a.scale2 * __int_as_float((127 - misc.q_scale[r]) << 23) : 0.f;
       const uint32_t lanes = (uint32_t)(warp * 32) << 16;
       const int32_t tok = r / a.group;
       // the keys that this row sees end here; rows beyond the tile's see what the last one does
@@ -938,19 +1074,16 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
         uint32_t s[64];
         tmem_load32(s_at, s);
         tmem_load32(s_at + 32, s + 32);
-        float2 block[4];                 // of 16 keys
+        // of a block of 16 keys: what a score is multiplied by, log2 v; each of eight lanes has one of them
+        const float mine = in_range(misc.scales.s[j & (kScaleSteps - 1)][lane >> 2 & 1][lane & 3]);
+        const float either = lane & 4 ? __log2f(mine) : mine;
+        float2 block[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) block[b] = misc.step[j & (kScaleSteps - 1)][b];
+        for (int b = 0; b < 4; ++b)
+          block[b] = float2{fmaxf(c_all * __shfl_sync(0xffffffffu, either, b), 1e-37f), __shfl_sync(0xffffffffu, either, 4 + b)};
         tmem_wait_load();
         tmem_loaded(s);
-        // the weights' exponents, without the reference; -inf for what this row does not see
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float x, y;
-          const float2 b = block[i / 8];
-          halves(fma2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), two(b.x, b.x), two(b.y, b.y)), &x, &y);
-          s[2 * i] = __float_as_uint(x), s[2 * i + 1] = __float_as_uint(y);
-        }
+        // -inf for what this row does not see (its multipliers are > 0)
         if (k0 < it.lo || k0 + kKeys > all_see) {
           const int below = it.lo > k0 ? it.lo - k0 : 0, upto = end - k0 < 0 ? 0 : end - k0 < kKeys ? end - k0 : kKeys;
           const uint64_t sees = upto <= below ? 0 : (upto == 64 ? ~0ull : (1ull << upto) - 1) & ~((1ull << below) - 1);
@@ -958,10 +1091,14 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
           for (int i = 0; i < 64; ++i)
             if (!(sees >> i & 1)) s[i] = 0xff800000u;
         }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float top = -INFINITY;           // of s c + log2 v
 #pragma unroll
-        for (int i = 0; i < 32; ++i) mx[i & 3] = max3(mx[i & 3], s[2 * i], s[2 * i + 1]);
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        for (int b = 0; b < 4; ++b) {
+          float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 8 * b; i < 8 * b + 8; ++i) mx[i & 1] = max3(mx[i & 1], s[2 * i], s[2 * i + 1]);
+          top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), block[b].x, block[b].y));
+        }
         const bool raise = top > m + kMost || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, raise)) {
           const float f = raise ? (m == -INFINITY ? 0.f : exp2_fast(m - top)) : 1.f;
@@ -984,15 +1121,15 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
           }
         }
         const float shift = m == -INFINITY ? 0.f : kBias - m;
-        const uint64_t shift2 = two(shift, shift);
         uint32_t p[32];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
+          const uint64_t c2 = two(block[b].x, block[b].x), shift2 = two(block[b].y + shift, block[b].y + shift);
           uint64_t sum[2] = {};
 #pragma unroll
           for (int i = 8 * b; i < 8 * b + 8; ++i) {
             float x, y;
-            halves(add2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), shift2), &x, &y);
+            halves(fma2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, shift2), &x, &y);
             x = exp2_fast(x), y = exp2_fast(y);
             sum[i & 1] = add2(sum[i & 1], two(x, y));
             p[i] = pack(__half(), x, y);
@@ -1022,7 +1159,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
         else if (a.lse) a.lse[t * a.n_heads + h] = lse2 * 0.69314718055994531f;
       }
 #pragma unroll 1
-      for (int d = 0; d < a.dim; d += 16) {
+      for (int d = 0; d < a.dim && warp * 32 < rows; d += 16) {
         uint32_t o[16];
         tmem_load16(tmem + lanes + d, o);
         tmem_wait_load();
@@ -1076,8 +1213,8 @@ cudaError_t launch_many(const op_attend_plan_t& p, const CUtensorMap& kv, const 
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
   auto kernel = attend8_kernel<T, DP>;
-  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<DP>::kSmem); })) return cudaErrorInvalidValue;
-  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<DP>::kSmem, st>>>(kv, g);
+  if (!once.done(dev, [&] { return allow_smem(kernel, Shape<T, DP>::kSmem); })) return cudaErrorInvalidValue;
+  kernel<<<(unsigned)(p.n_items * (int64_t)p.n_kv_heads), kThreads, Shape<T, DP>::kSmem, st>>>(kv, g);
   return cudaGetLastError();
 }
 
