@@ -24,7 +24,7 @@ SOURCES = ["gmgsim_host.cu", "gmgsim_kernels.cu", "gmgsim_full.cu", "gmgsim_inc.
 HEADERS = ["gmg_layout.h", "gmg_access.h", "gmg_arb.h", "gmg_arbw.h", "gmg_arb_events.h", "gmg_once.h", "gmgsim_sim.cuh", os.path.join("..", "..", "include", "gmgsim.h"),
            os.path.join("..", "..", "include", "gmgest.h"), os.path.join("..", "..", "include", "gmground.h"),
            os.path.join("..", "..", "include", "gmgop.h"), "gmgop_host.h", "gmgop_ptx.cuh", "gmgop_attend.cuh",
-           "gmgop_rope.cuh"]
+           "gmgop_rope.cuh", "gmgop_pairs.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 # A CUDA runtime of the library's own: it loads without a toolkit on the machine, and what another
 # library's calls leave as the last error is neither reported nor taken here.  (Sharing PyTorch's

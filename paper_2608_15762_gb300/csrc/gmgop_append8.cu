@@ -51,24 +51,28 @@ __device__ __forceinline__ float scale_for(float top) {
   return __uint_as_float((uint32_t)(127 + (e < -60 ? -60 : e > 60 ? 60 : e)) << 23);
 }
 
-// Two values to codes, rounded to nearest even; beyond 448 the largest, NaN stays.
-__device__ __forceinline__ uint16_t narrow2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ uint2 narrow8(const float* v, float by) {
   uint2 r;
-  r.x = narrow2(v[0] * by, v[1] * by) | (uint32_t)narrow2(v[2] * by, v[3] * by) << 16;
-  r.y = narrow2(v[4] * by, v[5] * by) | (uint32_t)narrow2(v[6] * by, v[7] * by) << 16;
+  r.x = codes2(v[0] * by, v[1] * by) | (uint32_t)codes2(v[2] * by, v[3] * by) << 16;
+  r.y = codes2(v[4] * by, v[5] * by) | (uint32_t)codes2(v[6] * by, v[7] * by) << 16;
   return r;
+}
+// The same of four pairs.
+__device__ __forceinline__ uint2 narrow8(const uint64_t* v, uint64_t by2) {
+  uint16_t c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x, y;
+    halves(fma2(v[i], by2, 0ull), &x, &y);
+    c[i] = codes2(x, y);
+  }
+  return uint2{c[0] | (uint32_t)c[1] << 16, c[2] | (uint32_t)c[3] << 16};
 }
 __device__ __forceinline__ void wide8(uint2 c, float* v) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t two;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(two) : "h"((uint16_t)(w[i / 2] >> (16 * (i % 2)))));
+    const uint32_t two = wide2((uint16_t)(w[i / 2] >> (16 * (i % 2))));
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&two));
     v[2 * i] = f.x, v[2 * i + 1] = f.y;
   }
@@ -122,83 +126,122 @@ __device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter
   }
 }
 
+__device__ __forceinline__ float most_of(const float* v, float top) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(v[k]));   // (NaN does not count)
+  return top;
+}
+__device__ __forceinline__ float most_finite(const float* v, float top) {
+  for (int k = 0; k < 8; ++k) {
+    const float m = fabsf(v[k]);
+    if (m <= 3.402823466e38f) top = fmaxf(top, m);
+  }
+  return top;
+}
+
 template <class T, bool kWide, bool kInter>
-__global__ void __launch_bounds__(kThreads) append8_kernel(const __grid_constant__ AppendArgs a) {
-  extern __shared__ float2 cs[];          // [chunk + 15][half]: of the block's own tokens, then of those that its last run takes beyond
-  __shared__ int32_t pos[kWindow], seq[kWindow];   // from kReach entries before the block's first; seq -1: not written
-  __shared__ int32_t run_n[kChunk], n_runs, n_more, more[kBlock];
-  __shared__ unsigned char run_at[kChunk][kBlock], run_cs[kChunk][kBlock];   // a run's tokens: their entries, their rows of cs
+__global__ void __launch_bounds__(kThreads, 3) append8_kernel(const __grid_constant__ AppendArgs a) {
+  // [chunk + 15][half] for the keys of the block's runs, then [chunk][half] for its queries (which are turned as dense
+  // ones are)
+  extern __shared__ __align__(16) float2 cs[];
+  // from kReach entries before the block's first; seq -1: not written
+  __shared__ int32_t pos[kWindow], seq[kWindow], page_at[kWindow];
+  __shared__ uint32_t written[4], heads[4];        // of the window's entries, by bit: those written, and those that begin a run
+  __shared__ int32_t run_n[kChunk], run_cs[kChunk], n_runs, n_turned, turned_at[kChunk + kBlock];
+  __shared__ unsigned char run_at[kChunk][kBlock];   // a run's entries
   const int64_t t0 = (int64_t)blockIdx.x * a.chunk;
   const int own = a.n_tokens - t0 < a.chunk ? int(a.n_tokens - t0) : a.chunk;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int32_t page = a.cache.page_tokens;
-  if (threadIdx.x < own + 2 * kReach) {
+  int32_t my_pos = 0, my_seq = -1, my_page = -1;
+  if (warp < 3) {
     const int64_t t = t0 + threadIdx.x - kReach;
-    int32_t p = 0, r = -1;
-    if (t >= 0 && t < a.n_tokens) {
-      p = a.pos[t], r = a.seq[t];
-      if (r >= 0) {
-        const int32_t col = p >= 0 ? p / page : -1;
-        int32_t at = -1;
-        if (r < a.cache.n_seq && col >= 0 && col < a.cache.max_pages) at = a.cache.table[int64_t(r) * a.cache.max_pages + col];
-        if (at < 0 || at >= a.cache.n_pages) {
-          r = -1;
+    if (threadIdx.x < own + 2 * kReach && t >= 0 && t < a.n_tokens) {
+      my_pos = a.pos[t], my_seq = a.seq[t];
+      if (my_seq >= 0) {
+        const int32_t col = my_pos >= 0 ? my_pos / page : -1;
+        if (my_seq < a.cache.n_seq && col >= 0 && col < a.cache.max_pages)
+          my_page = a.cache.table[int64_t(my_seq) * a.cache.max_pages + col];
+        if (my_page < 0 || my_page >= a.cache.n_pages) {
+          my_seq = -1;
           if (blockIdx.y == 0 && t >= t0 && t < t0 + own) atomicAdd(&a.cache.status[4], 1);
         }
       }
     }
-    pos[threadIdx.x] = p;
-    seq[threadIdx.x] = r;
+    if (threadIdx.x < kWindow) pos[threadIdx.x] = my_pos, seq[threadIdx.x] = my_seq, page_at[threadIdx.x] = my_page;
+    const uint32_t bits = __ballot_sync(0xffffffffu, my_seq >= 0);
+    if (lane == 0) written[warp] = bits;
+  } else if (threadIdx.x == 96) {
+    written[3] = heads[3] = 0;
   }
-  if (threadIdx.x == 0) n_more = 0;
   __syncthreads();
-  if (warp == 0) {
-    // the tokens with which a run begins: the one written before them is another block's
-    const int i = lane + kReach;
-    bool head = lane < own && seq[i] >= 0;
-    auto joined = [&](int x, int y) { return seq[x] == seq[y] && pos[x] < pos[y] && pos[x] / kBlock == pos[y] / kBlock; };
-    if (head) {
-      int x = i - 1;
-      while (x > i - kReach && seq[x] < 0) --x;
-      if (seq[x] >= 0 && joined(x, i)) head = false;
-    }
-    const uint32_t heads = __ballot_sync(0xffffffffu, head);
-    if (head) {
-      const int r = __popc(heads & ((1u << lane) - 1));
-      int n = 0, beyond = 0;
-      for (int x = i, y = i; y < i + kReach && n < kBlock; ++y) {
-        if (seq[y] < 0) continue;
-        if (y > i && !joined(x, y)) break;
-        run_at[r][n] = (unsigned char)y;
-        if (y - kReach < own) {
-          run_cs[r][n] = (unsigned char)(y - kReach);
-        } else {   // (the block's last run alone comes here)
-          more[beyond] = y;
-          run_cs[r][n] = (unsigned char)(own + beyond++);
-        }
-        ++n;
-        x = y;
+  // 32 of the window's bits from entry i on
+  auto bits_at = [](const uint32_t* words, int i) { return __funnelshift_r(words[i / 32], words[i / 32 + 1], i % 32); };
+  if (warp < 3) {
+    // an entry goes with the one written before it where that is an earlier token of its block
+    bool head = my_seq >= 0;
+    if (head && threadIdx.x > 0) {
+      const int from = threadIdx.x < 31 ? 0 : threadIdx.x - 31;
+      const uint32_t before = bits_at(written, from) & ((1u << (threadIdx.x - from)) - 1);
+      if (before) {
+        const int x = from + 31 - __clz(before);
+        head = !(seq[x] == my_seq && pos[x] < my_pos && pos[x] / kBlock == my_pos / kBlock);
       }
-      run_n[r] = n;
-      if (beyond) n_more = beyond;
     }
-    if (lane == 0) n_runs = __popc(heads);
+    const uint32_t bits = __ballot_sync(0xffffffffu, head);
+    if (lane == 0) heads[warp] = bits;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < (own + n_more) * a.half; i += kThreads) {
+  {
+    // a run is what is written from its head to the next, within kReach entries; a warp lists every eighth
+    const uint32_t mine = bits_at(heads, kReach) & ((1u << own) - 1);   // (own <= 16)
+    const int n = __popc(mine);
+    uint32_t rest = mine;
+    int before = 0;
+    for (int r = 0; r < n; ++r, rest &= rest - 1) {
+      const int i = kReach + __ffs(rest) - 1;
+      const uint32_t next = bits_at(heads, i) & ~1u;
+      const uint32_t run = bits_at(written, i) & (next ? (1u << (__ffs(next) - 1)) - 1 : ~0u);
+      const int tokens = __popc(run);    // at most kBlock, of one block and in increasing order
+      if (r % (kThreads / 32) == warp) {
+        if (run >> lane & 1) {
+          const int k = __popc(run & ((1u << lane) - 1));
+          run_at[r][k] = (unsigned char)(i + lane);
+          turned_at[before + k] = i + lane;
+        }
+        if (lane == 0) run_n[r] = tokens, run_cs[r] = before;
+      }
+      before += tokens;
+    }
+    if (threadIdx.x == 0) n_runs = n, n_turned = before;
+  }
+  __syncthreads();
+  // a head that is turned whole, in halves: both of a pair's elements in one lane
+  const int eights = kWide && !kInter && 2 * a.half == a.dim && a.half % 8 == 0 ? a.half / 8 : 0;
+  float2* const cs_q = cs + (a.chunk + kBlock - 1) * a.half;
+  const int q_rows = a.n_heads > 0 ? own : 0;
+  for (int i = threadIdx.x; i < (n_turned + q_rows) * a.half; i += kThreads) {
     const int t = i / a.half, p = i - t * a.half;
-    // (a token that is not written is turned all the same: its query)
-    cs[i] = turn_of(a.freq[p], pos[t < own ? t + kReach : more[t - own]], a.factor, a.factor);
+    if (t < n_turned) {
+      const float2 turn = near_turn_of(a.freq[p], pos[turned_at[t]], a.factor);
+      // in a head that is turned whole eight pairs a lane: two pairs' cosines, then their sines, and neighbouring
+      // lanes' next to each other; else in order
+      float* at = reinterpret_cast<float*>(cs + t * a.half);
+      at += eights ? (p % 8 / 2 * eights + p / 8) * 4 + p % 2 : 2 * p;
+      at[0] = turn.x, at[eights ? 2 : 1] = turn.y;
+    } else cs_q[i - n_turned * a.half] = turn_of(a.freq[p], pos[kReach + t - n_turned], a.factor, a.factor);
   }
   __syncthreads();
 
   // runs: a warp a head's keys or values
   const int vecs = a.dim / 8, units = n_runs * 2 * a.n_kv;
+  const uint32_t per_vec = 65536 / vecs + 1, per_eight = eights ? 65536 / eights + 1 : 0;   // i * per_x >> 16 is i / x, for i below 256
   for (int u = blockIdx.y * (kThreads / 32) + warp; u < units; u += gridDim.y * (kThreads / 32)) {
     const int run = u / (2 * a.n_kv), x = u - run * 2 * a.n_kv, is_v = x / a.n_kv, h = x - is_v * a.n_kv;
-    const int at = run_at[run][0], n = run_n[run] * vecs;
+    const int at = run_at[run][0], n = run_n[run];
+    const float2* turns = cs + run_cs[run] * a.half;
     const int32_t p0 = pos[at];
-    const int64_t p = a.cache.table[int64_t(seq[at]) * a.cache.max_pages + p0 / page];
+    const int64_t p = page_at[at];
     unsigned char* in = static_cast<unsigned char*>(a.cache.pool) + p * a.page_bytes;
     const int head = is_v * a.n_kv + h, slot0 = p0 % page / kBlock * kBlock;
     float* scale_at = reinterpret_cast<float*>(in + a.scales_at) + head * (page / kBlock) + slot0 / kBlock;
@@ -208,45 +251,148 @@ __global__ void __launch_bounds__(kThreads) append8_kernel(const __grid_constant
     const T* from = is_v ? static_cast<const T*>(a.v) + (t0 - kReach) * a.v_tok + h * a.v_head
                          : static_cast<const T*>(a.k) + (t0 - kReach) * a.k_tok + h * a.k_head;
     const int64_t row = is_v ? a.v_tok : a.k_tok;
-    float v[kSteps][8], top = 0.f;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int i = lane + 32 * s, tok = i / vecs, c = i - tok * vecs;
-      if (32 * s >= n) break;
-      if (i < n) {
-        const T* x = from + run_at[run][tok] * row;
-        if (is_v) load8<T, kWide>(x + c * 8, v[s]);
-        else turned8<T, kWide>(x, c * 8, a.half, kInter, cs + run_cs[run][tok] * a.half, v[s]);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float m = fabsf(v[s][k]);
-          if (m <= 3.402823466e38f) top = fmaxf(top, m);   // (infinities and NaN do not count)
+    const bool paired = eights && !is_v;
+    // step s of a lane: elements from .. on of a token (of a pair of steps, its halves')
+    auto place = [&](int s, int* tok, int* elem) {
+      const int i = lane + 32 * (paired ? s / 2 : s);
+      *tok = i * (paired ? per_eight : per_vec) >> 16;
+      *elem = (i - *tok * (paired ? eights : vecs)) * 8 + (paired && s % 2 ? a.half : 0);
+      return *tok < n;
+    };
+    float scale, by;
+    // the block's scale for values of up to top; what it holds before this run is rounded to it where it is larger
+    auto settle = [&](float top) {
+      scale = scale_for(top);
+      if (kept) {
+        old = fminf(fmaxf(old, 8.67361738e-19f), 1.15292150e18f);   // 2^-60 .. 2^60, NaN the least
+        if (scale > old) {
+          const float to = old / scale;
+          for (int i = lane; i < kept * vecs; i += 32) {
+            float w[8];
+            uint2* c = reinterpret_cast<uint2*>(codes + i * 8);
+            wide8(*c, w);
+            *c = narrow8(w, to);
+          }
+        } else {
+          scale = old;
         }
       }
-    }
-    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-    float scale = scale_for(top);
-    if (kept) {
-      old = fminf(fmaxf(old, 8.67361738e-19f), 1.15292150e18f);   // 2^-60 .. 2^60, NaN the least
-      if (scale > old) {   // what the block holds before this run is rounded to the larger scale
-        const float by = old / scale;
-        for (int i = lane; i < kept * vecs; i += 32) {
-          float w[8];
-          uint2* c = reinterpret_cast<uint2*>(codes + i * 8);
-          wide8(*c, w);
-          *c = narrow8(w, by);
+      by = 1.f / scale;
+    };
+    auto most = [](float top) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))); };
+    auto put = [&](int tok, int e, const float* v) {
+      *reinterpret_cast<uint2*>(codes + (pos[run_at[run][tok]] % kBlock) * a.dim + e) = narrow8(v, by);
+    };
+    // Twice over the values: for their largest, and for their codes (with infinities, which do not count, thrice).
+    // They lie in registers as they came, or are read again.
+    auto twice = [&](auto&& each) {
+      float top = 0.f;
+      each([&](int, int, const float* v) { top = most_of(v, top); });
+      top = most(top);
+      if (!(top <= 3.402823466e38f)) {
+        top = 0.f;
+        each([&](int, int, const float* v) { top = most_finite(v, top); });
+        top = most(top);
+      }
+      settle(top);
+      each(put);
+    };
+    if (kWide && (is_v || paired)) {
+      uint4 raw[kSteps];
+      int32_t to[kSteps];                // in codes; negative: nothing
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        int tok, e;
+        to[s] = -1;
+        if (place(s, &tok, &e)) {
+          const int x = run_at[run][tok];
+          raw[s] = *reinterpret_cast<const uint4*>(from + x * row + e);
+          to[s] = (pos[x] % kBlock) * a.dim + e;
+        }
+      }
+      auto word = [&](int s, int i) { return i == 0 ? raw[s].x : i == 1 ? raw[s].y : i == 2 ? raw[s].z : raw[s].w; };
+      auto as_two = [](uint32_t w) { return two(unpack(T(), w, 0), unpack(T(), w, 1)); };
+      if (is_v) {
+        uint32_t both = 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          if (to[s] >= 0)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) both = most_of(T(), both, word(s, i) & 0x7fff7fff);
+        float top = most(fmaxf(unpack(T(), both, 0), unpack(T(), both, 1)));
+        if (!(top <= 3.402823466e38f)) {   // infinities do not count
+          top = 0.f;
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s)
+            for (int i = 0; i < 8; ++i) {
+              const float m = fabsf(unpack(T(), word(s, i / 2), i % 2));
+              if (to[s] >= 0 && m <= 3.402823466e38f) top = fmaxf(top, m);
+            }
+          top = most(top);
+        }
+        settle(top);
+        const uint64_t by2 = two(by, by);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          if (to[s] < 0) continue;
+          const uint64_t v[4] = {as_two(raw[s].x), as_two(raw[s].y), as_two(raw[s].z), as_two(raw[s].w)};
+          *reinterpret_cast<uint2*>(codes + to[s]) = narrow8(v, by2);
         }
       } else {
-        scale = old;
-      }
-    }
-    const float by = 1.f / scale;
+        // eight pairs: (u, w) -> (u c - w s, u s + w c)
+        auto each = [&](auto&& use) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int i = lane + 32 * s, tok = i / vecs, c = i - tok * vecs;
-      if (32 * s >= n) break;
-      if (i < n)
-        *reinterpret_cast<uint2*>(codes + (pos[run_at[run][tok]] % kBlock) * a.dim + c * 8) = narrow8(v[s], by);
+          for (int s = 0; s < kSteps; s += 2) {
+            if (to[s] < 0) continue;
+            int tok, e;
+            place(s, &tok, &e);
+            const float4* t = reinterpret_cast<const float4*>(turns + tok * a.half) + e / 8;
+            uint64_t v[4], w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float4 cs4 = t[i * eights];
+              const uint64_t c = two(cs4.x, cs4.y), d = two(cs4.z, cs4.w), y = as_two(word(s, i)), z = as_two(word(s + 1, i));
+              v[i] = fma2(y, c, fma2(z, two(-cs4.z, -cs4.w), 0ull));
+              w[i] = fma2(y, d, fma2(z, c, 0ull));
+            }
+            use(s, v, w);
+          }
+        };
+        auto largest = [&](auto&& of) {
+          float top = 0.f;
+          each([&](int, const uint64_t* v, const uint64_t* w) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float x0, x1, x2, x3;
+              halves(v[i], &x0, &x1);
+              halves(w[i], &x2, &x3);
+              top = fmaxf(fmaxf(top, fmaxf(of(x0), of(x1))), fmaxf(of(x2), of(x3)));
+            }
+          });
+          return most(top);
+        };
+        float top = largest([](float x) { return fabsf(x); });
+        if (!(top <= 3.402823466e38f)) top = largest([](float x) { return fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.f; });
+        settle(top);
+        const uint64_t by2 = two(by, by);
+        each([&](int s, const uint64_t* v, const uint64_t* w) {
+          *reinterpret_cast<uint2*>(codes + to[s]) = narrow8(v, by2);
+          *reinterpret_cast<uint2*>(codes + to[s + 1]) = narrow8(w, by2);
+        });
+      }
+    } else {
+      twice([&](auto&& use) {
+#pragma unroll 1
+        for (int s = 0; s < kSteps; ++s) {
+          int tok, e;
+          if (!place(s, &tok, &e)) continue;
+          const T* x = from + run_at[run][tok] * row;
+          float v[8];
+          if (is_v) load8<T, kWide>(x + e, v);
+          else turned8<T, kWide>(x, e, a.half, kInter, turns + tok * a.half, v);
+          use(tok, e, v);
+        }
+      });
     }
     if (lane == 0) *scale_at = scale;
   }
@@ -261,7 +407,7 @@ __global__ void __launch_bounds__(kThreads) append8_kernel(const __grid_constant
     const T* from = static_cast<const T*>(a.q) + (t0 + tok) * a.q_tok + h * a.q_head;
     T* to = static_cast<T*>(a.out) + (t0 + tok) * a.o_tok + h * a.o_head;
     if (step < turns) {
-      turn_step<T, N, kInter>(from, to, step, a.half, cs + tok * a.half);
+      turn_step<T, N, kInter>(from, to, step, a.half, cs_q + tok * a.half);
     } else {
       const int o = 2 * a.half + (step - turns) * N;
       *reinterpret_cast<V*>(to + o) = *reinterpret_cast<const V*>(from + o);
@@ -270,16 +416,13 @@ __global__ void __launch_bounds__(kThreads) append8_kernel(const __grid_constant
 }
 
 template <class T, bool kWide, bool kInter>
-cudaError_t launch(AppendArgs a, cudaStream_t st) {
-  // where there are many tokens a block takes 16 of them, so that most runs' sines are those of its
-  // queries too; else one, in shares
-  a.chunk = a.n_tokens >= 152 * 2 * kChunk ? kChunk : 1;
+cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
   const int64_t blocks = (a.n_tokens + a.chunk - 1) / a.chunk;
   const int64_t steps = int64_t(a.chunk) * (a.n_heads + 2 * a.n_kv) * (a.dim / 8);
   int64_t split = (152 * 4 + blocks - 1) / blocks;
   if (split > (steps + kThreads - 1) / kThreads) split = (steps + kThreads - 1) / kThreads;
   const dim3 grid((unsigned)blocks, (unsigned)(split < 1 ? 1 : split));
-  append8_kernel<T, kWide, kInter><<<grid, kThreads, (a.chunk + kBlock - 1) * a.half * sizeof(float2), st>>>(a);
+  append8_kernel<T, kWide, kInter><<<grid, kThreads, (2 * a.chunk + kBlock - 1) * a.half * sizeof(float2), st>>>(a);
   return cudaGetLastError();
 }
 
@@ -330,6 +473,17 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  // One token a block, its queries and its runs in shares; where there are many, the queries as dense ones, in a launch of
+  // their own with few registers a thread, and then 16 tokens a block
+  a.chunk = 1;
+  if (n_tokens >= 152 * 2 * kChunk) {
+    a.chunk = kChunk;
+    if (n_heads > 0) {
+      const int e = op_rope(rope, dtype, n_tokens, n_heads, a.dim, q, q_tok, q_head, pos, 0, q_out, o_tok, o_head, stream);
+      if (e != GMG_OK) return e;
+      a.n_heads = 0;
+    }
+  }
   const cudaError_t rc = dtype == GMG_OP_BF16 ? launch_type<__nv_bfloat16>(a, wide, st) : launch_type<__half>(a, wide, st);
   return rc == cudaSuccess ? GMG_OK : GMG_ECUDA;
 }

@@ -1,5 +1,5 @@
-// What the attention kernels share: work items and how a batch is cut into them, the join of partial
-// results, and small arithmetic.
+// What the attention kernels share: work items and how a batch is cut into them, and the join of
+// partial results.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/gmgop.h"
+#include "gmgop_pairs.cuh"
 
 namespace gop {
 namespace {
@@ -51,51 +52,6 @@ struct AttendArgs {
   float *part_o, *part_lse;            // [n_kv][part_rows][dim], [n_kv][part_rows], log2
   int64_t part_rows;
 };
-
-__device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float up(__half v) { return __half2float(v); }
-__device__ __forceinline__ uint32_t pack(__nv_bfloat16, float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t pack(__half, float a, float b) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float unpack(__nv_bfloat16, uint32_t v, int i) { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
-__device__ __forceinline__ float unpack(__half, uint32_t v, int i) {
-  return __half2float(__ushort_as_half((unsigned short)(i ? v >> 16 : v & 0xffff)));
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// Two fp32 in one 64-bit register pair: one instruction for both.
-__device__ __forceinline__ uint64_t two(float a, float b) {
-  uint64_t v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
-  return v;
-}
-__device__ __forceinline__ void halves(uint64_t v, float* a, float* b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t v;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
-  return v;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t v;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-  return v;
-}
-__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
-  float v;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
-  return v;
-}
 
 // Joins the parts of a query head: o = sum_i 2^(lse_i - L) o_i with L = log2 sum_i 2^lse_i.  A
 // warp takes one head of a token, a lane four elements; with more than 8 parts a block does: its

@@ -48,12 +48,6 @@ struct Args8 {
   int64_t page_bytes, scale_at;        // of a page; of the layer's scales in it
 };
 
-// Two e4m3 to two fp16, exactly.
-__device__ __forceinline__ uint32_t wide2(uint16_t v) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
-  return r;
-}
 __device__ __forceinline__ void wide16(uint4 v, uint32_t* o) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -348,11 +342,6 @@ __device__ __forceinline__ uint64_t tile_n16(uint32_t addr, uint32_t deeper, uin
   return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(deeper >> 4) << 16) | ((uint64_t)(further >> 4) << 32) | (1ull << 46);
 }
 
-__device__ __forceinline__ uint16_t codes2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 // The next term of x and y: its codes; x and y become 16 times what it leaves.
 __device__ __forceinline__ uint16_t next_term(uint64_t* xy) {
   float x, y;
@@ -728,18 +717,6 @@ struct Shape {
   static constexpr int kColumns = 256;                    // of TMEM: O, then two buffers of S
   static_assert(kSmem <= 115712, "two blocks an SM");
 };
-
-// The larger of two pairs of magnitudes.
-__device__ __forceinline__ uint32_t most_of(__nv_bfloat16, uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t most_of(__half, uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 
 // Full and empty, by slot.
 template <int N>

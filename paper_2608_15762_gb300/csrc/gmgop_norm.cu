@@ -37,10 +37,9 @@ struct alignas(16) Bytes16 {
 // aligned 16 bytes, single elements; `threads` apart.
 template <int kVecs, bool kWide>
 struct Share {
-  int tid, threads;
-  int64_t n;
-  __device__ int64_t at(int i) const {   // of element i of 8 * kVecs
-    return kWide ? ((int64_t)(i / 8) * threads + tid) * 8 + i % 8 : (int64_t)i * threads + tid;
+  int tid, threads, n;
+  __device__ int at(int i) const {       // of element i of 8 * kVecs
+    return kWide ? (i / 8 * threads + tid) * 8 + i % 8 : i * threads + tid;
   }
   template <class T>
   __device__ void load(const T* x, float* v) const {
@@ -100,16 +99,21 @@ __device__ __forceinline__ float row_sum(float v, float (*buf)[kMaxThreads / 32]
 }
 
 template <class T, class X, int kVecs, bool kWide, int kThreads>
-__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ op_norm_t a) {
+__global__ void __launch_bounds__(kThreads, 1) norm_kernel(const __grid_constant__ op_norm_t a) {
   constexpr int N = 8 * kVecs;
   __shared__ float buf[2][kMaxThreads / 32];
   int turn = 0;
   const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   if (row >= a.m) return;              // (a whole warp, where a block has several rows)
-  const Share<kVecs, kWide> s{(int)threadIdx.x, (int)blockDim.x, a.n};
+  const Share<kVecs, kWide> s{(int)threadIdx.x, (int)blockDim.x, (int)a.n};
   const float n = (float)a.n;          // (divided by, as 1 / n is rounded: a row of one number has that mean)
+  // Where rows are few their last weights are loaded with them: behind the sums they would be waited for once more
+  constexpr bool kAhead = kVecs == 1 && kThreads > 128;
+  float w_ahead[kAhead ? N : 1], b_ahead[kAhead ? N : 1];
+  if (kAhead && a.weight) s.load(static_cast<const T*>(a.weight), w_ahead);
+  if (kAhead && a.bias) s.load(static_cast<const T*>(a.bias), b_ahead);
   // v <- its norm with weight and bias
-  auto normed = [&](float* v, const void* weight, const void* bias) {
+  auto normed = [&](float* v, const void* weight, const void* bias, bool ahead) {
     if (a.kind == GMG_NORM_LAYER) {
       float sum = 0.f;
 #pragma unroll
@@ -126,15 +130,15 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     for (int i = 0; i < N; ++i) v[i] *= inv;
     if (weight) {
       float w[N];
-      s.load(static_cast<const T*>(weight), w);
+      if (!ahead) s.load(static_cast<const T*>(weight), w);
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] *= w[i] + a.shift;
+      for (int i = 0; i < N; ++i) v[i] *= (ahead ? w_ahead[kAhead ? i : 0] : w[i]) + a.shift;
     }
     if (bias) {
       float b[N];
-      s.load(static_cast<const T*>(bias), b);
+      if (!ahead) s.load(static_cast<const T*>(bias), b);
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += b[i];
+      for (int i = 0; i < N; ++i) v[i] += ahead ? b_ahead[kAhead ? i : 0] : b[i];
     }
   };
   float v[N];
@@ -142,7 +146,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
   if (a.y) {
     float z[N];
     s.load(static_cast<const T*>(a.y) + row * a.y_row, z);
-    if (a.after) normed(z, a.y_weight, a.y_bias);
+    if (a.after) normed(z, a.y_weight, a.y_bias, false);
     if (a.gate && a.gate_col) {
       float g[N];
       s.load(static_cast<const T*>(a.gate) + row * a.gate_row, g);
@@ -155,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     if (a.r) s.store(static_cast<X*>(a.r) + row * a.r_row, v);
   }
   if (a.h) {
-    normed(v, a.weight, a.bias);
+    normed(v, a.weight, a.bias, kAhead);
     s.store(static_cast<T*>(a.h) + row * a.h_row, v);
   }
 }
@@ -163,7 +167,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
 template <class T, class X, bool kWide>
 cudaError_t launch(const op_norm_t& a, cudaStream_t st) {
   const int64_t vecs = (a.n + 7) / 8;
-  // a warp a row up to 1,024 elements, then a block with 16 elements a thread
+  // a warp a row up to 1,024 elements; then a block, with 8 elements a thread where rows are few, so that a row's way is
+  // short, else with 16, which leaves more of them on an SM (%s)
   auto go = [&](auto kernel, int v) {
     int64_t threads = (vecs + v - 1) / v;
     threads = (threads + 31) / 32 * 32;
@@ -173,6 +178,7 @@ cudaError_t launch(const op_norm_t& a, cudaStream_t st) {
   };
   if (vecs <= 32) return go(norm_kernel<T, X, 1, kWide, 128>, 1);
   if (vecs <= 128) return go(norm_kernel<T, X, 4, kWide, 128>, 4);
+  if (vecs <= kMaxThreads && a.m <= 1216) return go(norm_kernel<T, X, 1, kWide, kMaxThreads>, 1);
   if (vecs <= 2 * 512) return go(norm_kernel<T, X, 2, kWide, 512>, 2);
   if (vecs <= 2 * kMaxThreads) return go(norm_kernel<T, X, 2, kWide, kMaxThreads>, 2);
   return go(norm_kernel<T, X, 4, kWide, kMaxThreads>, 4);

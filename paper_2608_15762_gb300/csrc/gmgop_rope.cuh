@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "gmgop_pairs.cuh"
+
 namespace gop {
 namespace {
 
@@ -21,9 +23,19 @@ __device__ __forceinline__ float2 turn_of(uint64_t freq, int32_t pos, float by_c
   return make_float2(c * by_c, s * by_s);
 }
 
+// The same, nearer by what the fp32 argument leaves out (up to 2^-26 turns), to first order: to the rounding of sine and
+// cosine.
+__device__ __forceinline__ float2 near_turn_of(uint64_t freq, int32_t pos, float by) {
+  const uint64_t turn = freq * (uint64_t)(int64_t)pos;
+  const int32_t top = (int32_t)(turn >> 32);
+  const float whole = (float)top;                                          // 2^31 half turns at most
+  float s, c;
+  sincospif(whole * 4.656612873077393e-10f, &s, &c);                       // 2^-31
+  const float left = (float)((int64_t)top - (int64_t)whole) * (4.656612873077393e-10f * 3.14159265f);
+  return make_float2(fmaf(-s, left, c) * by, fmaf(c, left, s) * by);
+}
+
 __device__ __forceinline__ float up(float v) { return v; }
-__device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float up(__half v) { return __half2float(v); }
 __device__ __forceinline__ void down(float v, float* o) { *o = v; }
 __device__ __forceinline__ void down(float v, __nv_bfloat16* o) { *o = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void down(float v, __half* o) { *o = __float2half_rn(v); }
