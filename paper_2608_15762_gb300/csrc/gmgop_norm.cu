@@ -4,6 +4,7 @@
 // One pass: a row lies in registers, in fp32, from its loads to its stores; a warp takes a short row, a
 // block a longer one.  The mean and the mean square of what deviates from it are sums over the row,
 // each by shuffles and once through shared memory, so that no cancellation hides in them.
+// The last weights are loaded with the row: behind the sums they would be waited for once more.
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -15,69 +16,77 @@
 
 #include "../../include/gmgop.h"
 #include "gmgop_host.h"
+#include "gmgop_pairs.cuh"
 
 namespace gop {
 namespace {
 
 constexpr int kMaxThreads = 1024;
 
-__device__ __forceinline__ float up(float v) { return v; }
-__device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float up(__half v) { return __half2float(v); }
-__device__ __forceinline__ void down(float v, float* o) { *o = v; }
-__device__ __forceinline__ void down(float v, __nv_bfloat16* o) { *o = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void down(float v, __half* o) { *o = __float2half_rn(v); }
-
+__device__ __forceinline__ float up(float, uint32_t w) { return __uint_as_float(w); }
 template <class T>
-struct alignas(16) Bytes16 {
-  T v[16 / sizeof(T)];
-};
+__device__ __forceinline__ float up(T, uint32_t w) { return unpack(T(), w, 0); }
+template <class T>
+__device__ __forceinline__ uint32_t down(T, float v) { return pack(T(), v, 0.f); }
+__device__ __forceinline__ float one(const float* x) { return *x; }
+template <class T>
+__device__ __forceinline__ float one(const T* x) { return gop::up(*x); }
 
-// A thread's share of a row: kVecs times 8 neighbouring elements or, where rows are not made of whole
-// aligned 16 bytes, single elements; `threads` apart.
-template <int kVecs, bool kWide>
+// A thread's share of a row, as it lies in memory: kVecs times 8 neighbouring elements, `threads` apart, or, where rows
+// are not made of whole aligned 16 bytes, single elements, kRow apart.
+template <class T, int kVecs, bool kWide, int kRow>
 struct Share {
-  int tid, threads, n;
-  __device__ int at(int i) const {       // of element i of 8 * kVecs
-    return kWide ? (i / 8 * threads + tid) * 8 + i % 8 : i * threads + tid;
+  static constexpr int N = 8 * kVecs, kEach = 4 / (int)sizeof(T), kWords = kWide ? N / kEach : N;
+  uint32_t w[kWords];
+
+  static __device__ __forceinline__ int at(int i) {   // of element i
+    return kWide ? (i / 8 * (int)blockDim.x + (int)threadIdx.x) * 8 + i % 8 : i * kRow + (int)threadIdx.x;
   }
-  template <class T>
-  __device__ void load(const T* x, float* v) const {
-    if (kWide) {
+  // (what is beyond the row is 0)
+  __device__ __forceinline__ void load(const T* x, int n) {
+    if constexpr (kWide) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        constexpr int per = 16 / sizeof(T);
-#pragma unroll
-        for (int b = 0; b < 8 / per; ++b) {
-          Bytes16<T> a{};
-          if (at(8 * k) < n) a = *reinterpret_cast<const Bytes16<T>*>(x + at(8 * k) + b * per);
-#pragma unroll
-          for (int i = 0; i < per; ++i) v[8 * k + b * per + i] = up(a.v[i]);
-        }
+      for (int i = 0; i < kWords; i += 4) {
+        uint4 v{};
+        const int e = at(i * kEach);
+        if (e < n) v = *reinterpret_cast<const uint4*>(x + e);
+        w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8 * kVecs; ++i) v[i] = at(i) < n ? up(x[at(i)]) : 0.f;
+      for (int i = 0; i < N; ++i) {
+        const int e = at(i);
+        uint32_t v = 0;
+        if (e < n) v = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(x + e) : *reinterpret_cast<const unsigned short*>(x + e);
+        w[i] = v;
+      }
     }
   }
-  template <class T>
-  __device__ void store(T* x, const float* v) const {
-    if (kWide) {
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (!kWide || sizeof(T) == 4) return up(T(), w[i]);
+    else return unpack(T(), w[i / 2], i % 2);
+  }
+  static __device__ __forceinline__ void store(T* x, int n, const float* v) {
+    if constexpr (kWide) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        constexpr int per = 16 / sizeof(T);
+      for (int i = 0; i < kWords; i += 4) {
+        uint32_t o[4];
 #pragma unroll
-        for (int b = 0; b < 8 / per; ++b) {
-          Bytes16<T> a;
-#pragma unroll
-          for (int i = 0; i < per; ++i) down(v[8 * k + b * per + i], &a.v[i]);
-          if (at(8 * k) < n) *reinterpret_cast<Bytes16<T>*>(x + at(8 * k) + b * per) = a;
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (sizeof(T) == 4) o[k] = __float_as_uint(v[i + k]);
+          else o[k] = pack(T(), v[2 * (i + k)], v[2 * (i + k) + 1]);
         }
+        const int e = at(i * kEach);
+        if (e < n) *reinterpret_cast<uint4*>(x + e) = uint4{o[0], o[1], o[2], o[3]};
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8 * kVecs; ++i)
-        if (at(i) < n) down(v[i], x + at(i));
+      for (int i = 0; i < N; ++i) {
+        const int e = at(i);
+        if (e >= n) continue;
+        if constexpr (sizeof(T) == 4) x[e] = v[i];
+        else *reinterpret_cast<unsigned short*>(x + e) = (unsigned short)down(T(), v[i]);
+      }
     }
   }
 };
@@ -98,90 +107,117 @@ __device__ __forceinline__ float row_sum(float v, float (*buf)[kMaxThreads / 32]
   return v;
 }
 
-template <class T, class X, int kVecs, bool kWide, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1) norm_kernel(const __grid_constant__ op_norm_t a) {
+template <class T, class X, int kVecs, bool kWide, int kRow, int kBlocks>
+__global__ void __launch_bounds__(kRow == 32 ? 256 : kRow, kBlocks) norm_kernel(const __grid_constant__ op_norm_t a) {
+  using ShareT = Share<T, kVecs, kWide, kRow>;
+  using ShareX = Share<X, kVecs, kWide, kRow>;
   constexpr int N = 8 * kVecs;
   __shared__ float buf[2][kMaxThreads / 32];
   int turn = 0;
-  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  if (row >= a.m) return;              // (a whole warp, where a block has several rows)
-  const Share<kVecs, kWide> s{(int)threadIdx.x, (int)blockDim.x, (int)a.n};
-  const float n = (float)a.n;          // (divided by, as 1 / n is rounded: a row of one number has that mean)
-  // Where rows are few their last weights are loaded with them: behind the sums they would be waited for once more
-  constexpr bool kAhead = kVecs == 1 && kThreads > 128;
-  float w_ahead[kAhead ? N : 1], b_ahead[kAhead ? N : 1];
-  if (kAhead && a.weight) s.load(static_cast<const T*>(a.weight), w_ahead);
-  if (kAhead && a.bias) s.load(static_cast<const T*>(a.bias), b_ahead);
-  // v <- its norm with weight and bias
-  auto normed = [&](float* v, const void* weight, const void* bias, bool ahead) {
+  const int n = (int)a.n;
+  const float count = (float)n;        // (divided by, as 1 / n is rounded: a row of one number has that mean)
+  auto in = [&](int i) { return ShareT::at(kWide ? i / 8 * 8 : i) < n; };
+  // v <- its norm, without weight and bias
+  auto normed = [&](float (&v)[N]) {
     if (a.kind == GMG_NORM_LAYER) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) sum += v[i];
-      const float mean = row_sum(sum, buf, &turn) / n;
+      const float mean = row_sum(sum, buf, &turn) / count;
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = s.at(i) < a.n ? v[i] - mean : 0.f;
+      for (int i = 0; i < N; ++i) v[i] = in(i) ? v[i] - mean : 0.f;
     }
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) sum = fmaf(v[i], v[i], sum);
-    const float inv = 1.f / sqrtf(row_sum(sum, buf, &turn) / n + a.eps);
+    const float inv = 1.f / sqrtf(row_sum(sum, buf, &turn) / count + a.eps);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] *= inv;
-    if (weight) {
-      float w[N];
-      if (!ahead) s.load(static_cast<const T*>(weight), w);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] *= (ahead ? w_ahead[kAhead ? i : 0] : w[i]) + a.shift;
-    }
-    if (bias) {
-      float b[N];
-      if (!ahead) s.load(static_cast<const T*>(bias), b);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += ahead ? b_ahead[kAhead ? i : 0] : b[i];
-    }
   };
+  auto weighted = [&](float (&v)[N], const ShareT& w) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= w.get(i) + a.shift;
+  };
+  auto biased = [&](float (&v)[N], const void* bias) {
+    ShareT b;
+    b.load(static_cast<const T*>(bias), n);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += b.get(i);
+  };
+  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  if (row >= a.m) return;              // (a whole warp, where a block has several rows)
+  constexpr bool kAhead = kVecs <= 2;  // (where there are registers for them)
+  ShareX x;
+  ShareT y, last;
+  x.load(static_cast<const X*>(a.x) + row * a.x_row, n);
+  if (a.y) y.load(static_cast<const T*>(a.y) + row * a.y_row, n);
+  if (kAhead && a.weight) last.load(static_cast<const T*>(a.weight), n);
   float v[N];
-  s.load(static_cast<const X*>(a.x) + row * a.x_row, v);
   if (a.y) {
     float z[N];
-    s.load(static_cast<const T*>(a.y) + row * a.y_row, z);
-    if (a.after) normed(z, a.y_weight, a.y_bias, false);
-    if (a.gate && a.gate_col) {
-      float g[N];
-      s.load(static_cast<const T*>(a.gate) + row * a.gate_row, g);
 #pragma unroll
-      for (int i = 0; i < N; ++i) z[i] *= g[i];
+    for (int i = 0; i < N; ++i) z[i] = y.get(i);
+    if (a.after) {
+      normed(z);
+      if (a.y_weight) {
+        ShareT w;
+        w.load(static_cast<const T*>(a.y_weight), n);
+        weighted(z, w);
+      }
+      if (a.y_bias) biased(z, a.y_bias);
     }
-    const float by = a.gate && !a.gate_col ? up(static_cast<const T*>(a.gate)[row * a.gate_row]) * a.scale : a.scale;
+    if (a.gate && a.gate_col) {
+      ShareT g;
+      g.load(static_cast<const T*>(a.gate) + row * a.gate_row, n);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = fmaf(by, z[i], v[i]);
-    if (a.r) s.store(static_cast<X*>(a.r) + row * a.r_row, v);
+      for (int i = 0; i < N; ++i) z[i] *= g.get(i);
+    }
+    const float by = a.gate && !a.gate_col ? one(static_cast<const T*>(a.gate) + row * a.gate_row) * a.scale : a.scale;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = in(i) ? fmaf(by, z[i], x.get(i)) : 0.f;
+    if (a.r) ShareX::store(static_cast<X*>(a.r) + row * a.r_row, n, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = x.get(i);
   }
   if (a.h) {
-    normed(v, a.weight, a.bias, kAhead);
-    s.store(static_cast<T*>(a.h) + row * a.h_row, v);
+    normed(v);
+    if (a.weight) {
+      if (!kAhead) last.load(static_cast<const T*>(a.weight), n);
+      weighted(v, last);
+    }
+    if (a.bias) biased(v, a.bias);
+    ShareT::store(static_cast<T*>(a.h) + row * a.h_row, n, v);
   }
 }
 
 template <class T, class X, bool kWide>
 cudaError_t launch(const op_norm_t& a, cudaStream_t st) {
-  const int64_t vecs = (a.n + 7) / 8;
-  // a warp a row up to 1,024 elements; then a block, with 8 elements a thread where rows are few, so that a row's way is
-  // short, else with 16, which leaves more of them on an SM (%s)
-  auto go = [&](auto kernel, int v) {
-    int64_t threads = (vecs + v - 1) / v;
-    threads = (threads + 31) / 32 * 32;
-    const int rows = threads == 32 ? 4 : 1;
+  auto go = [&](auto kernel, int threads, int rows) {
     kernel<<<(unsigned)((a.m + rows - 1) / rows), dim3((unsigned)threads, rows), 0, st>>>(a);
     return cudaGetLastError();
   };
-  if (vecs <= 32) return go(norm_kernel<T, X, 1, kWide, 128>, 1);
-  if (vecs <= 128) return go(norm_kernel<T, X, 4, kWide, 128>, 4);
-  if (vecs <= kMaxThreads && a.m <= 1216) return go(norm_kernel<T, X, 1, kWide, kMaxThreads>, 1);
-  if (vecs <= 2 * 512) return go(norm_kernel<T, X, 2, kWide, 512>, 2);
-  if (vecs <= 2 * kMaxThreads) return go(norm_kernel<T, X, 2, kWide, kMaxThreads>, 2);
-  return go(norm_kernel<T, X, 4, kWide, kMaxThreads>, 4);
+  // A warp a row up to 1,024 elements; then a block, with 8 elements a thread where rows are few, so that a row's way is
+  // short, else with 16 (32 beyond 16,384), which leaves more of them on an SM.  Narrow rows in blocks of a fixed
+  // size, which makes their distances constants.
+  const int n = (int)a.n;
+  auto round = [](int v) { return (v + 31) / 32 * 32; };
+  if (n <= 256) return go(norm_kernel<T, X, 1, kWide, 32, 1>, 32, 8);
+  if (n <= 1024) return go(norm_kernel<T, X, 4, kWide, 32, 1>, 32, 4);
+  const bool short_way = a.m <= 304 && n <= 8192;
+  if (kWide) {
+    const int vecs = n / 8;
+    if (short_way) return go(norm_kernel<T, X, 1, true, 1024, 1>, round(vecs), 1);
+    if (n <= 4096) return go(norm_kernel<T, X, 2, true, 256, 4>, round((vecs + 1) / 2), 1);
+    if (n <= 8192) return go(norm_kernel<T, X, 2, true, 512, 2>, round((vecs + 1) / 2), 1);
+    if (n <= 16384) return go(norm_kernel<T, X, 2, true, 1024, 1>, round((vecs + 1) / 2), 1);
+    return go(norm_kernel<T, X, 4, true, 1024, 1>, round((vecs + 3) / 4), 1);
+  }
+  if (n <= 2048) return go(norm_kernel<T, X, 1, false, 256, 1>, 256, 1);
+  if (n <= 4096) return go(norm_kernel<T, X, 2, false, 256, 4>, 256, 1);
+  if (n <= 8192) return short_way ? go(norm_kernel<T, X, 1, false, 1024, 1>, 1024, 1) : go(norm_kernel<T, X, 2, false, 512, 2>, 512, 1);
+  if (n <= 16384) return go(norm_kernel<T, X, 2, false, 1024, 1>, 1024, 1);
+  return go(norm_kernel<T, X, 4, false, 1024, 1>, 1024, 1);
 }
 
 template <class T, class X>
