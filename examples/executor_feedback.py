@@ -4,9 +4,9 @@ the what-if simulation then places a graph whose durations they predict.
 
 The requests share a prompt: one request runs it, the others are forked from it (their pages are the
 same until they write), and every step's attention reads the shared pages once.  Weights and inputs
-are random.
+are random.  With --bits 8 the cache holds codes of 8 bits, and the same memory twice the tokens.
 
-    python examples/executor_feedback.py [--layers 4 --hidden 2048 --requests 24 --prompt 1500 --steps 6]
+    python examples/executor_feedback.py [--layers 4 --hidden 2048 --requests 24 --prompt 1500 --steps 6 --bits 16]
 """
 from __future__ import annotations
 
@@ -33,7 +33,7 @@ COVERS = {"kvw": "rope", "add1": "oproj", "silu": "gateup", "add2": "down"}
 class Executor:
     """The layers' weights, a paged cache, and the times of the operators that have run."""
 
-    def __init__(self, layers, hidden, heads, kv_heads, ffn, n_seq, tokens, page=16, dtype=torch.bfloat16, seed=0):
+    def __init__(self, layers, hidden, heads, kv_heads, ffn, n_seq, tokens, page=16, dtype=torch.bfloat16, seed=0, bits=16):
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
         self.layers, self.hidden, self.heads, self.kv_heads, self.dim = layers, hidden, heads, kv_heads, hidden // heads
@@ -44,15 +44,22 @@ class Executor:
             return (torch.randn(n, k, generator=g, device="cuda") * k ** -0.5).to(dtype)
 
         self.w = [dict(qkv=weight((heads + 2 * kv_heads) * D, hidden), o=weight(hidden, heads * D),
-                       gate=weight(ffn, hidden), up=weight(ffn, hidden), down=weight(hidden, ffn))
+                       gate=weight(ffn, hidden), up=weight(ffn, hidden), down=weight(hidden, ffn),
+                       norm1=torch.ones(hidden, dtype=dtype, device="cuda"), norm2=torch.ones(hidden, dtype=dtype, device="cuda"))
                   for _ in range(layers)]
         cols = -(-tokens // page) + 1
-        pool = torch.zeros(n_seq * cols, layers, 2, kv_heads, page, D, dtype=dtype, device="cuda")
-        self.cache = P.PageCache(pool, n_seq=n_seq, max_pages=cols)
+        if bits == 8:
+            pool = torch.zeros(n_seq * cols, P.page8_bytes(layers, kv_heads, page, D), dtype=torch.uint8, device="cuda")
+            self.cache = P.PageCache8(pool, layers, kv_heads, page, D, n_seq=n_seq, max_pages=cols)
+            self.plan, self.append, self.attend = P.AttendPlan8, P.rope_append8, P.attend8
+        else:
+            pool = torch.zeros(n_seq * cols, layers, 2, kv_heads, page, D, dtype=dtype, device="cuda")
+            self.cache = P.PageCache(pool, n_seq=n_seq, max_pages=cols)
+            self.plan, self.append, self.attend = P.AttendPlan, P.rope_append, P.attend
         self.rope = P.Rope(D, device="cuda")
         self.len = [0] * n_seq
         self.ahead = torch.randn(4096, 4096, generator=g, device="cuda").to(dtype)
-        self.samples = {k: [] for k in ("qkv", "rope", "attn", "oproj", "gateup", "down")}
+        self.samples = {k: [] for k in ("rms1", "qkv", "rope", "attn", "oproj", "rms2", "gateup", "down")}
         self.timed = []
 
     def ints(self, v):
@@ -74,8 +81,8 @@ class Executor:
         self.cache.grow(self.ints(rows), self.ints([n] * B))
         pos, seq = self.ints(o + i for o in old for i in range(n)), self.ints(r for r in rows for _ in range(n))
         kv = [o + n for o in old]
-        plan = P.AttendPlan([n] * B, kv, H, Hk, D, self.page, seq=rows,
-                            group_off=None if group is None else [0, B], prefix=None if group is None else [group])
+        plan = self.plan([n] * B, kv, H, Hk, D, self.page, seq=rows,
+                         group_off=None if group is None else [0, B], prefix=None if group is None else [group])
         first = torch.randn(T, self.hidden, generator=self.gen, device="cuda").to(self.dtype)
         pairs = float(sum(n * (t - n) + n * (n + 1) // 2 for t in kv))
         read = float(sum(kv) - (B - 1) * (group or 0))
@@ -84,6 +91,9 @@ class Executor:
             m, k = a.shape
             return self.call(kind, (float(m) * weight.shape[0] * k, 1.0), lambda: P.linear(a, weight, **kw))
 
+        def norm(kind, a, weight):
+            return self.call(kind, (float(T), 1.0), lambda: P.norm(a, weight))
+
         # twice: the first pass brings memory and code, the second is timed, behind enough other work that
         # the host has issued it when the GPU comes to it
         for timed in (False, True):
@@ -91,13 +101,13 @@ class Executor:
             for _ in range(20 * self.layers if timed else 0):
                 P.linear(self.ahead, self.ahead)
             for layer, w in enumerate(self.w):
-                qkv = product("qkv", norm(x), w["qkv"])
+                qkv = product("qkv", norm("rms1", x, w["norm1"]), w["qkv"])
                 q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([H * D, Hk * D, Hk * D], 1))
                 q = self.call("rope", (float(T), 1.0),
-                              lambda: P.rope_append(self.rope, q, k, v, pos, seq, self.cache, layer))
-                o = self.call("attn", (pairs, read, 1.0), lambda: P.attend(plan, q, self.cache, layer))
+                              lambda: self.append(self.rope, q, k, v, pos, seq, self.cache, layer))
+                o = self.call("attn", (pairs, read, 1.0), lambda: self.attend(plan, q, self.cache, layer))
                 x = product("oproj", o.flatten(1), w["o"], residual=x)
-                h = product("gateup", norm(x), w["up"], gate=w["gate"], act="silu")
+                h = product("gateup", norm("rms2", x, w["norm2"]), w["up"], gate=w["gate"], act="silu")
                 x = product("down", h, w["down"], residual=x)
         for r in rows:
             self.len[r] += n
@@ -118,11 +128,6 @@ class Executor:
         self.cache.compact()
         for r in rows:
             self.len[r] = 0
-
-
-def norm(x):
-    f = x.float()
-    return (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
 
 def fit(samples):
@@ -170,8 +175,8 @@ def graph(layers, requests, n_dev, dur_of, out_bytes):
 
 
 def main(layers=4, hidden=2048, heads=16, kv_heads=2, ffn=5632, requests=24, prompt=1500, steps=6, n_dev=8,
-         candidates=1024, say=print):
-    ex = Executor(layers, hidden, heads, kv_heads, ffn, requests, prompt + 16 * steps + 64)
+         candidates=1024, say=print, bits=16):
+    ex = Executor(layers, hidden, heads, kv_heads, ffn, requests, prompt + 16 * steps + 64, bits=bits)
     ex.step([0], prompt, keep_times=False)                    # the shared prompt (and the first run of everything)
     others = list(range(1, requests))
     ex.fork(0, others)
@@ -192,7 +197,7 @@ def main(layers=4, hidden=2048, heads=16, kv_heads=2, ffn=5632, requests=24, pro
     T, D = requests, hidden // heads
     sizes = dict(qkv=(heads + 2 * kv_heads) * D * hidden, oproj=hidden * hidden, gateup=ffn * hidden, down=hidden * ffn)
     features = {k: (float(T) * v, 1.0) for k, v in sizes.items()}
-    features["rope"] = (float(T), 1.0)
+    features["rope"] = features["rms1"] = features["rms2"] = (float(T), 1.0)
     features["attn"] = (float(T * (prompt + 20)), float(prompt + 20 * T), 1.0)
     desc = graph(layers, requests // 4, n_dev, lambda kind: durations(fitted, list(kind), features, 5), T * hidden * 2)
     gmg = G.gmg_create(desc)
@@ -207,6 +212,6 @@ def main(layers=4, hidden=2048, heads=16, kv_heads=2, ffn=5632, requests=24, pro
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name, value in (("layers", 4), ("hidden", 2048), ("heads", 16), ("kv-heads", 2), ("ffn", 5632), ("requests", 24),
-                        ("prompt", 1500), ("steps", 6)):
+                        ("prompt", 1500), ("steps", 6), ("bits", 16)):
         ap.add_argument("--" + name, type=int, default=value)
     main(**{k.replace("-", "_"): v for k, v in vars(ap.parse_args()).items()})

@@ -725,3 +725,18 @@ def test_a_layer_on_a_cache_in_8_bits():
     cache.compact()
     step([4, 1], 40, [23, 206])
     assert cache.code()[0] == P.PAGE_OK and cache.status.tolist()[4:6] == [0, 0]
+
+
+def test_executor_example_in_8_bits():
+    """The example's layers on a cache in 8 bits: it runs, its operators are timed, a graph is placed on their times."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "executor_feedback.py")
+    spec = importlib.util.spec_from_file_location("executor_feedback_8", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    out = m.main(layers=2, hidden=256, heads=4, kv_heads=1, ffn=512, requests=8, prompt=200, steps=3, n_dev=4, candidates=64,
+                 say=lambda *_: None, bits=8)
+    ex = out["executor"]
+    assert ex.cache.status.tolist()[4:6] == [0, 0] and all(len(v) > 0 for v in ex.samples.values())
+    assert out["makespan"] > 0 and bool((ex.cache.scales >= 0).all())
