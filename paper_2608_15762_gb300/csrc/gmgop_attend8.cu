@@ -177,13 +177,18 @@ __device__ __forceinline__ void copy_pages(const CUtensorMap& map, const Args8& 
   __syncwarp();
 }
 
-// Codes that are NaN become zeros; first_nan, a byte a dimension, falls to the first query that sees one.
-__device__ __forceinline__ bool drop_nan(uint4* v, uint32_t* first_nan, uint32_t query) {
-  bool any = false;
-  uint32_t* w = reinterpret_cast<uint32_t*>(v);
+__device__ __forceinline__ bool has_nan(uint4 v) {
+  const uint32_t any = ((v.x & 0x7f7f7f7fu) + 0x01010101u) | ((v.y & 0x7f7f7f7fu) + 0x01010101u) |
+                       ((v.z & 0x7f7f7f7fu) + 0x01010101u) | ((v.w & 0x7f7f7f7fu) + 0x01010101u);
+  return any & 0x80808080u;
+}
+// Codes that are NaN become zeros; first_nan, a byte a dimension, falls to the first query that sees one.  (Apart from the
+// loops that need it so rarely: its instructions would lie between theirs.)
+__device__ __noinline__ uint4 without_nan(uint4 v, uint32_t* first_nan, uint32_t query) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (!(((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) continue;
+  for (int i = 0; i < 4; ++i)
+#pragma unroll 1
     for (int b = 0; b < 4; ++b)
       if ((w[i] >> (8 * b) & 0x7f) == 0x7f) {
         uint32_t was = *reinterpret_cast<volatile uint32_t*>(first_nan + i);
@@ -193,10 +198,8 @@ __device__ __forceinline__ bool drop_nan(uint4* v, uint32_t* first_nan, uint32_t
           was = found;
         }
         w[i] &= ~(0xffu << (8 * b));
-        any = true;
       }
-  }
-  return any;
+  return uint4{w[0], w[1], w[2], w[3]};
 }
 
 // 16 columns over the warp's lanes (two a register pair), summed or their largest: lane 2 i has column i's in the end.
@@ -636,7 +639,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
         for (int c16 = 0; c16 < 8; ++c16) {
           uint4* at = codes_at<128>(base + S::kRingAt + slot * S::kSlot, r, c16);
           uint4 v = in ? *at : uint4{};
-          drop_nan(&v, misc.first_nan + 4 * c16, query);
+          if (has_nan(v)) v = without_nan(v, misc.first_nan + 4 * c16, query);
           *at = v;
         }
       }
@@ -848,7 +851,10 @@ __device__ __forceinline__ void widen(unsigned char* codes, unsigned char* wide,
         // Keys outside the item: whatever lies there must not meet the zeros of P.  Nor must a NaN that
         // some row does not see; those that see it get theirs at the end.
         if (key < it.lo || key >= it.hi) v = uint4{};
-        if (drop_nan(&v, misc.first_nan + 4 * c16, key <= it.pos0 ? 0 : min(key - it.pos0, 254))) misc.any_nan = 1;
+        if (has_nan(v)) {
+          v = without_nan(v, misc.first_nan + 4 * c16, key <= it.pos0 ? 0 : min(key - it.pos0, 254));
+          misc.any_nan = 1;
+        }
       }
       uint32_t o[8];
       wide16(v, o);
