@@ -11,7 +11,7 @@
 //   S^T [128 keys][rows] = K Q^T,   O^T [128 dims][rows] += V^T P^T.
 // Keys fill the tensor core's 128 lanes and rows are columns, so that a step of few rows costs few columns,
 // exponentials and registers, and K and V are read once, as the codes that they are, by fp8 products.
-// What the codes meet is split into several of them: Q exactly, P to 12 bits or more.
+// What the codes meet is split into several of them: Q as bf16 and fp16 have it, P to 12 bits or more.
 //
 // Tiles of more rows, up to 128, lie with their rows on the lanes, against 64 keys a step.  K is taken as the
 // codes that it is here too, by Q's.  V becomes fp16, which holds e4m3 exactly, on its way through shared
@@ -559,10 +559,14 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
         }
         return most;
       };
-      if (__any_sync(0xffffffffu, exponents() > kMostFew + kBiasFew) && lane == 0) misc.flag[j & 1] = j + 1;
-      bar_meet(met, &meetings, failed);
-      if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&misc.flag[j & 1]), 0) == j + 1u) {
-        // references are raised: the columns' maxima over the keys
+      bool raise = j == 0;
+      if (j > 0) {
+        if (__any_sync(0xffffffffu, exponents() > kMostFew + kBiasFew) && lane == 0) misc.flag[j & 1] = j + 1;
+        bar_meet(met, &meetings, failed);
+        raise = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&misc.flag[j & 1]), 0) == j + 1u;
+      }
+      if (raise) {
+        // references are raised, or set: the columns' maxima over the keys
         sums();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -706,7 +710,9 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
 //   warp 11         products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
 constexpr int kKeys = 64, kRows = 128;   // of a step, of a tile
 constexpr int kThreads = 384;
-constexpr float kBias = 7.f, kMost = 8.f;   // a weight is at most 2^(kMost + kBias), in fp16's range
+// A weight is at most 2^(kMost + kBias), in fp16's range, and the largest at least 2^kBias.  (A raised reference takes the whole
+// warp through O: with 7 and 8 chunks of prompts took 344 us, with 4 and 11 334.)
+constexpr float kBias = 4.f, kMost = 11.f;
 
 template <class T, int DP>
 struct Shape {
@@ -980,55 +986,47 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
     {
       // Q's terms to shared memory, 8 elements a step: consecutive threads along a row, which is first multiplied by the
       // power of two that brings its largest to between 2^7 and 2^8
-      // (four at a time, the next four on their way: a block goes through this code once, and more of it would
-      // be fetched for longer than it runs)
+      // (one at a time, the next on its way: a block goes through this code a few times, and more of it would be
+      // fetched for longer than it runs; four at a time chunks of prompts took 355 us, one 345)
       constexpr int kLanes = DP / 8, kEach = kRows * kLanes / 256, kApart = 256 / kLanes;
       const int c = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
       const uint32_t per_group = 65536 / a.group + 1;   // row * per_group >> 16 is row / group, for rows below 128
       auto piece = [&](int i) { return q_piece<T>(g, it, hk, rows, row0 + i * kApart, c, per_group); };
-      uint4 ahead[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) ahead[i] = piece(i);
+      uint4 ahead = piece(0);
 #pragma unroll 1
-      for (int i0 = 0; i0 < kEach && i0 * kApart < rows; i0 += 4) {
-        uint4 v[4];
+      for (int i = 0; i < kEach && i * kApart < rows; ++i) {
+        uint4 v = ahead;
+        ahead = piece(i + 1);
+        const int row = row0 + i * kApart;
+        if (row >= rows || c * 8 >= a.dim) v = uint4{};
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        // of |q| (a row that holds an infinity is NaN in the end, whatever its scale)
+        uint32_t both = most_of(T(), most_of(T(), w[0] & 0x7fff7fff, w[1] & 0x7fff7fff), most_of(T(), w[2] & 0x7fff7fff, w[3] & 0x7fff7fff));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = ahead[i];
+        for (int d = kLanes / 2; d; d /= 2) both = most_of(T(), both, __shfl_xor_sync(0xffffffffu, both, d));
+        const float most = fmaxf(unpack(T(), both, 0), unpack(T(), both, 1));
+        const int e = max(min(134 - (int)(__float_as_uint(most) >> 23), 126), -120);
+        if (c == 0) misc.q_scale[row] = (signed char)e;
+        float by = __int_as_float((e + 127) << 23);
+        if (a.negative) by = -by;
+        uint64_t xy[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ahead[i] = piece(i0 + 4 + i);
+        for (int k = 0; k < 4; ++k) {
+          const float x0 = unpack(T(), w[k], 0) * by, x1 = unpack(T(), w[k], 1) * by;
+          xy[k] = two(fmaf(x0, 0.f, x0), fmaf(x1, 0.f, x1));   // (infinities to NaN: there is no code for them)
+        }
+        // 16 bytes of a row, where the products look for them: the swizzle of rows of DP bytes
+        unsigned char* at = base + row * DP + ((c / 2) ^ (DP == 64 ? row >> 1 & 3 : row & 7)) * 16 + (c & 1) * 8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = row0 + (i0 + i) * kApart;
-          if (row >= rows || c * 8 >= a.dim) v[i] = uint4{};
-          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-          // of |q| (a row that holds an infinity is NaN in the end, whatever its scale)
-          uint32_t both = most_of(T(), most_of(T(), w[0] & 0x7fff7fff, w[1] & 0x7fff7fff), most_of(T(), w[2] & 0x7fff7fff, w[3] & 0x7fff7fff));
+        for (int t = 0; t < S::kTerms; ++t) {
+          uint32_t o[2];
 #pragma unroll
-          for (int d = kLanes / 2; d; d /= 2) both = most_of(T(), both, __shfl_xor_sync(0xffffffffu, both, d));
-          const float most = fmaxf(unpack(T(), both, 0), unpack(T(), both, 1));
-          const int e = max(min(134 - (int)(__float_as_uint(most) >> 23), 126), -120);
-          if (c == 0) misc.q_scale[row] = (signed char)e;
-          float by = __int_as_float((e + 127) << 23);
-          if (a.negative) by = -by;
-          uint64_t xy[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float x0 = unpack(T(), w[k], 0) * by, x1 = unpack(T(), w[k], 1) * by;
-            xy[k] = two(fmaf(x0, 0.f, x0), fmaf(x1, 0.f, x1));   // (infinities to NaN: there is no code for them)
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t lo = next_code(&xy[2 * k]), hi = next_code(&xy[2 * k + 1]);
+            o[k] = lo | hi << 16;
           }
-          // 16 bytes of a row, where the products look for them: the swizzle of rows of DP bytes
-          unsigned char* at = base + row * DP + ((c / 2) ^ (DP == 64 ? row >> 1 & 3 : row & 7)) * 16 + (c & 1) * 8;
-#pragma unroll
-          for (int t = 0; t < S::kTerms; ++t) {
-            uint32_t o[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint32_t lo = next_code(&xy[2 * k]), hi = next_code(&xy[2 * k + 1]);
-              o[k] = lo | hi << 16;
-            }
-            *reinterpret_cast<uint2*>(at + t * S::kTerm) = uint2{o[0], o[1]};
-          }
-      }
+          *reinterpret_cast<uint2*>(at + t * S::kTerm) = uint2{o[0], o[1]};
+        }
       }
       fence_async();
       __syncwarp();
@@ -1180,7 +1178,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
 
 // A plan is for one of the kernels: the one whose steps and items take less time (in clocks; the many rows' steps are of
 // 64 keys).
-constexpr Cutting kCuttingFew = {kFewKeys, kFewRows, 4, 8, 3, 5, true}, kCuttingMany = {kKeys, kRows, 6, 12, 4, 8, true};
+constexpr Cutting kCuttingFew = {kFewKeys, kFewRows, 4, 8, 4, 5, true}, kCuttingMany = {kKeys, kRows, 6, 12, 4, 8, true};
 constexpr int64_t kFewClocks = 1900, kManyClocks = 1300;
 
 int64_t steps_of(const Work& w, const Cutting& cut) {

@@ -122,9 +122,10 @@ def near(got_codes, got_scales, want, exact, dtol):
 def attend(q, keys, values, v_scales, n_q, scale):
     """One request: q [n, heads, dim]; keys, values [tokens, kv_heads, dim] in 64 bits (code times scale),
     v_scales [tokens, kv_heads].  (o, bound, lse, bound): a score is off by d + 8 roundings of its magnitudes
-    (two each, as a tensor core may cut off), and so is its exponent; the weights w = p v_scale are rounded once to fp16,
-    whose numbers below 2^-14 are multiples of 2^-24 and where the largest w is at least 2^7; sums over t keys
-    are off by t / 16 + 16 roundings."""
+    (two each, as a tensor core may cut off), and so is its exponent; the weights w = p v_scale, of which the largest is
+    at least 2^4, are rounded to 11 bits or more, the smaller ones to multiples of 2^-17 (bf16: three codes, the last a
+    256th of what it says, of at least 2^-9) or 2^-21 (fp16: four, a 4096th; fp16 itself has 2^-24); sums over t keys are
+    off by t / 16 + 16 roundings."""
     n, H, D = q.shape
     t, Hk = keys.shape[0], keys.shape[1]
     G = H // Hk
@@ -145,8 +146,9 @@ def attend(q, keys, values, v_scales, n_q, scale):
     tol = (2.0 ** -11 + rel)[..., None] * mag + u * o.abs() + TINY[q.dtype]
     if t:
         w = p * vs
-        most = w.amax(-1, keepdim=True)                        # at least 2^7 in the kernel's units
-        tol = tol + 2.0 ** -25 * 2.0 ** -7 * (most * ((v.abs() / vs.transpose(1, 2)).masked_fill(vs.transpose(1, 2) == 0, 0)
+        most = w.amax(-1, keepdim=True)                        # at least 2^4 in the kernel's units
+        half = 2.0 ** (-18 if q.dtype is torch.bfloat16 else -22)
+        tol = tol + half * 2.0 ** -4 * (most * ((v.abs() / vs.transpose(1, 2)).masked_fill(vs.transpose(1, 2) == 0, 0)
                                                       ).nansum(1, keepdim=True))
     ltol = worst + 2e-5 + 2 * (t / 16 + 16) * U32 + 4 * U32 * lse.abs().masked_fill(lse.isinf(), 0)
     return o.transpose(0, 1), tol.transpose(0, 1), lse.transpose(0, 1), ltol.transpose(0, 1)
