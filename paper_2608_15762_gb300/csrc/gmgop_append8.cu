@@ -2,10 +2,14 @@
 // declared in include/gmgop.h.
 //
 // The unit is a run: the tokens of the call that one block of 16 takes, one after another in the
-// lists (what is not written may lie between).  Its first token speaks for it.  A warp takes a run of one head's keys or values: up to
-// 16 tokens lie in its registers while their largest magnitude is found, the block's scale
-// follows, and the codes are written once.  Scales are powers of two, so a block whose scale grows
+// lists (what is not written may lie between).  Its first token speaks for it.  A warp takes a run of
+// one head's keys or values: up to 16 tokens lie in its registers while their largest magnitude is
+// found, the block's scale follows, and the codes are written once.  Scales are powers of two, so a block whose scale grows
 // is rounded again only where its codes become subnormal, and x / scale is exact.
+// What bounds it is memory, as far as the few registers allow that keep a run's loads in flight (a prompt of 32,768
+// tokens, 32 + 8 + 8 heads of 128: 141 us, of them 59 for keys and values, 173 MB at 2.9 TB/s, and
+// 82 for queries), and where tokens are few the chain of loads from a token's position to
+// its block's scale (16 tokens 4.8 us).
 // A thread block serves a share of `chunk` tokens' heads: sines and cosines once for all of them, as
 // in the cache of 16-bit values.  A run that reaches past its block's tokens is taken whole by the
 // block that it begins in.
@@ -14,6 +18,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "../../include/gmgop.h"
 #include "gmgop_host.h"
@@ -473,12 +479,15 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  // One token a block, its queries and its runs in shares; where there are many, the queries as dense ones, in a launch of
-  // their own with few registers a thread, and then 16 tokens a block
+  // One token a block, its queries and its runs in shares: a decode step of 16 tokens 5.1 us, with 16 a block 8.4.
+  // Where there are many, and not each a sequence's only one, 16 a block, which has few runs then (2,432 tokens, 32 + 8 + 8
+  // heads of 128: 20.0 us, one a block 27.8; 608 12.5 and 13.3; 304 12.0 and 9.7; 1,216 of as many sequences 28.4 and
+  // 21.9, 4,864 87.2 and 88.1); many queries then as dense ones, in a launch of their own with few registers a thread
+  // (32,768 tokens 141 us, in one launch 156; 777 of 20 heads of 80 10.0 and 8.4).
   a.chunk = 1;
-  if (n_tokens >= 152 * 2 * kChunk) {
+  if (n_tokens >= 152 * 4 && n_tokens >= std::min<int64_t>(int64_t(kBlock) * cache->n_seq, 152 * 2 * kChunk)) {
     a.chunk = kChunk;
-    if (n_heads > 0) {
+    if (n_tokens * n_heads * a.dim >= 1 << 22) {
       const int e = op_rope(rope, dtype, n_tokens, n_heads, a.dim, q, q_tok, q_head, pos, 0, q_out, o_tok, o_head, stream);
       if (e != GMG_OK) return e;
       a.n_heads = 0;

@@ -1,6 +1,11 @@
 // Norms before and after a block, with its gate and residual scale.  The C ABI is declared in
 // include/gmgop.h.
 //
+// N(v; w, b) = (v - mean) / sqrt(mean((v - mean)^2) + eps) (w + shift) + b, with mean 0 for rms, of
+// x + scale * gate * z, and z = N(y) or y.  What bounds it is memory (16,384 rows of 4,096, x in 32 bits:
+// 126.5 us, 6.4 TB/s of the 805 MB that it has to move), and a launch's and two loads' latency where rows
+// are few (one of 4,096: 2.0 us).
+//
 // One pass: a row lies in registers, in fp32, from its loads to its stores; a warp takes a short row, a
 // block a longer one.  The mean and the mean square of what deviates from it are sums over the row,
 // each by shuffles and once through shared memory, so that no cancellation hides in them.
@@ -146,7 +151,8 @@ __global__ void __launch_bounds__(kRow == 32 ? 256 : kRow, kBlocks) norm_kernel(
   };
   const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   if (row >= a.m) return;              // (a whole warp, where a block has several rows)
-  constexpr bool kAhead = kVecs <= 2;  // (where there are registers for them)
+  // (where there are registers for them: 16 rows of 4,096 2.41 us, behind the sums 2.54; 2,048 of 32,768 90.5, with them 95.6)
+  constexpr bool kAhead = kVecs <= 2;
   ShareX x;
   ShareT y, last;
   x.load(static_cast<const X*>(a.x) + row * a.x_row, n);
@@ -197,25 +203,25 @@ cudaError_t launch(const op_norm_t& a, cudaStream_t st) {
     kernel<<<(unsigned)((a.m + rows - 1) / rows), dim3((unsigned)threads, rows), 0, st>>>(a);
     return cudaGetLastError();
   };
-  // A warp a row up to 1,024 elements; then a block, with 8 elements a thread where rows are few, so that a row's way is
-  // short, else with 16 (32 beyond 16,384), which leaves more of them on an SM.  Narrow rows in blocks of a fixed
-  // size, which makes their distances constants.
+  // A warp a row up to 256 elements (100,000 rows of 128 28.8 us, a block each 52.8), else a block (50,000 rows of 1,024
+  // 60.9 us, a warp each 64.6; of 1,003 177, a warp each 349), with 16 elements a thread, 32 beyond 16,384.  Where rows are
+  // few, 8 a thread make a row's way shorter: 16 rows of 4,096 2.41 us, with 16 a thread 2.55, but 608 rows 4.9 against 3.9
+  // and 16 of 8,192 2.98 against 2.83; of 5,003, element by element, 3.65 against 5.03, and 304 rows 6.5 against 6.75.
+  // Rows that are loaded element by element (16,384 x 4,096 so: 134 us, in 16 bytes 83) have blocks of a fixed size,
+  // which makes their distances constants.
   const int n = (int)a.n;
-  auto round = [](int v) { return (v + 31) / 32 * 32; };
   if (n <= 256) return go(norm_kernel<T, X, 1, kWide, 32, 1>, 32, 8);
-  if (n <= 1024) return go(norm_kernel<T, X, 4, kWide, 32, 1>, 32, 4);
-  const bool short_way = a.m <= 304 && n <= 8192;
   if (kWide) {
     const int vecs = n / 8;
-    if (short_way) return go(norm_kernel<T, X, 1, true, 1024, 1>, round(vecs), 1);
-    if (n <= 4096) return go(norm_kernel<T, X, 2, true, 256, 4>, round((vecs + 1) / 2), 1);
-    if (n <= 8192) return go(norm_kernel<T, X, 2, true, 512, 2>, round((vecs + 1) / 2), 1);
+    auto round = [](int v) { return (v + 31) / 32 * 32; };
+    if (a.m <= 152 && n <= 4096) return go(norm_kernel<T, X, 1, true, 1024, 1>, round(vecs), 1);
     if (n <= 16384) return go(norm_kernel<T, X, 2, true, 1024, 1>, round((vecs + 1) / 2), 1);
     return go(norm_kernel<T, X, 4, true, 1024, 1>, round((vecs + 3) / 4), 1);
   }
   if (n <= 2048) return go(norm_kernel<T, X, 1, false, 256, 1>, 256, 1);
   if (n <= 4096) return go(norm_kernel<T, X, 2, false, 256, 4>, 256, 1);
-  if (n <= 8192) return short_way ? go(norm_kernel<T, X, 1, false, 1024, 1>, 1024, 1) : go(norm_kernel<T, X, 2, false, 512, 2>, 512, 1);
+  if (n <= 8192)
+    return a.m <= 304 ? go(norm_kernel<T, X, 1, false, 1024, 1>, 1024, 1) : go(norm_kernel<T, X, 2, false, 512, 2>, 512, 1);
   if (n <= 16384) return go(norm_kernel<T, X, 2, false, 1024, 1>, 1024, 1);
   return go(norm_kernel<T, X, 4, false, 1024, 1>, 1024, 1);
 }
