@@ -75,6 +75,16 @@ def test_norm_sizes(m, n, dt, xt):
         _check_norm(P.norm(x, **kw), x, kw, kind)
 
 
+@pytest.mark.parametrize("dt,xt", [(BF, BF), (HF, FF), (FF, FF)])
+@pytest.mark.parametrize("m,n", [(152, 4096), (153, 4096), (200, 264), (153, 2040), (304, 5003), (305, 5003), (310, 301), (160, 16384),
+                                 (257, 129), (1027, 8)])
+def test_norm_many_rows(m, n, dt, xt):
+    g = _gen(m + 3 * n)
+    for kind, after, gate, bias in (("rms", True, "column", False), ("layer", False, "row", True)):
+        x, kw = _norm_case(g, m, n, dt, xt, kind, after, gate, bias)
+        _check_norm(P.norm(x, **kw), x, kw, "%s %s" % (kind, gate))
+
+
 def test_norm_without_weights_and_with_shifted_ones():
     g = _gen(2)
     x, y = _rand(g, 5, 640, dtype=FF), _rand(g, 5, 640)
@@ -256,6 +266,23 @@ def test_append8(T, H, Hk, D, rot, page, inter, dtype):
         dropped += sum(s == seq[T - 1] and p // page == pos[T - 1] // page for s, p in zip(seq, pos))
     _check_append(c, 1, T, H, _ints(pos), _ints(seq), plan, f, inter, dtype, g, 1.25)
     assert c.status.tolist()[4] == dropped
+
+
+@pytest.mark.parametrize("T,n_seq,H,Hk,D,rot,page,inter", [(608, 38, 5, 1, 128, 128, 16, False), (607, 3, 4, 2, 64, 64, 32, False),
+                                                           (777, 2, 5, 3, 80, 32, 64, True), (1300, 100, 4, 1, 48, 16, 16, False),
+                                                           (4000, 5, 17, 1, 64, 64, 16, False), (4900, 700, 9, 1, 96, 96, 16, False)])
+def test_append8_tokens_in_sixteens_and_queries_apart(T, n_seq, H, Hk, D, rot, page, inter):
+    g = _gen(T + D)
+    per = -(-T // n_seq)
+    cols = -(-(per + 20) // page) + 1
+    c = _cache8(g, n_seq * cols + 3, 1, Hk, page, D, n_seq, cols)
+    f = P.rope_freqs(rot, 500.0)[0]
+    seq = [t // per for t in range(T)]
+    pos = [s % 19 + t % per for t, s in enumerate(seq)]
+    for t in range(5, T, 40):
+        seq[t] = -1
+    _check_append(c, 0, T, H, _ints(pos), _ints(seq), P.Rope(rot, freqs=f, interleaved=inter), f, inter, BF, g)
+    assert c.status.tolist()[4] == 0
 
 
 def test_append8_one_token_at_a_time():
