@@ -7,9 +7,9 @@
 // found, the block's scale follows, and the codes are written once.  Scales are powers of two, so a block whose scale grows
 // is rounded again only where its codes become subnormal, and x / scale is exact.
 // What bounds it is memory, as far as the few registers allow that keep a run's loads in flight (a prompt of 32,768
-// tokens, 32 + 8 + 8 heads of 128: 141 us, of them 59 for keys and values, 173 MB at 2.9 TB/s, and
+// tokens, 32 + 8 + 8 heads of 128: 136 us, of them 54 for keys and values, 201 MB at 3.7 TB/s, and
 // 82 for queries), and where tokens are few the chain of loads from a token's position to
-// its block's scale (16 tokens 4.8 us).
+// its block's scale (16 tokens 4.5 us).
 // A thread block serves a share of `chunk` tokens' heads: sines and cosines once for all of them, as
 // in the cache of 16-bit values.  A run that reaches past its block's tokens is taken whole by the
 // block that it begins in.
@@ -28,7 +28,7 @@
 namespace gop {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;       // (blocks of 256: a prompt 142 us for 136, 304 requests' tokens 10.1 for 7.6)
 constexpr int kChunk = 16;          // tokens of a block where there are many
 constexpr int kBlock = kScaleTokens;
 constexpr int kReach = 32;          // entries of the lists that a run lies in
@@ -146,7 +146,7 @@ __device__ __forceinline__ float most_finite(const float* v, float top) {
 }
 
 template <class T, bool kWide, bool kInter>
-__global__ void __launch_bounds__(kThreads, 3) append8_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_constant__ AppendArgs a) {
   // [chunk + 15][half] for the keys of the block's runs, then [chunk][half] for its queries (which are turned as dense
   // ones are)
   extern __shared__ __align__(16) float2 cs[];
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 3) append8_kernel(const __grid_const
   }
   __syncthreads();
   {
-    // a run is what is written from its head to the next, within kReach entries; a warp lists every eighth
+    // a run is what is written from its head to the next, within kReach entries; a warp lists every fourth
     const uint32_t mine = bits_at(heads, kReach) & ((1u << own) - 1);   // (own <= 16)
     const int n = __popc(mine);
     uint32_t rest = mine;
@@ -428,7 +428,7 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
   int64_t split = (152 * 4 + blocks - 1) / blocks;
   if (split > (steps + kThreads - 1) / kThreads) split = (steps + kThreads - 1) / kThreads;
   const dim3 grid((unsigned)blocks, (unsigned)(split < 1 ? 1 : split));
-  append8_kernel<T, kWide, kInter><<<grid, kThreads, (2 * a.chunk + kBlock - 1) * a.half * sizeof(float2), st>>>(a);
+  append8_kernel<T, kWide, kInter><<<grid, kThreads, ((a.n_heads > 0 ? 2 : 1) * a.chunk + kBlock - 1) * a.half * sizeof(float2), st>>>(a);
   return cudaGetLastError();
 }
 
@@ -475,19 +475,19 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   a.page_bytes = page8_bytes(*cache);
   a.codes_at = int64_t(layer) * 2 * a.n_kv * cache->page_tokens * a.dim;
   a.scales_at = page8_scales(*cache) + int64_t(layer) * 2 * a.n_kv * (cache->page_tokens / kScaleTokens) * 4;
-  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps
+  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps (else a prompt takes 255 us for 136)
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  // One token a block, its queries and its runs in shares: a decode step of 16 tokens 5.1 us, with 16 a block 8.4.
-  // Where there are many, and not each a sequence's only one, 16 a block, which has few runs then (2,432 tokens, 32 + 8 + 8
-  // heads of 128: 20.0 us, one a block 27.8; 608 12.5 and 13.3; 304 12.0 and 9.7; 1,216 of as many sequences 28.4 and
-  // 21.9, 4,864 87.2 and 88.1); many queries then as dense ones, in a launch of their own with few registers a thread
-  // (32,768 tokens 141 us, in one launch 156; 777 of 20 heads of 80 10.0 and 8.4).
+  // One token a block, its queries and its runs in shares: a decode step of 16 tokens 4.5 us, with 16 a block 9.2.
+  // Where there are many, and not each a sequence's only one, 16 a block, which has few runs then (with 32 + 8 + 8 heads of
+  // 128, 2,432 tokens 20.8 us, one a block 26.0; 608 12.0 and 13.3; 304 11.4 and 10.5; 1,216 of as many sequences 25.5 and
+  // 20.3, 4,864 81.7 and 82.1).  Very many queries then as dense ones, in a launch of their own with few registers a thread
+  // (32,768 tokens 136 us, in one launch 161; 4,864 32.6 and 34.8; 2,432 21.8 and 20.8; 16,384 of 8 heads of 64 21.5 and 17.3).
   a.chunk = 1;
   if (n_tokens >= 152 * 4 && n_tokens >= std::min<int64_t>(int64_t(kBlock) * cache->n_seq, 152 * 2 * kChunk)) {
     a.chunk = kChunk;
-    if (n_tokens * n_heads * a.dim >= 1 << 22) {
+    if (n_tokens * n_heads * a.dim >= 1 << 24) {
       const int e = op_rope(rope, dtype, n_tokens, n_heads, a.dim, q, q_tok, q_head, pos, 0, q_out, o_tok, o_head, stream);
       if (e != GMG_OK) return e;
       a.n_heads = 0;

@@ -270,7 +270,8 @@ def test_append8(T, H, Hk, D, rot, page, inter, dtype):
 
 @pytest.mark.parametrize("T,n_seq,H,Hk,D,rot,page,inter", [(608, 38, 5, 1, 128, 128, 16, False), (607, 3, 4, 2, 64, 64, 32, False),
                                                            (777, 2, 5, 3, 80, 32, 64, True), (1300, 100, 4, 1, 48, 16, 16, False),
-                                                           (4000, 5, 17, 1, 64, 64, 16, False), (4900, 700, 9, 1, 96, 96, 16, False)])
+                                                           (4000, 5, 17, 1, 64, 64, 16, False), (4900, 700, 9, 1, 96, 96, 16, False),
+                                                           (4400, 3, 30, 1, 128, 128, 16, False)])
 def test_append8_tokens_in_sixteens_and_queries_apart(T, n_seq, H, Hk, D, rot, page, inter):
     g = _gen(T + D)
     per = -(-T // n_seq)
