@@ -117,6 +117,28 @@ def test_norm_strides_and_alignment(off, ld, xt):
     _check_norm(P.norm(x, **kw), x, kw)
 
 
+@pytest.mark.parametrize("dt,xt", [(BF, BF), (HF, FF), (FF, FF)])
+@pytest.mark.parametrize("m,n", [(5, 100), (9, 300), (4, 3001), (3, 5003), (306, 5003), (2, 16384), (2, 20001), (2, 32753), (2, 32755), (2, 32768)])
+def test_norm_rows_that_lie_alike_and_anyhow(m, n, dt, xt):
+    g = _gen(n)
+    x, kw = _norm_case(g, m, n, dt, xt, "layer", True, "full", True)
+    want = P.norm(x, **kw)
+    _check_norm(want, x, kw)
+
+    def strided(t, more, off=0):                       # the same numbers in longer rows
+        b = torch.full((m, n + more + off), 7.0, dtype=t.dtype, device="cuda")
+        b[:, off:off + n] = t
+        return b[:, off:off + n]
+    for more, off in (((1,) * 5, 0), ((3, 11, 3, 3, 19), 0), ((1, 2, 3, 4, 5), 0), ((1,) * 5, 1)):
+        a, b = dict(kw, y=strided(kw["y"], more[1], off), gate=strided(kw["gate"], more[2], off)), strided(x, more[0], off)
+        h, r = strided(torch.zeros(m, n, dtype=dt, device="cuda"), more[3], off), strided(x, more[4], off)
+        P.norm(b, out=h, x_out=r, **a)
+        _check_norm((h, r), x, kw)
+        for t, k in ((h, more[3]), (r, more[4])):      # nothing beside the rows is written
+            whole = t.as_strided((m, n + k + off), t.stride(), t.storage_offset() - off)
+            assert bool((whole[:, :off] == 7).all()) and bool((whole[:, off + n:] == 7).all())
+
+
 @pytest.mark.parametrize("n", [96, 4096, 5003, 32768])
 def test_norm_in_place(n):
     g = _gen(n)
@@ -497,6 +519,28 @@ def _check_attend8(q_len, kv, H, Hk, D, page, dtype=BF, groups=None, prefix=None
 def test_attend8_lengths(H, Hk, D, page, dtype):
     kv = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500, 1000]
     _check_attend8([1] * len(kv), kv, H, Hk, D, page, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("H,Hk,D,page", [(128, 1, 64, 16), (128, 1, 128, 64), (16, 1, 128, 256), (17, 1, 80, 16), (32, 2, 64, 16), (1, 1, 16, 16)])
+def test_attend8_the_largest_and_the_smallest_groups(H, Hk, D, page, dtype):
+    _check_attend8([1, 2, 1], [1, 4097, 700], H, Hk, D, page, dtype)
+
+
+def test_attend8_two_streams_at_once():
+    first = _check_attend8([1, 2], [20000, 9000], 8, 2, 128, 16)
+    second = _check_attend8([1] * 5, [3000, 7000, 1, 900, 12000], 8, 1, 64, 32, seed=1)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(6):
+        for one, other in ((first, second), (second, first)):        # each plan on both streams
+            for case, s in zip((one, other), streams):
+                cache, plan, q, o, lse, _ = case
+                got.append((P.attend8(plan, q, cache, 1, lse=True, stream=s), (o, lse)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for pair, want in got for a, b in zip(pair, want))
 
 
 def test_attend8_rows_that_see_nothing():
