@@ -84,51 +84,24 @@ __device__ __forceinline__ void wide8(uint2 c, float* v) {
   }
 }
 
-template <class T, bool kWide>
+template <class T>
 __device__ __forceinline__ void load8(const T* x, float* v) {
-  if (kWide) {
-    const Vec<T, 8> a = *reinterpret_cast<const Vec<T, 8>*>(x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = up(a.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = up(x[i]);
-  }
+  for (int i = 0; i < 8; ++i) v[i] = up(x[i]);
 }
 
 // Elements at .. at + 7 of a head x, rotated.
-template <class T, bool kWide>
+template <class T>
 __device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter, const float2* cs, float* v) {
-  load8<T, kWide>(x + at, v);
-  if (at >= 2 * half) return;
-  if (kWide) {
-    if (inter) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 t = cs[at / 2 + i];
-        const float u = v[2 * i], w = v[2 * i + 1];
-        v[2 * i] = u * t.x - w * t.y, v[2 * i + 1] = u * t.y + w * t.x;
-      }
-    } else {
-      const bool second = at >= half;
-      float o[8];
-      load8<T, true>(x + (second ? at - half : at + half), o);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 t = cs[(second ? at - half : at) + i];
-        v[i] = second ? o[i] * t.y + v[i] * t.x : v[i] * t.x - o[i] * t.y;
-      }
-    }
-  } else {
-    for (int i = 0; i < 8; ++i) {
-      const int e = at + i;
-      if (e >= 2 * half) break;
-      const bool second = inter ? e & 1 : e >= half;
-      const int pair = inter ? e / 2 : second ? e - half : e;
-      const float o = up(x[inter ? e ^ 1 : second ? e - half : e + half]);
-      const float2 t = cs[pair];
-      v[i] = second ? o * t.y + v[i] * t.x : v[i] * t.x - o * t.y;
-    }
+  load8(x + at, v);
+  for (int i = 0; i < 8; ++i) {
+    const int e = at + i;
+    if (e >= 2 * half) break;
+    const bool second = inter ? e & 1 : e >= half;
+    const int pair = inter ? e / 2 : second ? e - half : e;
+    const float o = up(x[inter ? e ^ 1 : second ? e - half : e + half]);
+    const float2 t = cs[pair];
+    v[i] = second ? o * t.y + v[i] * t.x : v[i] * t.x - o * t.y;
   }
 }
 
@@ -222,16 +195,16 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
     if (threadIdx.x == 0) n_runs = n, n_turned = before;
   }
   __syncthreads();
-  // a head that is turned whole, in halves: both of a pair's elements in one lane
-  const int eights = kWide && !kInter && 2 * a.half == a.dim && a.half % 8 == 0 ? a.half / 8 : 0;
+  // in halves: eight pairs a lane, both elements of each
+  const int eights = kWide && !kInter ? a.half / 8 : 0;
   float2* const cs_q = cs + (a.chunk + kBlock - 1) * a.half;
   const int q_rows = a.n_heads > 0 ? own : 0;
   for (int i = threadIdx.x; i < (n_turned + q_rows) * a.half; i += kThreads) {
     const int t = i / a.half, p = i - t * a.half;
     if (t < n_turned) {
       const float2 turn = near_turn_of(a.freq[p], pos[turned_at[t]], a.factor);
-      // in a head that is turned whole eight pairs a lane: two pairs' cosines, then their sines, and neighbouring
-      // lanes' next to each other; else in order
+      // for eight pairs a lane: two pairs' cosines, then their sines, and neighbouring lanes' next to each other; else in
+      // order
       float* at = reinterpret_cast<float*>(cs + t * a.half);
       at += eights ? (p % 8 / 2 * eights + p / 8) * 4 + p % 2 : 2 * p;
       at[0] = turn.x, at[eights ? 2 : 1] = turn.y;
@@ -241,7 +214,8 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
 
   // runs: a warp a head's keys or values
   const int vecs = a.dim / 8, units = n_runs * 2 * a.n_kv;
-  const uint32_t per_vec = 65536 / vecs + 1, per_eight = eights ? 65536 / eights + 1 : 0;   // i * per_x >> 16 is i / x, for i below 256
+  const int doubles = a.dim / 16;      // of a token
+  const uint32_t per_vec = 65536 / vecs + 1, per_double = 65536 / doubles + 1;   // i * per_x >> 16 is i / x, for i below 256
   for (int u = blockIdx.y * (kThreads / 32) + warp; u < units; u += gridDim.y * (kThreads / 32)) {
     const int run = u / (2 * a.n_kv), x = u - run * 2 * a.n_kv, is_v = x / a.n_kv, h = x - is_v * a.n_kv;
     const int at = run_at[run][0], n = run_n[run];
@@ -257,12 +231,13 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
     const T* from = is_v ? static_cast<const T*>(a.v) + (t0 - kReach) * a.v_tok + h * a.v_head
                          : static_cast<const T*>(a.k) + (t0 - kReach) * a.k_tok + h * a.k_head;
     const int64_t row = is_v ? a.v_tok : a.k_tok;
-    const bool paired = eights && !is_v;
-    // step s of a lane: elements from .. on of a token (of a pair of steps, its halves')
+    // step s of a lane: elements from .. on of a token; two steps of keys are eight pairs' elements, or 16 one after another
+    const bool paired = kWide && !is_v;
     auto place = [&](int s, int* tok, int* elem) {
       const int i = lane + 32 * (paired ? s / 2 : s);
-      *tok = i * (paired ? per_eight : per_vec) >> 16;
-      *elem = (i - *tok * (paired ? eights : vecs)) * 8 + (paired && s % 2 ? a.half : 0);
+      *tok = i * (paired ? per_double : per_vec) >> 16;
+      const int d = i - *tok * (paired ? doubles : vecs);
+      *elem = !paired ? d * 8 : d < eights ? d * 8 + (s % 2 ? a.half : 0) : d * 16 + s % 2 * 8;
       return *tok < n;
     };
     float scale, by;
@@ -290,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
       *reinterpret_cast<uint2*>(codes + (pos[run_at[run][tok]] % kBlock) * a.dim + e) = narrow8(v, by);
     };
     // Twice over the values: for their largest, and for their codes (with infinities, which do not count, thrice).
-    // They lie in registers as they came, or are read again.
+    // (Where loads are of 16 bytes they lie in registers as they came, else they are read again.)
     auto twice = [&](auto&& each) {
       float top = 0.f;
       each([&](int, int, const float* v) { top = most_of(v, top); });
@@ -303,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
       settle(top);
       each(put);
     };
-    if (kWide && (is_v || paired)) {
+    if (kWide) {
       uint4 raw[kSteps];
       int32_t to[kSteps];                // in codes; negative: nothing
 #pragma unroll
@@ -345,21 +320,41 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
           *reinterpret_cast<uint2*>(codes + to[s]) = narrow8(v, by2);
         }
       } else {
-        // eight pairs: (u, w) -> (u c - w s, u s + w c)
+        // pairs: (u, w) -> (u c - w s, u s + w c)
         auto each = [&](auto&& use) {
 #pragma unroll
           for (int s = 0; s < kSteps; s += 2) {
             if (to[s] < 0) continue;
             int tok, e;
             place(s, &tok, &e);
-            const float4* t = reinterpret_cast<const float4*>(turns + tok * a.half) + e / 8;
+            const float2* turn = turns + tok * a.half;
             uint64_t v[4], w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float4 cs4 = t[i * eights];
-              const uint64_t c = two(cs4.x, cs4.y), d = two(cs4.z, cs4.w), y = as_two(word(s, i)), z = as_two(word(s + 1, i));
-              v[i] = fma2(y, c, fma2(z, two(-cs4.z, -cs4.w), 0ull));
-              w[i] = fma2(y, d, fma2(z, c, 0ull));
+            for (int i = 0; i < 4; ++i) v[i] = as_two(word(s, i)), w[i] = as_two(word(s + 1, i));
+            if (kInter) {
+              auto turned = [&](uint64_t* x, int at) {
+                if (at >= 2 * a.half) return;
+                const float4* t = reinterpret_cast<const float4*>(turn + at / 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float4 cs4 = t[i / 2];
+                  const float c = i % 2 ? cs4.z : cs4.x, d = i % 2 ? cs4.w : cs4.y;
+                  float y, z;
+                  halves(x[i], &y, &z);
+                  x[i] = fma2(x[i], two(c, c), fma2(two(z, y), two(-d, d), 0ull));
+                }
+              };
+              turned(v, e);
+              turned(w, e + 8);
+            } else if (e < a.half) {
+              const float4* t = reinterpret_cast<const float4*>(turn) + e / 8;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float4 cs4 = t[i * eights];
+                const uint64_t c = two(cs4.x, cs4.y), d = two(cs4.z, cs4.w), y = v[i], z = w[i];
+                v[i] = fma2(y, c, fma2(z, two(-cs4.z, -cs4.w), 0ull));
+                w[i] = fma2(y, d, fma2(z, c, 0ull));
+              }
             }
             use(s, v, w);
           }
@@ -394,8 +389,8 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
           if (!place(s, &tok, &e)) continue;
           const T* x = from + run_at[run][tok] * row;
           float v[8];
-          if (is_v) load8<T, kWide>(x + e, v);
-          else turned8<T, kWide>(x, e, a.half, kInter, turns + tok * a.half, v);
+          if (is_v) load8(x + e, v);
+          else turned8(x, e, a.half, kInter, turns + tok * a.half, v);
           use(tok, e, v);
         }
       });
