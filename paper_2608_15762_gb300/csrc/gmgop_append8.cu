@@ -7,9 +7,9 @@
 // found, the block's scale follows, and the codes are written once.  Scales are powers of two, so a block whose scale grows
 // is rounded again only where its codes become subnormal, and x / scale is exact.
 // What bounds it is memory, as far as the few registers allow that keep a run's loads in flight (a prompt of 32,768
-// tokens, 32 + 8 + 8 heads of 128: 136 us, of them 54 for keys and values, 201 MB at 3.7 TB/s, and
+// tokens, 32 + 8 + 8 heads of 128: 148 us, of them 66 for keys and values, 201 MB at 3.0 TB/s, and
 // 82 for queries), and where tokens are few the chain of loads from a token's position to
-// its block's scale (16 tokens 4.5 us).
+// its block's scale (16 tokens 4.8 us).
 // A thread block serves a share of `chunk` tokens' heads: sines and cosines once for all of them, as
 // in the cache of 16-bit values.  A run that reaches past its block's tokens is taken whole by the
 // block that it begins in.
@@ -102,6 +102,37 @@ __device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter
     const float o = up(x[inter ? e ^ 1 : second ? e - half : e + half]);
     const float2 t = cs[pair];
     v[i] = second ? o * t.y + v[i] * t.x : v[i] * t.x - o * t.y;
+  }
+}
+
+// Turned in 32 bits, a number may lie on the wrong side of the middle between two codes: not where it is more than
+// kNear of its last bits from it (its error is about three of them, more where a pair cancels).  Looking for such numbers
+// and turning them again costs a prompt of 32,768 tokens 12 us of 148 (18 with a kNear of 16), and leaves codes 50 times
+// nearer to the exact ones': 8e-7 of their norm for 4e-5.
+constexpr uint32_t kNear = 4, kNearTop = 2 * kNear << 12;
+__device__ __forceinline__ uint32_t from_middle(float x) {   // below kNearTop: near one (codes have the first 3 of the 23 bits)
+  return (__float_as_uint(x) << 12) + ((0x80000 + kNear) << 12);
+}
+// Those pairs of the eight that have a number near the middle of two codes, again in 64 bits.  x: as turned, to be put
+// right; from: as they came; halves: their elements are 8 apart (else neighbours).  (Out of line: few warps come here.)
+__device__ __noinline__ void turn_exactly(float* x, const float* from, bool halves, int32_t pair, int32_t half,
+                                          const uint64_t* freq, int32_t pos, float factor) {
+#pragma unroll 1
+  for (int p = 0; p < 8 && pair + p < half; ++p) {
+    const int i = halves ? p : 2 * p, j = halves ? p + 8 : 2 * p + 1;
+    if (from_middle(x[i]) >= kNearTop && from_middle(x[j]) >= kNearTop) continue;
+    const uint64_t turn = freq[pair + p] * (uint64_t)(int64_t)pos;
+    double s, c;
+    sincospi((double)(int64_t)turn * 1.0842021724855044e-19, &s, &c);   // 2^-63: half turns
+    const double u = from[i], w = from[j], v[2] = {(u * c - w * s) * factor, (u * s + w * c) * factor};
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+      float f = (float)v[k];
+      // a middle itself that was rounded to goes back to its side
+      if ((__float_as_uint(f) & 0xfffff) == 0x80000 && (double)f != v[k])
+        f = __uint_as_float(__float_as_uint(f) + (fabs(v[k]) > fabs((double)f) ? 1 : -1));
+      x[k ? j : i] = f;
+    }
   }
 }
 
@@ -361,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
         };
         auto largest = [&](auto&& of) {
           float top = 0.f;
-          each([&](int, const uint64_t* v, const uint64_t* w) {
+          each([&](int, uint64_t* v, uint64_t* w) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float x0, x1, x2, x3;
@@ -376,7 +407,31 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
         if (!(top <= 3.402823466e38f)) top = largest([](float x) { return fabsf(x) <= 3.402823466e38f ? fabsf(x) : 0.f; });
         settle(top);
         const uint64_t by2 = two(by, by);
-        each([&](int s, const uint64_t* v, const uint64_t* w) {
+        each([&](int s, uint64_t* v, uint64_t* w) {
+          uint32_t nearest = ~0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x0, x1, x2, x3;
+            halves(v[i], &x0, &x1);
+            halves(w[i], &x2, &x3);
+            nearest = min(nearest, min(min(from_middle(x0), from_middle(x1)), min(from_middle(x2), from_middle(x3))));
+          }
+          if (nearest < kNearTop) {
+            int tok, e;
+            place(s, &tok, &e);
+            float x[16], from[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              halves(v[i], &x[2 * i], &x[2 * i + 1]);
+              halves(w[i], &x[8 + 2 * i], &x[9 + 2 * i]);
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+                from[2 * i + k] = unpack(T(), word(s, i), k), from[8 + 2 * i + k] = unpack(T(), word(s + 1, i), k);
+            }
+            turn_exactly(x, from, !kInter, kInter ? e / 2 : e, a.half, a.freq, pos[run_at[run][tok]], a.factor);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = two(x[2 * i], x[2 * i + 1]), w[i] = two(x[8 + 2 * i], x[9 + 2 * i]);
+          }
           *reinterpret_cast<uint2*>(codes + to[s]) = narrow8(v, by2);
           *reinterpret_cast<uint2*>(codes + to[s + 1]) = narrow8(w, by2);
         });
@@ -470,7 +525,7 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   a.page_bytes = page8_bytes(*cache);
   a.codes_at = int64_t(layer) * 2 * a.n_kv * cache->page_tokens * a.dim;
   a.scales_at = page8_scales(*cache) + int64_t(layer) * 2 * a.n_kv * (cache->page_tokens / kScaleTokens) * 4;
-  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps (else a prompt takes 255 us for 136)
+  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps (else a prompt took 255 us for 136)
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -478,7 +533,7 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   // Where there are many, and not each a sequence's only one, 16 a block, which has few runs then (with 32 + 8 + 8 heads of
   // 128, 2,432 tokens 20.8 us, one a block 26.0; 608 12.0 and 13.3; 304 11.4 and 10.5; 1,216 of as many sequences 25.5 and
   // 20.3, 4,864 81.7 and 82.1).  Very many queries then as dense ones, in a launch of their own with few registers a thread
-  // (32,768 tokens 136 us, in one launch 161; 4,864 32.6 and 34.8; 2,432 21.8 and 20.8; 16,384 of 8 heads of 64 21.5 and 17.3).
+  // (32,768 tokens 136 us, without the search for numbers near a middle, in one launch 161; 4,864 32.6 and 34.8; 2,432 21.8 and 20.8; 16,384 of 8 heads of 64 21.5 and 17.3).
   a.chunk = 1;
   if (n_tokens >= 152 * 4 && n_tokens >= std::min<int64_t>(int64_t(kBlock) * cache->n_seq, 152 * 2 * kChunk)) {
     a.chunk = kChunk;
