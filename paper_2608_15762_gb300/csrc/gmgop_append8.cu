@@ -108,7 +108,7 @@ __device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter
 // Turned in 32 bits, a number may lie on the wrong side of the middle between two codes: not where it is more than
 // kNear of its last bits from it (its error is about three of them, more where a pair cancels).  Looking for such numbers
 // and turning them again costs a prompt of 32,768 tokens 12 us of 148 (18 with a kNear of 16), and leaves codes 50 times
-// nearer to the exact ones': 8e-7 of their norm for 4e-5.
+// nearer to the exact ones': 8e-7 of their norm for 4e-5.  (Rows that are loaded element by element are not searched.)
 constexpr uint32_t kNear = 4, kNearTop = 2 * kNear << 12;
 __device__ __forceinline__ uint32_t from_middle(float x) {   // below kNearTop: near one (codes have the first 3 of the 23 bits)
   return (__float_as_uint(x) << 12) + ((0x80000 + kNear) << 12);
@@ -529,11 +529,12 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  // One token a block, its queries and its runs in shares: a decode step of 16 tokens 4.5 us, with 16 a block 9.2.
-  // Where there are many, and not each a sequence's only one, 16 a block, which has few runs then (with 32 + 8 + 8 heads of
-  // 128, 2,432 tokens 20.8 us, one a block 26.0; 608 12.0 and 13.3; 304 11.4 and 10.5; 1,216 of as many sequences 25.5 and
-  // 20.3, 4,864 81.7 and 82.1).  Very many queries then as dense ones, in a launch of their own with few registers a thread
-  // (32,768 tokens 136 us, without the search for numbers near a middle, in one launch 161; 4,864 32.6 and 34.8; 2,432 21.8 and 20.8; 16,384 of 8 heads of 64 21.5 and 17.3).
+  // One token a block, its queries and its runs in shares: a decode step of 16 tokens 4.5 us, with 16 a block 9.2 (these
+  // without the search for numbers near a middle, which adds about a tenth to each).  Where there are many, and not
+  // each a sequence's only one, 16 a block, which has few runs then (with 32 + 8 + 8 heads of 128, 2,432 tokens 20.8 us,
+  // one a block 26.0; 608 12.0 and 13.3; 304 11.4 and 10.5; 1,216 of as many sequences 25.5 and 20.3, 4,864 81.7 and 82.1).
+  // Very many queries then as dense ones, in a launch of their own with few registers a thread (32,768 tokens 136 us, in one
+  // launch 161; 4,864 32.6 and 34.8; 2,432 21.8 and 20.8; 16,384 of 8 heads of 64 21.5 and 17.3).
   a.chunk = 1;
   if (n_tokens >= 152 * 4 && n_tokens >= std::min<int64_t>(int64_t(kBlock) * cache->n_seq, 152 * 2 * kChunk)) {
     a.chunk = kChunk;
