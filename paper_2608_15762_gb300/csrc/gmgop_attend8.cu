@@ -11,7 +11,7 @@
 //   S^T [128 keys][rows] = K Q^T,   O^T [128 dims][rows] += V^T P^T.
 // Keys fill the tensor core's 128 lanes and rows are columns, so that a step of few rows costs few columns,
 // exponentials and registers, and K and V are read once, as the codes that they are, by fp8 products.
-// What the codes meet is split into several of them: Q as bf16 and fp16 have it, P to 12 bits or more.
+// What the codes meet is split into several of them: Q as bf16 and fp16 have it, P to 12 bits, small weights too.
 // Memory bounds it where there is enough to read (the decode step below: 161 us, 6.7 TB/s); a small step is a
 // launch and the chain of its few steps (8 requests behind 500 tokens 9.6 us).
 //
@@ -290,26 +290,27 @@ __device__ __forceinline__ uint4 q_piece(const Args8& g, const Item& it, int32_t
 // Few rows: codes straight into the products
 // ---------------------------------------------------------------------------
 
-// Numbers of more bits than a code has, as a sum of codes: x = t_0 + t_1 / 16 + t_2 / 256, each the
-// nearest to 16 times what the ones before it leave.  Two terms hold bf16 exactly (as far as 2^-14, of
-// 2^8 at most), three 12 bits and more (as far as 2^-18), four 16 (2^-22).
+// Numbers of more bits than a code has, as a sum of codes.  Q's are of K's type (e4m3, 4 bits): x = t_0 + t_1 / 16 + t_2 / 256,
+// each the nearest to 16 times what the ones before it leave.  Two terms hold bf16 exactly (as far as 2^-14, of 2^8 at
+// most), three fp16 (as far as 2^-18).
+//
+// P's are e5m2 (3 bits, from 2^-16 to 57,344): x = t_0 + t_1 / 8 + t_2 / 64 + t_3 / 512, off by at most 2^-12 of itself or 2^-26.
+// A row's largest weight is at least 2^kBiasFew: weights have their 12 bits down to 2^-25 of it, and
+// what is below 2^-37 of it is lost.  That range is for rows where one key has most of the weight and a small value: the result is then
+// the sum of very many small weights, of which e4m3, with 2^-26, loses too much (131,072 keys of one weight, e^-17 of the largest, whose
+// value is a fiftieth of theirs: 3.2e-2 of the result, in three terms of e4m3 1.1e-1, in these 2e-6).
 constexpr int kFewKeys = 128, kFewRows = 16;   // of a step, of a tile
-constexpr float kBiasFew = 4.f, kMostFew = 4.75f;   // a weight is at most 2^8.75 < 448
+constexpr float kBiasFew = 11.f, kMostFew = 4.75f;   // a weight is at most 2^15.75 < 57,344
 
 template <class T>
 struct TermsQ {
   static constexpr int kN = std::is_same<T, __nv_bfloat16>::value ? 2 : 3;
 };
-// Of P, whose numbers below 2^-18 (2^-22) times the largest are lost: bf16's results have 8 bits, fp16's 11.
-template <class T>
-struct TermsP {
-  static constexpr int kN = std::is_same<T, __nv_bfloat16>::value ? 3 : 4;
-};
+constexpr int kTermsP = 4;
 
 template <class T>
 struct FewShape {
   static constexpr int kTerms = TermsQ<T>::kN;
-  static constexpr int kTermsP = TermsP<T>::kN;
   static constexpr int kQ = 6144, kP = kTermsP * kFewKeys * 16;   // Q: terms of 16 rows of 128 bytes
   static constexpr int kSlot = kFewKeys * 128, kSlots = 6;
   static constexpr int kRingAt = (kQ + kP + 1023) / 1024 * 1024;
@@ -337,9 +338,9 @@ __device__ __forceinline__ void mma8_ss(uint32_t d, uint64_t a, uint64_t b, uint
       "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
       : "memory");
 }
-// e4m3 both (types 0), fp32 sums.
-__host__ __device__ constexpr uint32_t mma8_desc(int m, int n, bool a_rows, bool b_rows) {
-  return (1u << 4) | ((a_rows ? 1u : 0u) << 15) | ((b_rows ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+// A of e4m3 (type 0), B of e4m3 or of e5m2 (1), fp32 sums.
+__host__ __device__ constexpr uint32_t mma8_desc(int m, int n, bool a_rows, bool b_rows, bool b_e5m2) {
+  return (1u << 4) | ((b_e5m2 ? 1u : 0u) << 10) | ((a_rows ? 1u : 0u) << 15) | ((b_rows ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(m >> 4) << 24);
 }
 // No swizzle, rows (N) contiguous, 16 of a column in 16 bytes: eight columns after each other; the next eight are
@@ -348,7 +349,7 @@ __device__ __forceinline__ uint64_t tile_n16(uint32_t addr, uint32_t deeper, uin
   return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(deeper >> 4) << 16) | ((uint64_t)(further >> 4) << 32) | (1ull << 46);
 }
 
-// The next term of x and y: its codes; x and y become 16 times what it leaves.
+// The next term of Q's x and y: its codes; x and y become 16 times what it leaves.
 __device__ __forceinline__ uint16_t next_term(uint64_t* xy) {
   float x, y;
   halves(*xy, &x, &y);
@@ -359,11 +360,22 @@ __device__ __forceinline__ uint16_t next_term(uint64_t* xy) {
   return c;
 }
 
+// The same of P's, with 8 times what is left (the codes are the upper bytes of fp16).
+__device__ __forceinline__ uint16_t next_weight(uint64_t* xy) {
+  float x, y;
+  halves(*xy, &x, &y);
+  uint16_t c;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(c) : "f"(y), "f"(x));
+  const uint32_t h = __byte_perm(c, 0, 0x1404);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  *xy = fma2(two(f.x, f.y), two(-8.f, -8.f), fma2(*xy, two(8.f, 8.f), 0ull));
+  return c;
+}
+
 template <class T>
 __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(const __grid_constant__ CUtensorMap map_kv,
                                                                              const __grid_constant__ Args8 g) {
   using S = FewShape<T>;
-  constexpr int kTermsP = S::kTermsP;
   extern __shared__ __align__(1024) unsigned char base[];
   const AttendArgs& a = g.a;
   unsigned char* const p_mem = base + S::kQ;
@@ -403,8 +415,8 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
     copy_pages<kFewKeys, 128, S::kSlots>(map_kv, g, it, hk, first, n, warp - 4, lane, smem_addr(base + S::kRingAt), full, empty, misc.scales,
                                failed);
   } else if (warp == 7) {
-    constexpr uint32_t desc_s = mma8_desc(kFewKeys, kFewRows * S::kTerms, false, false),
-                       desc_o = mma8_desc(128, kFewRows * kTermsP, true, true);
+    constexpr uint32_t desc_s = mma8_desc(kFewKeys, kFewRows * S::kTerms, false, false, false),
+                       desc_o = mma8_desc(128, kFewRows * kTermsP, true, true, true);
     const uint64_t q = tile_k(smem_addr(base)), p = tile_n16(smem_addr(p_mem), 128, kFewKeys * 16);
     const uint64_t k_ring = tile_k(smem_addr(base + S::kRingAt)), v_ring = tile_n(smem_addr(base + S::kRingAt), kFewKeys * 128);
     const int k_steps = (a.dim + 31) / 32;
@@ -628,7 +640,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
         l2[i] = fma2(left, two(inv, inv), l2[i]);
 #pragma unroll
         for (int k = 0; k < kTermsP; ++k) {
-          const uint32_t both = next_term(&left);
+          const uint32_t both = next_weight(&left);
           p[k][i / 2] = i & 1 ? p[k][i / 2] | both << 16 : both;
         }
       }
@@ -689,7 +701,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       for (int i = 0; i < 4; ++i) {
         float v = __uint_as_float(o[kTermsP - 1][i]);
 #pragma unroll
-        for (int k = kTermsP - 2; k >= 0; --k) v = fmaf(v, 0.0625f, __uint_as_float(o[k][i]));
+        for (int k = kTermsP - 2; k >= 0; --k) v = fmaf(v, 0.125f, __uint_as_float(o[k][i]));
         if (row + i < rows && r < a.dim) at.put(a, it, v, total[4 * kFewRows + row + i], nan_at);
         at.next(a);
       }
@@ -937,7 +949,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
                                              failed);
     } else if (warp == 11) {
       // the whole warp goes along; one lane issues
-      constexpr uint32_t desc_s = mma8_desc(kRows, kKeys, false, false), desc_o = mma_desc(false, kRows, DP, true);
+      constexpr uint32_t desc_s = mma8_desc(kRows, kKeys, false, false, false), desc_o = mma_desc(false, kRows, DP, true);
       const uint32_t k_at = smem_addr(base + S::kCodesAt);
       const uint64_t q = DP == 64 ? tile_k64(smem_addr(base)) : tile_k(smem_addr(base)),
                      k_ring = DP == 64 ? tile_k64(k_at) : tile_k(k_at), v_ring = tile_n(smem_addr(base + S::kWideAt), kKeys * 128);

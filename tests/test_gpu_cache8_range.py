@@ -1,0 +1,104 @@
+"""GPU parity of the operators on a cache in 8 bits (include/gmgop.h) at the ends of their ranges: rows of attention
+in which one key has most of the weight."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import op_ref as R  # noqa: E402
+from paper_2608_15762_gb300 import gmgop as P  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+F8 = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2608_15762_gb300 import build
+    build.build()
+    assert torch.cuda.is_available()
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _codes(x):
+    return x.clamp(-448, 448).to(F8).view(torch.uint8)
+
+
+def _one_row(keys, values, ks, vs, page=64, tail=0):
+    """A cache of one request: codes [tokens, heads, dim] under one scale for keys and one for values."""
+    t, hk, dim = keys.shape
+    n = -(-t // page)
+    c = P.PageCache8(torch.zeros(n, P.page8_bytes(1, hk, page, dim), dtype=torch.uint8, device="cuda"), 1, hk, page, dim, 1, n)
+    c.table.copy_(torch.randperm(n, generator=_gen(t), device="cuda").int()[None])
+    c.scales[:, 0, 0], c.scales[:, 0, 1] = ks, vs
+    for which, x in ((0, keys), (1, values)):
+        whole = torch.zeros(n * page, hk, dim, dtype=torch.uint8, device="cuda")
+        whole[:t] = x
+        c.codes.view(torch.uint8)[c.table[0].long(), 0, which] = whole.view(n, page, hk, dim).transpose(1, 2)
+    return c
+
+
+def _exact(q, keys, values, ks, vs, n, scale, floor):
+    """(o, bound) in 64 bits.  A score is off by d + 8 roundings of its magnitudes (two each), a weight by that of its own
+    score and of the row's others, by 2^-11 of itself where it is rounded, and by `floor` of the row's largest; sums
+    over t keys are off by t / 16 + 16 roundings."""
+    t, hk, dim = keys.shape
+    H = q.shape[1]
+    k = (keys.view(F8).double() * ks).transpose(0, 1)
+    v = (values.view(F8).double() * vs).transpose(0, 1)
+    o, tol = torch.empty(q.shape, dtype=torch.float64, device="cuda"), torch.empty(q.shape, dtype=torch.float64, device="cuda")
+    sees = torch.arange(t, device="cuda")[None] <= torch.arange(t - n, t, device="cuda")[:, None]
+    for h in range(H):
+        x, kh, vh = q[:, h].double(), k[h * hk // H], v[h * hk // H]
+        z = (x @ kh.t() * scale).masked_fill(~sees, -math.inf)
+        worst = (2 * (dim + 8) * R.U32 * scale * (x.abs() @ kh.t().abs())).masked_fill(~sees, 0).amax(-1, keepdim=True)
+        p = torch.softmax(z, -1)
+        o[:, h] = p @ vh
+        rel = 2.0 ** -11 + 4 * worst + 2e-5 + 2 * (t / 16 + 16) * R.U32
+        tol[:, h] = (rel * (p @ vh.abs()) + floor * p.amax(-1, keepdim=True) * vh.abs().sum(0) + R.U[q.dtype] * o[:, h].abs()
+                     + R.TINY[q.dtype])
+    return o, tol
+
+
+# What a weight is off by where it is far below a row's largest, of which it is a share: half of the last code's least
+# step, 2^-26, where the largest is at least 2^11; half of fp16's, 2^-25, where it is at least 2^4.
+FLOOR = {1: 2.0 ** -37, 0: 2.0 ** -29}
+# (keys, how far the first key's score is ahead, the others' deviation)
+PEAKS = [(300, 17.0, 0.0), (8992, 14.0, 0.2), (16000, 15.0, 0.2), (32000, 16.0, 0.2), (131072, 12.0, 0.0), (131072, 16.0, 1.0),
+         (131072, 17.0, 0.0), (131072, 20.0, 0.0)]
+
+
+def _peaked(t, ahead, spread, H, hk, dim, n, dtype):
+    """Heads whose first key is `ahead` of the others, with a value of a fiftieth of theirs, whose mean is 0.5: the
+    result is what very many small weights give."""
+    g = _gen(int(t + ahead))
+    ks, vs, scale = 2.0 ** -5, 2.0 ** -6, dim ** -0.5
+    sign = torch.randint(0, 2, (hk, dim), generator=g, device="cuda") * 2.0 - 1
+    keys = torch.randn(t, hk, dim, generator=g, device="cuda") * spread
+    keys[0] = sign * (ahead * dim ** -0.5)
+    values = torch.randn(t, hk, dim, generator=g, device="cuda") + 0.5
+    values[0] = 0.01
+    by = 1 + 0.02 * torch.rand(n, H, 1, generator=g, device="cuda")
+    q = (sign.repeat_interleave(H // hk, 0) * by).to(dtype)
+    return q, _codes(keys / ks), _codes(values / vs), ks, vs, scale
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("t,ahead,spread", PEAKS)
+@pytest.mark.parametrize("H,hk,dim", [(4, 1, 128), (16, 1, 64)])
+def test_attend8_one_key_with_most_of_the_weight(t, ahead, spread, H, hk, dim, dtype, monkeypatch):
+    q, keys, values, ks, vs, scale = _peaked(t, ahead, spread, H, hk, dim, 1, dtype)
+    c = _one_row(keys, values, ks, vs)
+    for sms in (1, 152):                                 # all its keys one item's; cut into many
+        monkeypatch.setattr(P, "_n_sm", lambda device: sms)
+        plan = P.AttendPlan8([1], [t], H, hk, dim, 64)
+        assert plan.c.few == (t > 1000) and (sms > 1 or plan.c.n_items <= 2)
+        want, tol = _exact(q, keys, values, ks, vs, 1, scale, FLOOR[plan.c.few])
+        R.within(P.attend8(plan, q, c, 0, scale=scale), want, tol, "%d items" % plan.c.n_items)
