@@ -725,9 +725,11 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
 //   warp 11         products: S_j = Q K_j^T into one of two TMEM buffers, O += P_j V_j into TMEM
 constexpr int kKeys = 64, kRows = 128;   // of a step, of a tile
 constexpr int kThreads = 384;
-// A weight is at most 2^(kMost + kBias), in fp16's range, and the largest at least 2^kBias.  (A raised reference takes the whole
-// warp through O: with 7 and 8 chunks of prompts took 344 us, with 4 and 11 334.)
-constexpr float kBias = 4.f, kMost = 11.f;
+// A weight is at most 2^(kMost + kBias), in fp16's range, and the largest at least 2^kBias: weights have fp16's 11 bits down to
+// 2^-22 of it, and what is below 2^-33 of it is lost.  (With 4 and 11, 2^-29: 131,072 keys of one weight, e^-20 of the largest, whose
+// value is a fiftieth of theirs, were 1% off.)  A raised reference takes the whole warp through O, so all of its rows are
+// raised then: a call on chunks of prompts 337 us, with 4 and 11 335, with 10 and 5 342; each row by itself with 7 and 8 345.
+constexpr float kBias = 8.f, kMost = 7.f;
 
 template <class T, int DP>
 struct Shape {
@@ -1097,8 +1099,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
         }
         const bool raise = top > m + kMost || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, raise)) {
-          const float f = raise ? (m == -INFINITY ? 0.f : exp2_fast(m - top)) : 1.f;
-          if (raise) m = top;
+          const float f = top > m ? (m == -INFINITY ? 0.f : exp2_fast(m - top)) : 1.f;
+          m = fmaxf(m, top);
           l *= f;
           if (j > 0) {
             bar_pass(o_done + 8 * ((j - 1) & 1), ((j - 1) >> 1) & 1, failed);

@@ -68,8 +68,8 @@ def _exact(q, keys, values, ks, vs, n, scale, floor):
 
 
 # What a weight is off by where it is far below a row's largest, of which it is a share: half of the last code's least
-# step, 2^-26, where the largest is at least 2^11; half of fp16's, 2^-25, where it is at least 2^4.
-FLOOR = {1: 2.0 ** -37, 0: 2.0 ** -29}
+# step, 2^-26, where the largest is at least 2^11; half of fp16's, 2^-25, where it is at least 2^8.
+FLOOR = {1: 2.0 ** -37, 0: 2.0 ** -33}
 # (keys, how far the first key's score is ahead, the others' deviation)
 PEAKS = [(300, 17.0, 0.0), (8992, 14.0, 0.2), (16000, 15.0, 0.2), (32000, 16.0, 0.2), (131072, 12.0, 0.0), (131072, 16.0, 1.0),
          (131072, 17.0, 0.0), (131072, 20.0, 0.0)]
@@ -101,4 +101,19 @@ def test_attend8_one_key_with_most_of_the_weight(t, ahead, spread, H, hk, dim, d
         plan = P.AttendPlan8([1], [t], H, hk, dim, 64)
         assert plan.c.few == (t > 1000) and (sms > 1 or plan.c.n_items <= 2)
         want, tol = _exact(q, keys, values, ks, vs, 1, scale, FLOOR[plan.c.few])
+        R.within(P.attend8(plan, q, c, 0, scale=scale), want, tol, "%d items" % plan.c.n_items)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("t,ahead,spread", PEAKS)
+@pytest.mark.parametrize("H,hk,dim", [(4, 1, 128), (40, 1, 64)])
+def test_attend8_one_key_with_most_of_the_weight_of_many_rows(t, ahead, spread, H, hk, dim, dtype, monkeypatch):
+    n = 160 // H
+    q, keys, values, ks, vs, scale = _peaked(t, ahead, spread, H, hk, dim, n, dtype)
+    c = _one_row(keys, values, ks, vs)
+    want, tol = _exact(q, keys, values, ks, vs, n, scale, FLOOR[0])
+    for sms in (1, 152):
+        monkeypatch.setattr(P, "_n_sm", lambda device: sms)
+        plan = P.AttendPlan8([n], [t], H, hk, dim, 64)
+        assert not plan.c.few
         R.within(P.attend8(plan, q, c, 0, scale=scale), want, tol, "%d items" % plan.c.n_items)
