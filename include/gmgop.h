@@ -203,9 +203,10 @@ int op_attend(const op_attend_plan_t* plan, const int32_t* d_items, const op_cac
               float* lse, void* work, size_t work_bytes, gmg_stream_t stream);
 
 /* The same over a cache in 8 bits, for q and out of type dtype (bf16 or fp16); n_heads /
- * n_kv_heads at most 128.  In the products codes are exact, q is to 2^-17 of its row's largest (2^-21 of its tile's
- * in tiles of up to 16 rows).  A probability (times its value's scale) is off by at most 2^-12 of itself, or by 2^-37 of the
- * row's largest where that is more (tiles of more rows: 2^-11, 2^-33). */
+ * n_kv_heads at most 128.  In the products codes are exact, q is to 2^-17 of its row's largest (2^-21 in tiles of
+ * up to 16 rows).  A probability (times its value's scale) is off by at most 2^-12 of itself, or by 2^-37 of the
+ * row's largest where that is more (tiles of more rows: 2^-11, 2^-33).  A row with
+ * scores beyond 2^21, in magnitude, is not defined; the other rows are. */
 typedef struct {
   op_attend_plan_t p;
   int32_t few, reserved;        /* whether its items have few rows (query heads times queries of a key/value head) */

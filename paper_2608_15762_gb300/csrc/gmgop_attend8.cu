@@ -41,7 +41,7 @@ namespace gop {
 namespace {
 
 constexpr int kCopiers = 3;
-constexpr float kNone = -1e30f;        // the reference of a row that has seen nothing
+constexpr float kNone = -3e38f;        // the reference of a row that has seen nothing: below any score
 
 struct Args8 {
   AttendArgs a;
@@ -324,6 +324,7 @@ struct FewShape {
 struct FewMisc {
   ScaleRing<kFewKeys> scales;
   float top[4][kFewRows];              // the warps' largest weights where references are raised
+  float unit[kFewRows];                // of a row's Q: the power of two that its terms are multiples of
   uint32_t first_nan[32];
   uint64_t bars[2 * 6 + 8];
   uint32_t tmem_at, failed, flag[2];
@@ -463,39 +464,33 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     uint32_t meetings = 0;
     int32_t key = first * kFewKeys + r;
-    float unit;                          // of Q's terms
     {
-      // a row's 8 elements a step, to its terms: codes of row `term * 16 + row`
+      // a row's 8 elements a step, to its terms: codes of row `term * 16 + row`.  Each row is first multiplied by the power of
+      // two that brings its largest to between 2^7 and 2^8: a tile's rows may be of several requests.
       constexpr int kEach = kFewRows * 16 / 128;
       const uint32_t per_group = 65536 / a.group + 1;   // row * per_group >> 16 is row / group
       uint4 v[kEach];
-      uint32_t top = 0;
-      auto raise = [&](uint32_t x) {
-        constexpr uint32_t kInf = std::is_same<T, __nv_bfloat16>::value ? 0x7f80 : 0x7c00;
-        if (x < kInf && x > top) top = x;
-      };
+      constexpr uint32_t kInf = std::is_same<T, __nv_bfloat16>::value ? 0x7f80 : 0x7c00;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) v[i] = q_piece<T>(g, it, hk, rows, (r + 128 * i) / 16, (r + 128 * i) % 16, per_group);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         if (r / 16 + 8 * i >= rows || r % 16 * 8 >= a.dim) v[i] = uint4{};
-        for (const uint32_t w : {v[i].x, v[i].y, v[i].z, v[i].w}) raise(w & 0x7fff), raise(w >> 16 & 0x7fff);
       }
-      top = __reduce_max_sync(0xffffffffu, top);
-      uint32_t* tops = reinterpret_cast<uint32_t*>(p_mem);
-      if (lane == 0) tops[warp] = top;
-      bar_meet(met, &meetings, failed);
-      top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-      // the tile's largest to between 2^7 and 2^8
-      const float most = up(from_bits<T>(top));
-      const int e = max(min(134 - (int)(__float_as_uint(most) >> 23), 126), -120);
-      float by = __int_as_float((e + 127) << 23);
-      unit = __int_as_float((127 - e) << 23);
-      if (a.negative) by = -by;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int x = r + 128 * i, row = x / 16, c = x % 16;
         const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        uint32_t top = 0;                // of the row's finite |q|
+        for (const uint32_t y : w)
+          for (const uint32_t z : {y & 0x7fff, y >> 16 & 0x7fff})
+            if (z < kInf && z > top) top = z;
+#pragma unroll
+        for (int d = 8; d; d /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const int e = max(min(134 - (int)(__float_as_uint(up(from_bits<T>(top))) >> 23), 126), -120);
+        float by = __int_as_float((e + 127) << 23);
+        if (c == 0) misc.unit[row] = __int_as_float((127 - e) << 23);
+        if (a.negative) by = -by;
         uint64_t xy[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -518,7 +513,6 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       __syncwarp();
       if (lane == 0) bar_arrive(q_ready);
     }
-    const float c_all = a.scale2 * unit;
     const int32_t all_see = it.pos0 + 1 < it.hi ? it.pos0 + 1 : it.hi;    // keys that the first row sees
     uint64_t l2[8];                      // of this key's share of the rows' sums
 #pragma unroll
@@ -538,9 +532,13 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       tc_after_sync();
       const uint32_t s_at = tmem_s + lanes + (j & 1) * S::kSTwo;
       const float ks = misc.scales.s[j & (kScaleSteps - 1)][0][r / 16], vs = misc.scales.s[j & (kScaleSteps - 1)][1][r / 16];
-      const float c = c_all * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
+      const float c = a.scale2 * fminf(fmaxf(ks, 8.6736174e-19f), 1.1529215e18f);   // 2^-60 .. 2^60
       const float lv0 = __log2f(fminf(fmaxf(vs, 8.6736174e-19f), 1.1529215e18f)), lv = lv0 + kBiasFew;
       uint64_t x[8];                     // scores, then exponents, of two rows each
+      auto scale_of = [&](int i) {       // of rows 2 i and 2 i + 1
+        const float4 u = reinterpret_cast<const float4*>(misc.unit)[i / 2];
+        return fma2(i & 1 ? two(u.z, u.w) : two(u.x, u.y), two(c, c), 0ull);
+      };
       auto sums = [&]() {
         uint32_t t[S::kTerms][16];
 #pragma unroll
@@ -559,10 +557,10 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
       auto exponents = [&]() {
         sums();
         float most = -INFINITY;
-        const uint64_t c2 = two(c, c), lv2 = two(lv, lv);
+        const uint64_t lv2 = two(lv, lv);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          x[i] = fma2(x[i], c2, add2(neg_m[i], lv2));
+          x[i] = fma2(x[i], scale_of(i), add2(neg_m[i], lv2));
           float u, w;
           halves(x[i], &u, &w);
           if (masked) {
@@ -586,8 +584,7 @@ __global__ void __launch_bounds__(FewShape<T>::kThreads, 2) attend8_few_kernel(c
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           float u, w;
-          halves(x[i], &u, &w);
-          u = fmaf(u, c, lv), w = fmaf(w, c, lv);
+          halves(fma2(x[i], scale_of(i), two(lv, lv)), &u, &w);
           if (!(u == u) || !(sees >> (2 * i) & 1)) u = -INFINITY;
           if (!(w == w) || !(sees >> (2 * i + 1) & 1)) w = -INFINITY;
           x[i] = two(u, w);

@@ -117,3 +117,27 @@ def test_attend8_one_key_with_most_of_the_weight_of_many_rows(t, ahead, spread, 
         plan = P.AttendPlan8([n], [t], H, hk, dim, 64)
         assert not plan.c.few
         R.within(P.attend8(plan, q, c, 0, scale=scale), want, tol, "%d items" % plan.c.n_items)
+
+
+@pytest.mark.parametrize("dtype,size,scale", [(BF, 2.0 ** 30, 0.125), (BF, 2.0 ** 100, 0.125), (HF, 2.0 ** 20, 16.0)])
+@pytest.mark.parametrize("B", [1, 4, 24])
+def test_attend8_rows_of_very_different_size(B, dtype, size, scale):
+    """A tile's rows may be several requests' and heads': what one of them holds is not lost for another's size."""
+    g = _gen(41)
+    H, hk, dim, pre = 8, 2, 64, 4000
+    q = torch.randn(B, H, dim, generator=g, device="cuda") * (0.125 / scale)
+    big = torch.zeros(B, H, dtype=torch.bool, device="cuda")
+    big[1::4], big[::3, 1], big[2::4, 4:7] = True, True, True
+    q = torch.where(big[..., None], (q * size).clamp(-6e4, 6e4) if dtype is HF else q * size, q).to(dtype)
+    kv = [pre + 1 + 3 * b for b in range(B)]
+    keys = _codes(torch.randn(max(kv), hk, dim, generator=g, device="cuda") * 80)
+    values = _codes(torch.randn(max(kv), hk, dim, generator=g, device="cuda") * 80)
+    c = _one_row(keys, values, 2.0 ** -6, 2.0 ** -6, page=16)
+    c = P.PageCache8(c.pool, 1, hk, 16, dim, table=c.table.expand(B, -1).contiguous())
+    plan = P.AttendPlan8([1] * B, kv, H, hk, dim, 16, group_off=[0, B], prefix=[pre])
+    assert plan.c.few == (B < 24)
+    got = P.attend8(plan, q, c, 0, scale=scale)
+    for b in range(B):
+        want, tol = _exact(q[b:b + 1], keys[:kv[b]], values[:kv[b]], 2.0 ** -6, 2.0 ** -6, 1, scale, FLOOR[plan.c.few])
+        small = ~big[b:b + 1]
+        R.within(got[b:b + 1][small], want[small], tol[small], "request %d" % b)
