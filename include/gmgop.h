@@ -146,7 +146,8 @@ int op_rope_append(const op_rope_t* rope, const op_cache_t* cache, int32_t layer
  *   and what it was; tokens before the first one written keep their values, rounded again where the
  *   scale has grown (tokens behind it are no longer valid, as where a row is cut back and grown again);
  *   a new value's code is (k rotated or v) / scale, rounded once, to nearest even; infinities become
- *   +-448, NaN stays.
+ *   +-448, NaN stays.  (k is rotated in 32 bits, and again in 64 where it is within four last bits of the middle between
+ *   two codes; what the block gets does not depend on where the tensors lie.)
  * Tokens of one row that lie in one block come one after another in the lists, in increasing order,
  * within 32 entries (some that are not written, as padding, may lie between): else what that block
  * holds is not defined. */

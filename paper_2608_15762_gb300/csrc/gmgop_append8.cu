@@ -90,49 +90,63 @@ __device__ __forceinline__ void load8(const T* x, float* v) {
   for (int i = 0; i < 8; ++i) v[i] = up(x[i]);
 }
 
-// Elements at .. at + 7 of a head x, rotated.
+// Turned in 32 bits, a number may lie on the wrong side of the middle between two codes: not where it is more than
+// kNear of its last bits from it (its error is about three of them, more where a pair cancels).  Looking for such numbers
+// and turning them again costs a prompt of 32,768 tokens 12 us of 148 (18 with a kNear of 16), and leaves codes 50 times
+// nearer to the exact ones': 8e-7 of their norm for 4e-5.
+constexpr uint32_t kNear = 4, kNearTop = 2 * kNear << 12;
+__device__ __forceinline__ uint32_t from_middle(float x) {   // below kNearTop: near one (codes have the first 3 of the 23 bits)
+  return (__float_as_uint(x) << 12) + ((0x80000 + kNear) << 12);
+}
+// A pair again in 64 bits.  (Out of line: few warps come here.)
+__device__ __noinline__ float2 turn_exactly(float u, float w, uint64_t freq, int32_t pos, float factor) {
+  const uint64_t turn = freq * (uint64_t)(int64_t)pos;
+  double s, c;
+  sincospi((double)(int64_t)turn * 1.0842021724855044e-19, &s, &c);   // 2^-63: half turns
+  const double v[2] = {((double)u * c - (double)w * s) * factor, ((double)u * s + (double)w * c) * factor};
+  float f[2];
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    f[k] = (float)v[k];
+    // a middle itself that was rounded to goes back to its side
+    if ((__float_as_uint(f[k]) & 0xfffff) == 0x80000 && (double)f[k] != v[k])
+      f[k] = __uint_as_float(__float_as_uint(f[k]) + (fabs(v[k]) > fabs((double)f[k]) ? 1 : -1));
+  }
+  return make_float2(f[0], f[1]);
+}
+// Those pairs of the eight that have a number near the middle of two codes.  x: as turned, to be put right; from: as they
+// came; halves: their elements are 8 apart (else neighbours).
+__device__ __noinline__ void turn_eight_exactly(float* x, const float* from, bool halves, int32_t pair, int32_t half,
+                                                const uint64_t* freq, int32_t pos, float factor) {
+#pragma unroll 1
+  for (int p = 0; p < 8 && pair + p < half; ++p) {
+    const int i = halves ? p : 2 * p, j = halves ? p + 8 : 2 * p + 1;
+    if (from_middle(x[i]) >= kNearTop && from_middle(x[j]) >= kNearTop) continue;
+    const float2 v = turn_exactly(from[i], from[j], freq[pair + p], pos, factor);
+    x[i] = v.x, x[j] = v.y;
+  }
+}
+
+// Elements at .. at + 7 of a head x, rotated, one by one: in the same steps as whole pieces, so that codes do not depend on
+// where a tensor lies.  exactly: those near a middle as above.
 template <class T>
-__device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter, const float2* cs, float* v) {
+__device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter, const float2* cs, bool exactly, const uint64_t* freq,
+                                        int32_t pos, float factor, float* v) {
   load8(x + at, v);
+#pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int e = at + i;
     if (e >= 2 * half) break;
     const bool second = inter ? e & 1 : e >= half;
     const int pair = inter ? e / 2 : second ? e - half : e;
     const float o = up(x[inter ? e ^ 1 : second ? e - half : e + half]);
+    const float u = second ? o : v[i], w = second ? v[i] : o;
     const float2 t = cs[pair];
-    v[i] = second ? o * t.y + v[i] * t.x : v[i] * t.x - o * t.y;
-  }
-}
-
-// Turned in 32 bits, a number may lie on the wrong side of the middle between two codes: not where it is more than
-// kNear of its last bits from it (its error is about three of them, more where a pair cancels).  Looking for such numbers
-// and turning them again costs a prompt of 32,768 tokens 12 us of 148 (18 with a kNear of 16), and leaves codes 50 times
-// nearer to the exact ones': 8e-7 of their norm for 4e-5.  (Rows that are loaded element by element are not searched.)
-constexpr uint32_t kNear = 4, kNearTop = 2 * kNear << 12;
-__device__ __forceinline__ uint32_t from_middle(float x) {   // below kNearTop: near one (codes have the first 3 of the 23 bits)
-  return (__float_as_uint(x) << 12) + ((0x80000 + kNear) << 12);
-}
-// Those pairs of the eight that have a number near the middle of two codes, again in 64 bits.  x: as turned, to be put
-// right; from: as they came; halves: their elements are 8 apart (else neighbours).  (Out of line: few warps come here.)
-__device__ __noinline__ void turn_exactly(float* x, const float* from, bool halves, int32_t pair, int32_t half,
-                                          const uint64_t* freq, int32_t pos, float factor) {
-#pragma unroll 1
-  for (int p = 0; p < 8 && pair + p < half; ++p) {
-    const int i = halves ? p : 2 * p, j = halves ? p + 8 : 2 * p + 1;
-    if (from_middle(x[i]) >= kNearTop && from_middle(x[j]) >= kNearTop) continue;
-    const uint64_t turn = freq[pair + p] * (uint64_t)(int64_t)pos;
-    double s, c;
-    sincospi((double)(int64_t)turn * 1.0842021724855044e-19, &s, &c);   // 2^-63: half turns
-    const double u = from[i], w = from[j], v[2] = {(u * c - w * s) * factor, (u * s + w * c) * factor};
-#pragma unroll 1
-    for (int k = 0; k < 2; ++k) {
-      float f = (float)v[k];
-      // a middle itself that was rounded to goes back to its side
-      if ((__float_as_uint(f) & 0xfffff) == 0x80000 && (double)f != v[k])
-        f = __uint_as_float(__float_as_uint(f) + (fabs(v[k]) > fabs((double)f) ? 1 : -1));
-      x[k ? j : i] = f;
-    }
+    float2 r;
+    r.x = __fmaf_rn(u, t.x, __fmul_rn(w, -t.y));
+    r.y = inter ? __fmaf_rn(w, t.x, __fmul_rn(u, t.y)) : __fmaf_rn(u, t.y, __fmul_rn(w, t.x));
+    if (exactly && (from_middle(r.x) < kNearTop || from_middle(r.y) < kNearTop)) r = turn_exactly(u, w, freq[pair], pos, factor);
+    v[i] = second ? r.y : r.x;
   }
 }
 
@@ -293,21 +307,22 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
     };
     auto most = [](float top) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))); };
     auto put = [&](int tok, int e, const float* v) {
-      *reinterpret_cast<uint2*>(codes + (pos[run_at[run][tok]] % kBlock) * a.dim + e) = narrow8(v, by);
+      const uint64_t w[4] = {two(v[0], v[1]), two(v[2], v[3]), two(v[4], v[5]), two(v[6], v[7])};
+      *reinterpret_cast<uint2*>(codes + (pos[run_at[run][tok]] % kBlock) * a.dim + e) = narrow8(w, two(by, by));
     };
     // Twice over the values: for their largest, and for their codes (with infinities, which do not count, thrice).
     // (Where loads are of 16 bytes they lie in registers as they came, else they are read again.)
     auto twice = [&](auto&& each) {
       float top = 0.f;
-      each([&](int, int, const float* v) { top = most_of(v, top); });
+      each([&](int, int, const float* v) { top = most_of(v, top); }, false);
       top = most(top);
       if (!(top <= 3.402823466e38f)) {
         top = 0.f;
-        each([&](int, int, const float* v) { top = most_finite(v, top); });
+        each([&](int, int, const float* v) { top = most_finite(v, top); }, false);
         top = most(top);
       }
       settle(top);
-      each(put);
+      each(put, true);
     };
     if (kWide) {
       uint4 raw[kSteps];
@@ -428,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
               for (int k = 0; k < 2; ++k)
                 from[2 * i + k] = unpack(T(), word(s, i), k), from[8 + 2 * i + k] = unpack(T(), word(s + 1, i), k);
             }
-            turn_exactly(x, from, !kInter, kInter ? e / 2 : e, a.half, a.freq, pos[run_at[run][tok]], a.factor);
+            turn_eight_exactly(x, from, !kInter, kInter ? e / 2 : e, a.half, a.freq, pos[run_at[run][tok]], a.factor);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = two(x[2 * i], x[2 * i + 1]), w[i] = two(x[8 + 2 * i], x[9 + 2 * i]);
           }
@@ -437,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
         });
       }
     } else {
-      twice([&](auto&& use) {
+      twice([&](auto&& use, bool codes_now) {
 #pragma unroll 1
         for (int s = 0; s < kSteps; ++s) {
           int tok, e;
@@ -445,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
           const T* x = from + run_at[run][tok] * row;
           float v[8];
           if (is_v) load8(x + e, v);
-          else turned8(x, e, a.half, kInter, turns + tok * a.half, v);
+          else turned8(x, e, a.half, kInter, turns + tok * a.half, codes_now, a.freq, pos[run_at[run][tok]], a.factor, v);
           use(tok, e, v);
         }
       });
@@ -525,7 +540,8 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   a.page_bytes = page8_bytes(*cache);
   a.codes_at = int64_t(layer) * 2 * a.n_kv * cache->page_tokens * a.dim;
   a.scales_at = page8_scales(*cache) + int64_t(layer) * 2 * a.n_kv * (cache->page_tokens / kScaleTokens) * 4;
-  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps (else a prompt took 255 us for 136)
+  // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps (else a
+  // call on a prompt takes 413 us for 158)
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -6,6 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+import op8_ref as R8  # noqa: E402
 import op_ref as R  # noqa: E402
 from paper_2608_15762_gb300 import gmgop as P  # noqa: E402
 
@@ -141,3 +142,108 @@ def test_attend8_rows_of_very_different_size(B, dtype, size, scale):
         want, tol = _exact(q[b:b + 1], keys[:kv[b]], values[:kv[b]], 2.0 ** -6, 2.0 ** -6, 1, scale, FLOOR[plan.c.few])
         small = ~big[b:b + 1]
         R.within(got[b:b + 1][small], want[small], tol[small], "request %d" % b)
+
+
+# ---------------------------------------------------------------------------
+# Appending
+# ---------------------------------------------------------------------------
+
+def _near_middles(freq, dtype, seed, want=400):
+    """Pairs (u, w), positions and pair numbers whose turn, in 64 bits, lies within one last bit of fp32 of the middle
+    between two codes (of any scale that is a power of two), from below and from above: (u, w, pos, pair, which)."""
+    g = _gen(seed)
+    n = 1 << 24
+    found = []
+    for _ in range(40):
+        u, w = (torch.randn(n, generator=g, device="cuda").to(dtype) for _ in range(2))
+        pos = torch.randint(0, 200000, (n,), generator=g, device="cuda")
+        pair = torch.randint(0, freq.numel(), (n,), generator=g, device="cuda")
+        x, y = _turned(u.double(), w.double(), pos, freq[pair])
+        for which, v in ((0, x), (1, y)):
+            m, e = torch.frexp(v.abs())                        # v = m 2^e, m from 0.5 to 1: 4 bits are multiples of 1 / 16
+            off = m * 16 - torch.floor(m * 16) - 0.5           # in steps of codes; a last bit is 2^-20 of one
+            # (where pairs cancel, the error in 32 bits is more last bits than are looked at)
+            ok = (off.abs() < 2.0 ** -20) & (off != 0) & (v.abs() > 0.7 * torch.maximum(u.abs(), w.abs())) & (v.abs() > 0.05)
+            i = ok.nonzero()[:, 0]
+            found.append(torch.stack((u[i].double(), w[i].double(), pos[i].double(), pair[i].double(),
+                                      torch.full_like(u[i], which, dtype=torch.float64), torch.sign(off[i]))))
+        if sum(f.shape[1] for f in found) >= want:
+            break
+    f = torch.cat(found, 1)[:, :want]
+    assert f.shape[1] == want and min(int((f[5] < 0).sum()), int((f[5] > 0).sum())) > want // 4
+    return f[0].to(dtype), f[1].to(dtype), f[2].int(), f[3].long()
+
+
+def _turned(u, w, pos, freq):
+    """In 64 bits, by angles that are whole 64-bit fractions of a turn."""
+    a = (freq * pos.long()).double() * (math.pi * 2.0 ** -63)      # (the product wraps)
+    return u * torch.cos(a) - w * torch.sin(a), u * torch.sin(a) + w * torch.cos(a)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D,rotary,inter", [(64, 64, False), (64, 64, True), (80, 32, False), (128, 64, True), (32, 8, True), (48, 6, False),
+                                            (16, 10, True)])
+@pytest.mark.parametrize("off", [0, 1])
+def test_append8_keys_near_the_middle_of_two_codes(D, rotary, inter, off, dtype):
+    """The code is the nearer one, wherever the keys lie in memory."""
+    freqs, _ = P.rope_freqs(rotary, 10000.0 if rotary > 8 else 100.0)
+    plan = P.Rope(rotary, freqs=freqs, interleaved=inter)
+    u, w, pos, pair = _near_middles(plan.freq, dtype, D + rotary)
+    # a token each, in blocks of their own
+    T, half = u.numel(), rotary // 2
+    order = torch.argsort(pos // 16, stable=True)
+    keep = torch.cat((torch.ones(1, dtype=torch.bool, device="cuda"), (pos[order] // 16).diff() != 0))
+    order = order[keep]
+    u, w, pos, pair = u[order], w[order], pos[order], pair[order]
+    T = order.numel()
+    assert T > 300
+    g = _gen(3)
+    x = torch.randn(T, 1, D, generator=g, device="cuda").to(dtype)
+    i, j = (2 * pair, 2 * pair + 1) if inter else (pair, pair + half)
+    rows = torch.arange(T, device="cuda")
+    x[rows, 0, i], x[rows, 0, j] = u, w
+    cols = int(pos.max()) // 16 + 1
+    cache = P.PageCache8(torch.zeros(T, P.page8_bytes(1, 1, 16, D), dtype=torch.uint8, device="cuda"), 1, 1, 16, D, 1, cols)
+    cache.table[0, (pos // 16).long()] = torch.randperm(T, generator=g, device="cuda").int()
+    buf = torch.zeros(T, D + 16, dtype=dtype, device="cuda")
+    buf[:, off:off + D] = x[:, 0]
+    k = buf[:, off:off + D].unflatten(1, (1, D))
+    P.rope_append8(plan, x[:, :0], k, x, pos, torch.zeros_like(pos), cache, 0)
+    page = cache.table[0, (pos // 16).long()].long()
+    code = cache.codes[page, 0, 0, 0, (pos % 16).long()].double()
+    scale = cache.scales[page, 0, 0, 0, 0].double()[:, None]
+    want = x[:, 0].double().clone()
+    p = torch.arange(half, device="cuda")
+    a, b = (2 * p, 2 * p + 1) if inter else (p, p + half)
+    want[:, a], want[:, b] = _turned(want[:, a], want[:, b], pos[:, None], plan.freq[None])
+    assert bool((want.abs() <= 448 * scale).all()) and bool((want.abs().amax(1, keepdim=True) > 224 * scale).all())
+    # of the pairs that were looked for both, of the others all but what lies within 32 bits' error of a middle
+    near = torch.zeros_like(want, dtype=torch.bool)
+    near[rows, i], near[rows, j] = True, True
+    wrong = code != R8.rounded((want / scale).cpu()).cuda()
+    assert not bool(wrong[near].any()), "%d of %d" % (int(wrong[near].sum()), int(near.sum()))
+    assert float(wrong.double().mean()) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D,rotary,inter", [(64, 64, False), (80, 32, True), (128, 128, False), (96, 16, False), (64, 8, True)])
+def test_append8_codes_do_not_depend_on_where_tensors_lie(D, rotary, inter, dtype):
+    g = _gen(D)
+    T, H, hk, page = 6000, 2, 2, 32
+    plan = P.Rope(rotary, freqs=P.rope_freqs(rotary)[0], interleaved=inter)
+    pos, seq = torch.arange(37, 37 + T, device="cuda").int(), torch.zeros(T, dtype=torch.int32, device="cuda")
+    row = torch.randn(T, (H + 2 * hk) * D, generator=g, device="cuda").to(dtype)
+    row[::7, 3 * D:3 * D + 9] = -0.0
+    start = torch.randint(0, 120, ((T + 37) // page + 1, P.page8_bytes(1, hk, page, D)), generator=g, device="cuda").to(torch.uint8)
+    got = []
+    for off in (0, 1, 3):
+        buf = torch.zeros(T, row.shape[1] + 8, dtype=dtype, device="cuda")
+        buf[:, off:off + row.shape[1]] = row
+        at = buf[:, off:off + row.shape[1]]
+        q, k, v = (at[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, H), (H, H + hk), (H + hk, H + 2 * hk)))
+        pool = start.clone()
+        cache = P.PageCache8(pool, 1, hk, page, D, 1, pool.shape[0], table=torch.arange(pool.shape[0], device="cuda").int()[None])
+        cache.scales.fill_(2.0 ** -8)
+        P.rope_append8(plan, q, k, v, pos, seq, cache, 0)
+        got.append(pool)
+    assert all(torch.equal(pool, got[0]) for pool in got[1:])
