@@ -53,7 +53,8 @@ extern "C" {
  *   lists that has a fault (of equal rows the second; GMG_PAGE_FULL: how many pages are missing), [2]
  *   pages moved (op_compact), [3] pages in use (op_compact), [4] tokens that
  *   op_rope_append had no page for, added up, [5] blocks of op_attend with a wait
- *   that gave up (0 unless the GPU is at fault: their output is not a result), added up. */
+ *   that gave up (0 unless the GPU is at fault: their output is not a result), added up, [6] tokens that
+ *   op_rope_append8 found out of the order that it needs, added up. */
 typedef struct {
   void* pool;
   int32_t* table;
@@ -150,7 +151,8 @@ int op_rope_append(const op_rope_t* rope, const op_cache_t* cache, int32_t layer
  *   two codes; what the block gets does not depend on where the tensors lie.)
  * Tokens of one row that lie in one block come one after another in the lists, in increasing order,
  * within 32 entries (some that are not written, as padding, may lie between): else what that block
- * holds is not defined. */
+ * holds is not defined.  status[6] counts the tokens that come behind others of their block, but not next, up to 31 entries
+ * after one of them, and those that are more than 31 entries behind the first that they follow. */
 int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, int32_t layer, int32_t dtype, int64_t n_tokens,
                     int32_t n_heads, const void* q, int64_t q_tok, int64_t q_head, const void* k, int64_t k_tok,
                     int64_t k_head, const void* v, int64_t v_tok, int64_t v_head, const int32_t* pos,

@@ -32,7 +32,9 @@ constexpr int kThreads = 128;       // (blocks of 256: a prompt 142 us for 136, 
 constexpr int kChunk = 16;          // tokens of a block where there are many
 constexpr int kBlock = kScaleTokens;
 constexpr int kReach = 32;          // entries of the lists that a run lies in
-constexpr int kWindow = kChunk + 2 * kReach;
+constexpr int kBefore = 2 * kReach; // entries before a block's first that it looks at: a run's head, and what that might follow
+constexpr int kWindow = 4 * 32;
+static_assert(kBefore + kChunk + kReach <= kWindow && kWindow == kThreads, "an entry a thread");
 constexpr int kSteps = kBlock * 128 / 8 / 32;   // 8 elements each, of a lane
 
 struct AppendArgs {
@@ -168,9 +170,9 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
   // [chunk + 15][half] for the keys of the block's runs, then [chunk][half] for its queries (which are turned as dense
   // ones are)
   extern __shared__ __align__(16) float2 cs[];
-  // from kReach entries before the block's first; seq -1: not written
+  // from kBefore entries before the block's first; seq -1: not written
   __shared__ int32_t pos[kWindow], seq[kWindow], page_at[kWindow];
-  __shared__ uint32_t written[4], heads[4];        // of the window's entries, by bit: those written, and those that begin a run
+  __shared__ uint32_t written[5], heads[5];        // of the window's entries, by bit: those written, and those that begin a run
   __shared__ int32_t run_n[kChunk], run_cs[kChunk], n_runs, n_turned, turned_at[kChunk + kBlock];
   __shared__ unsigned char run_at[kChunk][kBlock];   // a run's entries
   const int64_t t0 = (int64_t)blockIdx.x * a.chunk;
@@ -178,9 +180,9 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int32_t page = a.cache.page_tokens;
   int32_t my_pos = 0, my_seq = -1, my_page = -1;
-  if (warp < 3) {
-    const int64_t t = t0 + threadIdx.x - kReach;
-    if (threadIdx.x < own + 2 * kReach && t >= 0 && t < a.n_tokens) {
+  {
+    const int64_t t = t0 + threadIdx.x - kBefore;
+    if (threadIdx.x < own + kBefore + kReach && t >= 0 && t < a.n_tokens) {
       my_pos = a.pos[t], my_seq = a.seq[t];
       if (my_seq >= 0) {
         const int32_t col = my_pos >= 0 ? my_pos / page : -1;
@@ -192,16 +194,15 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
         }
       }
     }
-    if (threadIdx.x < kWindow) pos[threadIdx.x] = my_pos, seq[threadIdx.x] = my_seq, page_at[threadIdx.x] = my_page;
+    pos[threadIdx.x] = my_pos, seq[threadIdx.x] = my_seq, page_at[threadIdx.x] = my_page;
     const uint32_t bits = __ballot_sync(0xffffffffu, my_seq >= 0);
     if (lane == 0) written[warp] = bits;
-  } else if (threadIdx.x == 96) {
-    written[3] = heads[3] = 0;
+    if (threadIdx.x == 0) written[4] = heads[4] = 0;
   }
   __syncthreads();
   // 32 of the window's bits from entry i on
   auto bits_at = [](const uint32_t* words, int i) { return __funnelshift_r(words[i / 32], words[i / 32 + 1], i % 32); };
-  if (warp < 3) {
+  {
     // an entry goes with the one written before it where that is an earlier token of its block
     bool head = my_seq >= 0;
     if (head && threadIdx.x > 0) {
@@ -218,12 +219,12 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
   __syncthreads();
   {
     // a run is what is written from its head to the next, within kReach entries; a warp lists every fourth
-    const uint32_t mine = bits_at(heads, kReach) & ((1u << own) - 1);   // (own <= 16)
+    const uint32_t mine = bits_at(heads, kBefore) & ((1u << own) - 1);   // (own <= 16)
     const int n = __popc(mine);
     uint32_t rest = mine;
     int before = 0;
     for (int r = 0; r < n; ++r, rest &= rest - 1) {
-      const int i = kReach + __ffs(rest) - 1;
+      const int i = kBefore + __ffs(rest) - 1;
       const uint32_t next = bits_at(heads, i) & ~1u;
       const uint32_t run = bits_at(written, i) & (next ? (1u << (__ffs(next) - 1)) - 1 : ~0u);
       const int tokens = __popc(run);    // at most kBlock, of one block and in increasing order
@@ -234,10 +235,18 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
           turned_at[before + k] = i + lane;
         }
         if (lane == 0) run_n[r] = tokens, run_cs[r] = before;
+        // out of order: an entry of the kReach up to this one is in the same block
+        const int e = i - 1 - lane;
+        const bool twice = lane < kReach - 1 && seq[e] == seq[i] && pos[e] / kBlock == pos[i] / kBlock;
+        if (__any_sync(0xffffffffu, twice) && lane == 0 && blockIdx.y == 0) atomicAdd(&a.cache.status[6], tokens);
       }
       before += tokens;
     }
     if (threadIdx.x == 0) n_runs = n, n_turned = before;
+    // or too far behind its run's head, and in no run
+    if (blockIdx.y == 0 && threadIdx.x < own && seq[kBefore + threadIdx.x] >= 0 && !(mine >> threadIdx.x & 1) &&
+        !(bits_at(heads, kBefore + threadIdx.x - (kReach - 1)) & ~(1u << (kReach - 1))))
+      atomicAdd(&a.cache.status[6], 1);
   }
   __syncthreads();
   // in halves: eight pairs a lane, both elements of each
@@ -253,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
       float* at = reinterpret_cast<float*>(cs + t * a.half);
       at += eights ? (p % 8 / 2 * eights + p / 8) * 4 + p % 2 : 2 * p;
       at[0] = turn.x, at[eights ? 2 : 1] = turn.y;
-    } else cs_q[i - n_turned * a.half] = turn_of(a.freq[p], pos[kReach + t - n_turned], a.factor, a.factor);
+    } else cs_q[i - n_turned * a.half] = turn_of(a.freq[p], pos[kBefore + t - n_turned], a.factor, a.factor);
   }
   __syncthreads();
 
@@ -273,8 +282,8 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
     unsigned char* codes = in + a.codes_at + (int64_t(head) * page + slot0) * a.dim;
     const int kept = p0 % kBlock;
     float old = kept ? *scale_at : 0.f;
-    const T* from = is_v ? static_cast<const T*>(a.v) + (t0 - kReach) * a.v_tok + h * a.v_head
-                         : static_cast<const T*>(a.k) + (t0 - kReach) * a.k_tok + h * a.k_head;
+    const T* from = is_v ? static_cast<const T*>(a.v) + (t0 - kBefore) * a.v_tok + h * a.v_head
+                         : static_cast<const T*>(a.k) + (t0 - kBefore) * a.k_tok + h * a.k_head;
     const int64_t row = is_v ? a.v_tok : a.k_tok;
     // step s of a lane: elements from .. on of a token; two steps of keys are eight pairs' elements, or 16 one after another
     const bool paired = kWide && !is_v;

@@ -421,7 +421,8 @@ def rope_append8(plan: Rope, q, k, v, pos, seq, cache: PageCache8, layer: int, o
     """``rope_append`` into a cache in 8 bits, from q, k and v in bf16 or fp16.  A block of 16 tokens gets the
     least power of two as its scale with which its largest value is at most 448; what it held before its first
     token of this call is rounded again where the scale grows.  Tokens of one row that lie in one block follow
-    one another in the lists, in increasing order and (padding between them included) within 32 entries."""
+    one another in the lists, in increasing order and (padding between them included) within 32 entries: others,
+    as far as the call sees them, are counted in ``cache.status[6]``, and what their block holds is not defined."""
     T, H, D = q.shape
     kv, dt, dev, kind = (T, cache.n_kv_heads, D), q.dtype, cache.device, _TYPES.get(q.dtype)
     if cache.dtype is not torch.uint8:

@@ -247,3 +247,42 @@ def test_append8_codes_do_not_depend_on_where_tensors_lie(D, rotary, inter, dtyp
         P.rope_append8(plan, q, k, v, pos, seq, cache, 0)
         got.append(pool)
     assert all(torch.equal(pool, got[0]) for pool in got[1:])
+
+
+def _append_in_order(entries, n_seq=40, page=16):
+    """(seq, pos) entries, in their order, into an empty cache: (cache, what was appended, seq, pos)."""
+    g = _gen(len(entries))
+    T, D = len(entries), 32
+    cache = P.PageCache8(torch.zeros(n_seq * 4, P.page8_bytes(1, 1, page, D), dtype=torch.uint8, device="cuda"), 1, 1, page, D,
+                         n_seq, 4, table=torch.arange(n_seq * 4, device="cuda").int().view(n_seq, 4))
+    x = torch.randn(T, 1, D, generator=g, device="cuda").to(BF)
+    seq, pos = (torch.tensor([e[i] for e in entries], dtype=torch.int32, device="cuda") for i in (0, 1))
+    P.rope_append8(P.Rope(0), x, x, x, pos, seq, cache, 0)
+    return cache, x, seq, pos
+
+
+@pytest.mark.parametrize("lead", [0, 3, 15, 16, 700])
+def test_append8_counts_tokens_out_of_order(lead):
+    """Tokens that break the lists' order within 32 entries are seen, wherever thread blocks begin."""
+    none = (-1, 0)
+    before = [(1 + t // 64, t % 64) for t in range(lead)]
+    cases = [([(0, 0), (0, 1), (0, 2)], 0),
+             ([(0, 0)] + [none] * 9 + [(0, 1)] + [none] * 20 + [(0, 2)], 0),        # 31 entries from the first to the last
+             ([(0, 0)] + [none] * 9 + [(0, 1)] + [none] * 21 + [(0, 2)], 1),        # one too far
+             ([(0, 0)] + [none] * 19 + [(0, 1)] + [none] * 19 + [(0, 2)] + [none] * 19 + [(0, 3)], 2),
+             ([(0, t) for t in range(40)], 0),
+             ([(0, 5), (0, 4), (0, 3)], 2),                                         # backwards
+             ([(0, 5), (0, 5)], 1),                                                 # the same token twice
+             ([(0, 3), (0, 4), (0, 30), (0, 5), (0, 6), (0, 31)], 3),               # a block, another one, the first again
+             ([(r, t) for t in range(8) for r in (0, 39)], 14),                     # two rows in turn
+             ([(r, 16 * t + 2) for t in range(4) for r in (0, 39)], 0)]             # but blocks of their own
+    for entries, count in cases:
+        cache, x, seq, pos = _append_in_order(before + entries)
+        assert cache.status.tolist()[4:7] == [0, 0, count], entries
+        if count == 0:
+            on = seq >= 0
+            at = cache.table[seq[on].long(), (pos[on] // 16).long()].long()
+            for which in (0, 1):
+                code = cache.codes[at, 0, which, 0, (pos[on] % 16).long()].double()
+                s = cache.scales[at, 0, which, 0, 0].double()[:, None]
+                assert torch.equal(code.cpu(), R8.rounded((x[on, 0].double() / s).cpu()))
