@@ -192,7 +192,8 @@ typedef struct {
 } op_attend_plan_t;
 
 /* Fills *plan and, if items is not NULL, items[plan->plan_bytes / 4] (host
- * int32, on the device 16-byte aligned; item_bytes is what it holds).  n_sm: SMs to spread the work over. */
+ * int32, on the device 16-byte aligned; item_bytes is what it holds: where that is too little, GMG_EWS, and *plan
+ * says what is needed).  n_sm: SMs to spread the work over. */
 int op_attend_plan(const op_attend_desc_t* desc, int32_t n_sm, op_attend_plan_t* plan, int32_t* items,
                    size_t item_bytes);
 

@@ -482,8 +482,10 @@ extern "C" {
 int op_attend_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend_plan_t* plan, int32_t* items,
                    size_t item_bytes) try {
   if (!desc_ok(d, kRows) || !plan || n_sm < 1) return GMG_EINVAL;
+  Runs runs;
+  list_runs(*d, n_sm, kCutting, &runs);
   Work w;
-  plan_items(*d, n_sm, kCutting, &w);
+  cut_runs(*d, runs, kCutting, &w);
   return fill_plan(d, w, plan, items, item_bytes);
 } catch (const std::bad_alloc&) {
   return GMG_ENOMEM;

@@ -10,6 +10,8 @@
 
 #include <algorithm>
 #include <functional>
+#include <map>
+#include <utility>
 #include <vector>
 
 #include "../../include/gmgop.h"
@@ -168,40 +170,65 @@ struct Cutting {
   bool balanced;         // cut so that the blocks' rounds come out even, not only into as many items as blocks run at once
 };
 
+inline int64_t steps_of(const Run& r, const Cutting& cut) {
+  return r.hi > r.lo ? (r.hi + cut.keys - 1) / cut.keys - r.lo / cut.keys : 0;
+}
+inline int64_t parts_of(int64_t steps, int64_t most) { return std::max<int64_t>(1, (steps + most - 1) / most); }
+
 // Of some lengths up to `most`, the one with which blocks that start one after another, the longest first, on
-// `slots` places end first.
-template <class F>
-int64_t even_cut(const std::vector<Run>& runs, const F& steps_of, int32_t heads, int32_t slots, int64_t most, const Cutting& cut) {
+// `slots` places end first.  Equal blocks and places that are free at the same time are taken together: a decode
+// step of 64 requests is a few dozen moves and not 500 (a plan 40 us where block by block it took 529).
+inline int64_t even_cut(const std::vector<Run>& runs, int32_t heads, int64_t slots, int64_t most, const Cutting& cut) {
   int64_t best = most, best_end = -1;
-  std::vector<int64_t> sizes, places;
+  bool pooled = false;
+  std::vector<int64_t> lengths;
+  lengths.reserve(runs.size());
+  for (const Run& r : runs) lengths.push_back(steps_of(r, cut)), pooled |= r.pooled;
+  std::sort(lengths.begin(), lengths.end(), std::greater<int64_t>());
+  std::vector<std::pair<int64_t, int64_t>> sizes;                // and how many there are
+  std::map<int64_t, int64_t> places;                             // when they are free, and how many then
   for (int64_t k = 1; k <= 6; ++k) {
     const int64_t most_k = std::max(cut.min_steps, (most + k - 1) / k);
     sizes.clear();
-    bool joins = false;
-    for (const Run& r : runs) {
-      const int64_t n = steps_of(r), parts = std::max<int64_t>(1, (n + most_k - 1) / most_k);
-      joins |= parts > 1 || r.pooled;
-      for (int64_t p = 0; p < parts; ++p) sizes.push_back(n * (p + 1) / parts - n * p / parts + cut.item_steps);
+    bool joins = pooled;
+    int64_t blocks = 0;
+    for (size_t i = 0; i < lengths.size();) {
+      const int64_t n = lengths[i], parts = parts_of(n, most_k);
+      int64_t same = 0;
+      for (; i < lengths.size() && lengths[i] == n; ++i) ++same;
+      joins |= parts > 1;
+      blocks += same * parts;
+      if (n % parts) sizes.emplace_back(n / parts + 1 + cut.item_steps, same * (n % parts));
+      sizes.emplace_back(n / parts + cut.item_steps, same * (parts - n % parts));
     }
-    if ((int64_t)sizes.size() * heads > 40 * slots) break;       // (so many come out even by themselves)
-    std::sort(sizes.begin(), sizes.end(), std::greater<int64_t>());
-    places.assign(slots, 0);                                     // when they are free, as a heap
-    for (const int64_t n : sizes)
-      for (int32_t h = 0; h < heads; ++h) {
-        std::pop_heap(places.begin(), places.end(), std::greater<int64_t>());
-        places.back() += n;
-        std::push_heap(places.begin(), places.end(), std::greater<int64_t>());
+    if (blocks * heads > 40 * slots) break;                      // (so many come out even by themselves)
+    std::sort(sizes.begin(), sizes.end(), std::greater<std::pair<int64_t, int64_t>>());
+    places.clear();
+    places[0] = slots;
+    for (const auto& size : sizes)
+      for (int64_t left = size.second * heads; left > 0;) {
+        const auto first = places.begin();
+        const int64_t now = first->first, n = std::min(left, first->second);
+        if (n == first->second) places.erase(first);
+        else first->second -= n;
+        places[now + size.first] += n;
+        left -= n;
       }
-    const int64_t end = *std::max_element(places.begin(), places.end()) + (joins ? cut.join_steps : 0);
+    const int64_t end = places.rbegin()->first + (joins ? cut.join_steps : 0);
     if (best_end < 0 || end < best_end) best = most_k, best_end = end;
     if (most_k == cut.min_steps) break;
   }
   return best;
 }
 
-inline void plan_items(const op_attend_desc_t& d, int32_t n_sm, const Cutting& cut, Work* w) {
-  const int32_t keys = cut.keys, group = d.n_heads / d.n_kv_heads, tile = cut.rows / group;
-  auto steps_of = [&](const Run& r) { return r.hi > r.lo ? (r.hi + keys - 1) / keys - r.lo / keys : 0; };
+// A batch's runs and the longest part that they are cut into.
+struct Runs {
+  std::vector<Run> runs;
+  int64_t most;
+};
+
+inline void list_runs(const op_attend_desc_t& d, int64_t n_sm, const Cutting& cut, Runs* to) {
+  const int32_t keys = cut.keys, tile = cut.rows / (d.n_heads / d.n_kv_heads);
   // a small step, which one round of blocks takes with a few steps each: apart and uncut, so that
   // nothing is left to join
   int64_t alone = 0, longest = 0;
@@ -210,7 +237,7 @@ inline void plan_items(const op_attend_desc_t& d, int32_t n_sm, const Cutting& c
     if (d.q_len[b] > 0) longest = std::max<int64_t>(longest, (d.kv_len[b] + keys - 1) / keys);
   }
   const bool small = alone * d.n_kv_heads <= 2 * n_sm && longest <= cut.alone_steps;
-  std::vector<Run> runs;
+  std::vector<Run>& runs = to->runs;
   const int32_t ng = d.n_groups > 0 ? d.n_groups : 1;
   int32_t tok = 0;
   for (int32_t g = 0; g < ng; ++g) {
@@ -241,16 +268,28 @@ inline void plan_items(const op_attend_desc_t& d, int32_t n_sm, const Cutting& c
     }
   }
   int64_t steps = 0;
-  for (const Run& r : runs) steps += steps_of(r) + cut.item_steps;
-  int64_t most = std::max(small ? cut.alone_steps : cut.min_steps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
-  if (cut.balanced && !small) most = even_cut(runs, steps_of, d.n_kv_heads, 2 * n_sm, most, cut);
+  for (const Run& r : runs) steps += steps_of(r, cut) + cut.item_steps;
+  to->most = std::max(small ? cut.alone_steps : cut.min_steps, (steps * d.n_kv_heads + 2 * n_sm - 1) / (2 * n_sm));
+  if (cut.balanced && !small) to->most = even_cut(runs, d.n_kv_heads, 2 * n_sm, to->most, cut);
+}
+
+// What they come to in steps, with what the items cost beyond theirs.
+inline int64_t all_steps(const Runs& from, const Cutting& cut) {
+  int64_t steps = 0;
+  for (const Run& r : from.runs) steps += steps_of(r, cut) + parts_of(steps_of(r, cut), from.most) * cut.item_steps;
+  return steps;
+}
+
+inline void cut_runs(const op_attend_desc_t& d, const Runs& from, const Cutting& cut, Work* w) {
+  const std::vector<Run>& runs = from.runs;
+  const int32_t keys = cut.keys, group = d.n_heads / d.n_kv_heads, tile = cut.rows / group;
   // cut; then longest first, so that short items fill the end (equal ones keep their order:
   // tiles that read the same keys stay together)
   struct Cut {
     int32_t run, part, parts;
   };
   std::vector<int32_t> parts(runs.size()), base(runs.size(), -1), joined(runs.size(), 0);
-  for (size_t i = 0; i < runs.size(); ++i) parts[i] = int32_t(std::max<int64_t>(1, (steps_of(runs[i]) + most - 1) / most));
+  for (size_t i = 0; i < runs.size(); ++i) parts[i] = int32_t(parts_of(steps_of(runs[i], cut), from.most));
   // a request's queries are joined where a pooled run covers them too, or where they are cut
   size_t pooled = 0, pooled_end = 0;   // runs of the current group's pool
   for (size_t i = 0; i < runs.size(); ++i) {
@@ -294,11 +333,11 @@ inline void plan_items(const op_attend_desc_t& d, int32_t n_sm, const Cutting& c
       for (size_t k = i; k < last; ++k) cuts.push_back(Cut{int32_t(k), p, parts[k]});
   }
   std::stable_sort(cuts.begin(), cuts.end(), [&](const Cut& x, const Cut& y) {
-    return steps_of(runs[x.run]) / x.parts > steps_of(runs[y.run]) / y.parts;
+    return steps_of(runs[x.run], cut) / x.parts > steps_of(runs[y.run], cut) / y.parts;
   });
   for (const Cut& c : cuts) {
     const Run& r = runs[c.run];
-    const int64_t s0 = r.lo / keys, n = steps_of(r);
+    const int64_t s0 = r.lo / keys, n = steps_of(r, cut);
     const int64_t a = s0 + n * c.part / c.parts, b = s0 + n * (c.part + 1) / c.parts;
     Item it{};
     it.tok0 = r.tok0, it.n_tok = r.n_tok, it.row = r.row, it.pos0 = r.pos0;
@@ -329,13 +368,13 @@ inline int fill_plan(const op_attend_desc_t* d, const Work& w, op_attend_plan_t*
   p.part_rows = w.part_rows;
   p.plan_bytes = sizeof(Item) * w.items.size() + sizeof(Join) * w.joins.size();
   p.work_bytes = 256 + size_t(w.part_rows) * d->n_kv_heads * (d->head_dim + 1) * 4;
+  *plan = p;
   if (items) {
     if (item_bytes < p.plan_bytes) return GMG_EWS;
     Item* to = reinterpret_cast<Item*>(items);
     std::copy(w.items.begin(), w.items.end(), to);
     std::copy(w.joins.begin(), w.joins.end(), reinterpret_cast<Join*>(to + w.items.size()));
   }
-  *plan = p;
   return GMG_OK;
 }
 

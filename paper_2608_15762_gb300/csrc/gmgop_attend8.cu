@@ -1199,13 +1199,6 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
 constexpr Cutting kCuttingFew = {kFewKeys, kFewRows, 4, 8, 4, 5, true}, kCuttingMany = {kKeys, kRows, 6, 12, 4, 8, true};
 constexpr int64_t kFewClocks = 1900, kManyClocks = 1300;
 
-int64_t steps_of(const Work& w, const Cutting& cut) {
-  int64_t steps = 0;
-  for (const Item& it : w.items)
-    steps += cut.item_steps + (it.hi > it.lo ? (it.hi + cut.keys - 1) / cut.keys - it.lo / cut.keys : 0);
-  return steps;
-}
-
 template <class T, int DP>
 cudaError_t launch_many(const op_attend_plan_t& p, const CUtensorMap& kv, const Args8& g, cudaStream_t st) {
   static gsim::OncePerDevice once;
@@ -1247,15 +1240,17 @@ extern "C" {
 int op_attend8_plan(const op_attend_desc_t* d, int32_t n_sm, op_attend8_plan_t* plan, int32_t* items,
                     size_t item_bytes) try {
   if (!desc_ok(d, kRows) || d->head_dim % 16 || d->page_tokens < 16 || !plan || n_sm < 1) return GMG_EINVAL;
-  Work few, many;
-  plan_items(*d, n_sm, kCuttingMany, &many);
+  Runs few, many;
+  list_runs(*d, n_sm, kCuttingMany, &many);
   bool is_few = d->n_heads / d->n_kv_heads <= kFewRows;
   if (is_few) {
-    plan_items(*d, n_sm, kCuttingFew, &few);
-    is_few = steps_of(few, kCuttingFew) * kFewClocks <= steps_of(many, kCuttingMany) * kManyClocks;
+    list_runs(*d, n_sm, kCuttingFew, &few);
+    is_few = all_steps(few, kCuttingFew) * kFewClocks <= all_steps(many, kCuttingMany) * kManyClocks;
   }
-  const int rc = fill_plan(d, is_few ? few : many, &plan->p, items, item_bytes);
-  if (rc == GMG_OK) plan->few = is_few, plan->reserved = 0;
+  Work w;
+  cut_runs(*d, is_few ? few : many, is_few ? kCuttingFew : kCuttingMany, &w);
+  const int rc = fill_plan(d, w, &plan->p, items, item_bytes);
+  if (rc == GMG_OK || rc == GMG_EWS) plan->few = is_few, plan->reserved = 0;
   return rc;
 } catch (const std::bad_alloc&) {
   return GMG_ENOMEM;

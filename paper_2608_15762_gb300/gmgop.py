@@ -474,7 +474,6 @@ def attend_items(q_len, kv_len, n_heads, n_kv_heads, head_dim, page_tokens, seq=
     call = getattr(_LIB or lib(), name)
     rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
     if rc == G.GMG_EWS:
-        _check(call(C.addressof(d), n_sm, C.addressof(plan), None, 0), name)
         items = np.empty(plan.plan_bytes // 4, np.int32)
         rc = call(C.addressof(d), n_sm, C.addressof(plan), items.ctypes.data, items.nbytes)
     _check(rc, name)
