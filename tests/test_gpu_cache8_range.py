@@ -9,6 +9,7 @@ torch = pytest.importorskip("torch")
 import op8_ref as R8  # noqa: E402
 import op_ref as R  # noqa: E402
 from paper_2608_15762_gb300 import gmgop as P  # noqa: E402
+from test_gpu_more_operators import _check_attend8, _kv8  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -142,6 +143,62 @@ def test_attend8_rows_of_very_different_size(B, dtype, size, scale):
         want, tol = _exact(q[b:b + 1], keys[:kv[b]], values[:kv[b]], 2.0 ** -6, 2.0 ** -6, 1, scale, FLOOR[plan.c.few])
         small = ~big[b:b + 1]
         R.within(got[b:b + 1][small], want[small], tol[small], "request %d" % b)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,H", [(1, 4), (1, 16), (4, 4), (40, 4), (13, 40)])
+@pytest.mark.parametrize("t", [300, 7001, 65536])
+def test_attend8_every_part_counts(n, H, t, dtype):
+    """64 keys, anywhere, share the weight, and each has a dimension of its own: where one is lost, or a part of the keys is
+    joined with another weight, that dimension shows it."""
+    dim, ks, vs, scale = 128, 2.0 ** -4, 2.0 ** -6, 128 ** -0.5
+    g = _gen(t + n)
+    sign = torch.randint(0, 2, (1, dim), generator=g, device="cuda") * 2.0 - 1
+    keys = torch.zeros(t, 1, dim, device="cuda")
+    values = torch.randn(t, 1, dim, generator=g, device="cuda") * 0.01
+    spots = torch.randperm(t - n, generator=g, device="cuda")[:64]
+    keys[spots] = sign * (20 * dim ** -0.5)
+    values[spots] = 0
+    values[spots, 0, torch.arange(64, device="cuda") * 2] = 1 + torch.rand(64, generator=g, device="cuda")
+    q = (sign[None] * (1 + 0.02 * torch.rand(n, H, 1, generator=g, device="cuda"))).to(dtype)
+    keys, values = _codes(keys / ks), _codes(values / vs)
+    plan = P.AttendPlan8([n], [t], H, 1, dim, 64)
+    got = P.attend8(plan, q, _one_row(keys, values, ks, vs), 0, scale=scale)
+    want, tol = _exact(q, keys, values, ks, vs, n, scale, FLOOR[plan.c.few])
+    assert bool((want[..., ::2].abs() > 0.01).all()) and bool((tol[..., ::2] < 0.01 * want[..., ::2].abs()).all())
+    R.within(got, want, tol)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("q_len,H,few", [([1], 8, 1), ([4], 8, 1), ([64], 8, 0)])
+def test_attend8_long_as_a_whole(q_len, H, few, dtype):
+    """The whole result's error, beside each element's bound: weights that are rounded to 2^-11 or less, independently, and one
+    rounding to the result's type."""
+    t = [50000 + q_len[0]]
+    _, plan, q, o, _, held = _check_attend8(q_len, t, H, 2, 64, 32, dtype, seed=q_len[0])
+    assert plan.c.few == few
+    k, v, _ = _kv8(*held[0])
+    G = H // 2
+    want = torch.empty(q.shape, dtype=torch.float64, device="cuda")
+    hide = torch.arange(t[0], device="cuda")[None] > torch.arange(t[0] - q_len[0], t[0], device="cuda")[:, None]
+    for h in range(H):
+        z = (q[:, h].double() @ k[:, h // G].t() * 64 ** -0.5).masked_fill(hide, -math.inf)
+        want[:, h] = torch.softmax(z, -1) @ v[:, h // G]
+    assert float((o.double() - want).norm() / want.norm()) <= R.U[dtype] + 2.0 ** -10
+
+
+@pytest.mark.parametrize("lo,hi", [(-60, -40), (-30, 4), (-12, 4)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_attend8_scales_of_values_far_apart(lo, hi, dtype):
+    """In both types, through tiles of few rows and of many."""
+    def some(blocks):
+        g = _gen(blocks + hi)
+        s = torch.full((blocks, 2, 2), 2.0 ** -7, device="cuda")
+        s[:, 1] = torch.exp2(torch.randint(lo, hi + 1, (blocks, 2), generator=g, device="cuda").float())
+        return s
+    kinds = [_check_attend8(q, kv, 8, 2, 64, 16, dtype, scales=some)[1].c.few
+             for q, kv in (([1, 3], [4000, 3000]), ([1, 3, 140], [700, 300, 5000]))]
+    assert kinds == [1, 0]
 
 
 # ---------------------------------------------------------------------------
