@@ -32,9 +32,7 @@ constexpr int kThreads = 128;       // (blocks of 256: a prompt 142 us for 136, 
 constexpr int kChunk = 16;          // tokens of a block where there are many
 constexpr int kBlock = kScaleTokens;
 constexpr int kReach = 32;          // entries of the lists that a run lies in
-constexpr int kBefore = 2 * kReach; // entries before a block's first that it looks at: a run's head, and what that might follow
-constexpr int kWindow = 4 * 32;
-static_assert(kBefore + kChunk + kReach <= kWindow && kWindow == kThreads, "an entry a thread");
+constexpr int kWindow = kChunk + 2 * kReach;
 constexpr int kSteps = kBlock * 128 / 8 / 32;   // 8 elements each, of a lane
 
 struct AppendArgs {
@@ -100,32 +98,27 @@ constexpr uint32_t kNear = 4, kNearTop = 2 * kNear << 12;
 __device__ __forceinline__ uint32_t from_middle(float x) {   // below kNearTop: near one (codes have the first 3 of the 23 bits)
   return (__float_as_uint(x) << 12) + ((0x80000 + kNear) << 12);
 }
-// A pair again in 64 bits.  (Out of line: few warps come here.)
-__device__ __noinline__ float2 turn_exactly(float u, float w, uint64_t freq, int32_t pos, float factor) {
-  const uint64_t turn = freq * (uint64_t)(int64_t)pos;
-  double s, c;
-  sincospi((double)(int64_t)turn * 1.0842021724855044e-19, &s, &c);   // 2^-63: half turns
-  const double v[2] = {((double)u * c - (double)w * s) * factor, ((double)u * s + (double)w * c) * factor};
-  float f[2];
-#pragma unroll 1
-  for (int k = 0; k < 2; ++k) {
-    f[k] = (float)v[k];
-    // a middle itself that was rounded to goes back to its side
-    if ((__float_as_uint(f[k]) & 0xfffff) == 0x80000 && (double)f[k] != v[k])
-      f[k] = __uint_as_float(__float_as_uint(f[k]) + (fabs(v[k]) > fabs((double)f[k]) ? 1 : -1));
-  }
-  return make_float2(f[0], f[1]);
-}
-// Those pairs of the eight that have a number near the middle of two codes.  x: as turned, to be put right; from: as they
-// came; halves: their elements are 8 apart (else neighbours).
-__device__ __noinline__ void turn_eight_exactly(float* x, const float* from, bool halves, int32_t pair, int32_t half,
-                                                const uint64_t* freq, int32_t pos, float factor) {
+// Those pairs of the eight that have a number near the middle of two codes, again in 64 bits.  x: as turned, to be put
+// right; from: as they came; halves: their elements are 8 apart (else neighbours).  (Out of line: few warps come here.
+// And short, as it is fetched then: with a function for a pair in it, 304 requests' tokens took 17.4 us for 16.4.)
+__device__ __noinline__ void turn_exactly(float* x, const float* from, bool halves, int32_t pair, int32_t half,
+                                          const uint64_t* freq, int32_t pos, float factor) {
 #pragma unroll 1
   for (int p = 0; p < 8 && pair + p < half; ++p) {
     const int i = halves ? p : 2 * p, j = halves ? p + 8 : 2 * p + 1;
     if (from_middle(x[i]) >= kNearTop && from_middle(x[j]) >= kNearTop) continue;
-    const float2 v = turn_exactly(from[i], from[j], freq[pair + p], pos, factor);
-    x[i] = v.x, x[j] = v.y;
+    const uint64_t turn = freq[pair + p] * (uint64_t)(int64_t)pos;
+    double s, c;
+    sincospi((double)(int64_t)turn * 1.0842021724855044e-19, &s, &c);   // 2^-63: half turns
+    const double u = from[i], w = from[j], v[2] = {(u * c - w * s) * factor, (u * s + w * c) * factor};
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+      float f = (float)v[k];
+      // a middle itself that was rounded to goes back to its side
+      if ((__float_as_uint(f) & 0xfffff) == 0x80000 && (double)f != v[k])
+        f = __uint_as_float(__float_as_uint(f) + (fabs(v[k]) > fabs((double)f) ? 1 : -1));
+      x[k ? j : i] = f;
+    }
   }
 }
 
@@ -144,11 +137,13 @@ __device__ __forceinline__ void turned8(const T* x, int at, int half, bool inter
     const float o = up(x[inter ? e ^ 1 : second ? e - half : e + half]);
     const float u = second ? o : v[i], w = second ? v[i] : o;
     const float2 t = cs[pair];
-    float2 r;
-    r.x = __fmaf_rn(u, t.x, __fmul_rn(w, -t.y));
-    r.y = inter ? __fmaf_rn(w, t.x, __fmul_rn(u, t.y)) : __fmaf_rn(u, t.y, __fmul_rn(w, t.x));
-    if (exactly && (from_middle(r.x) < kNearTop || from_middle(r.y) < kNearTop)) r = turn_exactly(u, w, freq[pair], pos, factor);
-    v[i] = second ? r.y : r.x;
+    float r[2] = {__fmaf_rn(u, t.x, __fmul_rn(w, -t.y)),
+                  inter ? __fmaf_rn(w, t.x, __fmul_rn(u, t.y)) : __fmaf_rn(u, t.y, __fmul_rn(w, t.x))};
+    if (exactly && (from_middle(r[0]) < kNearTop || from_middle(r[1]) < kNearTop)) {
+      const float from[2] = {u, w};
+      turn_exactly(r, from, false, pair, pair + 1, freq, pos, factor);
+    }
+    v[i] = second ? r[1] : r[0];
   }
 }
 
@@ -170,9 +165,9 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
   // [chunk + 15][half] for the keys of the block's runs, then [chunk][half] for its queries (which are turned as dense
   // ones are)
   extern __shared__ __align__(16) float2 cs[];
-  // from kBefore entries before the block's first; seq -1: not written
+  // from kReach entries before the block's first; seq -1: not written
   __shared__ int32_t pos[kWindow], seq[kWindow], page_at[kWindow];
-  __shared__ uint32_t written[5], heads[5];        // of the window's entries, by bit: those written, and those that begin a run
+  __shared__ uint32_t written[4], heads[4];        // of the window's entries, by bit: those written, and those that begin a run
   __shared__ int32_t run_n[kChunk], run_cs[kChunk], n_runs, n_turned, turned_at[kChunk + kBlock];
   __shared__ unsigned char run_at[kChunk][kBlock];   // a run's entries
   const int64_t t0 = (int64_t)blockIdx.x * a.chunk;
@@ -180,29 +175,35 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int32_t page = a.cache.page_tokens;
   int32_t my_pos = 0, my_seq = -1, my_page = -1;
-  {
-    const int64_t t = t0 + threadIdx.x - kBefore;
-    if (threadIdx.x < own + kBefore + kReach && t >= 0 && t < a.n_tokens) {
+  // the page that an entry is written to, or -1
+  auto page_of = [&](int32_t p, int32_t row) {
+    const int32_t col = p >= 0 ? p / page : -1;
+    if (row < 0 || row >= a.cache.n_seq || col < 0 || col >= a.cache.max_pages) return -1;
+    const int32_t x = a.cache.table[int64_t(row) * a.cache.max_pages + col];
+    return x < a.cache.n_pages ? x : -1;
+  };
+  if (warp < 3) {
+    const int64_t t = t0 + threadIdx.x - kReach;
+    if (threadIdx.x < own + 2 * kReach && t >= 0 && t < a.n_tokens) {
       my_pos = a.pos[t], my_seq = a.seq[t];
       if (my_seq >= 0) {
-        const int32_t col = my_pos >= 0 ? my_pos / page : -1;
-        if (my_seq < a.cache.n_seq && col >= 0 && col < a.cache.max_pages)
-          my_page = a.cache.table[int64_t(my_seq) * a.cache.max_pages + col];
-        if (my_page < 0 || my_page >= a.cache.n_pages) {
+        my_page = page_of(my_pos, my_seq);
+        if (my_page < 0) {
           my_seq = -1;
           if (blockIdx.y == 0 && t >= t0 && t < t0 + own) atomicAdd(&a.cache.status[4], 1);
         }
       }
     }
-    pos[threadIdx.x] = my_pos, seq[threadIdx.x] = my_seq, page_at[threadIdx.x] = my_page;
+    if (threadIdx.x < kWindow) pos[threadIdx.x] = my_pos, seq[threadIdx.x] = my_seq, page_at[threadIdx.x] = my_page;
     const uint32_t bits = __ballot_sync(0xffffffffu, my_seq >= 0);
     if (lane == 0) written[warp] = bits;
-    if (threadIdx.x == 0) written[4] = heads[4] = 0;
+  } else if (threadIdx.x == 96) {
+    written[3] = heads[3] = 0;
   }
   __syncthreads();
   // 32 of the window's bits from entry i on
   auto bits_at = [](const uint32_t* words, int i) { return __funnelshift_r(words[i / 32], words[i / 32 + 1], i % 32); };
-  {
+  if (warp < 3) {
     // an entry goes with the one written before it where that is an earlier token of its block
     bool head = my_seq >= 0;
     if (head && threadIdx.x > 0) {
@@ -219,12 +220,12 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
   __syncthreads();
   {
     // a run is what is written from its head to the next, within kReach entries; a warp lists every fourth
-    const uint32_t mine = bits_at(heads, kBefore) & ((1u << own) - 1);   // (own <= 16)
+    const uint32_t mine = bits_at(heads, kReach) & ((1u << own) - 1);   // (own <= 16)
     const int n = __popc(mine);
     uint32_t rest = mine;
     int before = 0;
     for (int r = 0; r < n; ++r, rest &= rest - 1) {
-      const int i = kBefore + __ffs(rest) - 1;
+      const int i = kReach + __ffs(rest) - 1;
       const uint32_t next = bits_at(heads, i) & ~1u;
       const uint32_t run = bits_at(written, i) & (next ? (1u << (__ffs(next) - 1)) - 1 : ~0u);
       const int tokens = __popc(run);    // at most kBlock, of one block and in increasing order
@@ -243,10 +244,20 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
       before += tokens;
     }
     if (threadIdx.x == 0) n_runs = n, n_turned = before;
-    // or too far behind its run's head, and in no run
-    if (blockIdx.y == 0 && threadIdx.x < own && seq[kBefore + threadIdx.x] >= 0 && !(mine >> threadIdx.x & 1) &&
-        !(bits_at(heads, kBefore + threadIdx.x - (kReach - 1)) & ~(1u << (kReach - 1))))
-      atomicAdd(&a.cache.status[6], 1);
+    // or too far behind its run's head, and in no run: none of the entries up to kReach - 1 before it is a head.  (Only of the
+    // first that the window shows is it not certain that it is one: what it may follow lies before the window.)
+    if (blockIdx.y == 0 && threadIdx.x < own && seq[kReach + threadIdx.x] >= 0 && !(mine >> threadIdx.x & 1)) {
+      const uint32_t shown = written[0] & ~1u, near = bits_at(heads, threadIdx.x + 1) & ~(1u << (kReach - 1));
+      const int x = __ffs(shown) - 1;      // (entry 0 is before those)
+      bool lost = near == 0;
+      if (!lost && !(written[0] & 1) && x > (int)threadIdx.x && near == 1u << (x - 1 - threadIdx.x))
+        for (int64_t t = t0 - kReach + x - 1; t >= 0 && t > t0 - 2 * kReach + x; --t)
+          if (page_of(a.pos[t], a.seq[t]) >= 0) {
+            lost = a.seq[t] == seq[x] && a.pos[t] < pos[x] && a.pos[t] / kBlock == pos[x] / kBlock;
+            break;
+          }
+      if (lost) atomicAdd(&a.cache.status[6], 1);
+    }
   }
   __syncthreads();
   // in halves: eight pairs a lane, both elements of each
@@ -262,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
       float* at = reinterpret_cast<float*>(cs + t * a.half);
       at += eights ? (p % 8 / 2 * eights + p / 8) * 4 + p % 2 : 2 * p;
       at[0] = turn.x, at[eights ? 2 : 1] = turn.y;
-    } else cs_q[i - n_turned * a.half] = turn_of(a.freq[p], pos[kBefore + t - n_turned], a.factor, a.factor);
+    } else cs_q[i - n_turned * a.half] = turn_of(a.freq[p], pos[kReach + t - n_turned], a.factor, a.factor);
   }
   __syncthreads();
 
@@ -282,8 +293,8 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
     unsigned char* codes = in + a.codes_at + (int64_t(head) * page + slot0) * a.dim;
     const int kept = p0 % kBlock;
     float old = kept ? *scale_at : 0.f;
-    const T* from = is_v ? static_cast<const T*>(a.v) + (t0 - kBefore) * a.v_tok + h * a.v_head
-                         : static_cast<const T*>(a.k) + (t0 - kBefore) * a.k_tok + h * a.k_head;
+    const T* from = is_v ? static_cast<const T*>(a.v) + (t0 - kReach) * a.v_tok + h * a.v_head
+                         : static_cast<const T*>(a.k) + (t0 - kReach) * a.k_tok + h * a.k_head;
     const int64_t row = is_v ? a.v_tok : a.k_tok;
     // step s of a lane: elements from .. on of a token; two steps of keys are eight pairs' elements, or 16 one after another
     const bool paired = kWide && !is_v;
@@ -452,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 5) append8_kernel(const __grid_const
               for (int k = 0; k < 2; ++k)
                 from[2 * i + k] = unpack(T(), word(s, i), k), from[8 + 2 * i + k] = unpack(T(), word(s + 1, i), k);
             }
-            turn_eight_exactly(x, from, !kInter, kInter ? e / 2 : e, a.half, a.freq, pos[run_at[run][tok]], a.factor);
+            turn_exactly(x, from, !kInter, kInter ? e / 2 : e, a.half, a.freq, pos[run_at[run][tok]], a.factor);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = two(x[2 * i], x[2 * i + 1]), w[i] = two(x[8 + 2 * i], x[9 + 2 * i]);
           }
@@ -550,7 +561,7 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   a.codes_at = int64_t(layer) * 2 * a.n_kv * cache->page_tokens * a.dim;
   a.scales_at = page8_scales(*cache) + int64_t(layer) * 2 * a.n_kv * (cache->page_tokens / kScaleTokens) * 4;
   // 16 bytes a step where every head starts on 16 bytes and the halves are whole steps (else a
-  // call on a prompt takes 413 us for 158)
+  // call on a prompt takes 423 us for 158)
   bool wide = rope->rotary % (rope->interleaved ? 8 : 16) == 0 && aligned(k, k_tok, k_head, 2) && aligned(v, v_tok, v_head, 2);
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -323,10 +323,14 @@ def test_append8_counts_tokens_out_of_order(lead):
     """Tokens that break the lists' order within 32 entries are seen, wherever thread blocks begin."""
     none = (-1, 0)
     before = [(1 + t // 64, t % 64) for t in range(lead)]
+    unseen = [(0, 0)] + [none] * 31 + [(0, 1)] + [none] * 29 + [(0, 2)]             # two runs of a block, too far apart
     cases = [([(0, 0), (0, 1), (0, 2)], 0),
              ([(0, 0)] + [none] * 9 + [(0, 1)] + [none] * 20 + [(0, 2)], 0),        # 31 entries from the first to the last
              ([(0, 0)] + [none] * 9 + [(0, 1)] + [none] * 21 + [(0, 2)], 1),        # one too far
              ([(0, 0)] + [none] * 19 + [(0, 1)] + [none] * 19 + [(0, 2)] + [none] * 19 + [(0, 3)], 2),
+             ([(0, 17)] + [none] * 24 + [(0, 1)] + [none] * 24 + [(0, 2)], 0),      # the one before is another block's
+             ([(0, 0)] + [none] * 30 + [(0, 1)] + [none] * 30 + [(0, 2)], 1),
+             (unseen, 0),
              ([(0, t) for t in range(40)], 0),
              ([(0, 5), (0, 4), (0, 3)], 2),                                         # backwards
              ([(0, 5), (0, 5)], 1),                                                 # the same token twice
@@ -336,7 +340,7 @@ def test_append8_counts_tokens_out_of_order(lead):
     for entries, count in cases:
         cache, x, seq, pos = _append_in_order(before + entries)
         assert cache.status.tolist()[4:7] == [0, 0, count], entries
-        if count == 0:
+        if count == 0 and entries is not unseen:
             on = seq >= 0
             at = cache.table[seq[on].long(), (pos[on] // 16).long()].long()
             for which in (0, 1):
