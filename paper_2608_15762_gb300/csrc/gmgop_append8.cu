@@ -7,9 +7,9 @@
 // found, the block's scale follows, and the codes are written once.  Scales are powers of two, so a block whose scale grows
 // is rounded again only where its codes become subnormal, and x / scale is exact.
 // What bounds it is memory, as far as the few registers allow that keep a run's loads in flight (a prompt of 32,768
-// tokens, 32 + 8 + 8 heads of 128: 148 us, of them 66 for keys and values, 201 MB at 3.0 TB/s, and
+// tokens, 32 + 8 + 8 heads of 128: 150 us, of them 68 for keys and values, 201 MB at 3.0 TB/s, and
 // 82 for queries), and where tokens are few the chain of loads from a token's position to
-// its block's scale (16 tokens 4.8 us).
+// its block's scale (16 tokens 4.9 us).
 // A thread block serves a share of `chunk` tokens' heads: sines and cosines once for all of them, as
 // in the cache of 16-bit values.  A run that reaches past its block's tokens is taken whole by the
 // block that it begins in.
@@ -566,8 +566,9 @@ extern "C" int op_rope_append8(const op_rope_t* rope, const op_cache_t* cache, i
   if (n_heads > 0) wide = wide && aligned(q, q_tok, q_head, 2) && aligned(q_out, o_tok, o_head, 2);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   // One token a block, its queries and its runs in shares: a decode step of 16 tokens 4.5 us, with 16 a block 9.2 (these
-  // without the search for numbers near a middle, which adds about a tenth to each).  Where there are many, and not
-  // each a sequence's only one, 16 a block, which has few runs then (with 32 + 8 + 8 heads of 128, 2,432 tokens 20.8 us,
+  // without the search for numbers near a middle, which adds about a tenth to each).  Where there are many, and 16 or more for each
+  // row that the cache has (which rows the tokens are of, the host does not know: of a cache of many rows a call for a few has
+  // one a block up to 4,864 tokens, though 16 would be better), 16 a block, which has few runs then (with 32 + 8 + 8 heads of 128, 2,432 tokens 20.8 us,
   // one a block 26.0; 608 12.0 and 13.3; 304 11.4 and 10.5; 1,216 of as many sequences 25.5 and 20.3, 4,864 81.7 and 82.1).
   // Very many queries then as dense ones, in a launch of their own with few registers a thread (32,768 tokens 136 us, in one
   // launch 161; 4,864 32.6 and 34.8; 2,432 21.8 and 20.8; 16,384 of 8 heads of 64 21.5 and 17.3).

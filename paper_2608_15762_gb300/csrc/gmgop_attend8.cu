@@ -12,15 +12,15 @@
 // Keys fill the tensor core's 128 lanes and rows are columns, so that a step of few rows costs few columns,
 // exponentials and registers, and K and V are read once, as the codes that they are, by fp8 products.
 // What the codes meet is split into several of them: Q as bf16 and fp16 have it, P to 12 bits, small weights too.
-// Memory bounds it where there is enough to read (the decode step below: 161 us, 6.7 TB/s); a small step is a
-// launch and the chain of its few steps (8 requests behind 500 tokens 9.6 us).
+// Memory bounds it where there is enough to read (the decode step below: 167 us, 6.5 TB/s); a small step is a
+// launch and the chain of its few steps (8 requests behind 500 tokens 9.9 us).
 //
 // Tiles of more rows, up to 128, lie with their rows on the lanes, against 64 keys a step.  K is taken as the
 // codes that it is here too, by Q's.  V becomes fp16, which holds e4m3 exactly, on its way through shared
 // memory, which costs fewer instructions than splitting P would; P is fp16: its rounding, 2^-11, is what the
 // tensor cores take.  The softmax warps' instructions and the latency of a step's chain bound it: chunks of prompts
-// take 333 us at 57% of the issue slots and 26% of the tensor cores' cycles, and 96 requests behind 32,768 shared tokens
-// 81 us at 51% and 39%.
+// take 335 us at 57% of the issue slots and 25% of the tensor cores' cycles, and 96 requests behind 32,768 shared tokens
+// 83 us at 50% and 38%.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -1191,9 +1191,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend8_kernel(const __grid_const
 }
 
 // A plan is for one of the kernels: the one whose steps and items take less time (in clocks, as measured; the many rows'
-// steps are of 64 keys).  Few rows and many: a decode step of 64 requests of 8,000 tokens or so, 32 + 8 heads of 128, 161 us and
-// 264; one request of 131,072 tokens (fp16, 4 tokens of 5 heads each) 47 and 60; 96 requests behind 32,768 shared tokens
-// 177 and 81; chunks of prompts behind 4,000 tokens, 24 + 8 heads of 64, 1,722 and 333.
+// steps are of 64 keys).  Few rows and many: a decode step of 64 requests of 8,000 tokens or so, 32 + 8 heads of 128, 167 us and
+// 243; one request of 131,072 tokens (fp16, 4 tokens of 5 heads each) 48 and 60; 96 requests behind 32,768 shared tokens
+// 195 and 83; chunks of prompts behind 4,000 tokens, 24 + 8 heads of 64, 1,846 and 335.
 // A tile's start and end count as so many steps where the keys are cut: 4 for few rows (with 3, three short decode steps
 // of 6.4, 7.5 and 121 us became 7.3, 8.9 and 129).
 constexpr Cutting kCuttingFew = {kFewKeys, kFewRows, 4, 8, 4, 5, true}, kCuttingMany = {kKeys, kRows, 6, 12, 4, 8, true};
