@@ -304,6 +304,19 @@ def test_append8_codes_do_not_depend_on_where_tensors_lie(D, rotary, inter, dtyp
         P.rope_append8(plan, q, k, v, pos, seq, cache, 0)
         got.append(pool)
     assert all(torch.equal(pool, got[0]) for pool in got[1:])
+    # and each code stands for its value: rounded once, of keys that are off by the rotation's error in 32 bits
+    exact = row[:, H * D:].double().unflatten(1, (2, hk, D)).clone()
+    p = torch.arange(rotary // 2, device="cuda")
+    i, j = (2 * p, 2 * p + 1) if inter else (p, p + rotary // 2)
+    exact[:, 0][..., i], exact[:, 0][..., j] = _turned(exact[:, 0][..., i], exact[:, 0][..., j], pos[:, None, None], plan.freq)
+    flat = lambda x: x[:, 0].permute(1, 2, 0, 3, *range(4, x.dim() - 1)).flatten(2, 3)  # noqa: E731
+    codes, scales = flat(cache.codes)[:, :, :T + 37], flat(cache.scales)
+    want = torch.zeros(2, hk, T + 37, D, dtype=torch.float64, device="cuda")
+    want[:, :, 37:] = exact.permute(1, 2, 0, 3)
+    scales = scales[:, :, :-(-(T + 37) // 16)]
+    pad = scales.shape[2] * 16 - (T + 37)
+    codes, want = torch.nn.functional.pad(codes.float(), (0, 0, 0, pad)), torch.nn.functional.pad(want, (0, 0, 0, pad))
+    assert bool(R8.near(codes, scales, None, want, 2e-6)[:, :, 37:].all())
 
 
 def _append_in_order(entries, n_seq=40, page=16):
